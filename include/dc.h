@@ -180,6 +180,121 @@ dc_status dc_head_euler(const dc_model_cfg* cfg, const dc_model_weights* w,
                         hipStream_t stream);
 
 /* ---------------------------------------------------------------------------
+ * Rotary positions, query/key norms, int8 products, quantised cache.
+ *
+ * What a generator with rotary positions or a reduced-precision refresh needs beside the
+ * steps above.  dc_block_forward_ext and dc_sampler_create_ext run them inside a block
+ * and a sample.  Calls are enqueued on `stream`, which belongs to the current device, as do
+ * the buffers.  None allocates, so all can be captured into a graph.
+ * ------------------------------------------------------------------------- */
+
+/* Rotary positions with three axes (time, height, width).  dim[a]: features of a head that
+ * turn with axis a (even, >= 0; sum at most head_dim).  The head_dim / 2 pairs of a head
+ * go to the axes in order; pair i of axis a turns by position[a] * theta^(-2 i / dim[a]),
+ * pairs behind the last axis do not turn.  Positions on the latent's grid: start[a] +
+ * step[a] * index[a], index = (frame, patch row, patch column). */
+typedef struct {
+  int32_t dim[3];
+  double theta;             /* > 0 */
+  double start[3], step[3];
+} dc_rope_axes;
+
+/* cos_sin out: f32 [N_v, head_dim / 2, 2], (cos, sin) of every video token's pairs; the
+ * angles are formed and reduced in f64.  pos: device f64 [N_v, 3], or NULL for the grid
+ * (start and step are read for the grid only). */
+dc_status dc_rope_table(const dc_model_cfg* cfg, const dc_rope_axes* axes, const double* pos,
+                        float* cos_sin, hipStream_t stream);
+
+/* Norms and rotation of a block's queries and keys. */
+typedef struct {
+  const float* q_weight;    /* [head_dim]: RMS norm of each query head with this weight; NULL: none */
+  const float* k_weight;    /* the same for the keys */
+  float eps;                /* > 0 where a weight is given */
+  const float* cos_sin;     /* f32 [N_v, head_dim / 2, 2] (dc_rope_table), or NULL: no rotation */
+  int32_t interleaved;      /* a pair is 1: features 2p and 2p + 1; 0: features p and p + head_dim / 2 */
+} dc_qk_cfg;
+
+/* Per head of Q and K: y = x / sqrt(mean(x^2) + eps) * weight, then on the N_v video rows each
+ * pair (a, b) -> (a cos - b sin, b cos + a sin), then Q times q_scale; one rounding.  in:
+ * [B, N, ld_in], model dtype, Q at columns [0, d), K at [d, 2d) (an [N, 3d] QKV product or
+ * [N, 2d] rows); out: [B, N, ld_out] likewise, other columns untouched.  out may be in with
+ * the same ld, or must not overlap it.  ld_in, ld_out: elements, >= 2d and multiples of 8 (bf16)
+ * or 4 (f32).  A row's mean square must be below the fp32 range (|x| < 1e18). */
+dc_status dc_qk_norm_rope(const dc_model_cfg* cfg, const dc_qk_cfg* qk, const void* in, int64_t ld_in,
+                          void* out, int64_t ld_out, float q_scale, const int32_t* idx, int32_t n,
+                          hipStream_t stream);
+
+/* Rows in 8 bits: scale[m] = max_k |x[m, k]| / 127, q[m, k] = x[m, k] / scale[m] rounded to the
+ * nearest integer (ties to even), both divisions rounded to fp32.  Columns from `cols` up to the
+ * next multiple of 128 are set to 0.  A row of zeros has scale 0 and codes 0; a row with an
+ * infinity or NaN has scale NaN and codes 0, so a product with it is NaN.  x: [rows, ld_x] of
+ * dtype (dc_dtype), any element-aligned address and ld_x >= cols; q: [rows, ld_q], ld_q at least
+ * cols rounded up to 128; scale: [rows].  Serves activations (a scale per token) and weights
+ * [out, in] (a scale per output channel).  rows <= 2^24 - 1; rows = 0 is a no-op. */
+dc_status dc_quantize_rows(const void* x, int32_t dtype, int64_t ld_x, int32_t rows, int32_t cols,
+                           int8_t* q, int64_t ld_q, float* scale, hipStream_t stream);
+
+/* out[m, n] = f(x_scale[m] w_scale[n] sum_k x[m, k] w[n, k] + bias[n]): the sum in int32 (exact),
+ * the rest in fp32, one rounding to out_dtype.  f: the value itself, GELU (tanh form), or
+ * residual[m, n] + gate[n] * value. */
+typedef struct {
+  int32_t rows, out_features;     /* M, N; rows = 0 is a no-op */
+  int32_t in_features;            /* K with its padding: a multiple of 128, at most 130,944 */
+  const int8_t* x;                /* [rows, ld_x], 16-byte aligned, ld_x a multiple of 16 */
+  const float* x_scale;           /* [rows] */
+  int64_t ld_x;
+  const int8_t* w;                /* [out_features, ld_w], as x */
+  const float* w_scale;           /* [out_features] */
+  int64_t ld_w;
+  const float* bias;              /* [out_features] or NULL */
+  int32_t gelu;                   /* 1: GELU; not with a gate */
+  const float* gate;              /* [out_features] or NULL: no residual */
+  const float* residual;          /* f32 [rows, ld_residual], with a gate; may be out (same ld) */
+  int64_t ld_residual;
+  void* out;                      /* [rows, ld_out] */
+  int32_t out_dtype;              /* dc_dtype; DC_F32 with a gate */
+  int64_t ld_out;                 /* >= out_features; any, vector stores need 16-byte rows */
+} dc_linear_i8_args;
+dc_status dc_linear_i8(const dc_linear_i8_args* args, hipStream_t stream);
+
+/* The residual cache in `bits` = 8 or 4 bits, a scale per 64 features: for r = h_out - h_in on the
+ * video rows, scale = max |r| / L over the group (L = 127 or 7), code = r / scale rounded to the
+ * nearest integer, as in dc_quantize_rows (zeros, infinities and NaN likewise, per group).
+ * codes: int8 [B, N_v, d], or [B, N_v, d / 2] bytes with feature 2i in the low and 2i + 1 in
+ * the high half (two's complement); scales: f32 [B, N_v, d / 64].  bf16's 2 bytes a value
+ * become 1.06 or 0.56. */
+dc_status dc_cache_store_q(const dc_model_cfg* cfg, int32_t bits, const float* h_out, const float* h_in,
+                           void* codes, float* scales, const int32_t* idx, int32_t n, hipStream_t stream);
+/* g = h_in + code * scale on the video rows (dc_cache_apply for such a cache; g may be h_in). */
+dc_status dc_cache_apply_q(const dc_model_cfg* cfg, int32_t bits, const float* h_in, const void* codes,
+                           const float* scales, float* g, const int32_t* idx, int32_t n,
+                           hipStream_t stream);
+
+/* One block's matrices in int8 (device memory): rows as dc_quantize_rows writes them with
+ * ld_q = the row's length, a scale per output channel. */
+typedef struct {
+  const int8_t* w_qkv; const float* s_qkv;  /* [3d, d], [3d] */
+  const int8_t* w_o;   const float* s_o;    /* [d, d], [d] */
+  const int8_t* w_1;   const float* s_1;    /* [F, d], [F] */
+  const int8_t* w_2;   const float* s_2;    /* [d, F], [d] */
+} dc_block_weights_i8;
+
+/* What a block does beyond dc_block_forward (host structs, read during the call). */
+typedef struct {
+  const dc_qk_cfg* qk;              /* norms and rotation between the QKV product and attention, or NULL */
+  const dc_block_weights_i8* i8;    /* bf16 models: int8 products (rows quantised as they come), or NULL.
+                                       The matrices of dc_block_weights are then not read and may be NULL */
+} dc_block_ext;
+
+/* Workspace of dc_block_forward_ext and of a sampler with extended blocks. */
+size_t dc_block_ext_workspace_bytes(const dc_model_cfg* cfg, int32_t batch);
+
+/* dc_block_forward with the extensions of ext (NULL, or both members NULL: the same). */
+dc_status dc_block_forward_ext(const dc_model_cfg* cfg, const dc_block_weights* blk,
+                               const dc_block_ext* ext, const float* mod, float* h, const int32_t* idx,
+                               int32_t n, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
  * Host schedule (pure; no device access).
  * ------------------------------------------------------------------------- */
 
@@ -333,6 +448,23 @@ dc_status dc_sampler_create_ex(const dc_model_cfg* cfg, const dc_model_weights* 
                                const dc_buffers* buf, const dc_sampler_opts* opts,
                                hipStream_t stream, dc_sampler** out);
 
+/* Extensions of a sample; zero-initialise, then set what is used. */
+typedef struct {
+  const dc_block_ext* blocks;     /* host [n_blocks] or NULL (what the entries point to is copied) */
+  const dc_block_ext* blocks_low; /* the same for w_low's blocks */
+  int32_t cache_bits;             /* 0: residual cache in the model dtype; 8 or 4: as dc_cache_store_q,
+                                     dc_buffers.resid then holds the codes */
+  float* cache_scales;            /* f32 [B or 2B (guidance), N_v, d / 64], with cache_bits */
+} dc_sampler_ext;
+
+/* dc_sampler_create_ex with the extensions of ext (NULL: the same).  With blocks or blocks_low
+ * the workspace is dc_block_ext_workspace_bytes.  A reuse step on a quantised cache writes
+ * g = h_in + r into dc_buffers.h. */
+dc_status dc_sampler_create_ext(const dc_model_cfg* cfg, const dc_model_weights* w, int32_t B,
+                                const dc_sched_problem* problems, const double* sigmas,
+                                const dc_buffers* buf, const dc_sampler_opts* opts,
+                                const dc_sampler_ext* ext, hipStream_t stream, dc_sampler** out);
+
 /* Denoising step k (1-based, called for k = 1..K in order) of every scene.
  * realized: host uint8 [B] out (1 = reused, 0 = backbone evaluated); drift: host f64
  * [B] out (observed drift, NaN where no check ran).  Waits on `stream` once if any
@@ -351,7 +483,8 @@ void dc_sampler_destroy(dc_sampler* s);
  * Classes: 0 attention, 1 QKV GEMM, 2 output-projection GEMM, 3 MLP-up GEMM,
  * 4 MLP-down GEMM, 5 AdaLN modulation, 6 patch embedding, 7 drift reduction,
  * 8 cache store, 9 cache apply, 10 head + Euler, 11 head + Euler on a reuse step of a
- * bf16 model (its input g = h_in + r formed in the kernel).
+ * bf16 model (its input g = h_in + r formed in the kernel), 12 query/key norms and rotation,
+ * 13 quantisation of rows (LN-modulated rows included).
  * ------------------------------------------------------------------------- */
 
 /* Bit c of mask enables timing of class c: each launch is bracketed by two

@@ -62,6 +62,37 @@ class SamplerOpts(C.Structure):
                 ("mod_low", vp), ("cfg", C.c_int32), ("guidance", C.c_float), ("txt_null", vp)]
 
 
+class RopeAxes(C.Structure):
+    _fields_ = [("dim", C.c_int32 * 3), ("theta", C.c_double), ("start", C.c_double * 3),
+                ("step", C.c_double * 3)]
+
+
+class QkCfg(C.Structure):
+    _fields_ = [("q_weight", vp), ("k_weight", vp), ("eps", C.c_float), ("cos_sin", vp),
+                ("interleaved", C.c_int32)]
+
+
+class LinearI8Args(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("out_features", C.c_int32), ("in_features", C.c_int32),
+                ("x", vp), ("x_scale", vp), ("ld_x", C.c_int64), ("w", vp), ("w_scale", vp),
+                ("ld_w", C.c_int64), ("bias", vp), ("gelu", C.c_int32), ("gate", vp), ("residual", vp),
+                ("ld_residual", C.c_int64), ("out", vp), ("out_dtype", C.c_int32), ("ld_out", C.c_int64)]
+
+
+class BlockWeightsI8(C.Structure):
+    _fields_ = [("w_qkv", vp), ("s_qkv", vp), ("w_o", vp), ("s_o", vp), ("w_1", vp), ("s_1", vp),
+                ("w_2", vp), ("s_2", vp)]
+
+
+class BlockExt(C.Structure):
+    _fields_ = [("qk", C.POINTER(QkCfg)), ("i8", C.POINTER(BlockWeightsI8))]
+
+
+class SamplerExt(C.Structure):
+    _fields_ = [("blocks", C.POINTER(BlockExt)), ("blocks_low", C.POINTER(BlockExt)),
+                ("cache_bits", C.c_int32), ("cache_scales", vp)]
+
+
 P = C.POINTER
 i32p = P(C.c_int32)
 
@@ -85,6 +116,16 @@ SIGNATURES = {
     "dc_calibrate_tables": (C.c_int32, [P(ModelCfg), P(ModelWeights), vp, vp, P(C.c_double), C.c_int32,
                                         C.c_int32, C.c_double, P(C.c_double), P(C.c_double), vp,
                                         C.c_size_t, vp]),
+    "dc_rope_table": (C.c_int32, [P(ModelCfg), P(RopeAxes), vp, vp, vp]),
+    "dc_qk_norm_rope": (C.c_int32, [P(ModelCfg), P(QkCfg), vp, C.c_int64, vp, C.c_int64, C.c_float, i32p,
+                                    C.c_int32, vp]),
+    "dc_quantize_rows": (C.c_int32, [vp, C.c_int32, C.c_int64, C.c_int32, C.c_int32, vp, C.c_int64, vp, vp]),
+    "dc_linear_i8": (C.c_int32, [P(LinearI8Args), vp]),
+    "dc_cache_store_q": (C.c_int32, [P(ModelCfg), C.c_int32, vp, vp, vp, vp, i32p, C.c_int32, vp]),
+    "dc_cache_apply_q": (C.c_int32, [P(ModelCfg), C.c_int32, vp, vp, vp, vp, i32p, C.c_int32, vp]),
+    "dc_block_ext_workspace_bytes": (C.c_size_t, [P(ModelCfg), C.c_int32]),
+    "dc_block_forward_ext": (C.c_int32, [P(ModelCfg), P(BlockWeights), P(BlockExt), vp, vp, i32p, C.c_int32,
+                                         vp, C.c_size_t, vp]),
     "dc_schedule_dp": (C.c_int32, [P(SchedProblem), P(Schedule)]),
     "dc_select_tau": (C.c_int32, [P(SchedProblem), C.c_int32, C.c_double, P(C.c_int64)]),
     "dc_motion_statistics": (C.c_int32, [P(C.c_double), P(C.c_double), C.c_int32, P(C.c_double),
@@ -95,6 +136,9 @@ SIGNATURES = {
                                       P(C.c_double), P(Buffers), C.c_int32, vp, P(vp)]),
     "dc_sampler_create_ex": (C.c_int32, [P(ModelCfg), P(ModelWeights), C.c_int32, P(SchedProblem),
                                          P(C.c_double), P(Buffers), P(SamplerOpts), vp, P(vp)]),
+    "dc_sampler_create_ext": (C.c_int32, [P(ModelCfg), P(ModelWeights), C.c_int32, P(SchedProblem),
+                                          P(C.c_double), P(Buffers), P(SamplerOpts), P(SamplerExt), vp,
+                                          P(vp)]),
     "dc_denoise_step": (C.c_int32, [vp, C.c_int32, vp, P(C.c_uint8), P(C.c_double)]),
     "dc_sampler_plan": (C.c_int32, [vp, C.c_int32, P(C.c_uint8), i32p, P(C.c_int64)]),
     "dc_sampler_destroy": (None, [vp]),
@@ -104,7 +148,8 @@ SIGNATURES = {
 }
 
 KERNEL_CLASSES = ("attention", "gemm_qkv", "gemm_out", "gemm_up", "gemm_down", "ln_modulate",
-                  "patch_embed", "drift", "cache_store", "cache_apply", "head", "head_reuse")
+                  "patch_embed", "drift", "cache_store", "cache_apply", "head", "head_reuse",
+                  "qk_norm_rope", "quantize")
 
 _lib = None
 

@@ -16,7 +16,8 @@ from .inputs import ModelShape, SchedProblem as PySchedProblem
 __all__ = ["model_cfg", "DeviceModel", "Workspace", "SamplerBuffers", "profile", "dc_workspace_bytes", "dc_time_modulation",
            "dc_patch_embed", "dc_block_forward", "dc_cache_store", "dc_cache_apply",
            "dc_drift_l1", "dc_head_euler", "dc_schedule_dp", "dc_select_tau", "dc_motion_statistics",
-           "dc_select_anchors", "Sampler"]
+           "dc_select_anchors", "Sampler", "rope_axes", "dc_rope_table", "dc_qk_norm_rope", "dc_quantize_rows",
+           "dc_linear_i8", "dc_cache_store_q", "dc_cache_apply_q", "BlockExt", "dc_block_forward_ext"]
 
 
 def _torch():
@@ -94,11 +95,14 @@ def dc_workspace_bytes(m: ModelShape, batch: int = 1) -> int:
 
 
 class Workspace:
-    """Device scratch of dc_workspace_bytes() bytes (256-byte aligned)."""
+    """Device scratch of dc_workspace_bytes() bytes (256-byte aligned); ext: of
+    dc_block_ext_workspace_bytes(), for extended blocks."""
 
-    def __init__(self, m: ModelShape, batch=1, device="cuda:0"):
+    def __init__(self, m: ModelShape, batch=1, device="cuda:0", ext=False):
         torch = _torch()
         self.nbytes = dc_workspace_bytes(m, batch)
+        if ext:
+            self.nbytes = int(L.load().dc_block_ext_workspace_bytes(C.byref(model_cfg(m)), batch))
         self.buf = torch.empty(self.nbytes + 256, dtype=torch.uint8, device=device)
         off = (-int(self.buf.data_ptr())) % 256
         self.ptr = C.c_void_p(int(self.buf.data_ptr()) + off)
@@ -179,6 +183,223 @@ def dc_calibrate_tables(dm: DeviceModel, x1, txt, sigmas, h_max: int, eps: float
         q.ctypes.data_as(C.POINTER(C.c_double)), d.ctypes.data_as(C.POINTER(C.c_double)),
         int(ws.data_ptr()), nbytes, _stream(stream)))
     return q, d
+
+
+# ----------------------------------------------------------------------------
+# rotary positions, query/key norms, int8 products, quantised cache
+# ----------------------------------------------------------------------------
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _on(stream, first, *more):
+    """The current stream of the tensors' device (or `stream`, which has to be one of it)."""
+    torch = _torch()
+    dev = first.device
+    _need(dev.type == "cuda", "tensors must be on a GPU")
+    for t in more:
+        _need(t is None or t.device == dev, "tensors must be on one device")
+    s = torch.cuda.current_stream(dev) if stream is None else stream
+    _need(s.device == dev, "the stream belongs to another device")
+    return C.c_void_p(int(s.cuda_stream)), torch.cuda.device(dev)
+
+
+def _dtype(t):
+    torch = _torch()
+    if t.dtype == torch.float32:
+        return L.DC_F32
+    _need(t.dtype == torch.bfloat16, "float32 or bfloat16 tensors only")
+    return L.DC_BF16
+
+
+def _tokens(cfg):
+    n_v = cfg.lat_t * (cfg.lat_h // cfg.patch) * (cfg.lat_w // cfg.patch)
+    return n_v, n_v + cfg.n_txt
+
+
+def _batch(t, shape, dtype, idx, what):
+    """A contiguous [B, *shape] tensor that holds every sample of idx."""
+    _need(t.dtype == dtype and t.is_contiguous() and tuple(t.shape[1:]) == shape,
+          f"{what}: a contiguous [B, {', '.join(map(str, shape))}] {dtype} tensor is wanted")
+    _need(not len(idx) or max(idx) < t.shape[0], f"{what}: a sample of idx lies outside the batch")
+
+
+def _rows(t, what):
+    """A 2-d tensor whose rows are contiguous: its row stride in elements."""
+    _need(t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1) and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1]),
+          f"{what}: a 2-d tensor with contiguous rows that do not overlap is wanted")
+    return int(t.stride(0)) if t.shape[0] > 1 else max(int(t.stride(0)), int(t.shape[1]))
+
+
+def _vector(t, n, what):
+    torch = _torch()
+    _need(t is None or (t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == (n,)),
+          f"{what}: a contiguous float32 [{n}] tensor is wanted")
+
+
+def rope_axes(dim, theta=10000.0, start=(0.0, 0.0, 0.0), step=(1.0, 1.0, 1.0)) -> L.RopeAxes:
+    """dc_rope_axes: features of a head that turn with time, height and width, and the grid's
+    positions start + step * index."""
+    return L.RopeAxes((C.c_int32 * 3)(*dim), theta, (C.c_double * 3)(*start), (C.c_double * 3)(*step))
+
+
+def dc_rope_table(cfg, axes: L.RopeAxes, pos, table, stream=None):
+    """table (f32 [N_v, head_dim / 2, 2]) := cos and sin; pos: f64 [N_v, 3] or None (the grid)."""
+    torch = _torch()
+    n_v = _tokens(cfg)[0]
+    _need(table.dtype == torch.float32 and table.is_contiguous()
+          and tuple(table.shape) == (n_v, cfg.head_dim // 2, 2), "table: a contiguous float32 [N_v, head_dim / 2, 2]")
+    _need(pos is None or (pos.dtype == torch.float64 and pos.is_contiguous() and tuple(pos.shape) == (n_v, 3)),
+          "pos: a contiguous float64 [N_v, 3] tensor or None")
+    s, dev = _on(stream, table, pos)
+    with dev:
+        L.check("dc_rope_table", L.load().dc_rope_table(C.byref(cfg), C.byref(axes), _ptr(pos), _ptr(table), s))
+
+
+def _qk_cfg(cfg, q_weight, k_weight, eps, table, interleaved):
+    torch = _torch()
+    _vector(q_weight, cfg.head_dim, "q_weight")
+    _vector(k_weight, cfg.head_dim, "k_weight")
+    _need(table is None or (table.dtype == torch.float32 and table.is_contiguous()
+                            and tuple(table.shape) == (_tokens(cfg)[0], cfg.head_dim // 2, 2)),
+          "table: a contiguous float32 [N_v, head_dim / 2, 2]")
+    return L.QkCfg(_ptr(q_weight), _ptr(k_weight), float(eps), _ptr(table), int(bool(interleaved)))
+
+
+def dc_qk_norm_rope(cfg, x, out, idx, q_weight=None, k_weight=None, eps=1e-6, table=None, interleaved=True,
+                    q_scale=1.0, stream=None):
+    """Norms and rotation of the queries (columns [0, d)) and keys ([d, 2d)) of x [B, N, >= 2d] into out
+    (x itself, or a tensor like it): RMS norm with q_weight / k_weight where given, rotation where table is."""
+    torch = _torch()
+    n_tok, d2 = _tokens(cfg)[1], 2 * cfg.hidden
+    dt = torch.bfloat16 if cfg.dtype == L.DC_BF16 else torch.float32
+    for t in (x, out):
+        _need(t.dtype == dt and t.dim() == 3 and t.shape[1] == n_tok and t.shape[2] >= d2 and t.stride(2) == 1
+              and (t.shape[0] <= 1 or t.stride(0) == n_tok * t.stride(1)),
+              f"x and out: [B, {n_tok}, at least {d2}] {dt} tensors of equally spaced rows are wanted")
+        _need(not len(idx) or max(idx) < t.shape[0], "a sample of idx lies outside the batch")
+    qk = _qk_cfg(cfg, q_weight, k_weight, eps, table, interleaved)
+    arr, p, n = _idx(idx)
+    s, dev = _on(stream, x, out, q_weight, k_weight, table)
+    with dev:
+        L.check("dc_qk_norm_rope", L.load().dc_qk_norm_rope(
+            C.byref(cfg), C.byref(qk), _ptr(x), int(x.stride(1)), _ptr(out), int(out.stride(1)), float(q_scale), p, n,
+            s))
+
+
+def dc_quantize_rows(x, q, scale, stream=None):
+    """q (int8 [rows, at least cols rounded up to 128]) and scale (f32 [rows]) := the rows of x [rows, cols]."""
+    torch = _torch()
+    rows, cols = x.shape
+    ldx, ldq = _rows(x, "x"), _rows(q, "q")
+    _need(q.dtype == torch.int8 and q.shape[0] == rows and q.shape[1] >= -(-cols // 128) * 128,
+          "q: an int8 tensor of x's rows, at least cols rounded up to 128 wide")
+    _vector(scale, rows, "scale")
+    s, dev = _on(stream, x, q, scale)
+    with dev:
+        L.check("dc_quantize_rows", L.load().dc_quantize_rows(_ptr(x), _dtype(x), ldx, rows, cols, _ptr(q), ldq,
+                                                              _ptr(scale), s))
+
+
+def dc_linear_i8(x, x_scale, w, w_scale, out, bias=None, gelu=False, gate=None, residual=None, stream=None):
+    """out [M, N] := the product of int8 rows x [M, K] and w [N, K] (K as padded by dc_quantize_rows) with
+    their scales, plus bias, through GELU or as residual + gate * (...)."""
+    torch = _torch()
+    m, k = x.shape
+    n = w.shape[0]
+    _need(x.dtype == torch.int8 and w.dtype == torch.int8 and w.dim() == 2 and w.shape[1] == k,
+          "x and w: int8 tensors of equally long rows")
+    _need(tuple(out.shape) == (m, n), "out: [rows of x, rows of w]")
+    for v, size, what in ((x_scale, m, "x_scale"), (w_scale, n, "w_scale"), (bias, n, "bias"), (gate, n, "gate")):
+        _vector(v, size, what)
+    _need(residual is None or (residual.dtype == torch.float32 and residual.shape == out.shape),
+          "residual: a float32 tensor of out's shape")
+    a = L.LinearI8Args(m, n, k, _ptr(x), _ptr(x_scale), _rows(x, "x"), _ptr(w), _ptr(w_scale), _rows(w, "w"),
+                       _ptr(bias), int(bool(gelu)), _ptr(gate), _ptr(residual),
+                       0 if residual is None else _rows(residual, "residual"), _ptr(out), _dtype(out),
+                       _rows(out, "out"))
+    s, dev = _on(stream, x, x_scale, w, w_scale, out, bias, gate, residual)
+    with dev:
+        L.check("dc_linear_i8", L.load().dc_linear_i8(C.byref(a), s))
+
+
+def _check_cache(cfg, bits, codes, scales, idx):
+    torch = _torch()
+    _need(bits in (8, 4), "bits must be 8 or 4")
+    n_v = _tokens(cfg)[0]
+    _batch(codes, (n_v, cfg.hidden * bits // 8), torch.int8 if bits == 8 else torch.uint8, idx, "codes")
+    _batch(scales, (n_v, cfg.hidden // 64), torch.float32, idx, "scales")
+
+
+def dc_cache_store_q(cfg, bits, h_out, h_in, codes, scales, idx, stream=None):
+    """codes (int8 [B, N_v, d], or uint8 [B, N_v, d / 2] for 4 bits) and scales (f32 [B, N_v, d / 64]) :=
+    h_out - h_in on the video rows."""
+    torch = _torch()
+    _check_cache(cfg, bits, codes, scales, idx)
+    for t, what in ((h_out, "h_out"), (h_in, "h_in")):
+        _batch(t, (_tokens(cfg)[1], cfg.hidden), torch.float32, idx, what)
+    arr, p, n = _idx(idx)
+    s, dev = _on(stream, h_out, h_in, codes, scales)
+    with dev:
+        L.check("dc_cache_store_q", L.load().dc_cache_store_q(
+            C.byref(cfg), bits, _ptr(h_out), _ptr(h_in), _ptr(codes), _ptr(scales), p, n, s))
+
+
+def dc_cache_apply_q(cfg, bits, h_in, codes, scales, g, idx, stream=None):
+    """g := h_in + the cached residual on the video rows."""
+    torch = _torch()
+    _check_cache(cfg, bits, codes, scales, idx)
+    for t, what in ((h_in, "h_in"), (g, "g")):
+        _batch(t, (_tokens(cfg)[1], cfg.hidden), torch.float32, idx, what)
+    arr, p, n = _idx(idx)
+    s, dev = _on(stream, h_in, codes, scales, g)
+    with dev:
+        L.check("dc_cache_apply_q", L.load().dc_cache_apply_q(
+            C.byref(cfg), bits, _ptr(h_in), _ptr(codes), _ptr(scales), _ptr(g), p, n, s))
+
+
+class BlockExt:
+    """Extensions of every block of a DeviceModel: norms and rotation of queries and keys (q_weight,
+    k_weight: one [head_dim] tensor per block, or None; table: dc_rope_table's, or None) and, with
+    int8=True, the blocks' matrices quantised per output channel."""
+
+    MATRICES = (("w_qkv", "s_qkv"), ("w_o", "s_o"), ("w_1", "s_1"), ("w_2", "s_2"))
+
+    def __init__(self, dm: DeviceModel, q_weight=None, k_weight=None, eps=1e-6, table=None, interleaved=True,
+                 int8=False):
+        torch = _torch()
+        n = len(dm.blocks)
+        self.keep = [q_weight, k_weight, table]
+        self.c = (L.BlockExt * n)()
+        for l, b in enumerate(dm.blocks):
+            if q_weight is not None or k_weight is not None or table is not None:
+                qk = _qk_cfg(dm.cfg, None if q_weight is None else q_weight[l],
+                             None if k_weight is None else k_weight[l], eps, table, interleaved)
+                self.keep.append(qk)
+                self.c[l].qk = C.pointer(qk)
+            if int8:
+                held = L.BlockWeightsI8()
+                for name, s_name in self.MATRICES:
+                    w = b[name]
+                    q = torch.empty(w.shape, dtype=torch.int8, device=w.device)
+                    s = torch.empty(w.shape[0], dtype=torch.float32, device=w.device)
+                    dc_quantize_rows(w, q, s)
+                    setattr(held, name, int(q.data_ptr()))
+                    setattr(held, s_name, int(s.data_ptr()))
+                    self.keep += [q, s]
+                self.keep.append(held)
+                self.c[l].i8 = C.pointer(held)
+
+    def block(self, l):
+        return C.pointer(self.c[l])
+
+
+def dc_block_forward_ext(dm: DeviceModel, l: int, ext: BlockExt, mod, h, idx, ws: Workspace, stream=None):
+    """dc_block_forward with block l's extensions; ws: Workspace(..., ext=True)."""
+    arr, p, n = _idx(idx)
+    L.check("dc_block_forward_ext", L.load().dc_block_forward_ext(
+        C.byref(dm.cfg), dm.block(l), ext.block(l), _ptr(mod), _ptr(h), p, n, ws.ptr, ws.nbytes, _stream(stream)))
 
 
 class _CProblem:
@@ -263,9 +484,11 @@ def dc_select_anchors(Ls, Ths, eps: float):
 class SamplerBuffers:
     """Caller-owned device buffers for a batch of B scenes (allocated once, reusable).
     branches = 2 (guidance): h_in, h and resid hold 2B entries and the workspace 2B;
-    experts = 2: a second modulation table for the low-noise expert."""
+    experts = 2: a second modulation table for the low-noise expert; ext: the workspace of
+    extended blocks; cache_bits = 8 or 4: resid holds codes, with their scales beside it."""
 
-    def __init__(self, m: ModelShape, B: int, K: int, device="cuda:0", branches=1, experts=1):
+    def __init__(self, m: ModelShape, B: int, K: int, device="cuda:0", branches=1, experts=1, ext=False,
+                 cache_bits=0):
         torch = _torch()
         mdt = torch.bfloat16 if m.dtype == "bf16" else torch.float32
         self.m, self.B, self.K = m, B, K
@@ -275,12 +498,20 @@ class SamplerBuffers:
         self.txt_null = torch.zeros_like(self.txt) if branches == 2 else None
         self.h_in = torch.empty((E, m.n_tok, m.hidden), device=device, dtype=torch.float32)
         self.h = torch.empty_like(self.h_in)
-        self.resid = torch.empty((E, m.n_v, m.hidden), device=device, dtype=mdt)
+        self.cache_bits, self.ext = cache_bits, ext
+        self.cache_scales = None
+        if cache_bits:
+            _need(cache_bits in (8, 4), "cache_bits must be 0, 8 or 4")
+            self.resid = torch.empty((E, m.n_v, m.hidden * cache_bits // 8), device=device,
+                                     dtype=torch.int8 if cache_bits == 8 else torch.uint8)
+            self.cache_scales = torch.empty((E, m.n_v, m.hidden // 64), device=device, dtype=torch.float32)
+        else:
+            self.resid = torch.empty((E, m.n_v, m.hidden), device=device, dtype=mdt)
         self.u_ref = torch.empty((B, m.n_v, m.hidden), device=device, dtype=mdt)
         self.mod = torch.empty((K, m.n_blocks + 1, 6, m.hidden), device=device, dtype=torch.float32)
         self.mod_low = torch.empty_like(self.mod) if experts == 2 else None
         self.sums = torch.zeros((B, 4), device=device, dtype=torch.float64)
-        self.ws = Workspace(m, E, device)
+        self.ws = Workspace(m, E, device, ext)
         self.c = L.Buffers(_ptr(self.x), _ptr(self.txt), _ptr(self.h_in), _ptr(self.h), _ptr(self.resid),
                            _ptr(self.u_ref), _ptr(self.mod), _ptr(self.sums), self.ws.ptr, self.ws.nbytes)
 
@@ -292,17 +523,21 @@ class Sampler:
     host or device); they are copied into `bufs` (allocated here if not given)."""
 
     def __init__(self, dm: DeviceModel, problems, sigmas, x1, txt, drift_metric=0, stream=None,
-                 bufs: SamplerBuffers = None, low_expert=None, guidance=None):
+                 bufs: SamplerBuffers = None, low_expert=None, guidance=None, ext: BlockExt = None,
+                 ext_low: BlockExt = None, cache_bits=0):
         """low_expert: (DeviceModel, k_switch), the low-noise expert from step k_switch on
         (every problem's segment must change there); guidance: (w, txt_null [B, N_t, d]),
-        guidance branches with separate caches."""
+        guidance branches with separate caches; ext, ext_low: extensions of dm's and of the low
+        expert's blocks; cache_bits: 8 or 4 for a quantised residual cache (as bufs were made for)."""
         B = len(problems)
         self.dm, self.B, self.K = dm, B, problems[0].K
         if bufs is None:
             bufs = SamplerBuffers(dm.m, B, self.K, dm.device, branches=2 if guidance else 1,
-                                  experts=2 if low_expert else 1)
+                                  experts=2 if low_expert else 1, ext=bool(ext or ext_low),
+                                  cache_bits=cache_bits)
         self.bufs = bufs
         assert self.bufs.B == B and self.bufs.K == self.K
+        _need(bufs.cache_bits == cache_bits, "bufs were made for another cache_bits")
         self.bufs.x.copy_(x1, non_blocking=True)
         if dm.m.n_txt:
             self.bufs.txt.copy_(txt, non_blocking=True)
@@ -328,9 +563,18 @@ class Sampler:
             opts.cfg = 1
             opts.guidance = float(w)
             opts.txt_null = int(self.bufs.txt_null.data_ptr())
-        L.check("dc_sampler_create_ex", L.load().dc_sampler_create_ex(
+        x = L.SamplerExt()
+        self._ext = (ext, ext_low)      # the device memory they point to lives as long as the sampler
+        if ext is not None:
+            x.blocks = ext.c
+        if ext_low is not None:
+            x.blocks_low = ext_low.c
+        x.cache_bits = int(cache_bits)
+        if cache_bits:
+            x.cache_scales = int(self.bufs.cache_scales.data_ptr())
+        L.check("dc_sampler_create_ext", L.load().dc_sampler_create_ext(
             C.byref(dm.cfg), C.byref(dm.cweights), B, arr, sig.ctypes.data_as(C.POINTER(C.c_double)),
-            C.byref(self.bufs.c), C.byref(opts), _stream(stream), C.byref(self._h)))
+            C.byref(self.bufs.c), C.byref(opts), C.byref(x), _stream(stream), C.byref(self._h)))
         self.k = 0
 
     def step(self, stream=None):

@@ -2,6 +2,7 @@
 // entry points.  The sampler (causal controller) is in sampler.cpp.
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstring>
 #include <string>
 
@@ -97,15 +98,19 @@ Workspace workspace_layout(const Geo& g, int batch) {
   w.tm_s = take(size_t(kModSteps) * g.d * 4);
   w.tm_m = take(size_t(kModSteps) * 6 * g.d * 4);
   w.total = off;
+  w.q8 = take(size_t(g.N) * std::max(g.d, g.F));
+  w.q8_scale = take(size_t(g.N) * sizeof(float));
+  w.total_ext = off;
   return w;
 }
 
-static Status check_ws(const Geo& g, int batch, void* ws, size_t ws_bytes, Workspace& w) {
+static Status check_ws(const Geo& g, int batch, void* ws, size_t ws_bytes, Workspace& w, bool ext = false) {
   w = workspace_layout(g, batch);
+  const size_t need = ext ? w.total_ext : w.total;
   if (!ws) return Status::make(DC_ERR_WORKSPACE, "workspace is NULL");
   if (reinterpret_cast<uintptr_t>(ws) % 256) return Status::make(DC_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-  if (ws_bytes < w.total)
-    return Status::make(DC_ERR_WORKSPACE, "workspace too small: need " + std::to_string(w.total) + " bytes");
+  if (ws_bytes < need)
+    return Status::make(DC_ERR_WORKSPACE, "workspace too small: need " + std::to_string(need) + " bytes");
   return Status::ok();
 }
 
@@ -117,6 +122,16 @@ static int max_index(const IdxList& il) {
 
 template <class T> T* at(void* base, size_t off) {
   return reinterpret_cast<T*>(static_cast<char*>(base) + off);
+}
+
+static bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// norms and rotation of one sample's [N, ld] rows in the workspace
+static Status qk_in_place(const Geo& g, const dc_qk_cfg& c, void* qk, int ld, float q_scale, hipStream_t s) {
+  ProfScope ps(KClass::kQkNormRope, s);
+  IdxList one{};
+  one.n = 1;
+  return qk_norm_rope(c, qk, ld, qk, ld, q_scale, one, g, s);
 }
 
 Status time_modulation(const Geo& g, const dc_model_weights* w, const double* sigmas, int K,
@@ -160,19 +175,79 @@ Status patch_embed(const Geo& g, const dc_model_weights* w, const float* x, cons
   return patch_embed_f32(x, w->w_pe, w->b_pe, static_cast<const float*>(w->pos), txt, h_in, il, g, s);
 }
 
-Status block_forward(const Geo& g, const dc_block_weights* bw, const float* mod, float* h,
+Status check_qk(const dc_qk_cfg& c) {
+  if (c.interleaved != 0 && c.interleaved != 1) return Status::arg("qk->interleaved must be 0 or 1");
+  if ((c.q_weight || c.k_weight) && !(c.eps > 0.f && std::isfinite(c.eps)))
+    return Status::arg("qk->eps must be positive");
+  return Status::ok();
+}
+
+Status check_ext(const Geo& g, const dc_block_ext& e) {
+  if (e.qk) DC_TRY(check_qk(*e.qk));
+  if (!e.i8) return Status::ok();
+  if (!g.bf16) return Status::make(DC_ERR_DTYPE, "int8 block products need a bf16 model");
+  const dc_block_weights_i8& w = *e.i8;
+  if (!w.w_qkv || !w.s_qkv || !w.w_o || !w.s_o || !w.w_1 || !w.s_1 || !w.w_2 || !w.s_2)
+    return Status::arg("int8 block weight pointer is NULL");
+  if (!aligned16(w.w_qkv) || !aligned16(w.w_o) || !aligned16(w.w_1) || !aligned16(w.w_2))
+    return Status::arg("int8 block weights must be 16-byte aligned");
+  return Status::ok();
+}
+
+// One sample's block with int8 products: every GEMM reads rows that were quantised as they came, the
+// modulated ones in the LN kernel, attention's and the MLP's hidden rows in a pass of their own.
+static Status block_rows_i8(const Geo& g, const dc_block_weights* bw, const dc_block_ext& e, const float* mod,
+                            float* hb, const Workspace& L, void* ws, hipStream_t s) {
+  const int N = g.N, d = g.d, F = g.F;
+  const float *shift1 = mod, *scale1 = mod + d, *gate1 = mod + 2 * d;
+  const float *shift2 = mod + 3 * d, *scale2 = mod + 4 * d, *gate2 = mod + 5 * d;
+  const dc_block_weights_i8& w = *e.i8;
+  int8_t* q = at<int8_t>(ws, L.q8);
+  float* qs = at<float>(ws, L.q8_scale);
+  uint16_t* qk = at<uint16_t>(ws, L.qk);
+  uint16_t* vt = at<uint16_t>(ws, L.vt);
+  uint16_t* o = at<uint16_t>(ws, L.o);
+  uint16_t* ff = at<uint16_t>(ws, L.ff);
+  const LinearI8 out{q, qs, d, w.w_o, w.s_o, d, N, d, d, bw->b_o, false, gate1, hb, d, hb, d, false};
+  const LinearI8 up{q, qs, d, w.w_1, w.s_1, d, N, F, d, bw->b_1, true, nullptr, nullptr, 0, ff, F, true};
+  const LinearI8 down{q, qs, F, w.w_2, w.s_2, F, N, d, F, bw->b_2, false, gate2, hb, d, hb, d, false};
+  const float qsc = attention_q_scale(g.Dh);
+  { ProfScope ps(KClass::kQuantize, s); DC_TRY(ln_modulate_i8(hb, N, shift1, scale1, q, qs, g, s)); }
+  {
+    ProfScope ps(KClass::kGemmQKV, s);
+    DC_TRY(gemm_i8_qkv(q, qs, w.w_qkv, w.s_qkv, bw->b_qkv, qk, vt, L.ldv, e.qk ? 1.f : qsc, g, N, s));
+  }
+  if (e.qk) DC_TRY(qk_in_place(g, *e.qk, qk, 2 * d, qsc, s));
+  {
+    ProfScope ps(KClass::kAttention, s);
+    DC_TRY(attention_bf16(qk, vt, L.ldv, o, g, N, at<float>(ws, L.attn_part), L.attn_part_bytes, s));
+  }
+  { ProfScope ps(KClass::kQuantize, s); DC_TRY(quantize_rows(o, true, d, N, d, q, d, qs, s)); }
+  { ProfScope ps(KClass::kGemmOut, s); DC_TRY(gemm_i8_linear(out, s)); }
+  { ProfScope ps(KClass::kQuantize, s); DC_TRY(ln_modulate_i8(hb, N, shift2, scale2, q, qs, g, s)); }
+  { ProfScope ps(KClass::kGemmUp, s); DC_TRY(gemm_i8_linear(up, s)); }
+  { ProfScope ps(KClass::kQuantize, s); DC_TRY(quantize_rows(ff, true, F, N, F, q, F, qs, s)); }
+  { ProfScope ps(KClass::kGemmDown, s); DC_TRY(gemm_i8_linear(down, s)); }
+  return Status::ok();
+}
+
+Status block_forward(const Geo& g, const dc_block_weights* bw, const dc_block_ext* ext, const float* mod, float* h,
                      const IdxList& il, void* ws, size_t ws_bytes, hipStream_t s) {
   if (!bw || !mod || !h) return Status::arg("NULL argument");
-  if (!bw->w_qkv || !bw->b_qkv || !bw->w_o || !bw->b_o || !bw->w_1 || !bw->b_1 || !bw->w_2 || !bw->b_2)
-    return Status::arg("block weight pointer is NULL");
+  const dc_block_ext e = ext ? *ext : dc_block_ext{};
+  DC_TRY(check_ext(g, e));
+  if (!e.i8 && (!bw->w_qkv || !bw->w_o || !bw->w_1 || !bw->w_2)) return Status::arg("block weight pointer is NULL");
+  if (!bw->b_qkv || !bw->b_o || !bw->b_1 || !bw->b_2) return Status::arg("block weight pointer is NULL");
   Workspace L;
-  DC_TRY(check_ws(g, max_index(il) + 1, ws, ws_bytes, L));
+  DC_TRY(check_ws(g, max_index(il) + 1, ws, ws_bytes, L, e.qk || e.i8));
   const int N = g.N, d = g.d, F = g.F;
   const float *shift1 = mod, *scale1 = mod + d, *gate1 = mod + 2 * d;
   const float *shift2 = mod + 3 * d, *scale2 = mod + 4 * d, *gate2 = mod + 5 * d;
   for (int i = 0; i < il.n; ++i) {
     float* hb = h + size_t(il.v[i]) * N * d;
-    if (g.bf16) {
+    if (e.i8) {
+      DC_TRY(block_rows_i8(g, bw, e, mod, hb, L, ws, s));
+    } else if (g.bf16) {
       uint16_t* a = at<uint16_t>(ws, L.a);
       uint16_t* qk = at<uint16_t>(ws, L.qk);
       uint16_t* vt = at<uint16_t>(ws, L.vt);
@@ -180,7 +255,12 @@ Status block_forward(const Geo& g, const dc_block_weights* bw, const float* mod,
       uint16_t* ff = at<uint16_t>(ws, L.ff);
       const uint16_t* wqkv = static_cast<const uint16_t*>(bw->w_qkv);
       { ProfScope ps(KClass::kLnModulate, s); DC_TRY(ln_modulate(hb, N, d, shift1, scale1, a, d, true, g, s)); }
-      { ProfScope ps(KClass::kGemmQKV, s); DC_TRY(gemm_bf16_qkv(a, wqkv, bw->b_qkv, qk, vt, L.ldv, g, N, s)); }
+      {
+        ProfScope ps(KClass::kGemmQKV, s);
+        const float qsc = attention_q_scale(g.Dh);
+        DC_TRY(gemm_bf16_qkv(a, wqkv, bw->b_qkv, qk, vt, L.ldv, e.qk ? 1.f : qsc, g, N, s));
+        if (e.qk) DC_TRY(qk_in_place(g, *e.qk, qk, 2 * d, qsc, s));
+      }
       {
         ProfScope ps(KClass::kAttention, s);
         DC_TRY(attention_bf16(qk, vt, L.ldv, o, g, N, at<float>(ws, L.attn_part), L.attn_part_bytes, s));
@@ -208,6 +288,7 @@ Status block_forward(const Geo& g, const dc_block_weights* bw, const float* mod,
       DC_TRY(ln_modulate(hb, N, d, shift1, scale1, a, d, false, g, s));
       DC_TRY(gemm_f32_bias_act(a, d, static_cast<const float*>(bw->w_qkv), d, bw->b_qkv, qkv, 3 * d, N,
                                3 * d, d, Act::kNone, s));
+      if (e.qk) DC_TRY(qk_in_place(g, *e.qk, qkv, 3 * d, 1.f, s));
       DC_TRY(attention_f32(qkv, o, g, N, s));
       DC_TRY(gemm_f32_gate_residual(o, d, static_cast<const float*>(bw->w_o), d, bw->b_o, gate1, hb,
                                     d, N, d, d, s));
@@ -261,15 +342,6 @@ Status drift_call(const Geo& g, const float* h_in, const float* mod0, void* u_re
 
 using namespace dc;
 
-#define DC_ENTRY(body)                                             \
-  try {                                                            \
-    ::dc::Status st_ = (body);                                     \
-    if (!st_) return ::dc::fail(st_);                              \
-    return DC_OK;                                                  \
-  } catch (const std::exception& ex_) {                            \
-    return ::dc::fail(Status::arg(std::string("exception: ") + ex_.what())); \
-  }
-
 extern "C" {
 
 const char* dc_last_error(void) { return g_last_error.c_str(); }
@@ -309,7 +381,137 @@ dc_status dc_block_forward(const dc_model_cfg* cfg, const dc_block_weights* blk,
     IdxList il;
     DC_TRY(make_geo(cfg, g));
     DC_TRY(make_idx(idx, n, il));
-    return block_forward(g, blk, mod, h, il, ws, ws_bytes, stream);
+    return block_forward(g, blk, nullptr, mod, h, il, ws, ws_bytes, stream);
+  })());
+}
+
+size_t dc_block_ext_workspace_bytes(const dc_model_cfg* cfg, int32_t batch) {
+  Geo g;
+  if (!make_geo(cfg, g) || batch < 1 || batch > DC_MAX_BATCH) return 0;
+  return workspace_layout(g, batch).total_ext;
+}
+
+dc_status dc_block_forward_ext(const dc_model_cfg* cfg, const dc_block_weights* blk, const dc_block_ext* ext,
+                               const float* mod, float* h, const int32_t* idx, int32_t n, void* ws,
+                               size_t ws_bytes, hipStream_t stream) {
+  DC_ENTRY(([&]() -> Status {
+    Geo g;
+    IdxList il;
+    DC_TRY(make_geo(cfg, g));
+    DC_TRY(make_idx(idx, n, il));
+    return block_forward(g, blk, ext, mod, h, il, ws, ws_bytes, stream);
+  })());
+}
+
+dc_status dc_rope_table(const dc_model_cfg* cfg, const dc_rope_axes* axes, const double* pos, float* cos_sin,
+                        hipStream_t stream) {
+  DC_ENTRY(([&]() -> Status {
+    Geo g;
+    DC_TRY(make_geo(cfg, g));
+    if (!axes || !cos_sin) return Status::arg("NULL argument");
+    int64_t sum = 0;
+    for (int a = 0; a < 3; ++a) {
+      if (axes->dim[a] < 0 || axes->dim[a] % 2) return Status::arg("axes->dim must be even and >= 0");
+      sum += axes->dim[a];
+      if (!pos && !(std::isfinite(axes->start[a]) && std::isfinite(axes->step[a])))
+        return Status::arg("axes->start and axes->step must be finite");
+    }
+    if (sum > g.Dh) return Status::arg("axes->dim add up to more than head_dim");
+    if (!(axes->theta > 0.0 && std::isfinite(axes->theta))) return Status::arg("axes->theta must be positive");
+    if (reinterpret_cast<uintptr_t>(cos_sin) % 8 || reinterpret_cast<uintptr_t>(pos) % 8)
+      return Status::arg("cos_sin and pos must be 8-byte aligned");
+    return rope_table(*axes, pos, cos_sin, g, stream);
+  })());
+}
+
+dc_status dc_qk_norm_rope(const dc_model_cfg* cfg, const dc_qk_cfg* qk, const void* in, int64_t ld_in, void* out,
+                          int64_t ld_out, float q_scale, const int32_t* idx, int32_t n, hipStream_t stream) {
+  DC_ENTRY(([&]() -> Status {
+    Geo g;
+    IdxList il;
+    DC_TRY(make_geo(cfg, g));
+    DC_TRY(make_idx(idx, n, il));
+    if (!qk || !in || !out) return Status::arg("NULL argument");
+    DC_TRY(check_qk(*qk));
+    const int ve = g.bf16 ? 8 : 4;
+    if (ld_in < 2 * g.d || ld_out < 2 * g.d || ld_in % ve || ld_out % ve)
+      return Status::arg("ld_in and ld_out must be at least 2 * hidden and multiples of 16 bytes");
+    if (!aligned16(in) || !aligned16(out) || reinterpret_cast<uintptr_t>(qk->cos_sin) % 8)
+      return Status::arg("in and out must be 16-byte, cos_sin 8-byte aligned");
+    if (in == out && ld_in != ld_out) return Status::arg("in place: ld_in and ld_out must be equal");
+    if (il.n == 0) return Status::ok();
+    ProfScope ps(KClass::kQkNormRope, stream);
+    return qk_norm_rope(*qk, in, ld_in, out, ld_out, q_scale, il, g, stream);
+  })());
+}
+
+dc_status dc_quantize_rows(const void* x, int32_t dtype, int64_t ld_x, int32_t rows, int32_t cols, int8_t* q,
+                           int64_t ld_q, float* scale, hipStream_t stream) {
+  DC_ENTRY(([&]() -> Status {
+    if (dtype != DC_F32 && dtype != DC_BF16) return Status::make(DC_ERR_DTYPE, "unknown dtype");
+    if (rows < 0 || rows >= (1 << 24) || cols < 1) return Status::arg("rows must be in [0, 2^24), cols positive");
+    if (rows == 0) return Status::ok();
+    if (!x || !q || !scale) return Status::arg("NULL argument");
+    if (ld_x < cols || ld_q < (int64_t(cols) + 127) / 128 * 128)
+      return Status::arg("ld_x must be at least cols, ld_q at least cols rounded up to 128");
+    if (reinterpret_cast<uintptr_t>(x) % (dtype == DC_BF16 ? 2 : 4)) return Status::arg("x is not element-aligned");
+    ProfScope ps(KClass::kQuantize, stream);
+    return quantize_rows(x, dtype == DC_BF16, ld_x, rows, cols, q, ld_q, scale, stream);
+  })());
+}
+
+dc_status dc_linear_i8(const dc_linear_i8_args* p, hipStream_t stream) {
+  DC_ENTRY(([&]() -> Status {
+    if (!p) return Status::arg("NULL argument");
+    if (p->out_dtype != DC_F32 && p->out_dtype != DC_BF16) return Status::make(DC_ERR_DTYPE, "unknown dtype");
+    if (p->rows < 0 || p->out_features < 1) return Status::arg("rows must be >= 0, out_features positive");
+    if (p->gelu != 0 && p->gelu != 1) return Status::arg("gelu must be 0 or 1");
+    if (!p->gate != !p->residual) return Status::arg("gate and residual go together");
+    if (p->gate && (p->gelu || p->out_dtype != DC_F32)) return Status::arg("a gated residual has fp32 outputs and no GELU");
+    if (p->ld_out < p->out_features || (p->gate && p->ld_residual < p->out_features))
+      return Status::arg("ld_out and ld_residual must be at least out_features");
+    if (p->rows == 0) return Status::ok();
+    if (!p->x || !p->x_scale || !p->w || !p->w_scale || !p->out) return Status::arg("NULL argument");
+    if (!aligned16(p->x) || !aligned16(p->w)) return Status::arg("x and w must be 16-byte aligned");
+    if (p->gate && p->residual == p->out && p->ld_residual != p->ld_out)
+      return Status::arg("in place: ld_residual and ld_out must be equal");
+    return gemm_i8_linear({p->x, p->x_scale, p->ld_x, p->w, p->w_scale, p->ld_w, p->rows, p->out_features,
+                           p->in_features, p->bias, p->gelu != 0, p->gate, p->residual, p->ld_residual, p->out,
+                           p->ld_out, p->out_dtype == DC_BF16}, stream);
+  })());
+}
+
+dc_status dc_cache_store_q(const dc_model_cfg* cfg, int32_t bits, const float* h_out, const float* h_in, void* codes,
+                           float* scales, const int32_t* idx, int32_t n, hipStream_t stream) {
+  DC_ENTRY(([&]() -> Status {
+    Geo g;
+    IdxList il;
+    DC_TRY(make_geo(cfg, g));
+    DC_TRY(make_idx(idx, n, il));
+    if (bits != 8 && bits != 4) return Status::arg("bits must be 8 or 4");
+    if (!h_out || !h_in || !codes || !scales) return Status::arg("NULL argument");
+    if (!aligned16(h_out) || !aligned16(h_in) || !aligned16(codes) || !aligned16(scales))
+      return Status::arg("device pointers must be 16-byte aligned");
+    if (il.n == 0) return Status::ok();
+    ProfScope ps(KClass::kCacheStore, stream);
+    return cache_store_q(h_out, h_in, bits, codes, scales, il, g, stream);
+  })());
+}
+
+dc_status dc_cache_apply_q(const dc_model_cfg* cfg, int32_t bits, const float* h_in, const void* codes,
+                           const float* scales, float* gout, const int32_t* idx, int32_t n, hipStream_t stream) {
+  DC_ENTRY(([&]() -> Status {
+    Geo g;
+    IdxList il;
+    DC_TRY(make_geo(cfg, g));
+    DC_TRY(make_idx(idx, n, il));
+    if (bits != 8 && bits != 4) return Status::arg("bits must be 8 or 4");
+    if (!h_in || !codes || !scales || !gout) return Status::arg("NULL argument");
+    if (!aligned16(h_in) || !aligned16(gout) || !aligned16(codes) || !aligned16(scales))
+      return Status::arg("device pointers must be 16-byte aligned");
+    if (il.n == 0) return Status::ok();
+    ProfScope ps(KClass::kCacheApply, stream);
+    return cache_apply_q(h_in, bits, codes, scales, gout, il, g, stream);
   })());
 }
 

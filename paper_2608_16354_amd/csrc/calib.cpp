@@ -33,7 +33,7 @@ Status time_modulation(const Geo& g, const dc_model_weights* w, const double* si
                        float* mod, void* ws, size_t ws_bytes, hipStream_t s);
 Status patch_embed(const Geo& g, const dc_model_weights* w, const float* x, const float* txt,
                    float* h_in, const IdxList& il, void* ws, size_t ws_bytes, hipStream_t s);
-Status block_forward(const Geo& g, const dc_block_weights* bw, const float* mod, float* h,
+Status block_forward(const Geo& g, const dc_block_weights* bw, const dc_block_ext* ext, const float* mod, float* h,
                      const IdxList& il, void* ws, size_t ws_bytes, hipStream_t s);
 Status head_euler(const Geo& g, const dc_model_weights* w, const float* head_mod, const float* gin,
                   float* x, float dsigma, const IdxList& il, void* ws, size_t ws_bytes,
@@ -118,7 +118,7 @@ struct Calib {
       DC_TRY(ln_modulate(F(L.h_in), g.Nv, g.d, mk, mk + g.d, u_at(k), g.d, false, g, s));
       DC_TRY(copy_rows(F(L.h_in), F(L.h), size_t(g.N) * g.d, s));
       for (int l = 0; l < g.L; ++l)
-        DC_TRY(block_forward(g, &w->blocks[l], mk + size_t(l) * 6 * g.d, F(L.h), one, blk(), L.blk_bytes, s));
+        DC_TRY(block_forward(g, &w->blocks[l], nullptr, mk + size_t(l) * 6 * g.d, F(L.h), one, blk(), L.blk_bytes, s));
       DC_TRY(lincomb(r_at(k), F(L.h), 1.0f, F(L.h_in), -1.0f, size_t(g.Nv) * g.d, s));   // r = h_out - h_in
       DC_HIP(hipMemcpyAsync(x_at(k + 1), x_at(k), lat * 4, hipMemcpyDeviceToDevice, s));
       DC_TRY(head_euler(g, w, mk + size_t(g.L) * 6 * g.d, F(L.h), x_at(k + 1), dsig(k), one, blk(),

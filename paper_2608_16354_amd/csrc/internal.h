@@ -2,7 +2,9 @@
 #pragma once
 
 #include <cstdint>
+#include <exception>
 #include <string>
+#include <type_traits>
 #include <vector>
 
 #include <hip/hip_runtime.h>
@@ -69,7 +71,8 @@ Status make_geo(const dc_model_cfg* cfg, Geo& g);
 
 // Kernel classes that can be timed (dc_profile_*); the numbering is part of the ABI.
 enum class KClass { kAttention = 0, kGemmQKV, kGemmOut, kGemmUp, kGemmDown, kLnModulate,
-                    kPatchEmbed, kDrift, kCacheStore, kCacheApply, kHead, kHeadReuse, kCount };
+                    kPatchEmbed, kDrift, kCacheStore, kCacheApply, kHead, kHeadReuse, kQkNormRope,
+                    kQuantize, kCount };
 
 // RAII: brackets the launches made in its scope with events when the class is enabled.
 class ProfScope {
@@ -95,6 +98,7 @@ Status make_idx(const int32_t* idx, int32_t n, IdxList& out);
 // Workspace layout (offsets in bytes, each 256-aligned).
 struct Workspace {
   size_t a, qk, vt, o, ff, drift_part, attn_part, attn_part_bytes, tm_e, tm_h, tm_c, tm_s, tm_m, total;
+  size_t q8, q8_scale, total_ext;   // extended blocks: int8 rows [N, max(d, F)] and their scales
   int ldv;               // row stride of the transposed value buffer (tokens, padded)
 };
 Workspace workspace_layout(const Geo& g, int batch);
@@ -108,6 +112,27 @@ constexpr int kDriftBlocks = 1024;  // fixed grid per sample: reproducible reduc
 
 // Compute units of the current device (looked up once per device); 0 if there is none.
 int compute_units();
+
+// For row kernels: calls f(std::integral_constant<int, NV>) with NV = ceil(d / 256) float4 per lane.
+template <class F>
+Status with_nv(int d, F&& f) {
+  switch ((d + 255) / 256) {
+    case 1: f(std::integral_constant<int, 1>{}); break;
+    case 2: f(std::integral_constant<int, 2>{}); break;
+    case 3: f(std::integral_constant<int, 3>{}); break;
+    case 4: f(std::integral_constant<int, 4>{}); break;
+    case 5: f(std::integral_constant<int, 5>{}); break;
+    case 6: f(std::integral_constant<int, 6>{}); break;
+    case 7: f(std::integral_constant<int, 7>{}); break;
+    case 8: f(std::integral_constant<int, 8>{}); break;
+    case 9: f(std::integral_constant<int, 9>{}); break;
+    case 10: f(std::integral_constant<int, 10>{}); break;
+    case 11: f(std::integral_constant<int, 11>{}); break;
+    case 12: f(std::integral_constant<int, 12>{}); break;
+    default: return Status::shape("row kernels support hidden sizes up to 3072");
+  }
+  return Status::ok();
+}
 
 // ---------------------------------------------------------------------------
 // kernel launchers (kernels_*.hip, gemm.hip, attention.hip)
@@ -140,8 +165,10 @@ Status gemm_f32_head_tangents(const float* A, const void* W, bool w_bf16, float*
 
 // bf16 MFMA GEMM variants.  block_gemm_tile: which of its six tiles a call takes (gemm.hip, kTiles).
 int block_gemm_tile(int M, int N, int K, int cus);
+// Q leaves times q_scale.
+float attention_q_scale(int head_dim);      // log2(e) / sqrt(head_dim), what the bf16 attention expects
 Status gemm_bf16_qkv(const uint16_t* A, const uint16_t* W, const float* bias, uint16_t* qk,
-                     uint16_t* vt, int ldv, const Geo& g, int M, hipStream_t s);
+                     uint16_t* vt, int ldv, float q_scale, const Geo& g, int M, hipStream_t s);
 Status gemm_bf16_gate_residual(const uint16_t* A, int lda, const uint16_t* W, const float* bias,
                                const float* gate, float* h, int ldh, int M, int N, int K,
                                hipStream_t s);
@@ -188,6 +215,38 @@ Status drift(const float* h_in, const float* mod0, void* u_ref, bool snapshot, d
 Status drift_noalloc(const float* h_in, const float* mod0, void* u_ref, bool snapshot, double* sums,
                      const IdxList& idx, const Geo& g, hipStream_t s);
 
+// Rotary table [Nv, Dh / 2, 2] from the latent's grid or given positions (f64 [Nv, 3]); norms and
+// rotation of Q | K at columns [0, 2d) of in [B, N, ld_in] (rope.hip).
+Status rope_table(const dc_rope_axes& ax, const double* pos, float* table, const Geo& g, hipStream_t s);
+Status qk_norm_rope(const dc_qk_cfg& c, const void* in, int64_t ld_in, void* out, int64_t ld_out, float q_scale,
+                    const IdxList& idx, const Geo& g, hipStream_t s);
+
+// int8 rows with a scale each (quant.hip) and their products (gemm_i8.hip).
+Status quantize_rows(const void* x, bool bf16, int64_t ldx, int rows, int cols, int8_t* q, int64_t ldq, float* scale,
+                     hipStream_t s);
+// quantised LN(x)(1 + scale) + shift: q [rows, d], q_scale [rows]
+Status ln_modulate_i8(const float* x, int rows, const float* shift, const float* scale, int8_t* q, float* q_scale,
+                      const Geo& g, hipStream_t s);
+struct LinearI8 {
+  const int8_t* x; const float* x_scale; int64_t ld_x;
+  const int8_t* w; const float* w_scale; int64_t ld_w;
+  int M, N, K;
+  const float* bias;                                            // or NULL
+  bool gelu;
+  const float* gate; const float* residual; int64_t ld_residual;   // gate NULL: no residual
+  void* out; int64_t ld_out; bool out_bf16;
+};
+Status gemm_i8_linear(const LinearI8& a, hipStream_t s);
+Status gemm_i8_qkv(const int8_t* A, const float* sx, const int8_t* W, const float* sw, const float* bias,
+                   uint16_t* qk, uint16_t* vt, int ldv, float q_scale, const Geo& g, int M, hipStream_t s);
+
+// The residual cache in 8 or 4 bits (quant.hip).
+constexpr int kCacheGroup = 64;
+Status cache_store_q(const float* h_out, const float* h_in, int bits, void* codes, float* scales, const IdxList& idx,
+                     const Geo& g, hipStream_t s);
+Status cache_apply_q(const float* h_in, int bits, const void* codes, const float* scales, float* gout,
+                     const IdxList& idx, const Geo& g, hipStream_t s);
+
 // Anchor calibration (Eq. 5-7): tangent-mode kernels of the fp32 network (calib.hip) and the
 // driver (calib.cpp).  Activations are stacked: the primal [rows], then n tangents [rows] each.
 constexpr int kMaxTangents = 32;
@@ -225,4 +284,15 @@ Status time_features(const double* sig, int K, float* e, int n_freq, hipStream_t
 Status assemble_modulation(const float* m, const float* c, const float* const* offsets,
                            const float* head_mod, int K, const Geo& g, float* mod, hipStream_t s);
 
+dc_status fail(const Status& s);         // keeps the message for dc_last_error(), returns the code
+
 }  // namespace dc
+
+#define DC_ENTRY(body)                                             \
+  try {                                                            \
+    ::dc::Status st_ = (body);                                     \
+    if (!st_) return ::dc::fail(st_);                              \
+    return DC_OK;                                                  \
+  } catch (const std::exception& ex_) {                            \
+    return ::dc::fail(::dc::Status::arg(std::string("exception: ") + ex_.what())); \
+  }

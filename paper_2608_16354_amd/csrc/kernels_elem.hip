@@ -305,27 +305,6 @@ inline int grid_for(size_t n, int per_block, int cap) {
 
 #define DC_LAUNCH_CHECK() DC_HIP(hipGetLastError())
 
-// Calls f(std::integral_constant<int, NV>) with NV = ceil(d / 256) float4 per lane.
-template <class F>
-Status with_nv(int d, F&& f) {
-  switch ((d + 255) / 256) {
-    case 1: f(std::integral_constant<int, 1>{}); break;
-    case 2: f(std::integral_constant<int, 2>{}); break;
-    case 3: f(std::integral_constant<int, 3>{}); break;
-    case 4: f(std::integral_constant<int, 4>{}); break;
-    case 5: f(std::integral_constant<int, 5>{}); break;
-    case 6: f(std::integral_constant<int, 6>{}); break;
-    case 7: f(std::integral_constant<int, 7>{}); break;
-    case 8: f(std::integral_constant<int, 8>{}); break;
-    case 9: f(std::integral_constant<int, 9>{}); break;
-    case 10: f(std::integral_constant<int, 10>{}); break;
-    case 11: f(std::integral_constant<int, 11>{}); break;
-    case 12: f(std::integral_constant<int, 12>{}); break;
-    default: return Status::shape("row kernels support hidden sizes up to 3072");
-  }
-  return Status::ok();
-}
-
 Status ln_modulate(const float* x, int rows, int ldx, const float* shift, const float* scale,
                    void* out, int ldo, bool out_bf16, const Geo& g, hipStream_t s) {
   if (rows <= 0) return Status::ok();

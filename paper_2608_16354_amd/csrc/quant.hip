@@ -1,0 +1,359 @@
+// Rows and cache groups in 8 or 4 bits.
+//
+// A row (or a group of 64 features of the residual cache) with largest magnitude a is held as codes
+// q = rint(x / s), s = a / L (L = 127, or 7 for 4 bits), both divisions as IEEE fp32 rounds them, so the
+// codes are a function of the inputs alone.  s = 0 (all zeros, or magnitudes that a / L takes below the
+// smallest fp32 number) gives codes 0; an infinity or NaN anywhere gives s = NaN and codes 0, so what
+// is read back is NaN there and not a wrong number.
+// All of it is bound by memory: one pass, the values in registers between the maximum and the codes.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "internal.h"
+
+namespace dc {
+
+namespace {
+
+constexpr int kWave = 64;
+constexpr uint32_t kInfBits = 0x7F800000u;
+
+__device__ inline float from_bf16(uint16_t u) { return __uint_as_float(uint32_t(u) << 16); }
+
+// |x| as an integer: ordered as the magnitudes are, infinities and then NaN above all numbers
+__device__ inline uint32_t mag(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+__device__ inline uint32_t wave_max(uint32_t v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = max(v, uint32_t(__shfl_xor(int(v), o, kWave)));
+  return v;
+}
+// maximum over the 16 lanes of a row of the wave (DPP rotations of 8, 4, 2 and 1)
+__device__ inline uint32_t row16_max(uint32_t v) {
+  v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x128, 0xF, 0xF, true)));
+  v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x124, 0xF, 0xF, true)));
+  v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x122, 0xF, 0xF, true)));
+  return max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x121, 0xF, 0xF, true)));
+}
+
+// the scale of a row or group whose largest magnitude is `m` (as mag() gives it)
+__device__ inline float scale_of(uint32_t m, float levels) {
+  return m >= kInfBits ? __uint_as_float(0x7FC00000u) : __uint_as_float(m) / levels;
+}
+// x's code under scale s: 0 where s is 0 or NaN.  The bound only matters where s is so small that
+// it has lost bits.
+__device__ inline int code_of(float x, float s, float levels) {
+  const float q = fminf(fmaxf(rintf(x / s), -levels), levels);
+  return s > 0.f ? int(q) : 0;
+}
+__device__ inline uint32_t pack4(int a, int b, int c, int d) {
+  return uint32_t(a & 255) | (uint32_t(b & 255) << 8) | (uint32_t(c & 255) << 16) | (uint32_t(d) << 24);
+}
+
+// 16 bytes of a row at any element
+typedef unsigned int u32x4a __attribute__((ext_vector_type(4), aligned(2)));
+typedef unsigned int u32x2a __attribute__((ext_vector_type(2), aligned(1)));
+typedef unsigned int u32a __attribute__((aligned(1)));
+
+template <bool BF>
+struct Piece {                         // VE consecutive values
+  static constexpr int VE = BF ? 8 : 4;
+  float v[VE];
+  __device__ void load(const void* row, int64_t e) {
+    const u32x4a w = *reinterpret_cast<const u32x4a*>(static_cast<const char*>(row) + e * (BF ? 2 : 4));
+    if constexpr (BF) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(w[i]);
+    }
+  }
+  __device__ uint32_t largest() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < VE; ++i) m = max(m, mag(v[i]));
+    return m;
+  }
+  __device__ void store(int8_t* q, float s) const {
+    int c[VE];
+#pragma unroll
+    for (int i = 0; i < VE; ++i) c[i] = code_of(v[i], s, 127.f);
+    if constexpr (BF) {
+      *reinterpret_cast<u32x2a*>(q) = u32x2a{pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7])};
+    } else {
+      *reinterpret_cast<u32a*>(q) = pack4(c[0], c[1], c[2], c[3]);
+    }
+  }
+};
+
+// zeros behind the last feature, up to a whole 128-byte block
+__device__ inline void zero_tail(int8_t* q, int cols, int at, int step) {
+  for (int i = cols + at; i < (cols + 127) / 128 * 128; i += step) q[i] = 0;
+}
+
+// WR waves to a row, NV pieces to a lane.  Pieces past the row's last re-read that one; a last piece
+// that the row does not fill starts VE before its end instead (the values it shares with the one before
+// it get the same codes twice).
+template <bool BF, int NV, int WR>
+__global__ void __launch_bounds__(256) k_quantize_rows(const void* __restrict__ x, int64_t ldx, int rows, int cols,
+                                                       int8_t* __restrict__ q, int64_t ldq,
+                                                       float* __restrict__ scale) {
+  constexpr int VE = Piece<BF>::VE, LR = WR * kWave;
+  __shared__ uint32_t s_max[4];
+  const int row = WR == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+  const int at = threadIdx.x & (LR - 1);
+  if (WR == 1 && row >= rows) return;
+  const char* const xr = static_cast<const char*>(x) + size_t(row) * ldx * (BF ? 2 : 4);
+  const int np = (cols + VE - 1) / VE;
+  Piece<BF> p[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) p[i].load(xr, min(min(at + i * LR, np - 1) * VE, cols - VE));
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) m = max(m, p[i].largest());
+  m = wave_max(m);
+  if constexpr (WR > 1) {
+    if ((threadIdx.x & 63) == 0) s_max[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
+  }
+  const float s = scale_of(m, 127.f);
+  int8_t* const qr = q + size_t(row) * ldq;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (at + i * LR < np) p[i].store(qr + min((at + i * LR) * VE, cols - VE), s);
+  zero_tail(qr, cols, at, LR);
+  if (at == 0) scale[row] = s;
+}
+
+// Rows of fewer values than a piece, or too long to stay in registers: one workgroup to a row, which
+// is read twice.
+template <bool BF>
+__global__ void __launch_bounds__(256) k_quantize_any(const void* __restrict__ x, int64_t ldx, int cols,
+                                                      int8_t* __restrict__ q, int64_t ldq,
+                                                      float* __restrict__ scale) {
+  __shared__ uint32_t s_max[4];
+  const int row = blockIdx.x, tid = threadIdx.x;
+  auto value = [&](int c) -> float {
+    if constexpr (BF) return from_bf16(static_cast<const uint16_t*>(x)[size_t(row) * ldx + c]);
+    else return static_cast<const float*>(x)[size_t(row) * ldx + c];
+  };
+  uint32_t m = 0;
+  for (int c = tid; c < cols; c += 256) m = max(m, mag(value(c)));
+  m = wave_max(m);
+  if ((tid & 63) == 0) s_max[tid >> 6] = m;
+  __syncthreads();
+  m = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
+  const float s = scale_of(m, 127.f);
+  int8_t* const qr = q + size_t(row) * ldq;
+  for (int c = tid; c < cols; c += 256) qr[c] = int8_t(code_of(value(c), s, 127.f));
+  zero_tail(qr, cols, tid, 256);
+  if (tid == 0) scale[row] = s;
+}
+
+__device__ inline float wave_sum(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+  return v;
+}
+
+// The quantised LN(x)(1 + scale) + shift, one wave to a row of NV float4 per lane: the modulated row
+// stays in registers and only its codes are written (k_ln_modulate writes bf16, which another pass
+// would read again).
+template <int NV>
+__global__ void __launch_bounds__(256) k_ln_modulate_i8(const float* __restrict__ x, int rows, int d,
+                                                        const float* __restrict__ shift,
+                                                        const float* __restrict__ scale, float eps,
+                                                        int8_t* __restrict__ q, float* __restrict__ q_scale) {
+  __shared__ float4 s_sh[NV * kWave], s_sc[NV * kWave];
+  const int n4 = d >> 2;
+  for (int i = threadIdx.x; i < n4; i += 256) {
+    s_sh[i] = reinterpret_cast<const float4*>(shift)[i];
+    s_sc[i] = reinterpret_cast<const float4*>(scale)[i];
+  }
+  const int lane = threadIdx.x & 63;
+  const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const float4* const xr = reinterpret_cast<const float4*>(x + size_t(min(row, rows - 1)) * d);
+  float4 v[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) v[i] = xr[min(lane + i * kWave, n4 - 1)];
+  __syncthreads();
+  if (row >= rows) return;
+  float sum = 0.f, sq = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) sum += lane + i * kWave < n4 ? (v[i].x + v[i].y) + (v[i].z + v[i].w) : 0.f;
+  const float mean = wave_sum(sum) / float(d);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    v[i].x -= mean; v[i].y -= mean; v[i].z -= mean; v[i].w -= mean;
+    sq += lane + i * kWave < n4 ? (v[i].x * v[i].x + v[i].y * v[i].y) + (v[i].z * v[i].z + v[i].w * v[i].w) : 0.f;
+  }
+  const float rstd = 1.0f / sqrtf(wave_sum(sq) / float(d) + eps);
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = min(lane + i * kWave, n4 - 1);
+    const float4 sh = s_sh[c], sc = s_sc[c];
+    v[i].x = v[i].x * rstd * (1.0f + sc.x) + sh.x;
+    v[i].y = v[i].y * rstd * (1.0f + sc.y) + sh.y;
+    v[i].z = v[i].z * rstd * (1.0f + sc.z) + sh.z;
+    v[i].w = v[i].w * rstd * (1.0f + sc.w) + sh.w;
+    m = max(max(m, max(mag(v[i].x), mag(v[i].y))), max(mag(v[i].z), mag(v[i].w)));
+  }
+  const float s = scale_of(wave_max(m), 127.f);
+  uint32_t* const qr = reinterpret_cast<uint32_t*>(q + size_t(row) * d);
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (lane + i * kWave < n4)
+      qr[lane + i * kWave] = pack4(code_of(v[i].x, s, 127.f), code_of(v[i].y, s, 127.f), code_of(v[i].z, s, 127.f),
+                                   code_of(v[i].w, s, 127.f));
+  if (lane == 0) q_scale[row] = s;
+}
+
+// ---------------------------------------------------------------------------
+// the residual cache in groups of 64 features: 16 lanes of four
+// ---------------------------------------------------------------------------
+template <int BITS>
+struct Codes {                         // four features of a lane
+  typedef typename std::conditional<BITS == 8, uint32_t, uint16_t>::type T;
+  static constexpr float L = BITS == 8 ? 127.f : 7.f;
+  static __device__ T pack(int a, int b, int c, int d) {
+    if constexpr (BITS == 8) return pack4(a, b, c, d);
+    else return T((a & 15) | ((b & 15) << 4) | ((c & 15) << 8) | ((d & 15) << 12));
+  }
+  static __device__ float4 unpack(T t) {
+    const int w = BITS == 8 ? int(t) : int(t) << 16;
+    if constexpr (BITS == 8)
+      return make_float4(float(w << 24 >> 24), float(w << 16 >> 24), float(w << 8 >> 24), float(w >> 24));
+    else
+      return make_float4(float(w << 12 >> 28), float(w << 8 >> 28), float(w << 4 >> 28), float(w >> 28));
+  }
+};
+
+// codes and scales of r = h_out - h_in on the video rows (n4 float4 a sample, a multiple of 32)
+template <int BITS>
+__global__ void __launch_bounds__(256) k_cache_store_q(const float* __restrict__ h_out,
+                                                       const float* __restrict__ h_in,
+                                                       typename Codes<BITS>::T* __restrict__ codes,
+                                                       float* __restrict__ scales, IdxList idx, size_t n4,
+                                                       size_t stride_h4) {
+  typedef Codes<BITS> C;
+  const int b = idx.v[blockIdx.y];
+  const float4* const ho = reinterpret_cast<const float4*>(h_out) + size_t(b) * stride_h4;
+  const float4* const hi = reinterpret_cast<const float4*>(h_in) + size_t(b) * stride_h4;
+  const size_t base = size_t(b) * n4;
+  for (size_t i = size_t(blockIdx.x) * 256 + threadIdx.x; i < n4; i += size_t(gridDim.x) * 256) {
+    const float4 a = ho[i], c = hi[i];
+    const float x = a.x - c.x, y = a.y - c.y, z = a.z - c.z, w = a.w - c.w;
+    const float s = scale_of(row16_max(max(max(mag(x), mag(y)), max(mag(z), mag(w)))), C::L);
+    codes[base + i] = C::pack(code_of(x, s, C::L), code_of(y, s, C::L), code_of(z, s, C::L), code_of(w, s, C::L));
+    if ((i & 15) == 0) scales[(base + i) >> 4] = s;
+  }
+}
+
+// g = h_in + codes * scale on the video rows (g may be h_in: a thread reads what it writes)
+template <int BITS>
+__global__ void __launch_bounds__(256) k_cache_apply_q(const float* h_in,
+                                                       const typename Codes<BITS>::T* __restrict__ codes,
+                                                       const float* __restrict__ scales, float* g,
+                                                       IdxList idx, size_t n4, size_t stride_h4) {
+  const int b = idx.v[blockIdx.y];
+  const float4* const hi = reinterpret_cast<const float4*>(h_in) + size_t(b) * stride_h4;
+  float4* const go = reinterpret_cast<float4*>(g) + size_t(b) * stride_h4;
+  const size_t base = size_t(b) * n4;
+  for (size_t i = size_t(blockIdx.x) * 256 + threadIdx.x; i < n4; i += size_t(gridDim.x) * 256) {
+    const float4 a = hi[i], r = Codes<BITS>::unpack(codes[base + i]);
+    const float s = scales[(base + i) >> 4];
+    go[i] = make_float4(a.x + r.x * s, a.y + r.y * s, a.z + r.z * s, a.w + r.w * s);
+  }
+}
+
+template <bool BF>
+Status quantize(const void* x, int64_t ldx, int rows, int cols, int8_t* q, int64_t ldq, float* scale, hipStream_t s) {
+  constexpr int VE = Piece<BF>::VE;
+  const int np = (cols + VE - 1) / VE;
+  if (cols < VE || np > 8 * 256) {
+    hipLaunchKernelGGL(k_quantize_any<BF>, dim3(rows), dim3(256), 0, s, x, ldx, cols, q, ldq, scale);
+    DC_HIP(hipGetLastError());
+    return Status::ok();
+  }
+  auto go = [&](auto nv, auto wr) {
+    constexpr int NV = decltype(nv)::value, WR = decltype(wr)::value;
+    hipLaunchKernelGGL((k_quantize_rows<BF, NV, WR>), dim3(WR == 1 ? (rows + 3) / 4 : rows), dim3(256), 0, s, x, ldx,
+                       rows, cols, q, ldq, scale);
+  };
+  auto with_nv = [&](int n, auto wr) {
+    if (n <= 1) go(std::integral_constant<int, 1>{}, wr);
+    else if (n <= 2) go(std::integral_constant<int, 2>{}, wr);
+    else if (n <= 3) go(std::integral_constant<int, 3>{}, wr);
+    else if (n <= 4) go(std::integral_constant<int, 4>{}, wr);
+    else if (n <= 6) go(std::integral_constant<int, 6>{}, wr);
+    else go(std::integral_constant<int, 8>{}, wr);
+  };
+  if (np <= 8 * 64) with_nv((np + 63) / 64, std::integral_constant<int, 1>{});
+  else with_nv((np + 255) / 256, std::integral_constant<int, 4>{});
+  DC_HIP(hipGetLastError());
+  return Status::ok();
+}
+
+int grid_for(size_t n, int cap) {
+  const size_t b = (n + 255) / 256;
+  return int(b > size_t(cap) ? size_t(cap) : b);
+}
+
+}  // namespace
+
+Status quantize_rows(const void* x, bool bf16, int64_t ldx, int rows, int cols, int8_t* q, int64_t ldq, float* scale,
+                     hipStream_t s) {
+  if (rows <= 0) return Status::ok();
+  return bf16 ? quantize<true>(x, ldx, rows, cols, q, ldq, scale, s)
+              : quantize<false>(x, ldx, rows, cols, q, ldq, scale, s);
+}
+
+Status ln_modulate_i8(const float* x, int rows, const float* shift, const float* scale, int8_t* q, float* q_scale,
+                      const Geo& g, hipStream_t s) {
+  if (rows <= 0) return Status::ok();
+  DC_TRY(with_nv(g.d, [&](auto nv) {
+    hipLaunchKernelGGL(k_ln_modulate_i8<decltype(nv)::value>, dim3((rows + 3) / 4), dim3(256), 0, s, x, rows, g.d,
+                       shift, scale, g.eps, q, q_scale);
+  }));
+  DC_HIP(hipGetLastError());
+  return Status::ok();
+}
+
+Status cache_store_q(const float* h_out, const float* h_in, int bits, void* codes, float* scales, const IdxList& idx,
+                     const Geo& g, hipStream_t s) {
+  const size_t n4 = size_t(g.Nv) * g.d / 4, sh4 = size_t(g.N) * g.d / 4;
+  if (n4 == 0) return Status::ok();
+  const dim3 grid(grid_for(n4, 4096), idx.n);
+  if (bits == 8)
+    hipLaunchKernelGGL(k_cache_store_q<8>, grid, dim3(256), 0, s, h_out, h_in, static_cast<uint32_t*>(codes), scales,
+                       idx, n4, sh4);
+  else
+    hipLaunchKernelGGL(k_cache_store_q<4>, grid, dim3(256), 0, s, h_out, h_in, static_cast<uint16_t*>(codes), scales,
+                       idx, n4, sh4);
+  DC_HIP(hipGetLastError());
+  return Status::ok();
+}
+
+Status cache_apply_q(const float* h_in, int bits, const void* codes, const float* scales, float* gout,
+                     const IdxList& idx, const Geo& g, hipStream_t s) {
+  const size_t n4 = size_t(g.Nv) * g.d / 4, sh4 = size_t(g.N) * g.d / 4;
+  if (n4 == 0) return Status::ok();
+  const dim3 grid(grid_for(n4, 4096), idx.n);
+  if (bits == 8)
+    hipLaunchKernelGGL(k_cache_apply_q<8>, grid, dim3(256), 0, s, h_in, static_cast<const uint32_t*>(codes), scales,
+                       gout, idx, n4, sh4);
+  else
+    hipLaunchKernelGGL(k_cache_apply_q<4>, grid, dim3(256), 0, s, h_in, static_cast<const uint16_t*>(codes), scales,
+                       gout, idx, n4, sh4);
+  DC_HIP(hipGetLastError());
+  return Status::ok();
+}
+
+}  // namespace dc

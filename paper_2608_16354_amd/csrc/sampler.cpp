@@ -27,16 +27,36 @@ Status time_modulation(const Geo& g, const dc_model_weights* w, const double* si
                        float* mod, void* ws, size_t ws_bytes, hipStream_t s);
 Status patch_embed(const Geo& g, const dc_model_weights* w, const float* x, const float* txt,
                    float* h_in, const IdxList& il, void* ws, size_t ws_bytes, hipStream_t s);
-Status block_forward(const Geo& g, const dc_block_weights* bw, const float* mod, float* h,
+Status block_forward(const Geo& g, const dc_block_weights* bw, const dc_block_ext* ext, const float* mod, float* h,
                      const IdxList& il, void* ws, size_t ws_bytes, hipStream_t s);
 Status head_euler(const Geo& g, const dc_model_weights* w, const float* head_mod, const float* gin,
                   float* x, float dsigma, const IdxList& il, void* ws, size_t ws_bytes,
                   hipStream_t s, const void* resid);
 Status drift_call(const Geo& g, const float* h_in, const float* mod0, void* u_ref, int snapshot,
                   double* sums, const IdxList& il, void* ws, size_t ws_bytes, hipStream_t s);
-dc_status fail(const Status& s);
+Status check_ext(const Geo& g, const dc_block_ext& e);
 
 namespace {
+
+// Deep copy of a network's block extensions (empty: none).
+struct OwnedExt {
+  std::vector<dc_block_ext> ext;
+  std::vector<dc_qk_cfg> qk;
+  std::vector<dc_block_weights_i8> i8;
+  Status assign(const Geo& g, const dc_block_ext* src) {
+    if (!src) return Status::ok();
+    ext.assign(src, src + g.L);
+    qk.resize(ext.size());
+    i8.resize(ext.size());
+    for (size_t l = 0; l < ext.size(); ++l) {
+      DC_TRY(check_ext(g, ext[l]));
+      if (ext[l].qk) { qk[l] = *ext[l].qk; ext[l].qk = &qk[l]; }
+      if (ext[l].i8) { i8[l] = *ext[l].i8; ext[l].i8 = &i8[l]; }
+    }
+    return Status::ok();
+  }
+  const dc_block_ext* at(int l) const { return ext.empty() ? nullptr : &ext[size_t(l)]; }
+};
 
 // Deep copy of one scene's scheduling problem (the caller's arrays are not kept).
 struct OwnedProblem {
@@ -82,6 +102,9 @@ struct dc_sampler {
   std::vector<dc_block_weights> blocks_low;
   int k_switch = 0;
   float* mod_low = nullptr;
+  dc::OwnedExt ext, ext_low;
+  int cache_bits = 0;                // quantised residual cache: codes in buf.resid
+  float* cache_scales = nullptr;
   bool cfg_on = false;               // guidance branches (entries B..2B-1 unconditional)
   float guidance = 1.0f;
   const float* txt_null = nullptr;
@@ -102,7 +125,7 @@ namespace {
 
 Status create(const dc_model_cfg* cfg, const dc_model_weights* w, int32_t B,
               const dc_sched_problem* problems, const double* sigmas, const dc_buffers* buf,
-              const dc_sampler_opts& o, hipStream_t stream, dc_sampler** out) {
+              const dc_sampler_opts& o, const dc_sampler_ext& x, hipStream_t stream, dc_sampler** out) {
   if (!out || !w || !problems || !sigmas || !buf) return Status::arg("NULL argument");
   *out = nullptr;
   const int32_t metric = o.drift_metric;
@@ -118,8 +141,17 @@ Status create(const dc_model_cfg* cfg, const dc_model_weights* w, int32_t B,
     return Status::arg("a device buffer is NULL");
   if (cfg_on && (!std::isfinite(o.guidance) || (s->g.Nt > 0 && !o.txt_null)))
     return Status::arg("guidance needs a finite scale and txt_null");
-  if (buf->ws_bytes < workspace_layout(s->g, cfg_on ? 2 * B : B).total)
-    return Status::make(DC_ERR_WORKSPACE, "workspace smaller than dc_workspace_bytes()");
+  if (x.cache_bits != 0 && x.cache_bits != 8 && x.cache_bits != 4) return Status::arg("cache_bits must be 0, 8 or 4");
+  if (x.cache_bits && !x.cache_scales) return Status::arg("cache_bits needs cache_scales");
+  const Workspace lay = workspace_layout(s->g, cfg_on ? 2 * B : B);
+  if (buf->ws_bytes < (x.blocks || x.blocks_low ? lay.total_ext : lay.total))
+    return Status::make(DC_ERR_WORKSPACE, "workspace smaller than dc_workspace_bytes() (with extended blocks "
+                                          "dc_block_ext_workspace_bytes())");
+  if (x.blocks_low && !o.w_low) return Status::arg("blocks_low needs w_low");
+  DC_TRY(s->ext.assign(s->g, x.blocks));
+  DC_TRY(s->ext_low.assign(s->g, x.blocks_low));
+  s->cache_bits = x.cache_bits;
+  s->cache_scales = x.cache_scales;
   if (!w->blocks) return Status::arg("weights->blocks is NULL");
   s->cfg = *cfg;
   s->blocks.assign(w->blocks, w->blocks + s->g.L);
@@ -181,6 +213,7 @@ Status step(dc_sampler* s, int k, hipStream_t st, uint8_t* realized, double* dri
   const bool low = s->two && k >= s->k_switch;
   const dc_model_weights* W = low ? &s->w_low : &s->w;
   const std::vector<dc_block_weights>& blocks = low ? s->blocks_low : s->blocks;
+  const OwnedExt& ext = low ? s->ext_low : s->ext;
   const float* mod_k = (low ? s->mod_low : bf.mod) + size_t(k - 1) * mstride;
   const size_t row_stride = size_t(g.N) * g.d;            // one entry of h_in / h
   // with guidance, scene b's unconditional branch is entry B + b of h_in, h, resid
@@ -238,22 +271,28 @@ Status step(dc_sampler* s, int k, hipStream_t st, uint8_t* realized, double* dri
     for (int b : rb)
       DC_TRY(copy_rows(bf.h_in + size_t(b) * row_stride, bf.h + size_t(b) * row_stride, row_stride, st));
     for (int l = 0; l < g.L; ++l)
-      DC_TRY(block_forward(g, &blocks[size_t(l)], mod_k + size_t(l) * 6 * g.d, bf.h, ilb, bf.ws,
+      DC_TRY(block_forward(g, &blocks[size_t(l)], ext.at(l), mod_k + size_t(l) * 6 * g.d, bf.h, ilb, bf.ws,
                            bf.ws_bytes, st));
     {
       ProfScope ps(KClass::kCacheStore, st);
-      DC_TRY(cache_store(bf.h, bf.h_in, bf.resid, ilb, g, st));
+      if (s->cache_bits)
+        DC_TRY(cache_store_q(bf.h, bf.h_in, s->cache_bits, bf.resid, s->cache_scales, ilb, g, st));
+      else
+        DC_TRY(cache_store(bf.h, bf.h_in, bf.resid, ilb, g, st));
     }
   }
   // reuse scenes: the fused bf16 head reads h_in and r itself; other models apply the
   // cache into h first
-  const bool fused_reuse = head_takes_resid(g);
+  const bool fused_reuse = head_takes_resid(g) && !s->cache_bits;
   if (!reuse.empty() && !fused_reuse) {
     IdxList il;
     const std::vector<int32_t> rb = with_branches(reuse);
     DC_TRY(make_idx(rb.data(), int(rb.size()), il));
     ProfScope ps(KClass::kCacheApply, st);
-    DC_TRY(cache_apply(bf.h_in, bf.resid, bf.h, il, g, st));
+    if (s->cache_bits)
+      DC_TRY(cache_apply_q(bf.h_in, s->cache_bits, bf.resid, s->cache_scales, bf.h, il, g, st));
+    else
+      DC_TRY(cache_apply(bf.h_in, bf.resid, bf.h, il, g, st));
   }
   // x += dsig v, with guidance v = v_u + w (v_c - v_u) = w v_c + (1 - w) v_u: the update is
   // linear in v, so each branch's head adds its share
@@ -327,7 +366,7 @@ dc_status dc_sampler_create(const dc_model_cfg* cfg, const dc_model_weights* w, 
   try {
     dc_sampler_opts o{};
     o.drift_metric = drift_metric;
-    Status st = create(cfg, w, B, problems, sigmas, buf, o, stream, out);
+    Status st = create(cfg, w, B, problems, sigmas, buf, o, dc_sampler_ext{}, stream, out);
     return st ? DC_OK : fail(st);
   } catch (const std::exception& e) {
     return fail(Status::arg(std::string("exception: ") + e.what()));
@@ -341,7 +380,20 @@ dc_status dc_sampler_create_ex(const dc_model_cfg* cfg, const dc_model_weights* 
   try {
     dc_sampler_opts o{};
     if (opts) o = *opts;
-    Status st = create(cfg, w, B, problems, sigmas, buf, o, stream, out);
+    Status st = create(cfg, w, B, problems, sigmas, buf, o, dc_sampler_ext{}, stream, out);
+    return st ? DC_OK : fail(st);
+  } catch (const std::exception& e) {
+    return fail(Status::arg(std::string("exception: ") + e.what()));
+  }
+}
+
+dc_status dc_sampler_create_ext(const dc_model_cfg* cfg, const dc_model_weights* w, int32_t B,
+                                const dc_sched_problem* problems, const double* sigmas,
+                                const dc_buffers* buf, const dc_sampler_opts* opts,
+                                const dc_sampler_ext* ext, hipStream_t stream, dc_sampler** out) {
+  try {
+    Status st = create(cfg, w, B, problems, sigmas, buf, opts ? *opts : dc_sampler_opts{},
+                       ext ? *ext : dc_sampler_ext{}, stream, out);
     return st ? DC_OK : fail(st);
   } catch (const std::exception& e) {
     return fail(Status::arg(std::string("exception: ") + e.what()));

@@ -1,0 +1,252 @@
+"""The rotary, int8 and quantised-cache entry points refuse bad arguments on the host: every call below
+ends before any device work (the pointers are never dereferenced), and the definitions they are tested
+against hold on small cases worked out by hand."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+from oracle import ext as X
+from paper_2608_16354_amd import _lib as L
+
+FAKE = 0x100000
+ARG, SHAPE, DTYPE, WS = L.DC_ERR_ARG, L.DC_ERR_SHAPE, L.DC_ERR_DTYPE, L.DC_ERR_WORKSPACE
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return L.load()
+
+
+def cfg(dtype=1, heads=4, head_dim=64, lat=(4, 16, 16), n_txt=16):
+    d = heads * head_dim
+    return L.ModelCfg(2, d, heads, head_dim, 4 * d, 16, *lat, 2, n_txt, dtype, 1e-6)
+
+
+def idx(*v):
+    return (C.c_int32 * max(len(v), 1))(*v), len(v)
+
+
+def axes(dim=(16, 24, 24), theta=1e4, start=(0.0, 0.0, 0.0), step=(1.0, 1.0, 1.0)):
+    return L.RopeAxes((C.c_int32 * 3)(*dim), theta, (C.c_double * 3)(*start), (C.c_double * 3)(*step))
+
+
+@pytest.mark.parametrize("bad", [dict(dim=(16, 24, 26)), dict(dim=(15, 24, 24)), dict(dim=(-2, 24, 24)),
+                                 dict(theta=0.0), dict(theta=math.nan), dict(theta=math.inf),
+                                 dict(start=(math.nan, 0, 0)), dict(step=(0, math.inf, 0))])
+def test_rope_table_refuses_axes(lib, bad):
+    c = cfg()
+    assert lib.dc_rope_table(C.byref(c), C.byref(axes(**bad)), None, FAKE, None) == ARG
+
+
+def test_rope_table_refuses_pointers(lib):
+    c, a = cfg(), axes()
+    assert lib.dc_rope_table(C.byref(c), None, None, FAKE, None) == ARG
+    assert lib.dc_rope_table(C.byref(c), C.byref(a), None, None, None) == ARG
+    assert lib.dc_rope_table(C.byref(c), C.byref(a), None, FAKE + 4, None) == ARG
+    assert lib.dc_rope_table(C.byref(c), C.byref(a), FAKE + 4, FAKE, None) == ARG
+    assert lib.dc_rope_table(None, C.byref(a), None, FAKE, None) == ARG
+
+
+def qk(q=FAKE, k=FAKE, eps=1e-6, table=FAKE, interleaved=1):
+    return L.QkCfg(q, k, eps, table, interleaved)
+
+
+@pytest.mark.parametrize("case", [
+    dict(qk=qk(eps=0.0)), dict(qk=qk(eps=math.nan)), dict(qk=qk(interleaved=2)), dict(qk=qk(table=FAKE + 4)),
+    dict(ld_in=504), dict(ld_out=504), dict(ld_in=516), dict(ld_out=517), dict(src=FAKE + 8), dict(dst=FAKE + 8),
+    dict(src=None), dict(dst=None), dict(dst=FAKE, ld_out=768), dict(idx=(1, 1)), dict(idx=(-1,)), dict(idx=(64,))])
+def test_qk_norm_rope_refuses(lib, case):
+    c = cfg()
+    a = dict(qk=qk(), src=FAKE, ld_in=512, dst=2 * FAKE, ld_out=512, idx=(0,))
+    a.update(case)
+    arr, n = idx(*a["idx"])
+    assert lib.dc_qk_norm_rope(C.byref(c), C.byref(a["qk"]), a["src"], a["ld_in"], a["dst"], a["ld_out"], 1.0, arr, n,
+                               None) == ARG
+
+
+def test_qk_norm_rope_of_no_samples_is_a_no_op(lib):
+    arr, n = idx()
+    assert lib.dc_qk_norm_rope(C.byref(cfg()), C.byref(qk()), FAKE, 512, FAKE, 512, 1.0, arr, n, None) == L.DC_OK
+
+
+@pytest.mark.parametrize("args,code", [
+    ((FAKE, 2, 64, 4, 64, FAKE, 128, FAKE), DTYPE), ((FAKE, 1, 63, 4, 64, FAKE, 128, FAKE), ARG),
+    ((FAKE, 1, 64, 4, 64, FAKE, 127, FAKE), ARG), ((FAKE, 1, 129, 4, 129, FAKE, 255, FAKE), ARG),
+    ((FAKE, 1, 64, -1, 64, FAKE, 128, FAKE), ARG), ((FAKE, 1, 64, 1 << 24, 64, FAKE, 128, FAKE), ARG),
+    ((FAKE, 1, 64, 4, 0, FAKE, 128, FAKE), ARG), ((None, 1, 64, 4, 64, FAKE, 128, FAKE), ARG),
+    ((FAKE, 1, 64, 4, 64, None, 128, FAKE), ARG), ((FAKE, 1, 64, 4, 64, FAKE, 128, None), ARG),
+    ((FAKE + 1, 1, 64, 4, 64, FAKE, 128, FAKE), ARG), ((FAKE + 2, 0, 64, 4, 64, FAKE, 128, FAKE), ARG),
+    ((None, 0, 64, 0, 64, None, 128, None), L.DC_OK)])
+def test_quantize_rows_refuses(lib, args, code):
+    assert lib.dc_quantize_rows(*args, None) == code
+
+
+def linear(**more):
+    a = dict(rows=4, out_features=32, in_features=128, x=FAKE, x_scale=FAKE, ld_x=128, w=FAKE, w_scale=FAKE, ld_w=128,
+             bias=FAKE, gelu=0, gate=None, residual=None, ld_residual=0, out=FAKE, out_dtype=0, ld_out=32)
+    a.update(more)
+    return L.LinearI8Args(**a)
+
+
+GATED = dict(gate=FAKE, residual=FAKE, ld_residual=32, out=2 * FAKE)
+
+
+@pytest.mark.parametrize("more,code", [
+    (dict(out_dtype=2), DTYPE), (dict(rows=-1), ARG), (dict(out_features=0), ARG), (dict(gelu=2), ARG),
+    (dict(gate=FAKE), ARG), (dict(residual=FAKE), ARG), (dict(GATED, gelu=1), ARG), (dict(GATED, out_dtype=1), ARG),
+    (dict(GATED, ld_residual=31), ARG), (dict(GATED, out=FAKE, ld_out=64), ARG), (dict(ld_out=31), ARG),
+    (dict(x=None), ARG), (dict(x_scale=None), ARG), (dict(w=None), ARG), (dict(w_scale=None), ARG), (dict(out=None), ARG),
+    (dict(x=FAKE + 8), ARG), (dict(w=FAKE + 8), ARG), (dict(in_features=64), SHAPE), (dict(in_features=192), SHAPE),
+    (dict(in_features=131072, ld_x=131072, ld_w=131072), SHAPE), (dict(ld_x=120), SHAPE), (dict(ld_w=136), SHAPE),
+    (dict(ld_x=(1 << 22) + 16), SHAPE), (dict(rows=1 << 24, out_features=1 << 20, ld_out=1 << 20), SHAPE),
+    (dict(rows=0, x=None, out=None), L.DC_OK)])
+def test_linear_i8_refuses(lib, more, code):
+    a = linear(**more)
+    assert lib.dc_linear_i8(C.byref(a), None) == code
+
+
+def test_linear_i8_refuses_null(lib):
+    assert lib.dc_linear_i8(None, None) == ARG
+
+
+@pytest.mark.parametrize("f", ["dc_cache_store_q", "dc_cache_apply_q"])
+def test_quantised_cache_refuses(lib, f):
+    call, c = getattr(lib, f), cfg()
+    arr, n = idx(0)
+    for bits in (0, 2, 16, -8):
+        assert call(C.byref(c), bits, FAKE, FAKE, FAKE, FAKE, arr, n, None) == ARG
+    for hole in range(4):
+        p = [FAKE] * 4
+        p[hole] = None
+        assert call(C.byref(c), 8, *p, arr, n, None) == ARG
+        p[hole] = FAKE + 8
+        assert call(C.byref(c), 4, *p, arr, n, None) == ARG
+    arr, n = idx(2, 2)
+    assert call(C.byref(c), 8, FAKE, FAKE, FAKE, FAKE, arr, n, None) == ARG
+    arr, n = idx()
+    assert call(C.byref(c), 8, FAKE, FAKE, FAKE, FAKE, arr, n, None) == L.DC_OK
+
+
+def test_block_ext_refuses(lib):
+    arr, n = idx(0)
+
+    def call(c, qk_cfg=None, i8=None, w=None, ws=FAKE, nbytes=None):
+        e = L.BlockExt()
+        if qk_cfg is not None:
+            e.qk = C.pointer(qk_cfg)
+        if i8 is not None:
+            e.i8 = C.pointer(i8)
+        nbytes = lib.dc_block_ext_workspace_bytes(C.byref(c), 1) if nbytes is None else nbytes
+        return lib.dc_block_forward_ext(C.byref(c), C.byref(w or L.BlockWeights(*[FAKE] * 9)), C.byref(e), FAKE, FAKE, arr,
+                                        n, ws, nbytes, None)
+
+    c = cfg()
+    plain = lib.dc_workspace_bytes(C.byref(c), 1)
+    assert lib.dc_block_ext_workspace_bytes(C.byref(c), 1) >= plain + 272 * 1024 + 272 * 4
+    assert lib.dc_block_ext_workspace_bytes(C.byref(c), 0) == 0
+    i8 = L.BlockWeightsI8(*[FAKE] * 8)
+    assert call(c, qk_cfg=qk(), nbytes=plain) == WS
+    assert call(c, i8=i8, nbytes=plain) == WS
+    assert call(c, i8=i8, ws=None) == WS
+    assert call(c, qk_cfg=qk(eps=-1.0)) == ARG
+    for hole in range(8):
+        p = [FAKE] * 8
+        p[hole] = None
+        assert call(c, i8=L.BlockWeightsI8(*p)) == ARG
+    assert call(c, i8=L.BlockWeightsI8(*[FAKE + 8] * 8)) == ARG
+    assert call(cfg(dtype=0), i8=i8) == DTYPE
+    # int8 products do not read the matrices of the model dtype, but need its biases
+    no_bias = L.BlockWeights(None, None, None, FAKE, None, FAKE, None, FAKE, None)
+    assert call(c, i8=i8, w=no_bias) == ARG
+    no_matrix = L.BlockWeights(None, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, None)
+    assert call(c, qk_cfg=qk(), w=no_matrix) == ARG
+
+
+def test_sampler_ext_refuses(lib):
+    from paper_2608_16354_amd import api
+    from paper_2608_16354_amd import inputs as I
+    w = I.WORKLOADS["dit-tiny-f32"]
+    c = api.model_cfg(w.model)
+    blocks = (L.BlockWeights * w.model.n_blocks)()
+    weights = L.ModelWeights()
+    weights.blocks = C.cast(blocks, C.POINTER(L.BlockWeights))
+    sig = np.ascontiguousarray(I.sigmas(w.K))
+    cp = api._CProblem(I.scene_problem(w, w.motions[0]))
+
+    def create(x, nbytes):
+        bufs = L.Buffers(*[FAKE] * 9, nbytes)
+        h = C.c_void_p()
+        rc = lib.dc_sampler_create_ext(C.byref(c), C.byref(weights), 1, C.byref(cp.c),
+                                       sig.ctypes.data_as(C.POINTER(C.c_double)), C.byref(bufs), None, C.byref(x), None,
+                                       C.byref(h))
+        assert not h.value
+        return rc
+
+    plain, full = lib.dc_workspace_bytes(C.byref(c), 1), lib.dc_block_ext_workspace_bytes(C.byref(c), 1)
+    ext = (L.BlockExt * 2)()
+    assert create(L.SamplerExt(None, None, 5, FAKE), full) == ARG
+    assert create(L.SamplerExt(None, None, 8, None), full) == ARG
+    assert create(L.SamplerExt(ext, None, 0, None), plain) == WS
+    assert create(L.SamplerExt(None, ext, 0, None), full) == ARG       # no low expert
+    bad = qk(eps=0.0)
+    ext[1].qk = C.pointer(bad)
+    assert create(L.SamplerExt(ext, None, 0, None), full) == ARG
+    i8 = L.BlockWeightsI8(*[FAKE] * 8)
+    ext[1] = L.BlockExt(None, C.pointer(i8))
+    assert create(L.SamplerExt(ext, None, 0, None), full) == DTYPE     # an fp32 model
+
+
+def test_binding_refuses_tensors_before_any_call():
+    import torch
+    from paper_2608_16354_amd import api
+    c = cfg()
+    x, q, s = torch.zeros(4, 100), torch.zeros(4, 128, dtype=torch.int8), torch.zeros(4)
+    for a in ((x, q[:, :64], s), (x, q[:3], s), (x, q.float(), s), (x.t(), q, s), (x, q, s.double()), (x, q, torch.zeros(5)),
+              (x[:1].expand(4, 100), q, s), (x, q, s)):     # the last: not on a GPU
+        with pytest.raises(ValueError):
+            api.dc_quantize_rows(*a)
+    w, ws, out = torch.zeros(8, 128, dtype=torch.int8), torch.zeros(8), torch.zeros(4, 8)
+    for a in ((q, s, w[:, :64], ws, out), (q, s, w, ws, out[:, :7]), (q, s, w, s, out), (q, ws, w, ws, out), (q, s, w, ws, out.t()),
+              (q.to(torch.uint8), s, w, ws, out), (q, s, w, ws, out)):
+        with pytest.raises(ValueError):
+            api.dc_linear_i8(*a)
+    h, k8 = torch.zeros(1, 272, 256), torch.zeros(1, 256, 256, dtype=torch.int8)
+    sc = torch.zeros(1, 256, 4)
+    for bits, codes, scales, i in ((8, k8, sc, [1]), (4, k8, sc, [0]), (8, k8.to(torch.uint8), sc, [0]), (8, k8, sc[:, :, :3], [0]),
+                                   (6, k8, sc, [0]), (8, k8, sc, [0])):
+        with pytest.raises(ValueError):
+            api.dc_cache_store_q(c, bits, h, h, codes, scales, i)
+        with pytest.raises(ValueError):
+            api.dc_cache_apply_q(c, bits, h, codes, scales, h, i)
+    b = torch.zeros(1, 272, 512, dtype=torch.bfloat16)
+    for src, dst, i in ((b.float(), b, [0]), (b, b[:, :, :500], [0]), (b[:, :271], b, [0]), (b, b, [1]), (b, b, [0])):
+        with pytest.raises(ValueError):
+            api.dc_qk_norm_rope(c, src, dst, i)
+    with pytest.raises(ValueError):
+        api.dc_rope_table(c, api.rope_axes((16, 24, 24)), None, torch.zeros(256, 32, 2))
+    with pytest.raises(ValueError):
+        api.dc_rope_table(c, api.rope_axes((16, 24, 24)), torch.zeros(256, 3), torch.zeros(256, 32, 2))
+
+
+# ----------------------------------------------------------------------------
+# the definitions, by hand
+# ----------------------------------------------------------------------------
+def test_codes_by_hand():
+    q, s = X.codes(np.array([[127.0, -63.5, 0.4, 62.5], [0, 0, 0, 0], [1, np.nan, 0, 0], [np.inf, 1, 0, 0]]), 127)
+    assert q.tolist() == [[127, -64, 0, 62], [0] * 4, [0] * 4, [0] * 4]      # ties go to the even code
+    assert s[0] == 1 and s[1] == 0 and np.isnan(s[2:]).all()
+    q, s = X.cache_codes(np.concatenate([np.full(64, -3.5), np.full(64, 0.5), [7.0] + [1.0] * 63])[None], 4)
+    assert q[0, 0] == -7 and q[0, 64] == 7 and q[0, 128] == 7 and q[0, 129] == 1
+    assert s[0].tolist() == [0.5, np.float32(0.5) / np.float32(7), 1.0]
+
+
+def test_rotation_by_hand():
+    t = X.rope_table(np.array([[math.pi / 2, 0.0, 0.0]]), (2, 0, 2), 100.0, 3)
+    assert np.allclose(t[0], [[0, 1], [1, 0], [1, 0]])
+    x = np.arange(1.0, 7.0).reshape(1, 1, 6)
+    assert np.allclose(X.qk_norm_rope(x, None, 0, t, True), [[[-2, 1, 3, 4, 5, 6]]])
+    assert np.allclose(X.qk_norm_rope(x, None, 0, t, False), [[[-4, 2, 3, 1, 5, 6]]])
+    y = X.qk_norm_rope(np.full((1, 1, 4), 3.0), np.arange(4.0), 0.0, None, True, 2.0)
+    assert np.allclose(y, [[[0, 2, 4, 6]]])
