@@ -188,29 +188,67 @@ def dc_calibrate_tables(dm: DeviceModel, x1, txt, sigmas, h_max: int, eps: float
 # ----------------------------------------------------------------------------
 # rotary positions, query/key norms, int8 products, quantised cache
 # ----------------------------------------------------------------------------
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
+# These calls take a few microseconds on the GPU, so the checks here are kept to attribute reads: about
+# 3 us a call beside the 3.4 us of the C call and its launch.
+def _fail(what):
+    raise ValueError(what)
+
+
+class _Same:
+    """A stand-in for torch.cuda.device() where the device is the current one already."""
+
+    def __enter__(self):
+        pass
+
+    def __exit__(self, *exc):
+        return False
+
+
+_SAME = _Same()
 
 
 def _on(stream, first, *more):
-    """The current stream of the tensors' device (or `stream`, which has to be one of it)."""
+    """The current stream of the tensors' device (or `stream`, which has to be one of it), and a context in which
+    that device is the current one."""
     torch = _torch()
-    dev = first.device
-    _need(dev.type == "cuda", "tensors must be on a GPU")
+    i = first.get_device()
+    if i < 0:
+        _fail("tensors must be on a GPU")
     for t in more:
-        _need(t is None or t.device == dev, "tensors must be on one device")
-    s = torch.cuda.current_stream(dev) if stream is None else stream
-    _need(s.device == dev, "the stream belongs to another device")
-    return C.c_void_p(int(s.cuda_stream)), torch.cuda.device(dev)
+        if t is not None and t.get_device() != i:
+            _fail("tensors must be on one GPU")
+    if stream is None:
+        s = torch._C._cuda_getCurrentRawStream(i)
+    else:
+        if stream.device.index != i:
+            _fail("the stream belongs to another device")
+        s = stream.cuda_stream
+    return s, _SAME if torch.cuda.current_device() == i else torch.cuda.device(i)
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 def _dtype(t):
     torch = _torch()
     if t.dtype == torch.float32:
         return L.DC_F32
-    _need(t.dtype == torch.bfloat16, "float32 or bfloat16 tensors only")
+    if t.dtype != torch.bfloat16:
+        _fail("float32 or bfloat16 tensors only")
     return L.DC_BF16
+
+
+def _samples(idx, *batched):
+    """idx as a C array; every sample of it has to lie inside each of the batched tensors."""
+    idx = [int(i) for i in idx]
+    n = len(idx)
+    if n:
+        most = max(idx)
+        for t in batched:
+            if most >= t.shape[0]:
+                _fail("a sample of idx lies outside the batch")
+    return (C.c_int32 * (n or 1))(*idx), n
 
 
 def _tokens(cfg):
@@ -218,53 +256,56 @@ def _tokens(cfg):
     return n_v, n_v + cfg.n_txt
 
 
-def _batch(t, shape, dtype, idx, what):
-    """A contiguous [B, *shape] tensor that holds every sample of idx."""
-    _need(t.dtype == dtype and t.is_contiguous() and tuple(t.shape[1:]) == shape,
-          f"{what}: a contiguous [B, {', '.join(map(str, shape))}] {dtype} tensor is wanted")
-    _need(not len(idx) or max(idx) < t.shape[0], f"{what}: a sample of idx lies outside the batch")
+def _whole(t, shape, dtype, what):
+    """A contiguous [B, *shape] tensor."""
+    if t.dtype != dtype or not t.is_contiguous() or t.shape[1:] != shape:
+        _fail(f"{what}: a contiguous [B, {', '.join(map(str, shape))}] {dtype} tensor is wanted")
 
 
 def _rows(t, what):
-    """A 2-d tensor whose rows are contiguous: its row stride in elements."""
-    _need(t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1) and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1]),
-          f"{what}: a 2-d tensor with contiguous rows that do not overlap is wanted")
-    return int(t.stride(0)) if t.shape[0] > 1 else max(int(t.stride(0)), int(t.shape[1]))
+    """A 2-d tensor whose rows are contiguous and apart: its row stride in elements."""
+    if t.dim() == 2:
+        (rows, cols), (ld, step) = t.shape, t.stride()
+        if rows <= 1:
+            ld = max(ld, cols)
+        if (cols <= 1 or step == 1) and ld >= cols:
+            return ld
+    _fail(f"{what}: a 2-d tensor with contiguous rows that do not overlap is wanted")
 
 
 def _vector(t, n, what):
-    torch = _torch()
-    _need(t is None or (t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == (n,)),
-          f"{what}: a contiguous float32 [{n}] tensor is wanted")
+    if t is not None and (t.dtype != _torch().float32 or t.shape != (n,) or not t.is_contiguous()):
+        _fail(f"{what}: a contiguous float32 [{n}] tensor is wanted")
+
+
+def _table(cfg, t):
+    if t.dtype != _torch().float32 or not t.is_contiguous() or t.shape != (_tokens(cfg)[0], cfg.head_dim // 2, 2):
+        _fail("table: a contiguous float32 [N_v, head_dim / 2, 2] tensor is wanted")
 
 
 def rope_axes(dim, theta=10000.0, start=(0.0, 0.0, 0.0), step=(1.0, 1.0, 1.0)) -> L.RopeAxes:
     """dc_rope_axes: features of a head that turn with time, height and width, and the grid's
     positions start + step * index."""
-    return L.RopeAxes((C.c_int32 * 3)(*dim), theta, (C.c_double * 3)(*start), (C.c_double * 3)(*step))
+    return L.RopeAxes(tuple(dim), theta, tuple(start), tuple(step))
 
 
 def dc_rope_table(cfg, axes: L.RopeAxes, pos, table, stream=None):
     """table (f32 [N_v, head_dim / 2, 2]) := cos and sin; pos: f64 [N_v, 3] or None (the grid)."""
-    torch = _torch()
-    n_v = _tokens(cfg)[0]
-    _need(table.dtype == torch.float32 and table.is_contiguous()
-          and tuple(table.shape) == (n_v, cfg.head_dim // 2, 2), "table: a contiguous float32 [N_v, head_dim / 2, 2]")
-    _need(pos is None or (pos.dtype == torch.float64 and pos.is_contiguous() and tuple(pos.shape) == (n_v, 3)),
-          "pos: a contiguous float64 [N_v, 3] tensor or None")
+    _table(cfg, table)
+    if pos is not None and (pos.dtype != _torch().float64 or not pos.is_contiguous()
+                            or pos.shape != (table.shape[0], 3)):
+        _fail("pos: a contiguous float64 [N_v, 3] tensor or None is wanted")
     s, dev = _on(stream, table, pos)
     with dev:
-        L.check("dc_rope_table", L.load().dc_rope_table(C.byref(cfg), C.byref(axes), _ptr(pos), _ptr(table), s))
+        L.check("dc_rope_table", L.load().dc_rope_table(C.byref(cfg), C.byref(axes), _at(pos), _at(table), s))
 
 
 def _qk_cfg(cfg, q_weight, k_weight, eps, table, interleaved):
-    torch = _torch()
     _vector(q_weight, cfg.head_dim, "q_weight")
     _vector(k_weight, cfg.head_dim, "k_weight")
-    _need(table is None or (table.dtype == torch.float32 and table.is_contiguous()
-                            and tuple(table.shape) == (_tokens(cfg)[0], cfg.head_dim // 2, 2)),
-          "table: a contiguous float32 [N_v, head_dim / 2, 2]")
-    return L.QkCfg(_ptr(q_weight), _ptr(k_weight), float(eps), _ptr(table), int(bool(interleaved)))
+    if table is not None:
+        _table(cfg, table)
+    return L.QkCfg(_at(q_weight), _at(k_weight), eps, _at(table), 1 if interleaved else 0)
 
 
 def dc_qk_norm_rope(cfg, x, out, idx, q_weight=None, k_weight=None, eps=1e-6, table=None, interleaved=True,
@@ -275,88 +316,85 @@ def dc_qk_norm_rope(cfg, x, out, idx, q_weight=None, k_weight=None, eps=1e-6, ta
     n_tok, d2 = _tokens(cfg)[1], 2 * cfg.hidden
     dt = torch.bfloat16 if cfg.dtype == L.DC_BF16 else torch.float32
     for t in (x, out):
-        _need(t.dtype == dt and t.dim() == 3 and t.shape[1] == n_tok and t.shape[2] >= d2 and t.stride(2) == 1
-              and (t.shape[0] <= 1 or t.stride(0) == n_tok * t.stride(1)),
-              f"x and out: [B, {n_tok}, at least {d2}] {dt} tensors of equally spaced rows are wanted")
-        _need(not len(idx) or max(idx) < t.shape[0], "a sample of idx lies outside the batch")
+        if t.dtype != dt or t.dim() != 3 or t.shape[1] != n_tok or t.shape[2] < d2 or t.stride(2) != 1 or (
+                n_tok > 1 and t.stride(1) < d2) or (t.shape[0] > 1 and t.stride(0) != n_tok * t.stride(1)):
+            _fail(f"x and out: [B, {n_tok}, at least {d2}] {dt} tensors of equally spaced rows are wanted")
     qk = _qk_cfg(cfg, q_weight, k_weight, eps, table, interleaved)
-    arr, p, n = _idx(idx)
+    arr, n = _samples(idx, x, out)
     s, dev = _on(stream, x, out, q_weight, k_weight, table)
     with dev:
         L.check("dc_qk_norm_rope", L.load().dc_qk_norm_rope(
-            C.byref(cfg), C.byref(qk), _ptr(x), int(x.stride(1)), _ptr(out), int(out.stride(1)), float(q_scale), p, n,
-            s))
+            C.byref(cfg), C.byref(qk), _at(x), x.stride(1), _at(out), out.stride(1), q_scale, arr, n, s))
 
 
 def dc_quantize_rows(x, q, scale, stream=None):
     """q (int8 [rows, at least cols rounded up to 128]) and scale (f32 [rows]) := the rows of x [rows, cols]."""
-    torch = _torch()
-    rows, cols = x.shape
     ldx, ldq = _rows(x, "x"), _rows(q, "q")
-    _need(q.dtype == torch.int8 and q.shape[0] == rows and q.shape[1] >= -(-cols // 128) * 128,
-          "q: an int8 tensor of x's rows, at least cols rounded up to 128 wide")
+    rows, cols = x.shape
+    if q.dtype != _torch().int8 or q.shape[0] != rows or q.shape[1] < -(-cols // 128) * 128:
+        _fail("q: an int8 tensor of x's rows, at least cols rounded up to 128 wide, is wanted")
     _vector(scale, rows, "scale")
     s, dev = _on(stream, x, q, scale)
     with dev:
-        L.check("dc_quantize_rows", L.load().dc_quantize_rows(_ptr(x), _dtype(x), ldx, rows, cols, _ptr(q), ldq,
-                                                              _ptr(scale), s))
+        L.check("dc_quantize_rows", L.load().dc_quantize_rows(_at(x), _dtype(x), ldx, rows, cols, _at(q), ldq,
+                                                              _at(scale), s))
 
 
 def dc_linear_i8(x, x_scale, w, w_scale, out, bias=None, gelu=False, gate=None, residual=None, stream=None):
     """out [M, N] := the product of int8 rows x [M, K] and w [N, K] (K as padded by dc_quantize_rows) with
     their scales, plus bias, through GELU or as residual + gate * (...)."""
     torch = _torch()
-    m, k = x.shape
-    n = w.shape[0]
-    _need(x.dtype == torch.int8 and w.dtype == torch.int8 and w.dim() == 2 and w.shape[1] == k,
-          "x and w: int8 tensors of equally long rows")
-    _need(tuple(out.shape) == (m, n), "out: [rows of x, rows of w]")
-    for v, size, what in ((x_scale, m, "x_scale"), (w_scale, n, "w_scale"), (bias, n, "bias"), (gate, n, "gate")):
-        _vector(v, size, what)
-    _need(residual is None or (residual.dtype == torch.float32 and residual.shape == out.shape),
-          "residual: a float32 tensor of out's shape")
-    a = L.LinearI8Args(m, n, k, _ptr(x), _ptr(x_scale), _rows(x, "x"), _ptr(w), _ptr(w_scale), _rows(w, "w"),
-                       _ptr(bias), int(bool(gelu)), _ptr(gate), _ptr(residual),
-                       0 if residual is None else _rows(residual, "residual"), _ptr(out), _dtype(out),
-                       _rows(out, "out"))
+    ldx, ldw, ldo, ldr = _rows(x, "x"), _rows(w, "w"), _rows(out, "out"), 0
+    (m, k), n = x.shape, w.shape[0]
+    if x.dtype != torch.int8 or w.dtype != torch.int8 or w.shape[1] != k:
+        _fail("x and w: int8 tensors of equally long rows are wanted")
+    if out.shape != (m, n):
+        _fail("out: a [rows of x, rows of w] tensor is wanted")
+    _vector(x_scale, m, "x_scale")
+    _vector(w_scale, n, "w_scale")
+    _vector(bias, n, "bias")
+    _vector(gate, n, "gate")
+    if residual is not None:
+        ldr = _rows(residual, "residual")
+        if residual.dtype != torch.float32 or residual.shape != (m, n):
+            _fail("residual: a float32 tensor of out's shape is wanted")
     s, dev = _on(stream, x, x_scale, w, w_scale, out, bias, gate, residual)
+    a = L.LinearI8Args(m, n, k, _at(x), _at(x_scale), ldx, _at(w), _at(w_scale), ldw, _at(bias), 1 if gelu else 0,
+                       _at(gate), _at(residual), ldr, _at(out), _dtype(out), ldo)
     with dev:
         L.check("dc_linear_i8", L.load().dc_linear_i8(C.byref(a), s))
 
 
-def _check_cache(cfg, bits, codes, scales, idx):
+def _cache_args(cfg, bits, a, b, codes, scales, idx):
     torch = _torch()
-    _need(bits in (8, 4), "bits must be 8 or 4")
-    n_v = _tokens(cfg)[0]
-    _batch(codes, (n_v, cfg.hidden * bits // 8), torch.int8 if bits == 8 else torch.uint8, idx, "codes")
-    _batch(scales, (n_v, cfg.hidden // 64), torch.float32, idx, "scales")
+    if bits not in (8, 4):
+        _fail("bits must be 8 or 4")
+    n_v, n_tok = _tokens(cfg)
+    d = cfg.hidden
+    _whole(a, (n_tok, d), torch.float32, "h_in, h_out and g")
+    _whole(b, (n_tok, d), torch.float32, "h_in, h_out and g")
+    _whole(codes, (n_v, d * bits // 8), torch.int8 if bits == 8 else torch.uint8, "codes")
+    _whole(scales, (n_v, d // 64), torch.float32, "scales")
+    return _samples(idx, a, b, codes, scales)
 
 
 def dc_cache_store_q(cfg, bits, h_out, h_in, codes, scales, idx, stream=None):
     """codes (int8 [B, N_v, d], or uint8 [B, N_v, d / 2] for 4 bits) and scales (f32 [B, N_v, d / 64]) :=
     h_out - h_in on the video rows."""
-    torch = _torch()
-    _check_cache(cfg, bits, codes, scales, idx)
-    for t, what in ((h_out, "h_out"), (h_in, "h_in")):
-        _batch(t, (_tokens(cfg)[1], cfg.hidden), torch.float32, idx, what)
-    arr, p, n = _idx(idx)
+    arr, n = _cache_args(cfg, bits, h_out, h_in, codes, scales, idx)
     s, dev = _on(stream, h_out, h_in, codes, scales)
     with dev:
         L.check("dc_cache_store_q", L.load().dc_cache_store_q(
-            C.byref(cfg), bits, _ptr(h_out), _ptr(h_in), _ptr(codes), _ptr(scales), p, n, s))
+            C.byref(cfg), bits, _at(h_out), _at(h_in), _at(codes), _at(scales), arr, n, s))
 
 
 def dc_cache_apply_q(cfg, bits, h_in, codes, scales, g, idx, stream=None):
-    """g := h_in + the cached residual on the video rows."""
-    torch = _torch()
-    _check_cache(cfg, bits, codes, scales, idx)
-    for t, what in ((h_in, "h_in"), (g, "g")):
-        _batch(t, (_tokens(cfg)[1], cfg.hidden), torch.float32, idx, what)
-    arr, p, n = _idx(idx)
+    """g := h_in + the cached residual on the video rows (g may be h_in)."""
+    arr, n = _cache_args(cfg, bits, h_in, g, codes, scales, idx)
     s, dev = _on(stream, h_in, codes, scales, g)
     with dev:
         L.check("dc_cache_apply_q", L.load().dc_cache_apply_q(
-            C.byref(cfg), bits, _ptr(h_in), _ptr(codes), _ptr(scales), _ptr(g), p, n, s))
+            C.byref(cfg), bits, _at(h_in), _at(codes), _at(scales), _at(g), arr, n, s))
 
 
 class BlockExt:
@@ -501,7 +539,8 @@ class SamplerBuffers:
         self.cache_bits, self.ext = cache_bits, ext
         self.cache_scales = None
         if cache_bits:
-            _need(cache_bits in (8, 4), "cache_bits must be 0, 8 or 4")
+            if cache_bits not in (8, 4):
+                _fail("cache_bits must be 0, 8 or 4")
             self.resid = torch.empty((E, m.n_v, m.hidden * cache_bits // 8), device=device,
                                      dtype=torch.int8 if cache_bits == 8 else torch.uint8)
             self.cache_scales = torch.empty((E, m.n_v, m.hidden // 64), device=device, dtype=torch.float32)
@@ -537,7 +576,8 @@ class Sampler:
                                   cache_bits=cache_bits)
         self.bufs = bufs
         assert self.bufs.B == B and self.bufs.K == self.K
-        _need(bufs.cache_bits == cache_bits, "bufs were made for another cache_bits")
+        if bufs.cache_bits != cache_bits:
+            _fail("bufs were made for another cache_bits")
         self.bufs.x.copy_(x1, non_blocking=True)
         if dm.m.n_txt:
             self.bufs.txt.copy_(txt, non_blocking=True)

@@ -179,6 +179,8 @@ Status check_qk(const dc_qk_cfg& c) {
   if (c.interleaved != 0 && c.interleaved != 1) return Status::arg("qk->interleaved must be 0 or 1");
   if ((c.q_weight || c.k_weight) && !(c.eps > 0.f && std::isfinite(c.eps)))
     return Status::arg("qk->eps must be positive");
+  if (!aligned16(c.q_weight) || !aligned16(c.k_weight) || !aligned16(c.cos_sin))
+    return Status::arg("qk->q_weight, k_weight and cos_sin must be 16-byte aligned");
   return Status::ok();
 }
 
@@ -418,8 +420,8 @@ dc_status dc_rope_table(const dc_model_cfg* cfg, const dc_rope_axes* axes, const
     }
     if (sum > g.Dh) return Status::arg("axes->dim add up to more than head_dim");
     if (!(axes->theta > 0.0 && std::isfinite(axes->theta))) return Status::arg("axes->theta must be positive");
-    if (reinterpret_cast<uintptr_t>(cos_sin) % 8 || reinterpret_cast<uintptr_t>(pos) % 8)
-      return Status::arg("cos_sin and pos must be 8-byte aligned");
+    if (!aligned16(cos_sin) || reinterpret_cast<uintptr_t>(pos) % 8)
+      return Status::arg("cos_sin must be 16-byte, pos 8-byte aligned");
     return rope_table(*axes, pos, cos_sin, g, stream);
   })());
 }
@@ -436,8 +438,7 @@ dc_status dc_qk_norm_rope(const dc_model_cfg* cfg, const dc_qk_cfg* qk, const vo
     const int ve = g.bf16 ? 8 : 4;
     if (ld_in < 2 * g.d || ld_out < 2 * g.d || ld_in % ve || ld_out % ve)
       return Status::arg("ld_in and ld_out must be at least 2 * hidden and multiples of 16 bytes");
-    if (!aligned16(in) || !aligned16(out) || reinterpret_cast<uintptr_t>(qk->cos_sin) % 8)
-      return Status::arg("in and out must be 16-byte, cos_sin 8-byte aligned");
+    if (!aligned16(in) || !aligned16(out)) return Status::arg("in and out must be 16-byte aligned");
     if (in == out && ld_in != ld_out) return Status::arg("in place: ld_in and ld_out must be equal");
     if (il.n == 0) return Status::ok();
     ProfScope ps(KClass::kQkNormRope, stream);

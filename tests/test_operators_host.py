@@ -44,7 +44,7 @@ def test_rope_table_refuses_pointers(lib):
     c, a = cfg(), axes()
     assert lib.dc_rope_table(C.byref(c), None, None, FAKE, None) == ARG
     assert lib.dc_rope_table(C.byref(c), C.byref(a), None, None, None) == ARG
-    assert lib.dc_rope_table(C.byref(c), C.byref(a), None, FAKE + 4, None) == ARG
+    assert lib.dc_rope_table(C.byref(c), C.byref(a), None, FAKE + 8, None) == ARG
     assert lib.dc_rope_table(C.byref(c), C.byref(a), FAKE + 4, FAKE, None) == ARG
     assert lib.dc_rope_table(None, C.byref(a), None, FAKE, None) == ARG
 
@@ -54,7 +54,7 @@ def qk(q=FAKE, k=FAKE, eps=1e-6, table=FAKE, interleaved=1):
 
 
 @pytest.mark.parametrize("case", [
-    dict(qk=qk(eps=0.0)), dict(qk=qk(eps=math.nan)), dict(qk=qk(interleaved=2)), dict(qk=qk(table=FAKE + 4)),
+    dict(qk=qk(eps=0.0)), dict(qk=qk(eps=math.nan)), dict(qk=qk(interleaved=2)), dict(qk=qk(table=FAKE + 8)), dict(qk=qk(q=FAKE + 4)), dict(qk=qk(k=FAKE + 8)),
     dict(ld_in=504), dict(ld_out=504), dict(ld_in=516), dict(ld_out=517), dict(src=FAKE + 8), dict(dst=FAKE + 8),
     dict(src=None), dict(dst=None), dict(dst=FAKE, ld_out=768), dict(idx=(1, 1)), dict(idx=(-1,)), dict(idx=(64,))])
 def test_qk_norm_rope_refuses(lib, case):
