@@ -53,9 +53,12 @@ __device__ inline float gelu_tanh_fast(float z) {
   return z * __builtin_amdgcn_rcpf(1.0f + __expf(-2.0f * y));
 }
 
-// The matrix instruction: 32 x 32 outputs, 32 bytes of k.
+// The matrix instruction: 32 x 32 outputs, 32 bytes of k.  kSwapped: the accumulator holds the
+// transposed tile (a lane one row of A and 16 columns), and the epilogue is the class's own (start,
+// once the first k-steps are on their way, and finish).
 struct OpsBf16 {
   typedef f32x16 Acc;
+  static constexpr bool kSwapped = false;
   static __device__ inline Acc mfma(uint4 a, uint4 b, const Acc& c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   }
@@ -306,6 +309,7 @@ __global__ void __launch_bounds__(WM * WN * 64) k_gemm_dma(const char* __restric
   // one array, so every stage address is a constant offset from one base
   constexpr int STAGE = (BM + BN) * 8;
   __shared__ uint4 lds[ST * STAGE];
+  __shared__ float4 s_vec[Ops::kSwapped ? (BM + 2 * BN) / 4 : 1];
 
   const int t = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
   if (t >= tiles) return;
@@ -388,6 +392,7 @@ __global__ void __launch_bounds__(WM * WN * 64) k_gemm_dma(const char* __restric
     if (i < KT)
 #pragma unroll
       for (int j = 0; j < AI + BI; ++j) dma_one(lds + i * STAGE, i, j);
+  if constexpr (Ops::kSwapped) epi.template start<BM, BN, NW * 64>(s_vec, m0, n0, M, N, tid);
   for (int kt0 = 0; kt0 < KT; kt0 += ST) {
 #pragma unroll
     for (int i = 0; i < ST; ++i) {
@@ -403,8 +408,13 @@ __global__ void __launch_bounds__(WM * WN * 64) k_gemm_dma(const char* __restric
     }
   }
 
-  static_assert(Epi::kRowVec == 0 || sizeof(lds) >= NW * 32 * kEpiStride * sizeof(float), "epilogue LDS");
-  gemm_epilogue<BM, BN, WM, WN>(acc, lds, m0, n0, M, N, wave, lane, rows_ok, epi);
+  if constexpr (Ops::kSwapped) {
+    static_assert(sizeof(lds) >= NW * Epi::kStrip, "epilogue LDS");
+    epi.template finish<BM, BN, WM, WN>(acc, lds, s_vec, m0, n0, M, N, wave, lane);
+  } else {
+    static_assert(Epi::kRowVec == 0 || sizeof(lds) >= NW * 32 * kEpiStride * sizeof(float), "epilogue LDS");
+    gemm_epilogue<BM, BN, WM, WN>(acc, lds, m0, n0, M, N, wave, lane, rows_ok, epi);
+  }
 }
 
 // 128 x 128 tile for the middle sizes (8 waves of 64 x 32).  A tile this small has little
@@ -424,6 +434,7 @@ __global__ void __launch_bounds__(512) k_gemm_pipe(const char* __restrict__ A, i
   static_assert(AI + BI == 4, "one DMA instruction per k-slice");
   constexpr int STAGE = (BM + BN) * 8;
   __shared__ uint4 lds[ST * STAGE];
+  __shared__ float4 s_vec[Ops::kSwapped ? (BM + 2 * BN) / 4 : 1];
   const int t = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
   if (t >= tiles) return;
   const int tiles_m = (M + BM - 1) / BM;
@@ -480,6 +491,7 @@ __global__ void __launch_bounds__(512) k_gemm_pipe(const char* __restrict__ A, i
     if (i < KT)
 #pragma unroll
       for (int j = 0; j < AI + BI; ++j) dma_one(i, i, j);
+  if constexpr (Ops::kSwapped) epi.template start<BM, BN, NW * 64>(s_vec, m0, n0, M, N, tid);
   if (KT >= ST - 1) wait_vmcnt<(ST - 2) * (AI + BI)>();          // k-step 0 has landed
   else wait_vmcnt<0>();
   __builtin_amdgcn_s_barrier();
@@ -513,8 +525,13 @@ __global__ void __launch_bounds__(512) k_gemm_pipe(const char* __restrict__ A, i
     }
   }
   __builtin_amdgcn_s_waitcnt(0x0070);            // the reads ahead are done: the epilogue reuses LDS
-  static_assert(sizeof(lds) >= NW * 32 * kEpiStride * sizeof(float), "epilogue LDS");
-  gemm_epilogue<BM, BN, WM, WN>(acc, lds, m0, n0, M, N, wave, lane, rows_ok, epi);
+  if constexpr (Ops::kSwapped) {
+    static_assert(sizeof(lds) >= NW * Epi::kStrip, "epilogue LDS");
+    epi.template finish<BM, BN, WM, WN>(acc, lds, s_vec, m0, n0, M, N, wave, lane);
+  } else {
+    static_assert(sizeof(lds) >= NW * 32 * kEpiStride * sizeof(float), "epilogue LDS");
+    gemm_epilogue<BM, BN, WM, WN>(acc, lds, m0, n0, M, N, wave, lane, rows_ok, epi);
+  }
 }
 
 // lda and ldw in bytes (multiples of 16), KT k-steps of 128 bytes
