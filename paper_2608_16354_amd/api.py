@@ -188,28 +188,15 @@ def dc_calibrate_tables(dm: DeviceModel, x1, txt, sigmas, h_max: int, eps: float
 # ----------------------------------------------------------------------------
 # rotary positions, query/key norms, int8 products, quantised cache
 # ----------------------------------------------------------------------------
-# These calls take a few microseconds on the GPU, so the checks here are kept to attribute reads: about
-# 3 us a call beside the 3.4 us of the C call and its launch.
+# These calls take a few microseconds on the GPU, so what surrounds the C call (3.4 us with its launch) is kept
+# to attribute reads: 2 us.
 def _fail(what):
     raise ValueError(what)
 
 
-class _Same:
-    """A stand-in for torch.cuda.device() where the device is the current one already."""
-
-    def __enter__(self):
-        pass
-
-    def __exit__(self, *exc):
-        return False
-
-
-_SAME = _Same()
-
-
 def _on(stream, first, *more):
-    """The current stream of the tensors' device (or `stream`, which has to be one of it), and a context in which
-    that device is the current one."""
+    """The current stream of the tensors' device (or `stream`, which has to be one of it), and that device where it
+    is not the current one."""
     torch = _torch()
     i = first.get_device()
     if i < 0:
@@ -223,7 +210,19 @@ def _on(stream, first, *more):
         if stream.device.index != i:
             _fail("the stream belongs to another device")
         s = stream.cuda_stream
-    return s, _SAME if torch.cuda.current_device() == i else torch.cuda.device(i)
+    return s, None if torch._C._cuda_getDevice() == i else i
+
+
+def _call(name, device, args):
+    """The C function on args, with `device` current if it is not None."""
+    f = getattr(L.load(), name)
+    if device is None:
+        rc = f(*args)
+    else:
+        with _torch().cuda.device(device):
+            rc = f(*args)
+    if rc:
+        L.check(name, rc)
 
 
 def _at(t):
@@ -241,14 +240,13 @@ def _dtype(t):
 
 def _samples(idx, *batched):
     """idx as a C array; every sample of it has to lie inside each of the batched tensors."""
-    idx = [int(i) for i in idx]
     n = len(idx)
     if n:
         most = max(idx)
         for t in batched:
             if most >= t.shape[0]:
                 _fail("a sample of idx lies outside the batch")
-    return (C.c_int32 * (n or 1))(*idx), n
+    return (C.c_int32 * (n or 1))(*[int(i) for i in idx]), n
 
 
 def _tokens(cfg):
@@ -296,8 +294,7 @@ def dc_rope_table(cfg, axes: L.RopeAxes, pos, table, stream=None):
                             or pos.shape != (table.shape[0], 3)):
         _fail("pos: a contiguous float64 [N_v, 3] tensor or None is wanted")
     s, dev = _on(stream, table, pos)
-    with dev:
-        L.check("dc_rope_table", L.load().dc_rope_table(C.byref(cfg), C.byref(axes), _at(pos), _at(table), s))
+    _call("dc_rope_table", dev, (C.byref(cfg), C.byref(axes), _at(pos), _at(table), s))
 
 
 def _qk_cfg(cfg, q_weight, k_weight, eps, table, interleaved):
@@ -322,9 +319,8 @@ def dc_qk_norm_rope(cfg, x, out, idx, q_weight=None, k_weight=None, eps=1e-6, ta
     qk = _qk_cfg(cfg, q_weight, k_weight, eps, table, interleaved)
     arr, n = _samples(idx, x, out)
     s, dev = _on(stream, x, out, q_weight, k_weight, table)
-    with dev:
-        L.check("dc_qk_norm_rope", L.load().dc_qk_norm_rope(
-            C.byref(cfg), C.byref(qk), _at(x), x.stride(1), _at(out), out.stride(1), q_scale, arr, n, s))
+    _call("dc_qk_norm_rope", dev, (C.byref(cfg), C.byref(qk), _at(x), x.stride(1), _at(out), out.stride(1), q_scale,
+                                   arr, n, s))
 
 
 def dc_quantize_rows(x, q, scale, stream=None):
@@ -335,9 +331,7 @@ def dc_quantize_rows(x, q, scale, stream=None):
         _fail("q: an int8 tensor of x's rows, at least cols rounded up to 128 wide, is wanted")
     _vector(scale, rows, "scale")
     s, dev = _on(stream, x, q, scale)
-    with dev:
-        L.check("dc_quantize_rows", L.load().dc_quantize_rows(_at(x), _dtype(x), ldx, rows, cols, _at(q), ldq,
-                                                              _at(scale), s))
+    _call("dc_quantize_rows", dev, (_at(x), _dtype(x), ldx, rows, cols, _at(q), ldq, _at(scale), s))
 
 
 def dc_linear_i8(x, x_scale, w, w_scale, out, bias=None, gelu=False, gate=None, residual=None, stream=None):
@@ -361,8 +355,7 @@ def dc_linear_i8(x, x_scale, w, w_scale, out, bias=None, gelu=False, gate=None, 
     s, dev = _on(stream, x, x_scale, w, w_scale, out, bias, gate, residual)
     a = L.LinearI8Args(m, n, k, _at(x), _at(x_scale), ldx, _at(w), _at(w_scale), ldw, _at(bias), 1 if gelu else 0,
                        _at(gate), _at(residual), ldr, _at(out), _dtype(out), ldo)
-    with dev:
-        L.check("dc_linear_i8", L.load().dc_linear_i8(C.byref(a), s))
+    _call("dc_linear_i8", dev, (C.byref(a), s))
 
 
 def _cache_args(cfg, bits, a, b, codes, scales, idx):
@@ -371,10 +364,12 @@ def _cache_args(cfg, bits, a, b, codes, scales, idx):
         _fail("bits must be 8 or 4")
     n_v, n_tok = _tokens(cfg)
     d = cfg.hidden
-    _whole(a, (n_tok, d), torch.float32, "h_in, h_out and g")
-    _whole(b, (n_tok, d), torch.float32, "h_in, h_out and g")
+    f32 = torch.float32
+    rows = (n_tok, d)
+    _whole(a, rows, f32, "h_in, h_out and g")
+    _whole(b, rows, f32, "h_in, h_out and g")
     _whole(codes, (n_v, d * bits // 8), torch.int8 if bits == 8 else torch.uint8, "codes")
-    _whole(scales, (n_v, d // 64), torch.float32, "scales")
+    _whole(scales, (n_v, d // 64), f32, "scales")
     return _samples(idx, a, b, codes, scales)
 
 
@@ -383,18 +378,14 @@ def dc_cache_store_q(cfg, bits, h_out, h_in, codes, scales, idx, stream=None):
     h_out - h_in on the video rows."""
     arr, n = _cache_args(cfg, bits, h_out, h_in, codes, scales, idx)
     s, dev = _on(stream, h_out, h_in, codes, scales)
-    with dev:
-        L.check("dc_cache_store_q", L.load().dc_cache_store_q(
-            C.byref(cfg), bits, _at(h_out), _at(h_in), _at(codes), _at(scales), arr, n, s))
+    _call("dc_cache_store_q", dev, (C.byref(cfg), bits, _at(h_out), _at(h_in), _at(codes), _at(scales), arr, n, s))
 
 
 def dc_cache_apply_q(cfg, bits, h_in, codes, scales, g, idx, stream=None):
     """g := h_in + the cached residual on the video rows (g may be h_in)."""
     arr, n = _cache_args(cfg, bits, h_in, g, codes, scales, idx)
     s, dev = _on(stream, h_in, codes, scales, g)
-    with dev:
-        L.check("dc_cache_apply_q", L.load().dc_cache_apply_q(
-            C.byref(cfg), bits, _at(h_in), _at(codes), _at(scales), _at(g), arr, n, s))
+    _call("dc_cache_apply_q", dev, (C.byref(cfg), bits, _at(h_in), _at(codes), _at(scales), _at(g), arr, n, s))
 
 
 class BlockExt:

@@ -71,6 +71,7 @@ __device__ inline uint32_t pack_bf16(float a, float b) {          // one v_cvt_p
 
 // 16 bytes of a row at any element
 typedef unsigned int u32x4a __attribute__((ext_vector_type(4), aligned(2)));
+typedef unsigned int u32x2a __attribute__((ext_vector_type(2), aligned(2)));
 typedef float f32x4a __attribute__((ext_vector_type(4), aligned(4)));
 
 // out = sx[m] sw[n] sum + bias[n], with GELU, or residual + gate (...), in rows of fp32 or bf16 at any element's
@@ -118,6 +119,34 @@ struct EpiLinear {
     if (tid < BN) {
       v[BM + tid] = w * g;
       v[BM + BN + tid] = b * g;
+    }
+  }
+
+  // four columns from n (a multiple of 4) of row m, the tile's row r and column c
+  template <int BM, int BN>
+  __device__ inline void four(int4 t, const float4* vec, int r, int c, int m, int n, int N) const {
+    const float s = reinterpret_cast<const float*>(vec)[r];
+    const float4 w = vec[(BM + c) / 4], o = vec[(BM + BN + c) / 4];
+    float z[4] = {act(fmaf(float(t.x) * s, w.x, o.x)), act(fmaf(float(t.y) * s, w.y, o.y)),
+                  act(fmaf(float(t.z) * s, w.z, o.z)), act(fmaf(float(t.w) * s, w.w, o.w))};
+    char* const at = static_cast<char*>(out) + (int64_t(m) * ldo + n) * (BF ? 2 : 4);
+    const float* const pr = GATED ? residual + int64_t(m) * ldr + n : nullptr;
+    if (n + 4 <= N) {
+      if constexpr (GATED) {
+        const f32x4a q = *reinterpret_cast<const f32x4a*>(pr);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z[j] += q[j];
+      }
+      if constexpr (BF) *reinterpret_cast<u32x2a*>(at) = u32x2a{pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3])};
+      else *reinterpret_cast<f32x4a*>(at) = f32x4a{z[0], z[1], z[2], z[3]};
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {
+      if (n + j >= N) break;
+      if constexpr (GATED) z[j] += pr[j];
+      if constexpr (BF) reinterpret_cast<uint16_t*>(at)[j] = to_bf16(z[j]);
+      else reinterpret_cast<float*>(at)[j] = z[j];
     }
   }
 
@@ -239,7 +268,176 @@ struct EpiLinear {
   }
 };
 
+// Few tiles, long sums: G groups of WM x WN waves share a workgroup's tile, group g taking every G-th k-step
+// through a two-stage ring of its own, and add their sums in LDS (whole numbers: the same in any order).  All
+// threads then finish the tile, four columns of a row each.  A group of one wave waits for its own fills alone.
+template <int BM, int BN, int WM, int WN, int G, class Epi>
+__global__ void __launch_bounds__(WM * WN * G * 64) k_i8_split(const char* __restrict__ A, int lda,
+                                                               const char* __restrict__ W, int ldw, int M, int N,
+                                                               int KT, int tiles_n, Epi epi) {
+  constexpr int NW = WM * WN, NT = NW * G * 64;
+  constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 32, TN = WTN / 32;
+  constexpr int AI = BM * 8 / 64 / NW, BI = BN * 8 / 64 / NW;     // DMA instructions per wave
+  static_assert(AI * NW * 64 == BM * 8 && BI * NW * 64 == BN * 8, "tile shape");
+  constexpr int STAGE = (BM + BN) * 8;                            // 16-byte chunks
+  constexpr int LS = BN + 4;                                      // ints of a row of partial sums
+  constexpr int RING = G * 2 * STAGE, JOIN = G * BM * LS / 4;
+  __shared__ uint4 lds[RING > JOIN ? RING : JOIN];
+  __shared__ float4 s_vec[(BM + 2 * BN) / 4];
+
+  const int m0 = int(blockIdx.x) / tiles_n * BM, n0 = int(blockIdx.x) % tiles_n * BN;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6), grp = w / NW, wave = w % NW;
+  const int wm = wave % WM, wn = wave / WM, r32 = lane & 31, hi = lane >> 5;
+  const char* const At = A + size_t(m0) * lda;
+  const char* const Wt = W + size_t(n0) * ldw;
+  uint32_t off[AI + BI];
+#pragma unroll
+  for (int i = 0; i < AI; ++i) {
+    const int slot = (wave * AI + i) * 64 + lane, r = slot >> 3, c = (slot & 7) ^ swz(r);
+    off[i] = uint32_t(min(r, M - 1 - m0) * lda + 16 * c);
+  }
+#pragma unroll
+  for (int i = 0; i < BI; ++i) {
+    const int slot = (wave * BI + i) * 64 + lane, r = slot >> 3, c = (slot & 7) ^ swz(r);
+    off[AI + i] = uint32_t(min(r, N - 1 - n0) * ldw + 16 * c);
+  }
+  uint4* const ring = lds + grp * 2 * STAGE;
+  auto fill = [&](int st, int kt) {
+    uint4* const to = ring + st * STAGE;
+#pragma unroll
+    for (int j = 0; j < AI; ++j) dma16(At + kt * 128, off[j], to + (wave * AI + j) * 64);
+#pragma unroll
+    for (int j = 0; j < BI; ++j) dma16(Wt + kt * 128, off[AI + j], to + BM * 8 + (wave * BI + j) * 64);
+  };
+  const int steps = (KT + G - 1) / G;                             // of every group; the last may be past KT
+  auto mine = [&](int i) { return i * G + grp; };
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (mine(i) < KT) fill(i, mine(i));
+  epi.template start<BM, BN, NT>(s_vec, m0, n0, M, N, tid);
+  i32x16 acc[TM][TN];
+#pragma unroll
+  for (int a = 0; a < TM; ++a)
+#pragma unroll
+    for (int b = 0; b < TN; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[a][b][i] = 0;
+  for (int i0 = 0; i0 < steps; i0 += 2) {
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+      const int i = i0 + st;
+      if (i >= steps) break;
+      if (mine(i + 1) < KT) wait_vmcnt<AI + BI>();                // this step has landed, the next may be on its way
+      else wait_vmcnt<0>();
+      if constexpr (NW > 1) __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (mine(i) < KT) {
+        const uint4* const sa = ring + st * STAGE;
+        const uint4* const sb = sa + BM * 8;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          const int ch = kk * 2 + hi;
+          uint4 af[TM], bf[TN];
+#pragma unroll
+          for (int a = 0; a < TM; ++a) {
+            const int r = wm * WTM + a * 32 + r32;
+            af[a] = sa[r * 8 + (ch ^ swz(r))];
+          }
+#pragma unroll
+          for (int b = 0; b < TN; ++b) {
+            const int r = wn * WTN + b * 32 + r32;
+            bf[b] = sb[r * 8 + (ch ^ swz(r))];
+          }
+#pragma unroll
+          for (int a = 0; a < TM; ++a)
+#pragma unroll
+            for (int b = 0; b < TN; ++b) acc[a][b] = OpsI8T::mfma(af[a], bf[b], acc[a][b]);
+        }
+      }
+      __builtin_amdgcn_s_waitcnt(0xC07F);                         // lgkmcnt(0): the reads of this stage have returned
+      if constexpr (NW > 1) __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (mine(i + 2) < KT) fill(st, mine(i + 2));
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0x0070);                             // nothing is on its way to the rings
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  int* const part = reinterpret_cast<int*>(lds) + grp * BM * LS;
+#pragma unroll
+  for (int a = 0; a < TM; ++a)
+#pragma unroll
+    for (int b = 0; b < TN; ++b)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<int4*>(part + (wm * WTM + a * 32 + r32) * LS + wn * WTN + b * 32 + 8 * g + 4 * hi) =
+            make_int4(acc[a][b][4 * g], acc[a][b][4 * g + 1], acc[a][b][4 * g + 2], acc[a][b][4 * g + 3]);
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  for (int e = tid; e < BM * BN / 4; e += NT) {
+    const int r = e / (BN / 4), c = e % (BN / 4) * 4;
+    if (m0 + r >= M || n0 + c >= N) continue;
+    int4 t = make_int4(0, 0, 0, 0);
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const int4 p = *reinterpret_cast<const int4*>(reinterpret_cast<const int*>(lds) + (g * BM + r) * LS + c);
+      t.x += p.x; t.y += p.y; t.z += p.z; t.w += p.w;
+    }
+    epi.template four<BM, BN>(t, s_vec, r, c, m0 + r, n0 + c, N);
+  }
+}
+
 constexpr int kMaxK = 131072 - 128;     // |sum| <= 128 * 128 * kMaxK < 2^31
+
+template <int BM, int BN, int WM, int WN, int G, class E>
+Status launch_split(const int8_t* A, int lda, const int8_t* W, int ldw, int M, int N, int KT, const E& epi,
+                    hipStream_t s) {
+  const int tn = (N + BN - 1) / BN, tiles = tn * ((M + BM - 1) / BM);
+  hipLaunchKernelGGL((k_i8_split<BM, BN, WM, WN, G, E>), dim3(tiles), dim3(WM * WN * G * 64), 0, s,
+                     reinterpret_cast<const char*>(A), lda, reinterpret_cast<const char*>(W), ldw, M, N, KT, tn, epi);
+  DC_HIP(hipGetLastError());
+  return Status::ok();
+}
+
+// Cost in us of tile i, as block_gemm_tile's: rounds of one workgroup per compute unit, each `fixed` plus k-steps (of
+// 128; the last tile's eight groups share them) of `alone` to `full`; the 64 x 64 tile runs up to three workgroups
+// per compute unit.  Fitted to timings of all seven on 228 shapes (M 1 to 17,776; N x K from 256 x 1,024 to 11,520 x
+// 1,920 and 1,920 x 7,680) on MI355X: the one it picks is 0.2 % slower than the best on average, 7 % at worst.  Few
+// rows take the split: 1 x 1,920 x 7,680 7.0 us (64 x 64 18.4), 50 x 1,920 x 1,920 4.6 (7.0), 50 x 11,520 x 1,920 10.9
+// (64 x 64, which it takes, 7.5).
+struct TileCost { int bm, bn; float alone, full, fixed; };
+constexpr TileCost kTiles[] = {{384, 192, 1.124f, 1.867f, 7.08f}, {320, 256, 1.268f, 1.997f, 6.85f},
+                               {256, 192, 0.783f, 1.267f, 5.77f}, {256, 128, 0.604f, 0.927f, 3.79f},
+                               {128, 128, 0.294f, 0.494f, 2.91f}, {64, 64, 0.f, 0.f, 1.29f},
+                               {32, 32, 0.396f, 0.740f, 1.16f}};
+constexpr float kSmallStep[3] = {0.248f, 0.372f, 0.567f};
+constexpr float kLaunch[7] = {0.f, 0.f, 0.f, 1.33f, 1.31f, 2.13f, 2.15f};
+constexpr int kSplitGroups = 8;
+
+}  // namespace
+
+int i8_tile(int M, int N, int ksteps, int cus, bool split) {
+  int best = 0;
+  float least = 0.f;
+  for (int i = 0; i < (split ? 7 : 6); ++i) {
+    const TileCost& c = kTiles[i];
+    const float steps = float(i == 6 ? (ksteps + kSplitGroups - 1) / kSplitGroups : ksteps);
+    const int64_t tiles = int64_t((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn);
+    const int64_t round = i == 5 ? 3 * cus : cus, rounds = tiles / round, rest = tiles % round;
+    float t = kLaunch[i] + float(rounds) * (steps * (i == 5 ? kSmallStep[2] : c.full) + c.fixed);
+    if (rest)
+      t += c.fixed + steps * (i == 5 ? kSmallStep[(rest - 1) / cus] : c.alone + (c.full - c.alone) * float(rest) / float(cus));
+    if (i == 0 || t < least) {
+      best = i;
+      least = t;
+    }
+  }
+  return best;
+}
+
+namespace {
 
 template <class Ops, class E>
 Status block_gemm(const int8_t* A, int64_t lda, const int8_t* W, int64_t ldw, int M, int N, int K, const E& epi,
@@ -252,15 +450,17 @@ Status block_gemm(const int8_t* A, int64_t lda, const int8_t* W, int64_t ldw, in
   const int cus = compute_units();
   if (cus <= 0) return Status::make(DC_ERR_HIP, "int8 product: no device");
   const int la = int(lda), lw = int(ldw), kt = K / 128;
-  // a k-step moves the bytes and takes the time of a bf16 k-step: the same choice
-  switch (block_gemm_tile(M, N, K / 2, cus)) {
+  switch (i8_tile(M, N, kt, cus, Ops::kSwapped)) {
     case 0: return launch_dma<Ops, 384, 192, 4, 2, 2, 2>(A, la, W, lw, M, N, kt, epi, s);
     case 1: return launch_dma<Ops, 320, 256, 2, 4, 2, 2>(A, la, W, lw, M, N, kt, epi, s);
     case 2: return launch_dma<Ops, 256, 192, 4, 2, 2, 2>(A, la, W, lw, M, N, kt, epi, s);
     case 3: return launch_dma<Ops, 256, 128, 4, 2, 2, 3>(A, la, W, lw, M, N, kt, epi, s);
     case 4: return launch_pipe<Ops>(A, la, W, lw, M, N, kt, epi, s);
-    default: return launch_dma<Ops, 64, 64, 2, 2, 2, 3>(A, la, W, lw, M, N, kt, epi, s);
+    case 5: return launch_dma<Ops, 64, 64, 2, 2, 2, 3>(A, la, W, lw, M, N, kt, epi, s);
+    default: break;
   }
+  if constexpr (Ops::kSwapped) return launch_split<32, 32, 1, 1, kSplitGroups>(A, la, W, lw, M, N, kt, epi, s);
+  else return Status::shape("int8 product: no such tile");
 }
 
 }  // namespace

@@ -229,9 +229,13 @@ def check_linear(got, x, xs, w, ws, bias, gate, residual, kind, bf16):
 
 
 TILE_SHAPES = {     # (M, N, K): the tile on 256 compute units
-    (2562, 5760, 1920): "384x192", (2879, 6528, 4352): "320x256", (1155, 7680, 3840): "256x192",
-    (1537, 3456, 2304): "256x128", (1155, 1920, 3840): "128x128", (129, 384, 256): "64x64",
+    (2562, 5760, 1920): "384x192", (1155, 11520, 1920): "320x256", (1155, 7680, 3840): "256x192",
+    (1537, 3456, 2304): "256x128", (1155, 1920, 3840): "128x128", (513, 1920, 256): "64x64", (67, 1153, 1408): "32x32",
 }
+
+
+def i8_tile(m, n, k, cus):
+    return (TILES + ("32x32",))[_native("_ZN2dc7i8_tileEiiiib", m, n, k // 128, cus, True)]
 
 
 @pytest.mark.parametrize("mnk", list(TILE_SHAPES))
@@ -240,7 +244,7 @@ def test_linear_tiles(api, dev, mnk, kind):
     """Every tile of the product, ragged in rows; fp32 outputs, and bf16 ones where there are any."""
     import torch
     m, n, k = mnk
-    assert TILES[_native("_ZN2dc15block_gemm_tileEiiii", m, n, k // 2, compute_units(dev))] == TILE_SHAPES[mnk]
+    assert i8_tile(m, n, k, compute_units(dev)) == TILE_SHAPES[mnk]
     x, xs, w, ws, bias, gate, res = linear_inputs(m, n, k, 7)
     dx, dw, dxs, dws, db = t(x, dev), t(w, dev), t(xs, dev), t(ws, dev), t(bias, dev)
     for dt in (torch.float32, torch.bfloat16):

@@ -230,6 +230,14 @@ def test_binding_refuses_tensors_before_any_call():
         api.dc_rope_table(c, api.rope_axes((16, 24, 24)), torch.zeros(256, 3), torch.zeros(256, 32, 2))
 
 
+def test_product_shapes_take_the_tiles_they_name():
+    """The GPU tests' shapes are the ones the library's rule sends to each of its tiles."""
+    from tests import test_gpu_operators as G
+    from tests.gpu_util import TILES
+    assert {k: G.i8_tile(*k, 256) for k in G.TILE_SHAPES} == G.TILE_SHAPES
+    assert set(G.TILE_SHAPES.values()) == set(TILES) | {"32x32"}
+
+
 # ----------------------------------------------------------------------------
 # the definitions, by hand
 # ----------------------------------------------------------------------------
