@@ -257,12 +257,12 @@ Status block_forward(const Geo& g, const dc_block_weights* bw, const dc_block_ex
       uint16_t* ff = at<uint16_t>(ws, L.ff);
       const uint16_t* wqkv = static_cast<const uint16_t*>(bw->w_qkv);
       { ProfScope ps(KClass::kLnModulate, s); DC_TRY(ln_modulate(hb, N, d, shift1, scale1, a, d, true, g, s)); }
+      const float qsc = attention_q_scale(g.Dh);
       {
         ProfScope ps(KClass::kGemmQKV, s);
-        const float qsc = attention_q_scale(g.Dh);
         DC_TRY(gemm_bf16_qkv(a, wqkv, bw->b_qkv, qk, vt, L.ldv, e.qk ? 1.f : qsc, g, N, s));
-        if (e.qk) DC_TRY(qk_in_place(g, *e.qk, qk, 2 * d, qsc, s));
       }
+      if (e.qk) DC_TRY(qk_in_place(g, *e.qk, qk, 2 * d, qsc, s));
       {
         ProfScope ps(KClass::kAttention, s);
         DC_TRY(attention_bf16(qk, vt, L.ldv, o, g, N, at<float>(ws, L.attn_part), L.attn_part_bytes, s));

@@ -15,51 +15,13 @@ namespace {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 
+// The tile transposed (W's rows as the first operand): a lane ends with one row m and, per 32 columns, four runs
+// of four of them.
 struct OpsI8 {
   typedef i32x16 Acc;
-  static constexpr bool kSwapped = false;
-  static __device__ inline Acc mfma(uint4 a, uint4 b, const Acc& c) {
-    return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
-  }
-};
-
-// The tile transposed: a lane ends with one row m and, per 32 columns, four runs of four of them.
-struct OpsI8T {
-  typedef i32x16 Acc;
   static constexpr bool kSwapped = true;
-  static __device__ inline Acc mfma(uint4 a, uint4 b, const Acc& c) { return OpsI8::mfma(b, a, c); }
-};
-
-// An epilogue E on sums that still lack their scales.
-template <class E>
-struct EpiScaled {
-  const float* sx;
-  const float* sw;
-  E e;
-  static constexpr int kRowVec = E::kRowVec;
-  __device__ bool isrow(int n) const { return e.isrow(n); }
-  bool rows_aligned() const { return e.rows_aligned() && al16(sw); }
-  template <int NP>
-  __device__ void rows(int m0, int dm, int n, int M, float (&v)[NP][kRowVec]) const {
-    float w[kRowVec];
-#pragma unroll
-    for (int j = 0; j < kRowVec; j += 4) {
-      const float4 t = *reinterpret_cast<const float4*>(sw + n + j);
-      w[j] = t.x; w[j + 1] = t.y; w[j + 2] = t.z; w[j + 3] = t.w;
-    }
-#pragma unroll
-    for (int k = 0; k < NP; ++k) {
-      const float s = sx[min(m0 + k * dm, M - 1)];
-#pragma unroll
-      for (int j = 0; j < kRowVec; ++j) v[k][j] = v[k][j] * s * w[j];
-    }
-    e.template rows<NP>(m0, dm, n, M, v);
-  }
-  __device__ void col(int mb, int n, int M, f32x16 v) const {
-    const float w = sw[n];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = v[i] * sx[min(mb + 8 * (i >> 2) + (i & 3), M - 1)] * w;
-    e.col(mb, n, M, v);
+  static __device__ inline Acc mfma(uint4 a, uint4 b, const Acc& c) {
+    return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, b), __builtin_bit_cast(i32x4, a), c, 0, 0, 0);
   }
 };
 
@@ -268,6 +230,99 @@ struct EpiLinear {
   }
 };
 
+// The QKV product of a bf16 model: Q (times q_scale) and K as rows of qk [M, 2d], V transposed, [d, ldv].  Strips
+// of one 32-column tile: rows of 32 features for Q and K, rows of 32 tokens for V, 64 bytes each; the padding tokens
+// [M, ldv) of V get zeros, as the bf16 product's epilogue gives them.
+struct EpiQKV {
+  const float* sx;
+  const float* sw;
+  const float* bias;
+  uint16_t* qk;
+  uint16_t* vt;
+  int d, ldv;
+  float q_scale;
+  static constexpr int kS = 64 + 16;
+  static constexpr int kStrip = 32 * kS;
+  bool rows_aligned() const { return true; }
+
+  template <int BM, int BN, int NT>
+  __device__ inline void start(float4* vec, int m0, int n0, int M, int N, int tid) const {
+    static_assert(NT >= BM && NT >= BN, "a thread to a row and a column");
+    float* const v = reinterpret_cast<float*>(vec);
+    const int n = min(n0 + min(tid, BN - 1), N - 1);
+    const float x = sx[min(m0 + min(tid, BM - 1), M - 1)], g = n < d ? q_scale : 1.f;
+    const float w = sw[n] * g, b = bias[n] * g;
+    if (tid < BM) v[tid] = x;
+    if (tid < BN) {
+      v[BM + tid] = w;
+      v[BM + BN + tid] = b;
+    }
+  }
+  template <int BM, int BN, int WM, int WN, int TM, int TN>
+  __device__ inline void finish(i32x16 (&acc)[TM][TN], uint4* lds, const float4* vec, int m0, int n0, int M, int N,
+                                int wave, int lane) const {
+    const int r32 = lane & 31, hi = lane >> 5;
+    const int mt = (wave % WM) * (TM * 32), nt = (wave / WM) * (TN * 32);
+    const int mw = m0 + mt, nw = n0 + nt;
+    __builtin_amdgcn_s_waitcnt(0xC07F);               // lgkmcnt(0): this wave's reads of the last stage
+    __builtin_amdgcn_s_barrier();                     // every wave is done with it
+    asm volatile("" ::: "memory");
+    char* const strip = reinterpret_cast<char*>(lds) + wave * kStrip;
+    float s[TM];
+#pragma unroll
+    for (int a = 0; a < TM; ++a) s[a] = reinterpret_cast<const float*>(vec)[mt + a * 32 + r32];
+    const int pr = lane / 4, pc = lane % 4 * 8;       // a lane's pieces: rows pr and pr + 16 of a strip
+#pragma unroll
+    for (int b = 0; b < TN; ++b) {
+      const int nb = nw + b * 32;                     // N is a multiple of 32
+      if (nb >= N) return;
+      const bool is_v = nb >= 2 * d;
+      float4 w[4], o[4];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        w[g] = vec[(BM + nt + b * 32 + 8 * g + 4 * hi) / 4];
+        o[g] = vec[(BM + BN + nt + b * 32 + 8 * g + 4 * hi) / 4];
+      }
+#pragma unroll
+      for (int a = 0; a < TM; ++a) {
+        const bool in = mw + a * 32 + r32 < M;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float z0 = fmaf(float(acc[a][b][4 * g]) * s[a], w[g].x, o[g].x);
+          const float z1 = fmaf(float(acc[a][b][4 * g + 1]) * s[a], w[g].y, o[g].y);
+          const float z2 = fmaf(float(acc[a][b][4 * g + 2]) * s[a], w[g].z, o[g].z);
+          const float z3 = fmaf(float(acc[a][b][4 * g + 3]) * s[a], w[g].w, o[g].w);
+          const uint32_t p0 = pack_bf16(z0, z1), p1 = pack_bf16(z2, z3);
+          const int c = 8 * g + 4 * hi;
+          if (!is_v) {
+            *reinterpret_cast<uint2*>(strip + r32 * kS + 2 * c) = make_uint2(p0, p1);
+          } else {
+            char* const at = strip + c * kS + 2 * r32;
+            *reinterpret_cast<uint16_t*>(at) = in ? uint16_t(p0) : uint16_t(0);
+            *reinterpret_cast<uint16_t*>(at + kS) = in ? uint16_t(p0 >> 16) : uint16_t(0);
+            *reinterpret_cast<uint16_t*>(at + 2 * kS) = in ? uint16_t(p1) : uint16_t(0);
+            *reinterpret_cast<uint16_t*>(at + 3 * kS) = in ? uint16_t(p1 >> 16) : uint16_t(0);
+          }
+        }
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int r = pr + 16 * j;
+          const uint4 v = *reinterpret_cast<const uint4*>(strip + r * kS + 2 * pc);
+          if (!is_v) {
+            const int m = mw + a * 32 + r;
+            if (m < M) store_nt(qk + size_t(m) * 2 * d + nb + pc, v);
+          } else {
+            const int m = mw + a * 32 + pc;           // ldv is a multiple of 64: a piece lies inside or outside it
+            if (m < ldv) store_nt(vt + size_t(nb - 2 * d + r) * ldv + m, v);
+          }
+        }
+        asm volatile("" ::: "memory");
+      }
+    }
+  }
+};
+
 // Few tiles, long sums: G groups of WM x WN waves share a workgroup's tile, group g taking every G-th k-step
 // through a two-stage ring of its own, and add their sums in LDS (whole numbers: the same in any order).  All
 // threads then finish the tile, four columns of a row each.  A group of one wave waits for its own fills alone.
@@ -352,7 +407,7 @@ __global__ void __launch_bounds__(WM * WN * G * 64) k_i8_split(const char* __res
 #pragma unroll
           for (int a = 0; a < TM; ++a)
 #pragma unroll
-            for (int b = 0; b < TN; ++b) acc[a][b] = OpsI8T::mfma(af[a], bf[b], acc[a][b]);
+            for (int b = 0; b < TN; ++b) acc[a][b] = OpsI8::mfma(af[a], bf[b], acc[a][b]);
         }
       }
       __builtin_amdgcn_s_waitcnt(0xC07F);                         // lgkmcnt(0): the reads of this stage have returned
@@ -439,7 +494,7 @@ int i8_tile(int M, int N, int ksteps, int cus, bool split) {
 
 namespace {
 
-template <class Ops, class E>
+template <bool SPLIT, class E>
 Status block_gemm(const int8_t* A, int64_t lda, const int8_t* W, int64_t ldw, int M, int N, int K, const E& epi,
                   hipStream_t s) {
   if (M <= 0 || N <= 0) return Status::ok();
@@ -450,16 +505,16 @@ Status block_gemm(const int8_t* A, int64_t lda, const int8_t* W, int64_t ldw, in
   const int cus = compute_units();
   if (cus <= 0) return Status::make(DC_ERR_HIP, "int8 product: no device");
   const int la = int(lda), lw = int(ldw), kt = K / 128;
-  switch (i8_tile(M, N, kt, cus, Ops::kSwapped)) {
-    case 0: return launch_dma<Ops, 384, 192, 4, 2, 2, 2>(A, la, W, lw, M, N, kt, epi, s);
-    case 1: return launch_dma<Ops, 320, 256, 2, 4, 2, 2>(A, la, W, lw, M, N, kt, epi, s);
-    case 2: return launch_dma<Ops, 256, 192, 4, 2, 2, 2>(A, la, W, lw, M, N, kt, epi, s);
-    case 3: return launch_dma<Ops, 256, 128, 4, 2, 2, 3>(A, la, W, lw, M, N, kt, epi, s);
-    case 4: return launch_pipe<Ops>(A, la, W, lw, M, N, kt, epi, s);
-    case 5: return launch_dma<Ops, 64, 64, 2, 2, 2, 3>(A, la, W, lw, M, N, kt, epi, s);
+  switch (i8_tile(M, N, kt, cus, SPLIT)) {
+    case 0: return launch_dma<OpsI8, 384, 192, 4, 2, 2, 2>(A, la, W, lw, M, N, kt, epi, s);
+    case 1: return launch_dma<OpsI8, 320, 256, 2, 4, 2, 2>(A, la, W, lw, M, N, kt, epi, s);
+    case 2: return launch_dma<OpsI8, 256, 192, 4, 2, 2, 2>(A, la, W, lw, M, N, kt, epi, s);
+    case 3: return launch_dma<OpsI8, 256, 128, 4, 2, 2, 3>(A, la, W, lw, M, N, kt, epi, s);
+    case 4: return launch_pipe<OpsI8>(A, la, W, lw, M, N, kt, epi, s);
+    case 5: return launch_dma<OpsI8, 64, 64, 2, 2, 2, 3>(A, la, W, lw, M, N, kt, epi, s);
     default: break;
   }
-  if constexpr (Ops::kSwapped) return launch_split<32, 32, 1, 1, kSplitGroups>(A, la, W, lw, M, N, kt, epi, s);
+  if constexpr (SPLIT) return launch_split<32, 32, 1, 1, kSplitGroups>(A, la, W, lw, M, N, kt, epi, s);
   else return Status::shape("int8 product: no such tile");
 }
 
@@ -467,14 +522,13 @@ Status block_gemm(const int8_t* A, int64_t lda, const int8_t* W, int64_t ldw, in
 
 Status gemm_i8_qkv(const int8_t* A, const float* sx, const int8_t* W, const float* sw, const float* bias,
                    uint16_t* qk, uint16_t* vt, int ldv, float q_scale, const Geo& g, int M, hipStream_t s) {
-  typedef EpiScaled<EpiQKVBf16> E;
-  return block_gemm<OpsI8>(A, g.d, W, g.d, M, 3 * g.d, g.d, E{sx, sw, EpiQKVBf16{bias, qk, vt, g.d, ldv, q_scale}}, s);
+  return block_gemm<false>(A, g.d, W, g.d, M, 3 * g.d, g.d, EpiQKV{sx, sw, bias, qk, vt, g.d, ldv, q_scale}, s);
 }
 
 Status gemm_i8_linear(const LinearI8& a, hipStream_t s) {
   auto run = [&](auto e) {
     e = {a.x_scale, a.w_scale, a.bias, a.gate, a.residual, a.ld_residual, a.out, a.ld_out};
-    return block_gemm<OpsI8T>(a.x, a.ld_x, a.w, a.ld_w, a.M, a.N, a.K, e, s);
+    return block_gemm<true>(a.x, a.ld_x, a.w, a.ld_w, a.M, a.N, a.K, e, s);
   };
   if (a.gate) return run(EpiLinear<false, false, true>{});
   if (a.out_bf16) return a.gelu ? run(EpiLinear<true, true, false>{}) : run(EpiLinear<true, false, false>{});
