@@ -226,7 +226,7 @@ dc_status dc_qk_norm_rope(const dc_model_cfg* cfg, const dc_qk_cfg* qk, const vo
 
 /* Rows in 8 bits: scale[m] = max_k |x[m, k]| / 127, q[m, k] = x[m, k] / scale[m] rounded to the
  * nearest integer (ties to even), both divisions rounded to fp32.  Columns from `cols` up to the
- * next multiple of 128 are set to 0.  A row of zeros has scale 0 and codes 0; a row with an
+ * next multiple of 128 are set to 0, later ones are left as they were.  A row of zeros has scale 0 and codes 0; a row with an
  * infinity or NaN has scale NaN and codes 0, so a product with it is NaN.  x: [rows, ld_x] of
  * dtype (dc_dtype), any element-aligned address and ld_x >= cols; q: [rows, ld_q], ld_q at least
  * cols rounded up to 128; scale: [rows].  Serves activations (a scale per token) and weights
@@ -238,7 +238,7 @@ dc_status dc_quantize_rows(const void* x, int32_t dtype, int64_t ld_x, int32_t r
  * the rest in fp32, one rounding to out_dtype.  f: the value itself, GELU (tanh form), or
  * residual[m, n] + gate[n] * value. */
 typedef struct {
-  int32_t rows, out_features;     /* M, N; rows = 0 is a no-op */
+  int32_t rows, out_features;     /* M, N, below 2^24; rows = 0 is a no-op */
   int32_t in_features;            /* K with its padding: a multiple of 128, at most 130,944 */
   const int8_t* x;                /* [rows, ld_x], 16-byte aligned, ld_x a multiple of 16 */
   const float* x_scale;           /* [rows] */
@@ -253,7 +253,7 @@ typedef struct {
   int64_t ld_residual;
   void* out;                      /* [rows, ld_out] */
   int32_t out_dtype;              /* dc_dtype; DC_F32 with a gate */
-  int64_t ld_out;                 /* >= out_features; any, vector stores need 16-byte rows */
+  int64_t ld_out;                 /* >= out_features, rows at any element's address */
 } dc_linear_i8_args;
 dc_status dc_linear_i8(const dc_linear_i8_args* args, hipStream_t stream);
 
@@ -279,7 +279,9 @@ typedef struct {
   const int8_t* w_2;   const float* s_2;    /* [d, F], [d] */
 } dc_block_weights_i8;
 
-/* What a block does beyond dc_block_forward (host structs, read during the call). */
+/* What a block does beyond dc_block_forward (host structs, read during the call).  The anchor
+ * calibration (dc_calibrate_tables) takes its tangents through the plain block: tables of a
+ * network with norms or rotation come from elsewhere. */
 typedef struct {
   const dc_qk_cfg* qk;              /* norms and rotation between the QKV product and attention, or NULL */
   const dc_block_weights_i8* i8;    /* bf16 models: int8 products (rows quantised as they come), or NULL.

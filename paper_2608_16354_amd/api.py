@@ -238,15 +238,20 @@ def _dtype(t):
     return L.DC_BF16
 
 
-def _samples(idx, *batched):
-    """idx as a C array; every sample of it has to lie inside each of the batched tensors."""
+_INDEX = [C.c_int32 * max(n, 1) for n in range(L.DC_MAX_BATCH + 1)]
+
+
+def _samples(idx, batch):
+    """idx as a C array and its length; every sample of it has to lie inside a batch of that size."""
     n = len(idx)
-    if n:
-        most = max(idx)
-        for t in batched:
-            if most >= t.shape[0]:
-                _fail("a sample of idx lies outside the batch")
-    return (C.c_int32 * (n or 1))(*[int(i) for i in idx]), n
+    if n > L.DC_MAX_BATCH:
+        _fail("idx holds more than DC_MAX_BATCH samples")
+    if n and (idx[0] if n == 1 else max(idx)) >= batch:
+        _fail("a sample of idx lies outside the batch")
+    try:
+        return _INDEX[n](*idx), n
+    except TypeError:               # not Python's own integers
+        return _INDEX[n](*[int(i) for i in idx]), n
 
 
 def _tokens(cfg):
@@ -255,9 +260,11 @@ def _tokens(cfg):
 
 
 def _whole(t, shape, dtype, what):
-    """A contiguous [B, *shape] tensor."""
-    if t.dtype != dtype or not t.is_contiguous() or t.shape[1:] != shape:
+    """The B of a contiguous [B, *shape] tensor."""
+    s = t.shape
+    if t.dtype != dtype or not t.is_contiguous() or s[1:] != shape:
         _fail(f"{what}: a contiguous [B, {', '.join(map(str, shape))}] {dtype} tensor is wanted")
+    return s[0]
 
 
 def _rows(t, what):
@@ -313,11 +320,14 @@ def dc_qk_norm_rope(cfg, x, out, idx, q_weight=None, k_weight=None, eps=1e-6, ta
     n_tok, d2 = _tokens(cfg)[1], 2 * cfg.hidden
     dt = torch.bfloat16 if cfg.dtype == L.DC_BF16 else torch.float32
     for t in (x, out):
-        if t.dtype != dt or t.dim() != 3 or t.shape[1] != n_tok or t.shape[2] < d2 or t.stride(2) != 1 or (
-                n_tok > 1 and t.stride(1) < d2) or (t.shape[0] > 1 and t.stride(0) != n_tok * t.stride(1)):
+        ok = t.dtype == dt and t.dim() == 3
+        if ok:
+            (b, rows, cols), (apart, ld, one) = t.shape, t.stride()
+            ok = rows == n_tok and cols >= d2 and one == 1 and (ld >= d2 or n_tok <= 1) and (b <= 1 or apart == n_tok * ld)
+        if not ok:
             _fail(f"x and out: [B, {n_tok}, at least {d2}] {dt} tensors of equally spaced rows are wanted")
     qk = _qk_cfg(cfg, q_weight, k_weight, eps, table, interleaved)
-    arr, n = _samples(idx, x, out)
+    arr, n = _samples(idx, min(x.shape[0], out.shape[0]))
     s, dev = _on(stream, x, out, q_weight, k_weight, table)
     _call("dc_qk_norm_rope", dev, (C.byref(cfg), C.byref(qk), _at(x), x.stride(1), _at(out), out.stride(1), q_scale,
                                    arr, n, s))
@@ -366,11 +376,9 @@ def _cache_args(cfg, bits, a, b, codes, scales, idx):
     d = cfg.hidden
     f32 = torch.float32
     rows = (n_tok, d)
-    _whole(a, rows, f32, "h_in, h_out and g")
-    _whole(b, rows, f32, "h_in, h_out and g")
-    _whole(codes, (n_v, d * bits // 8), torch.int8 if bits == 8 else torch.uint8, "codes")
-    _whole(scales, (n_v, d // 64), f32, "scales")
-    return _samples(idx, a, b, codes, scales)
+    return _samples(idx, min(_whole(a, rows, f32, "h_in, h_out and g"), _whole(b, rows, f32, "h_in, h_out and g"),
+                             _whole(codes, (n_v, d * bits // 8), torch.int8 if bits == 8 else torch.uint8, "codes"),
+                             _whole(scales, (n_v, d // 64), f32, "scales")))
 
 
 def dc_cache_store_q(cfg, bits, h_out, h_in, codes, scales, idx, stream=None):

@@ -124,7 +124,8 @@ template <class T> T* at(void* base, size_t off) {
   return reinterpret_cast<T*>(static_cast<char*>(base) + off);
 }
 
-static bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+static bool aligned(const void* p, unsigned to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+static bool aligned16(const void* p) { return aligned(p, 16); }
 
 // norms and rotation of one sample's [N, ld] rows in the workspace
 static Status qk_in_place(const Geo& g, const dc_qk_cfg& c, void* qk, int ld, float q_scale, hipStream_t s) {
@@ -420,7 +421,7 @@ dc_status dc_rope_table(const dc_model_cfg* cfg, const dc_rope_axes* axes, const
     }
     if (sum > g.Dh) return Status::arg("axes->dim add up to more than head_dim");
     if (!(axes->theta > 0.0 && std::isfinite(axes->theta))) return Status::arg("axes->theta must be positive");
-    if (!aligned16(cos_sin) || reinterpret_cast<uintptr_t>(pos) % 8)
+    if (!aligned16(cos_sin) || !aligned(pos, 8))
       return Status::arg("cos_sin must be 16-byte, pos 8-byte aligned");
     return rope_table(*axes, pos, cos_sin, g, stream);
   })());
@@ -455,7 +456,8 @@ dc_status dc_quantize_rows(const void* x, int32_t dtype, int64_t ld_x, int32_t r
     if (!x || !q || !scale) return Status::arg("NULL argument");
     if (ld_x < cols || ld_q < (int64_t(cols) + 127) / 128 * 128)
       return Status::arg("ld_x must be at least cols, ld_q at least cols rounded up to 128");
-    if (reinterpret_cast<uintptr_t>(x) % (dtype == DC_BF16 ? 2 : 4)) return Status::arg("x is not element-aligned");
+    if (!aligned(x, dtype == DC_BF16 ? 2 : 4) || !aligned(scale, 4))
+      return Status::arg("a pointer is not aligned to its element");
     ProfScope ps(KClass::kQuantize, stream);
     return quantize_rows(x, dtype == DC_BF16, ld_x, rows, cols, q, ld_q, scale, stream);
   })());
@@ -465,7 +467,8 @@ dc_status dc_linear_i8(const dc_linear_i8_args* p, hipStream_t stream) {
   DC_ENTRY(([&]() -> Status {
     if (!p) return Status::arg("NULL argument");
     if (p->out_dtype != DC_F32 && p->out_dtype != DC_BF16) return Status::make(DC_ERR_DTYPE, "unknown dtype");
-    if (p->rows < 0 || p->out_features < 1) return Status::arg("rows must be >= 0, out_features positive");
+    if (p->rows < 0 || p->rows >= (1 << 24) || p->out_features < 1 || p->out_features >= (1 << 24))
+      return Status::arg("rows must be in [0, 2^24), out_features in [1, 2^24)");
     if (p->gelu != 0 && p->gelu != 1) return Status::arg("gelu must be 0 or 1");
     if (!p->gate != !p->residual) return Status::arg("gate and residual go together");
     if (p->gate && (p->gelu || p->out_dtype != DC_F32)) return Status::arg("a gated residual has fp32 outputs and no GELU");
@@ -474,6 +477,9 @@ dc_status dc_linear_i8(const dc_linear_i8_args* p, hipStream_t stream) {
     if (p->rows == 0) return Status::ok();
     if (!p->x || !p->x_scale || !p->w || !p->w_scale || !p->out) return Status::arg("NULL argument");
     if (!aligned16(p->x) || !aligned16(p->w)) return Status::arg("x and w must be 16-byte aligned");
+    if (!aligned(p->x_scale, 4) || !aligned(p->w_scale, 4) || !aligned(p->bias, 4) || !aligned(p->gate, 4) ||
+        !aligned(p->residual, 4) || !aligned(p->out, p->out_dtype == DC_BF16 ? 2 : 4))
+      return Status::arg("a pointer is not aligned to its element");
     if (p->gate && p->residual == p->out && p->ld_residual != p->ld_out)
       return Status::arg("in place: ld_residual and ld_out must be equal");
     return gemm_i8_linear({p->x, p->x_scale, p->ld_x, p->w, p->w_scale, p->ld_w, p->rows, p->out_features,

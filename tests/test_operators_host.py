@@ -78,7 +78,7 @@ def test_qk_norm_rope_of_no_samples_is_a_no_op(lib):
     ((FAKE, 1, 64, 4, 0, FAKE, 128, FAKE), ARG), ((None, 1, 64, 4, 64, FAKE, 128, FAKE), ARG),
     ((FAKE, 1, 64, 4, 64, None, 128, FAKE), ARG), ((FAKE, 1, 64, 4, 64, FAKE, 128, None), ARG),
     ((FAKE + 1, 1, 64, 4, 64, FAKE, 128, FAKE), ARG), ((FAKE + 2, 0, 64, 4, 64, FAKE, 128, FAKE), ARG),
-    ((None, 0, 64, 0, 64, None, 128, None), L.DC_OK)])
+    ((FAKE, 0, 64, 4, 64, FAKE, 128, FAKE + 2), ARG), ((None, 0, 64, 0, 64, None, 128, None), L.DC_OK)])
 def test_quantize_rows_refuses(lib, args, code):
     assert lib.dc_quantize_rows(*args, None) == code
 
@@ -100,7 +100,10 @@ GATED = dict(gate=FAKE, residual=FAKE, ld_residual=32, out=2 * FAKE)
     (dict(x=None), ARG), (dict(x_scale=None), ARG), (dict(w=None), ARG), (dict(w_scale=None), ARG), (dict(out=None), ARG),
     (dict(x=FAKE + 8), ARG), (dict(w=FAKE + 8), ARG), (dict(in_features=64), SHAPE), (dict(in_features=192), SHAPE),
     (dict(in_features=131072, ld_x=131072, ld_w=131072), SHAPE), (dict(ld_x=120), SHAPE), (dict(ld_w=136), SHAPE),
-    (dict(ld_x=(1 << 22) + 16), SHAPE), (dict(rows=1 << 24, out_features=1 << 20, ld_out=1 << 20), SHAPE),
+    (dict(ld_x=(1 << 22) + 16), SHAPE), (dict(rows=(1 << 24) - 1, out_features=1 << 20, ld_out=1 << 20), SHAPE),
+    (dict(rows=1 << 24), ARG), (dict(out_features=1 << 24, ld_out=1 << 24), ARG), (dict(out=FAKE + 2), ARG),
+    (dict(out=FAKE + 1, out_dtype=1), ARG), (dict(x_scale=FAKE + 2), ARG), (dict(w_scale=FAKE + 1), ARG),
+    (dict(bias=FAKE + 2), ARG), (dict(GATED, gate=FAKE + 2), ARG), (dict(GATED, residual=FAKE + 3), ARG),
     (dict(rows=0, x=None, out=None), L.DC_OK)])
 def test_linear_i8_refuses(lib, more, code):
     a = linear(**more)
