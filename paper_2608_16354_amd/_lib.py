@@ -175,6 +175,27 @@ def load() -> C.CDLL:
     return _lib
 
 
+_binding = None
+
+
+def binding():
+    """The tensor binding (binding.cpp) on the loaded library; raises if it has not been built."""
+    global _binding
+    if _binding is None:
+        lib = load()
+        import torch  # noqa: F401  (the libraries that the binding is linked against)
+        try:
+            from . import _binding as b
+        except ImportError as e:
+            raise ImportError("_binding.so is missing or does not fit this torch: build it with "
+                              "python -m paper_2608_16354_amd.build") from e
+        b.init(*[C.cast(getattr(lib, n), vp).value for n in (
+            "dc_rope_table", "dc_qk_norm_rope", "dc_quantize_rows", "dc_linear_i8", "dc_cache_store_q",
+            "dc_cache_apply_q")])
+        _binding = b
+    return _binding
+
+
 def check(fn: str, code: int):
     if code != DC_OK:
         msg = load().dc_last_error().decode(errors="replace")

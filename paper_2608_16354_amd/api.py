@@ -188,104 +188,34 @@ def dc_calibrate_tables(dm: DeviceModel, x1, txt, sigmas, h_max: int, eps: float
 # ----------------------------------------------------------------------------
 # rotary positions, query/key norms, int8 products, quantised cache
 # ----------------------------------------------------------------------------
-# These calls take a few microseconds on the GPU, so what surrounds the C call (3.4 us with its launch) is kept
-# to attribute reads: 2 us.
-def _fail(what):
-    raise ValueError(what)
+# These calls take a few microseconds on the GPU: binding.cpp checks their tensors (ValueError) and makes the C call.
+_current = None         # torch's (raw stream of a device, current device)
 
 
-def _on(stream, first, *more):
-    """The current stream of the tensors' device (or `stream`, which has to be one of it), and that device where it
-    is not the current one."""
-    torch = _torch()
+def _call(name, stream, first, *args):
+    """The binding's function on args, on the current stream of the device that `first` is on (or on `stream`, which
+    has to be one of it), with that device current."""
+    global _current
+    if _current is None:
+        torch = _torch()
+        _current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
     i = first.get_device()
     if i < 0:
-        _fail("tensors must be on a GPU")
-    for t in more:
-        if t is not None and t.get_device() != i:
-            _fail("tensors must be on one GPU")
+        raise ValueError("tensors must be on a GPU")
     if stream is None:
-        s = torch._C._cuda_getCurrentRawStream(i)
-    else:
-        if stream.device.index != i:
-            _fail("the stream belongs to another device")
+        s = _current[0](i)
+    elif stream.device.index == i:
         s = stream.cuda_stream
-    return s, None if torch._C._cuda_getDevice() == i else i
-
-
-def _call(name, device, args):
-    """The C function on args, with `device` current if it is not None."""
-    f = getattr(L.load(), name)
-    if device is None:
-        rc = f(*args)
     else:
-        with _torch().cuda.device(device):
-            rc = f(*args)
+        raise ValueError("the stream belongs to another device")
+    f = getattr(L._binding or L.binding(), name)
+    if _current[1]() == i:
+        rc = f(*args, i, s)
+    else:
+        with _torch().cuda.device(i):
+            rc = f(*args, i, s)
     if rc:
         L.check(name, rc)
-
-
-def _at(t):
-    return None if t is None else t.data_ptr()
-
-
-def _dtype(t):
-    torch = _torch()
-    if t.dtype == torch.float32:
-        return L.DC_F32
-    if t.dtype != torch.bfloat16:
-        _fail("float32 or bfloat16 tensors only")
-    return L.DC_BF16
-
-
-_INDEX = [C.c_int32 * max(n, 1) for n in range(L.DC_MAX_BATCH + 1)]
-
-
-def _samples(idx, batch):
-    """idx as a C array and its length; every sample of it has to lie inside a batch of that size."""
-    n = len(idx)
-    if n > L.DC_MAX_BATCH:
-        _fail("idx holds more than DC_MAX_BATCH samples")
-    if n and (idx[0] if n == 1 else max(idx)) >= batch:
-        _fail("a sample of idx lies outside the batch")
-    try:
-        return _INDEX[n](*idx), n
-    except TypeError:               # not Python's own integers
-        return _INDEX[n](*[int(i) for i in idx]), n
-
-
-def _tokens(cfg):
-    n_v = cfg.lat_t * (cfg.lat_h // cfg.patch) * (cfg.lat_w // cfg.patch)
-    return n_v, n_v + cfg.n_txt
-
-
-def _whole(t, shape, dtype, what):
-    """The B of a contiguous [B, *shape] tensor."""
-    s = t.shape
-    if t.dtype != dtype or not t.is_contiguous() or s[1:] != shape:
-        _fail(f"{what}: a contiguous [B, {', '.join(map(str, shape))}] {dtype} tensor is wanted")
-    return s[0]
-
-
-def _rows(t, what):
-    """A 2-d tensor whose rows are contiguous and apart: its row stride in elements."""
-    if t.dim() == 2:
-        (rows, cols), (ld, step) = t.shape, t.stride()
-        if rows <= 1:
-            ld = max(ld, cols)
-        if (cols <= 1 or step == 1) and ld >= cols:
-            return ld
-    _fail(f"{what}: a 2-d tensor with contiguous rows that do not overlap is wanted")
-
-
-def _vector(t, n, what):
-    if t is not None and (t.dtype != _torch().float32 or t.shape != (n,) or not t.is_contiguous()):
-        _fail(f"{what}: a contiguous float32 [{n}] tensor is wanted")
-
-
-def _table(cfg, t):
-    if t.dtype != _torch().float32 or not t.is_contiguous() or t.shape != (_tokens(cfg)[0], cfg.head_dim // 2, 2):
-        _fail("table: a contiguous float32 [N_v, head_dim / 2, 2] tensor is wanted")
 
 
 def rope_axes(dim, theta=10000.0, start=(0.0, 0.0, 0.0), step=(1.0, 1.0, 1.0)) -> L.RopeAxes:
@@ -296,104 +226,47 @@ def rope_axes(dim, theta=10000.0, start=(0.0, 0.0, 0.0), step=(1.0, 1.0, 1.0)) -
 
 def dc_rope_table(cfg, axes: L.RopeAxes, pos, table, stream=None):
     """table (f32 [N_v, head_dim / 2, 2]) := cos and sin; pos: f64 [N_v, 3] or None (the grid)."""
-    _table(cfg, table)
-    if pos is not None and (pos.dtype != _torch().float64 or not pos.is_contiguous()
-                            or pos.shape != (table.shape[0], 3)):
-        _fail("pos: a contiguous float64 [N_v, 3] tensor or None is wanted")
-    s, dev = _on(stream, table, pos)
-    _call("dc_rope_table", dev, (C.byref(cfg), C.byref(axes), _at(pos), _at(table), s))
-
-
-def _qk_cfg(cfg, q_weight, k_weight, eps, table, interleaved):
-    _vector(q_weight, cfg.head_dim, "q_weight")
-    _vector(k_weight, cfg.head_dim, "k_weight")
-    if table is not None:
-        _table(cfg, table)
-    return L.QkCfg(_at(q_weight), _at(k_weight), eps, _at(table), 1 if interleaved else 0)
+    _call("dc_rope_table", stream, table, cfg, axes, pos, table)
 
 
 def dc_qk_norm_rope(cfg, x, out, idx, q_weight=None, k_weight=None, eps=1e-6, table=None, interleaved=True,
                     q_scale=1.0, stream=None):
     """Norms and rotation of the queries (columns [0, d)) and keys ([d, 2d)) of x [B, N, >= 2d] into out
     (x itself, or a tensor like it): RMS norm with q_weight / k_weight where given, rotation where table is."""
-    torch = _torch()
-    n_tok, d2 = _tokens(cfg)[1], 2 * cfg.hidden
-    dt = torch.bfloat16 if cfg.dtype == L.DC_BF16 else torch.float32
-    for t in (x, out):
-        ok = t.dtype == dt and t.dim() == 3
-        if ok:
-            (b, rows, cols), (apart, ld, one) = t.shape, t.stride()
-            ok = rows == n_tok and cols >= d2 and one == 1 and (ld >= d2 or n_tok <= 1) and (b <= 1 or apart == n_tok * ld)
-        if not ok:
-            _fail(f"x and out: [B, {n_tok}, at least {d2}] {dt} tensors of equally spaced rows are wanted")
-    qk = _qk_cfg(cfg, q_weight, k_weight, eps, table, interleaved)
-    arr, n = _samples(idx, min(x.shape[0], out.shape[0]))
-    s, dev = _on(stream, x, out, q_weight, k_weight, table)
-    _call("dc_qk_norm_rope", dev, (C.byref(cfg), C.byref(qk), _at(x), x.stride(1), _at(out), out.stride(1), q_scale,
-                                   arr, n, s))
+    _call("dc_qk_norm_rope", stream, x, cfg, x, out, idx, q_weight, k_weight, eps, table, interleaved, q_scale)
 
 
 def dc_quantize_rows(x, q, scale, stream=None):
     """q (int8 [rows, at least cols rounded up to 128]) and scale (f32 [rows]) := the rows of x [rows, cols]."""
-    ldx, ldq = _rows(x, "x"), _rows(q, "q")
-    rows, cols = x.shape
-    if q.dtype != _torch().int8 or q.shape[0] != rows or q.shape[1] < -(-cols // 128) * 128:
-        _fail("q: an int8 tensor of x's rows, at least cols rounded up to 128 wide, is wanted")
-    _vector(scale, rows, "scale")
-    s, dev = _on(stream, x, q, scale)
-    _call("dc_quantize_rows", dev, (_at(x), _dtype(x), ldx, rows, cols, _at(q), ldq, _at(scale), s))
+    _call("dc_quantize_rows", stream, x, x, q, scale)
 
 
 def dc_linear_i8(x, x_scale, w, w_scale, out, bias=None, gelu=False, gate=None, residual=None, stream=None):
     """out [M, N] := the product of int8 rows x [M, K] and w [N, K] (K as padded by dc_quantize_rows) with
     their scales, plus bias, through GELU or as residual + gate * (...)."""
-    torch = _torch()
-    ldx, ldw, ldo, ldr = _rows(x, "x"), _rows(w, "w"), _rows(out, "out"), 0
-    (m, k), n = x.shape, w.shape[0]
-    if x.dtype != torch.int8 or w.dtype != torch.int8 or w.shape[1] != k:
-        _fail("x and w: int8 tensors of equally long rows are wanted")
-    if out.shape != (m, n):
-        _fail("out: a [rows of x, rows of w] tensor is wanted")
-    _vector(x_scale, m, "x_scale")
-    _vector(w_scale, n, "w_scale")
-    _vector(bias, n, "bias")
-    _vector(gate, n, "gate")
-    if residual is not None:
-        ldr = _rows(residual, "residual")
-        if residual.dtype != torch.float32 or residual.shape != (m, n):
-            _fail("residual: a float32 tensor of out's shape is wanted")
-    s, dev = _on(stream, x, x_scale, w, w_scale, out, bias, gate, residual)
-    a = L.LinearI8Args(m, n, k, _at(x), _at(x_scale), ldx, _at(w), _at(w_scale), ldw, _at(bias), 1 if gelu else 0,
-                       _at(gate), _at(residual), ldr, _at(out), _dtype(out), ldo)
-    _call("dc_linear_i8", dev, (C.byref(a), s))
-
-
-def _cache_args(cfg, bits, a, b, codes, scales, idx):
-    torch = _torch()
-    if bits not in (8, 4):
-        _fail("bits must be 8 or 4")
-    n_v, n_tok = _tokens(cfg)
-    d = cfg.hidden
-    f32 = torch.float32
-    rows = (n_tok, d)
-    return _samples(idx, min(_whole(a, rows, f32, "h_in, h_out and g"), _whole(b, rows, f32, "h_in, h_out and g"),
-                             _whole(codes, (n_v, d * bits // 8), torch.int8 if bits == 8 else torch.uint8, "codes"),
-                             _whole(scales, (n_v, d // 64), f32, "scales")))
+    _call("dc_linear_i8", stream, x, x, x_scale, w, w_scale, out, bias, gelu, gate, residual)
 
 
 def dc_cache_store_q(cfg, bits, h_out, h_in, codes, scales, idx, stream=None):
     """codes (int8 [B, N_v, d], or uint8 [B, N_v, d / 2] for 4 bits) and scales (f32 [B, N_v, d / 64]) :=
     h_out - h_in on the video rows."""
-    arr, n = _cache_args(cfg, bits, h_out, h_in, codes, scales, idx)
-    s, dev = _on(stream, h_out, h_in, codes, scales)
-    _call("dc_cache_store_q", dev, (C.byref(cfg), bits, _at(h_out), _at(h_in), _at(codes), _at(scales), arr, n, s))
+    _call("dc_cache_store_q", stream, h_out, cfg, bits, h_out, h_in, codes, scales, idx)
 
 
 def dc_cache_apply_q(cfg, bits, h_in, codes, scales, g, idx, stream=None):
     """g := h_in + the cached residual on the video rows (g may be h_in)."""
-    arr, n = _cache_args(cfg, bits, h_in, g, codes, scales, idx)
-    s, dev = _on(stream, h_in, codes, scales, g)
-    _call("dc_cache_apply_q", dev, (C.byref(cfg), bits, _at(h_in), _at(codes), _at(scales), _at(g), arr, n, s))
+    _call("dc_cache_apply_q", stream, h_in, cfg, bits, h_in, g, codes, scales, idx)
+
+
+def _tokens(cfg):
+    n_v = cfg.lat_t * (cfg.lat_h // cfg.patch) * (cfg.lat_w // cfg.patch)
+    return n_v, n_v + cfg.n_txt
+
+
+def _floats(t, shape, what):
+    if t is not None and (t.dtype != _torch().float32 or tuple(t.shape) != shape or not t.is_contiguous()):
+        raise ValueError(f"{what}: a contiguous float32 {list(shape)} tensor is wanted")
+    return None if t is None else t.data_ptr()
 
 
 class BlockExt:
@@ -411,8 +284,10 @@ class BlockExt:
         self.c = (L.BlockExt * n)()
         for l, b in enumerate(dm.blocks):
             if q_weight is not None or k_weight is not None or table is not None:
-                qk = _qk_cfg(dm.cfg, None if q_weight is None else q_weight[l],
-                             None if k_weight is None else k_weight[l], eps, table, interleaved)
+                dh = (dm.cfg.head_dim,)
+                qk = L.QkCfg(_floats(None if q_weight is None else q_weight[l], dh, "q_weight"),
+                             _floats(None if k_weight is None else k_weight[l], dh, "k_weight"), eps,
+                             _floats(table, (_tokens(dm.cfg)[0], dh[0] // 2, 2), "table"), 1 if interleaved else 0)
                 self.keep.append(qk)
                 self.c[l].qk = C.pointer(qk)
             if int8:
@@ -539,7 +414,7 @@ class SamplerBuffers:
         self.cache_scales = None
         if cache_bits:
             if cache_bits not in (8, 4):
-                _fail("cache_bits must be 0, 8 or 4")
+                raise ValueError("cache_bits must be 0, 8 or 4")
             self.resid = torch.empty((E, m.n_v, m.hidden * cache_bits // 8), device=device,
                                      dtype=torch.int8 if cache_bits == 8 else torch.uint8)
             self.cache_scales = torch.empty((E, m.n_v, m.hidden // 64), device=device, dtype=torch.float32)
@@ -576,7 +451,7 @@ class Sampler:
         self.bufs = bufs
         assert self.bufs.B == B and self.bufs.K == self.K
         if bufs.cache_bits != cache_bits:
-            _fail("bufs were made for another cache_bits")
+            raise ValueError("bufs were made for another cache_bits")
         self.bufs.x.copy_(x1, non_blocking=True)
         if dm.m.n_txt:
             self.bufs.txt.copy_(txt, non_blocking=True)

@@ -1,22 +1,24 @@
-"""Build the HIP library libdrivecache.so (gfx950) in-tree.
+"""Build the HIP library libdrivecache.so (gfx950) and the tensor binding _binding.so in-tree.
 
     python -m paper_2608_16354_amd.build
 
 Device sources (*.hip) go through hipcc for gfx950; host sources (*.cpp) through
 amdclang++ with -ffp-contract=off, so the schedule's floating-point arithmetic
-is one IEEE operation at a time.
+is one IEEE operation at a time.  The binding (binding.cpp) is built against torch's headers.
 """
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libdrivecache.so")
+BINDING = os.path.join(PKG, "_binding.so")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 ARCH = "gfx950"
 
@@ -40,6 +42,16 @@ def sources():
     return sorted(f for f in os.listdir(CSRC) if f.endswith((".hip", ".cpp")))
 
 
+def _binding_cmd(clang, out):
+    import torch
+    t = os.path.dirname(torch.__file__)
+    return [clang, "-O2", "-fPIC", "-shared", "-std=c++17", "-Wall", "-D__HIP_PLATFORM_AMD__",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            "-isystem", f"{t}/include", "-isystem", f"{t}/include/torch/csrc/api/include",
+            "-isystem", sysconfig.get_paths()["include"], f"-I{ROCM}/include",
+            os.path.join(PKG, "binding.cpp"), "-o", out, f"-L{t}/lib", "-ltorch_python", "-ltorch_cpu", "-lc10"]
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     hipcc = os.path.join(ROCM, "bin", "hipcc")
@@ -54,6 +66,7 @@ def build(verbose: bool = False) -> str:
             jobs.append([hipcc, *HIPCC_FLAGS, *EXTRA_FLAGS.get(f, []), "-c", src, "-o", obj])
         else:
             jobs.append([clang, *HOST_FLAGS, "-c", src, "-o", obj])
+    jobs.append(_binding_cmd(clang, BINDING + ".tmp"))
     with ThreadPoolExecutor(max(1, min(8, os.cpu_count() or 1))) as ex:
         outs = list(ex.map(_run, jobs))
     if verbose:
@@ -64,6 +77,7 @@ def build(verbose: bool = False) -> str:
     _run([hipcc, "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp, *objs,
           f"-L{ROCM}/lib", "-lamdhip64"])
     os.replace(tmp, LIB)
+    os.replace(BINDING + ".tmp", BINDING)
     return LIB
 
 

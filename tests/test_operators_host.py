@@ -201,36 +201,121 @@ def test_sampler_ext_refuses(lib):
     assert create(L.SamplerExt(ext, None, 0, None), full) == DTYPE     # an fp32 model
 
 
-def test_binding_refuses_tensors_before_any_call():
+# ----------------------------------------------------------------------------
+# the binding: host tensors, which it refuses last, so that every other check is seen here
+# ----------------------------------------------------------------------------
+def refused(match, name, *args):
+    with pytest.raises(ValueError, match=match):
+        getattr(L.binding(), name)(*args, -1, 0)
+
+
+def test_binding_refuses_rows():
+    import torch
+    x, q, s = torch.zeros(4, 100), torch.zeros(4, 128, dtype=torch.int8), torch.zeros(4)
+    f = "dc_quantize_rows"
+    refused("on a GPU", f, x, q, s)
+    refused("on a GPU", f, x[:, 1:], q, s)
+    refused("on a GPU", f, x.bfloat16()[:1], q[:1], s[:1])
+    for bad in (q[:, :64], q[:3], q.float(), q.to(torch.uint8)):
+        refused("q: ", f, x, bad, s)
+    for bad in (x.t(), x[:1].expand(4, 100), x[0], x[:, ::2]):
+        refused("x: ", f, bad, q, s)
+    for bad in (s.double(), torch.zeros(5), torch.zeros(8)[::2], torch.zeros(4, 1)):
+        refused("scale: ", f, x, q, bad)
+    refused("bfloat16", f, x.half(), q, s)
+    refused("tensor", f, x, q, None)
+    refused("tensor", f, [1.0], q, s)
+    refused("arguments", f, x, q)
+
+
+def test_binding_refuses_products():
+    import torch
+    q, s = torch.zeros(4, 128, dtype=torch.int8), torch.zeros(4)
+    w, ws, out, n = torch.zeros(8, 128, dtype=torch.int8), torch.zeros(8), torch.zeros(4, 8), None
+
+    def f(match, x=q, xs=s, w=w, ws=ws, out=out, bias=n, gelu=False, gate=n, residual=n):
+        refused(match, "dc_linear_i8", x, xs, w, ws, out, bias, gelu, gate, residual)
+
+    f("on a GPU")
+    f("on a GPU", bias=ws, gate=ws, residual=out)
+    f("on a GPU", out=torch.zeros(4, 12)[:, 3:11])
+    f("equally long", w=w[:, :64])
+    f("equally long", x=q.to(torch.uint8))
+    f("rows of x, rows of w", out=out[:, :7])
+    f("rows of x, rows of w", out=out[:3])
+    f("contiguous rows", out=torch.zeros(8, 4).t())
+    f("contiguous rows", residual=out[:1].expand(4, 8), gate=ws)
+    f("x_scale", xs=ws)
+    f("w_scale", ws=s)
+    f("bias", bias=s)
+    f("gate", gate=ws.double(), residual=out)
+    f("residual", gate=ws, residual=out[:, :7])
+    f("residual", gate=ws, residual=out.bfloat16())
+    f("bfloat16", out=out.half())
+    f("tensor", xs=None)
+
+
+def test_binding_refuses_caches():
+    import torch
+    c = cfg()
+    h, k8, sc = torch.zeros(2, 272, 256), torch.zeros(2, 256, 256, dtype=torch.int8), torch.zeros(2, 256, 4)
+    k4 = torch.zeros(2, 256, 128, dtype=torch.uint8)
+    for f in ("dc_cache_store_q", "dc_cache_apply_q"):
+        refused("on a GPU", f, c, 8, h, h, k8, sc, [0, 1])
+        refused("on a GPU", f, c, 4, h, h, k4, sc, np.array([1]))
+        refused("on a GPU", f, c, 4, h, h, k4, sc, ())
+        for idx_ in ([2], [-1], [0, 1, 2], list(range(65)), [0.5], "x", 3):
+            with pytest.raises((ValueError, TypeError)):
+                getattr(L.binding(), f)(c, 8, h, h, k8, sc, idx_, -1, 0)
+        for bits, codes in ((4, k8), (8, k4), (8, k8.to(torch.uint8)), (8, k8[:, :255]), (8, k8[:, :, :255]), (8, k8[0])):
+            refused("codes: ", f, c, bits, h, h, codes, sc, [0])
+        for bad in (sc[:, :, :3], sc.double(), sc.transpose(1, 2)):
+            refused("scales: ", f, c, 8, h, h, k8, bad, [0])
+        for bad in (h[:, :271], h.bfloat16(), h[:, :, :255], h.transpose(0, 1)):
+            refused("h_in", f, c, 8, bad, h, k8, sc, [0])
+            refused("h_in", f, c, 8, h, bad, k8, sc, [0])
+        refused("bits", f, c, 6, h, h, k8, sc, [0])
+        refused("cfg", f, axes(), 8, h, h, k8, sc, [0])
+        refused("patch", f, L.ModelCfg(2, 256, 4, 64, 1024, 16, 4, 16, 16, 0, 16, 0, 1e-6), 8, h, h, k8, sc, [0])
+        # batches of different sizes: the smallest counts
+        refused("idx", f, c, 8, h, h, k8[:1], sc, [1])
+        refused("idx", f, c, 8, h, h[:1], k8, sc, [1])
+
+
+def test_binding_refuses_norms_and_tables():
+    import torch
+    c = cfg()
+    b = torch.zeros(2, 272, 768, dtype=torch.bfloat16)
+    o, wt, t = torch.zeros(2, 272, 512, dtype=torch.bfloat16), torch.zeros(64), torch.zeros(256, 32, 2)
+
+    def f(match, x=b, out=o, idx_=(0, 1), wq=wt, wk=wt, table=t):
+        refused(match, "dc_qk_norm_rope", c, x, out, idx_, wq, wk, 1e-6, table, True, 1.0)
+
+    f("on a GPU")
+    f("on a GPU", wq=None, wk=None, table=None)
+    f("on a GPU", x=b[:1], idx_=[0])
+    for bad in (b.float(), b[:, :, :500], b[:, :271], b[0], b[:, :, ::2][:, :, :384], b[:, :1].expand(2, 272, 768)):
+        f("x and out", x=bad)
+        f("x and out", out=bad)
+    f("idx", out=o[:1])
+    f("q_weight", wq=torch.zeros(63))
+    f("k_weight", wk=wt.double())
+    for bad in (t[:255], t[:, :31], t.double(), t[..., :1]):
+        f("table", table=bad)
+        refused("table", "dc_rope_table", c, axes(), None, bad)
+    refused("on a GPU", "dc_rope_table", c, axes(), None, t)
+    refused("on a GPU", "dc_rope_table", c, axes(), torch.zeros(256, 3, dtype=torch.float64), t)
+    for bad in (torch.zeros(256, 3), torch.zeros(255, 3, dtype=torch.float64), torch.zeros(3, 256, dtype=torch.float64).t()):
+        refused("pos", "dc_rope_table", c, axes(), bad, t)
+    refused("axes", "dc_rope_table", c, c, None, t)
+    refused("tensor", "dc_rope_table", c, axes(), None, None)
+
+
+def test_api_refuses_host_tensors():
     import torch
     from paper_2608_16354_amd import api
-    c = cfg()
-    x, q, s = torch.zeros(4, 100), torch.zeros(4, 128, dtype=torch.int8), torch.zeros(4)
-    for a in ((x, q[:, :64], s), (x, q[:3], s), (x, q.float(), s), (x.t(), q, s), (x, q, s.double()), (x, q, torch.zeros(5)),
-              (x[:1].expand(4, 100), q, s), (x, q, s)):     # the last: not on a GPU
-        with pytest.raises(ValueError):
-            api.dc_quantize_rows(*a)
-    w, ws, out = torch.zeros(8, 128, dtype=torch.int8), torch.zeros(8), torch.zeros(4, 8)
-    for a in ((q, s, w[:, :64], ws, out), (q, s, w, ws, out[:, :7]), (q, s, w, s, out), (q, ws, w, ws, out), (q, s, w, ws, out.t()),
-              (q.to(torch.uint8), s, w, ws, out), (q, s, w, ws, out)):
-        with pytest.raises(ValueError):
-            api.dc_linear_i8(*a)
-    h, k8 = torch.zeros(1, 272, 256), torch.zeros(1, 256, 256, dtype=torch.int8)
-    sc = torch.zeros(1, 256, 4)
-    for bits, codes, scales, i in ((8, k8, sc, [1]), (4, k8, sc, [0]), (8, k8.to(torch.uint8), sc, [0]), (8, k8, sc[:, :, :3], [0]),
-                                   (6, k8, sc, [0]), (8, k8, sc, [0])):
-        with pytest.raises(ValueError):
-            api.dc_cache_store_q(c, bits, h, h, codes, scales, i)
-        with pytest.raises(ValueError):
-            api.dc_cache_apply_q(c, bits, h, codes, scales, h, i)
-    b = torch.zeros(1, 272, 512, dtype=torch.bfloat16)
-    for src, dst, i in ((b.float(), b, [0]), (b, b[:, :, :500], [0]), (b[:, :271], b, [0]), (b, b, [1]), (b, b, [0])):
-        with pytest.raises(ValueError):
-            api.dc_qk_norm_rope(c, src, dst, i)
-    with pytest.raises(ValueError):
-        api.dc_rope_table(c, api.rope_axes((16, 24, 24)), None, torch.zeros(256, 32, 2))
-    with pytest.raises(ValueError):
-        api.dc_rope_table(c, api.rope_axes((16, 24, 24)), torch.zeros(256, 3), torch.zeros(256, 32, 2))
+    with pytest.raises(ValueError, match="on a GPU"):
+        api.dc_quantize_rows(torch.zeros(4, 100), torch.zeros(4, 128, dtype=torch.int8), torch.zeros(4))
 
 
 def test_product_shapes_take_the_tiles_they_name():
