@@ -3,9 +3,12 @@
 // The sums are whole numbers held in int32, so they are exact and any order gives the same: K <=
 // kMaxK keeps 128^2 K below 2^31.  They become fp32 (one rounding, none below 2^24), then the scales,
 // the bias and the rest of the epilogue follow in fp32 and the result is rounded once.
-// Tiles, pipeline and epilogues are gemm_tile.h's: a k-step is 128 bytes, here 128 k, and
-// v_mfma_i32_32x32x32_i8 takes the 16 bytes per lane that v_mfma_f32_32x32x16_bf16 takes, in as many
-// cycles, for twice the multiplications.
+// Tiles and pipelines are gemm_tile.h's: a k-step is 128 bytes, here 128 k, and v_mfma_i32_32x32x32_i8 takes the 16
+// bytes per lane that v_mfma_f32_32x32x16_bf16 takes, in as many cycles, for twice the multiplications.  The
+// epilogues are of their own, as is the kernel for few rows (k_i8_split).
+// Long calls are bound by the matrix pipe and the clock that it leaves (1.94 GHz): 16,384 x 16,384 x 8,192 1.69 ms, 2.60
+// POP/s (torch's int8 product 2.25), 2.95 with the LDS-DMA taken out; 17,776 x 1,920 x 7,680 with the gated residual 250 us,
+// 2.10, and at K = 1,920, where a tile has 15 k-steps, by what surrounds them too: MLP up with GELU 278 us, 1.89.
 #include "gemm_tile.h"
 
 namespace dc {
@@ -323,167 +326,128 @@ struct EpiQKV {
   }
 };
 
-// Few tiles, long sums: G groups of WM x WN waves share a workgroup's tile, group g taking every G-th k-step
-// through a two-stage ring of its own, and add their sums in LDS (whole numbers: the same in any order).  All
-// threads then finish the tile, four columns of a row each.  A group of one wave waits for its own fills alone.
-template <int BM, int BN, int WM, int WN, int G, class Epi>
-__global__ void __launch_bounds__(WM * WN * G * 64) k_i8_split(const char* __restrict__ A, int lda,
-                                                               const char* __restrict__ W, int ldw, int M, int N,
-                                                               int KT, int tiles_n, Epi epi) {
-  constexpr int NW = WM * WN, NT = NW * G * 64;
-  constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 32, TN = WTN / 32;
-  constexpr int AI = BM * 8 / 64 / NW, BI = BN * 8 / 64 / NW;     // DMA instructions per wave
-  static_assert(AI * NW * 64 == BM * 8 && BI * NW * 64 == BN * 8, "tile shape");
-  constexpr int STAGE = (BM + BN) * 8;                            // 16-byte chunks
-  constexpr int LS = BN + 4;                                      // ints of a row of partial sums
-  constexpr int RING = G * 2 * STAGE, JOIN = G * BM * LS / 4;
-  __shared__ uint4 lds[RING > JOIN ? RING : JOIN];
-  __shared__ float4 s_vec[(BM + 2 * BN) / 4];
+// Few tiles, long sums: G waves share a workgroup's 32 x 32 tile, wave g taking every G-th k-step through a two-stage
+// ring of its own (it waits for its own fills alone), and add their sums in LDS (whole numbers: the same in any
+// order).  All threads then finish the tile, four columns of a row each.
+template <int G, class Epi>
+__global__ void __launch_bounds__(G * 64) k_i8_split(const char* __restrict__ A, int lda, const char* __restrict__ W,
+                                                     int ldw, int M, int N, int KT, int tiles_n, Epi epi) {
+  constexpr int T = 32, NT = G * 64;
+  constexpr int FILL = T * 8 / 64;                                // DMA instructions of an operand's k-step
+  constexpr int STAGE = 2 * T * 8;                                // 16-byte chunks: 32 rows of each operand
+  constexpr int LS = T + 4;                                       // ints of a row of partial sums
+  static_assert(G * 2 * STAGE * 4 >= G * T * LS, "the partial sums fit where the rings were");
+  __shared__ uint4 lds[G * 2 * STAGE];
+  __shared__ float4 s_vec[3 * T / 4];
 
-  const int m0 = int(blockIdx.x) / tiles_n * BM, n0 = int(blockIdx.x) % tiles_n * BN;
+  const int m0 = int(blockIdx.x) / tiles_n * T, n0 = int(blockIdx.x) % tiles_n * T;
   const int tid = threadIdx.x, lane = tid & 63;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6), grp = w / NW, wave = w % NW;
-  const int wm = wave % WM, wn = wave / WM, r32 = lane & 31, hi = lane >> 5;
+  const int grp = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, hi = lane >> 5;
   const char* const At = A + size_t(m0) * lda;
   const char* const Wt = W + size_t(n0) * ldw;
-  uint32_t off[AI + BI];
+  uint32_t offA[FILL], offB[FILL];
 #pragma unroll
-  for (int i = 0; i < AI; ++i) {
-    const int slot = (wave * AI + i) * 64 + lane, r = slot >> 3, c = (slot & 7) ^ swz(r);
-    off[i] = uint32_t(min(r, M - 1 - m0) * lda + 16 * c);
-  }
-#pragma unroll
-  for (int i = 0; i < BI; ++i) {
-    const int slot = (wave * BI + i) * 64 + lane, r = slot >> 3, c = (slot & 7) ^ swz(r);
-    off[AI + i] = uint32_t(min(r, N - 1 - n0) * ldw + 16 * c);
+  for (int i = 0; i < FILL; ++i) {
+    const int slot = i * 64 + lane, r = slot >> 3, c = (slot & 7) ^ swz(r);
+    offA[i] = uint32_t(min(r, M - 1 - m0) * lda + 16 * c);
+    offB[i] = uint32_t(min(r, N - 1 - n0) * ldw + 16 * c);
   }
   uint4* const ring = lds + grp * 2 * STAGE;
   auto fill = [&](int st, int kt) {
     uint4* const to = ring + st * STAGE;
 #pragma unroll
-    for (int j = 0; j < AI; ++j) dma16(At + kt * 128, off[j], to + (wave * AI + j) * 64);
+    for (int j = 0; j < FILL; ++j) dma16(At + kt * 128, offA[j], to + j * 64);
 #pragma unroll
-    for (int j = 0; j < BI; ++j) dma16(Wt + kt * 128, off[AI + j], to + BM * 8 + (wave * BI + j) * 64);
+    for (int j = 0; j < FILL; ++j) dma16(Wt + kt * 128, offB[j], to + T * 8 + j * 64);
   };
-  const int steps = (KT + G - 1) / G;                             // of every group; the last may be past KT
-  auto mine = [&](int i) { return i * G + grp; };
 #pragma unroll
   for (int i = 0; i < 2; ++i)
-    if (mine(i) < KT) fill(i, mine(i));
-  epi.template start<BM, BN, NT>(s_vec, m0, n0, M, N, tid);
-  i32x16 acc[TM][TN];
+    if (grp + i * G < KT) fill(i, grp + i * G);
+  epi.template start<T, T, NT>(s_vec, m0, n0, M, N, tid);
+  i32x16 acc;
 #pragma unroll
-  for (int a = 0; a < TM; ++a)
-#pragma unroll
-    for (int b = 0; b < TN; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[a][b][i] = 0;
-  for (int i0 = 0; i0 < steps; i0 += 2) {
+  for (int i = 0; i < 16; ++i) acc[i] = 0;
+  for (int kt0 = grp; kt0 < KT; kt0 += 2 * G) {
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
-      const int i = i0 + st;
-      if (i >= steps) break;
-      if (mine(i + 1) < KT) wait_vmcnt<AI + BI>();                // this step has landed, the next may be on its way
+      const int kt = kt0 + st * G;
+      if (kt >= KT) break;
+      if (kt + G < KT) wait_vmcnt<2 * FILL>();                    // this step has landed, the next may be on its way
       else wait_vmcnt<0>();
-      if constexpr (NW > 1) __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      if (mine(i) < KT) {
-        const uint4* const sa = ring + st * STAGE;
-        const uint4* const sb = sa + BM * 8;
+      const uint4* const sa = ring + st * STAGE;
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          const int ch = kk * 2 + hi;
-          uint4 af[TM], bf[TN];
-#pragma unroll
-          for (int a = 0; a < TM; ++a) {
-            const int r = wm * WTM + a * 32 + r32;
-            af[a] = sa[r * 8 + (ch ^ swz(r))];
-          }
-#pragma unroll
-          for (int b = 0; b < TN; ++b) {
-            const int r = wn * WTN + b * 32 + r32;
-            bf[b] = sb[r * 8 + (ch ^ swz(r))];
-          }
-#pragma unroll
-          for (int a = 0; a < TM; ++a)
-#pragma unroll
-            for (int b = 0; b < TN; ++b) acc[a][b] = OpsI8::mfma(af[a], bf[b], acc[a][b]);
-        }
+      for (int kk = 0; kk < 4; ++kk) {
+        const int at = r32 * 8 + ((kk * 2 + hi) ^ swz(r32));
+        acc = OpsI8::mfma(sa[at], sa[T * 8 + at], acc);
       }
       __builtin_amdgcn_s_waitcnt(0xC07F);                         // lgkmcnt(0): the reads of this stage have returned
-      if constexpr (NW > 1) __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      if (mine(i + 2) < KT) fill(st, mine(i + 2));
+      if (kt + 2 * G < KT) fill(st, kt + 2 * G);
     }
   }
   __builtin_amdgcn_s_waitcnt(0x0070);                             // nothing is on its way to the rings
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-  int* const part = reinterpret_cast<int*>(lds) + grp * BM * LS;
+  int* const part = reinterpret_cast<int*>(lds) + grp * T * LS;
 #pragma unroll
-  for (int a = 0; a < TM; ++a)
-#pragma unroll
-    for (int b = 0; b < TN; ++b)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<int4*>(part + (wm * WTM + a * 32 + r32) * LS + wn * WTN + b * 32 + 8 * g + 4 * hi) =
-            make_int4(acc[a][b][4 * g], acc[a][b][4 * g + 1], acc[a][b][4 * g + 2], acc[a][b][4 * g + 3]);
+  for (int g = 0; g < 4; ++g)
+    *reinterpret_cast<int4*>(part + r32 * LS + 8 * g + 4 * hi) = make_int4(acc[4 * g], acc[4 * g + 1], acc[4 * g + 2], acc[4 * g + 3]);
   __builtin_amdgcn_s_waitcnt(0xC07F);
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-  for (int e = tid; e < BM * BN / 4; e += NT) {
-    const int r = e / (BN / 4), c = e % (BN / 4) * 4;
+  for (int e = tid; e < T * T / 4; e += NT) {
+    const int r = e / (T / 4), c = e % (T / 4) * 4;
     if (m0 + r >= M || n0 + c >= N) continue;
     int4 t = make_int4(0, 0, 0, 0);
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      const int4 p = *reinterpret_cast<const int4*>(reinterpret_cast<const int*>(lds) + (g * BM + r) * LS + c);
+      const int4 p = *reinterpret_cast<const int4*>(reinterpret_cast<const int*>(lds) + (g * T + r) * LS + c);
       t.x += p.x; t.y += p.y; t.z += p.z; t.w += p.w;
     }
-    epi.template four<BM, BN>(t, s_vec, r, c, m0 + r, n0 + c, N);
+    epi.template four<T, T>(t, s_vec, r, c, m0 + r, n0 + c, N);
   }
 }
 
 constexpr int kMaxK = 131072 - 128;     // |sum| <= 128 * 128 * kMaxK < 2^31
 
-template <int BM, int BN, int WM, int WN, int G, class E>
+template <int G, class E>
 Status launch_split(const int8_t* A, int lda, const int8_t* W, int ldw, int M, int N, int KT, const E& epi,
                     hipStream_t s) {
-  const int tn = (N + BN - 1) / BN, tiles = tn * ((M + BM - 1) / BM);
-  hipLaunchKernelGGL((k_i8_split<BM, BN, WM, WN, G, E>), dim3(tiles), dim3(WM * WN * G * 64), 0, s,
-                     reinterpret_cast<const char*>(A), lda, reinterpret_cast<const char*>(W), ldw, M, N, KT, tn, epi);
+  const int tn = (N + 31) / 32, tiles = tn * ((M + 31) / 32);
+  hipLaunchKernelGGL((k_i8_split<G, E>), dim3(tiles), dim3(G * 64), 0, s, reinterpret_cast<const char*>(A), lda,
+                     reinterpret_cast<const char*>(W), ldw, M, N, KT, tn, epi);
   DC_HIP(hipGetLastError());
   return Status::ok();
 }
 
-// Cost in us of tile i, as block_gemm_tile's: rounds of one workgroup per compute unit, each `fixed` plus k-steps (of
-// 128; the last tile's eight groups share them) of `alone` to `full`; the 64 x 64 tile runs up to three workgroups
-// per compute unit.  Fitted to timings of all seven on 228 shapes (M 1 to 17,776; N x K from 256 x 1,024 to 11,520 x
-// 1,920 and 1,920 x 7,680) on MI355X: the one it picks is 0.2 % slower than the best on average, 7 % at worst.  Few
-// rows take the split: 1 x 1,920 x 7,680 7.0 us (64 x 64 18.4), 50 x 1,920 x 1,920 4.6 (7.0), 50 x 11,520 x 1,920 10.9
-// (64 x 64, which it takes, 7.5).
-struct TileCost { int bm, bn; float alone, full, fixed; };
-constexpr TileCost kTiles[] = {{384, 192, 1.124f, 1.867f, 7.08f}, {320, 256, 1.268f, 1.997f, 6.85f},
-                               {256, 192, 0.783f, 1.267f, 5.77f}, {256, 128, 0.604f, 0.927f, 3.79f},
-                               {128, 128, 0.294f, 0.494f, 2.91f}, {64, 64, 0.f, 0.f, 1.29f},
-                               {32, 32, 0.396f, 0.740f, 1.16f}};
-constexpr float kSmallStep[3] = {0.248f, 0.372f, 0.567f};
-constexpr float kLaunch[7] = {0.f, 0.f, 0.f, 1.33f, 1.31f, 2.13f, 2.15f};
-constexpr int kSplitGroups = 8;
+// Cost in us of tile i, as block_gemm_tile's: rounds of `per_cu` workgroups on each compute unit, each round `fixed`
+// plus k-steps (of 128; groups share them).  One workgroup per compute unit: a k-step takes step[0] on a nearly empty
+// chip to step[1] on a full one; more: step[n - 1] with n of them.  Fitted to timings on MI355X of 228 shapes (M 1 to
+// 17,776; N x K from 256 x 1,024 to 11,520 x 1,920 and 1,920 x 7,680; the splits 132 of them, M up to 800): the tile it
+// picks is 0.3 % slower than the best on average, 10 % at worst.  Few rows take the splits: 1 x 1,920 x 7,680 6.8 us
+// (64 x 64 18.4), 50 x 1,920 x 1,920 4.5 (7.1), 32 x 11,520 x 1,920 6.0 (7.4); 50 x 11,520 x 1,920 stays with 64 x 64,
+// 7.5 (8.7).  Four groups fit a compute unit twice, five once, which is better for sums of many k-steps.
+struct TileCost { int bm, bn, groups, per_cu; float step[3], fixed, launch; };
+constexpr TileCost kTiles[] = {{384, 192, 1, 1, {1.124f, 1.867f}, 7.08f, 0.f},   {320, 256, 1, 1, {1.268f, 1.997f}, 6.85f, 0.f},
+                               {256, 192, 1, 1, {0.783f, 1.267f}, 5.77f, 0.f},   {256, 128, 1, 1, {0.604f, 0.927f}, 3.79f, 1.33f},
+                               {128, 128, 1, 1, {0.294f, 0.494f}, 2.91f, 1.31f}, {64, 64, 1, 3, {0.248f, 0.372f, 0.567f}, 1.29f, 2.13f},
+                               {32, 32, 4, 2, {0.341f, 0.662f}, 0.81f, 2.48f},   {32, 32, 5, 1, {0.245f, 0.525f}, 1.09f, 2.21f}};
 
 }  // namespace
 
 int i8_tile(int M, int N, int ksteps, int cus, bool split) {
   int best = 0;
   float least = 0.f;
-  for (int i = 0; i < (split ? 7 : 6); ++i) {
+  for (int i = 0; i < (split ? 8 : 6); ++i) {
     const TileCost& c = kTiles[i];
-    const float steps = float(i == 6 ? (ksteps + kSplitGroups - 1) / kSplitGroups : ksteps);
+    const float steps = float((ksteps + c.groups - 1) / c.groups);
     const int64_t tiles = int64_t((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn);
-    const int64_t round = i == 5 ? 3 * cus : cus, rounds = tiles / round, rest = tiles % round;
-    float t = kLaunch[i] + float(rounds) * (steps * (i == 5 ? kSmallStep[2] : c.full) + c.fixed);
+    const int64_t round = int64_t(c.per_cu) * cus, rounds = tiles / round, rest = tiles % round;
+    float t = c.launch + float(rounds) * (steps * c.step[c.per_cu == 1 ? 1 : c.per_cu - 1] + c.fixed);
     if (rest)
-      t += c.fixed + steps * (i == 5 ? kSmallStep[(rest - 1) / cus] : c.alone + (c.full - c.alone) * float(rest) / float(cus));
+      t += c.fixed + steps * (c.per_cu == 1 ? c.step[0] + (c.step[1] - c.step[0]) * float(rest) / float(cus)
+                                            : c.step[(rest - 1) / cus]);
     if (i == 0 || t < least) {
       best = i;
       least = t;
@@ -512,10 +476,10 @@ Status block_gemm(const int8_t* A, int64_t lda, const int8_t* W, int64_t ldw, in
     case 3: return launch_dma<OpsI8, 256, 128, 4, 2, 2, 3>(A, la, W, lw, M, N, kt, epi, s);
     case 4: return launch_pipe<OpsI8>(A, la, W, lw, M, N, kt, epi, s);
     case 5: return launch_dma<OpsI8, 64, 64, 2, 2, 2, 3>(A, la, W, lw, M, N, kt, epi, s);
-    default: break;
+    case 6: if constexpr (SPLIT) return launch_split<4>(A, la, W, lw, M, N, kt, epi, s); break;
+    default: if constexpr (SPLIT) return launch_split<5>(A, la, W, lw, M, N, kt, epi, s); break;
   }
-  if constexpr (SPLIT) return launch_split<32, 32, 1, 1, kSplitGroups>(A, la, W, lw, M, N, kt, epi, s);
-  else return Status::shape("int8 product: no such tile");
+  return Status::shape("int8 product: no such tile");
 }
 
 }  // namespace

@@ -230,12 +230,14 @@ def check_linear(got, x, xs, w, ws, bias, gate, residual, kind, bf16):
 
 TILE_SHAPES = {     # (M, N, K): the tile on 256 compute units
     (2562, 5760, 1920): "384x192", (1155, 11520, 1920): "320x256", (1155, 7680, 3840): "256x192",
-    (1537, 3456, 2304): "256x128", (1155, 1920, 3840): "128x128", (513, 1920, 256): "64x64", (67, 1153, 1408): "32x32",
+    (1537, 3456, 2304): "256x128", (1155, 1920, 3840): "128x128", (513, 1920, 256): "64x64",
+    (67, 1153, 1408): "32x32 x 4", (33, 1153, 7680): "32x32 x 5",
 }
+I8_TILES = TILES + ("32x32 x 4", "32x32 x 5")
 
 
 def i8_tile(m, n, k, cus):
-    return (TILES + ("32x32",))[_native("_ZN2dc7i8_tileEiiiib", m, n, k // 128, cus, True)]
+    return I8_TILES[_native("_ZN2dc7i8_tileEiiiib", m, n, k // 128, cus, True)]
 
 
 @pytest.mark.parametrize("mnk", list(TILE_SHAPES))

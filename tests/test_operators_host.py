@@ -321,9 +321,8 @@ def test_api_refuses_host_tensors():
 def test_product_shapes_take_the_tiles_they_name():
     """The GPU tests' shapes are the ones the library's rule sends to each of its tiles."""
     from tests import test_gpu_operators as G
-    from tests.gpu_util import TILES
     assert {k: G.i8_tile(*k, 256) for k in G.TILE_SHAPES} == G.TILE_SHAPES
-    assert set(G.TILE_SHAPES.values()) == set(TILES) | {"32x32"}
+    assert set(G.TILE_SHAPES.values()) == set(G.I8_TILES)
 
 
 # ----------------------------------------------------------------------------
