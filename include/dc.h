@@ -230,7 +230,7 @@ dc_status dc_qk_norm_rope(const dc_model_cfg* cfg, const dc_qk_cfg* qk, const vo
  * infinity or NaN has scale NaN and codes 0, so a product with it is NaN.  x: [rows, ld_x] of
  * dtype (dc_dtype), any element-aligned address and ld_x >= cols; q: [rows, ld_q], ld_q at least
  * cols rounded up to 128; scale: [rows].  Serves activations (a scale per token) and weights
- * [out, in] (a scale per output channel).  rows <= 2^24 - 1; rows = 0 is a no-op. */
+ * [out, in] (a scale per output channel).  rows and cols below 2^24; rows = 0 is a no-op.  q must not overlap x. */
 dc_status dc_quantize_rows(const void* x, int32_t dtype, int64_t ld_x, int32_t rows, int32_t cols,
                            int8_t* q, int64_t ld_q, float* scale, hipStream_t stream);
 

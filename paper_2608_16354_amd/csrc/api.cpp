@@ -451,7 +451,8 @@ dc_status dc_quantize_rows(const void* x, int32_t dtype, int64_t ld_x, int32_t r
                            int64_t ld_q, float* scale, hipStream_t stream) {
   DC_ENTRY(([&]() -> Status {
     if (dtype != DC_F32 && dtype != DC_BF16) return Status::make(DC_ERR_DTYPE, "unknown dtype");
-    if (rows < 0 || rows >= (1 << 24) || cols < 1) return Status::arg("rows must be in [0, 2^24), cols positive");
+    if (rows < 0 || rows >= (1 << 24) || cols < 1 || cols >= (1 << 24))
+      return Status::arg("rows must be in [0, 2^24), cols in [1, 2^24)");
     if (rows == 0) return Status::ok();
     if (!x || !q || !scale) return Status::arg("NULL argument");
     if (ld_x < cols || ld_q < (int64_t(cols) + 127) / 128 * 128)

@@ -75,7 +75,8 @@ def test_qk_norm_rope_of_no_samples_is_a_no_op(lib):
     ((FAKE, 2, 64, 4, 64, FAKE, 128, FAKE), DTYPE), ((FAKE, 1, 63, 4, 64, FAKE, 128, FAKE), ARG),
     ((FAKE, 1, 64, 4, 64, FAKE, 127, FAKE), ARG), ((FAKE, 1, 129, 4, 129, FAKE, 255, FAKE), ARG),
     ((FAKE, 1, 64, -1, 64, FAKE, 128, FAKE), ARG), ((FAKE, 1, 64, 1 << 24, 64, FAKE, 128, FAKE), ARG),
-    ((FAKE, 1, 64, 4, 0, FAKE, 128, FAKE), ARG), ((None, 1, 64, 4, 64, FAKE, 128, FAKE), ARG),
+    ((FAKE, 1, 64, 4, 0, FAKE, 128, FAKE), ARG), ((FAKE, 1, 1 << 24, 4, 1 << 24, FAKE, 1 << 24, FAKE), ARG),
+    ((FAKE, 0, 2**31 - 1, 1, 2**31 - 1, FAKE, 1 << 31, FAKE), ARG), ((None, 1, 64, 4, 64, FAKE, 128, FAKE), ARG),
     ((FAKE, 1, 64, 4, 64, None, 128, FAKE), ARG), ((FAKE, 1, 64, 4, 64, FAKE, 128, None), ARG),
     ((FAKE + 1, 1, 64, 4, 64, FAKE, 128, FAKE), ARG), ((FAKE + 2, 0, 64, 4, 64, FAKE, 128, FAKE), ARG),
     ((FAKE, 0, 64, 4, 64, FAKE, 128, FAKE + 2), ARG), ((None, 0, 64, 0, 64, None, 128, None), L.DC_OK)])
