@@ -52,10 +52,12 @@ Status make_geo(const dc_model_cfg* cfg, Geo& g) {
   if (g.F % 128) return Status::shape("mlp_hidden must be a multiple of 128");
   if (g.bf16 ? (g.Dh != 64 && g.Dh != 72) : (g.Dh != 64))
     return Status::shape("head_dim must be 64 (or 72 with bf16)");
+  if (g.Hl < 0 || g.Wl < 0) return Status::shape("latent height/width must not be negative");
   if (g.Hl % g.p || g.Wl % g.p) return Status::shape("latent height/width must be divisible by patch");
   g.P = g.C * g.p * g.p;
   if (g.P != 64) return Status::shape("lat_c * patch^2 must be 64");
   g.Hp = g.Hl / g.p; g.Wp = g.Wl / g.p;
+  if (double(g.T) * g.Hp * g.Wp + g.Nt > double(INT32_MAX)) return Status::shape("too many tokens");
   g.Nv = g.T * g.Hp * g.Wp;
   g.N = g.Nv + g.Nt;
   if (!(g.eps > 0.f)) return Status::shape("ln_eps must be positive");

@@ -66,6 +66,17 @@ def test_qk_norm_rope_refuses(lib, case):
                                None) == ARG
 
 
+@pytest.mark.parametrize("more", [dict(lat=(4, -16, 16)), dict(lat=(4, 16, -16)), dict(lat=(1, -16, -16)),
+                                  dict(lat=(1 << 16, 1 << 16, 1 << 16)), dict(n_txt=2**31 - 1)])
+def test_token_counts_outside_32_bits_are_refused(lib, more):
+    c = cfg(**more)
+    arr, n = idx(0)
+    assert lib.dc_rope_table(C.byref(c), C.byref(axes()), None, FAKE, None) == SHAPE
+    assert lib.dc_qk_norm_rope(C.byref(c), C.byref(qk()), FAKE, 512, FAKE, 512, 1.0, arr, n, None) == SHAPE
+    assert lib.dc_cache_apply_q(C.byref(c), 8, FAKE, FAKE, FAKE, FAKE, arr, n, None) == SHAPE
+    assert lib.dc_block_ext_workspace_bytes(C.byref(c), 1) == 0
+
+
 def test_qk_norm_rope_of_no_samples_is_a_no_op(lib):
     arr, n = idx()
     assert lib.dc_qk_norm_rope(C.byref(cfg()), C.byref(qk()), FAKE, 512, FAKE, 512, 1.0, arr, n, None) == L.DC_OK
