@@ -240,7 +240,7 @@ dc_status dc_quantize_rows(const void* x, int32_t dtype, int64_t ld_x, int32_t r
 typedef struct {
   int32_t rows, out_features;     /* M, N, below 2^24; rows = 0 is a no-op */
   int32_t in_features;            /* K with its padding: a multiple of 128, at most 130,944 */
-  const int8_t* x;                /* [rows, ld_x], 16-byte aligned, ld_x a multiple of 16 */
+  const int8_t* x;                /* [rows, ld_x], 16-byte aligned; ld_x: K to 2^22, a multiple of 16 */
   const float* x_scale;           /* [rows] */
   int64_t ld_x;
   const int8_t* w;                /* [out_features, ld_w], as x */
@@ -251,7 +251,7 @@ typedef struct {
   const float* gate;              /* [out_features] or NULL: no residual */
   const float* residual;          /* f32 [rows, ld_residual], with a gate; may be out (same ld) */
   int64_t ld_residual;
-  void* out;                      /* [rows, ld_out] */
+  void* out;                      /* [rows, ld_out]; overlaps no other operand */
   int32_t out_dtype;              /* dc_dtype; DC_F32 with a gate */
   int64_t ld_out;                 /* >= out_features, rows at any element's address */
 } dc_linear_i8_args;
@@ -271,7 +271,7 @@ dc_status dc_cache_apply_q(const dc_model_cfg* cfg, int32_t bits, const float* h
                            hipStream_t stream);
 
 /* One block's matrices in int8 (device memory): rows as dc_quantize_rows writes them with
- * ld_q = the row's length, a scale per output channel. */
+ * ld_q = the row's length (16-byte aligned), a scale per output channel. */
 typedef struct {
   const int8_t* w_qkv; const float* s_qkv;  /* [3d, d], [3d] */
   const int8_t* w_o;   const float* s_o;    /* [d, d], [d] */

@@ -263,16 +263,18 @@ def _tokens(cfg):
     return n_v, n_v + cfg.n_txt
 
 
-def _floats(t, shape, what):
-    if t is not None and (t.dtype != _torch().float32 or tuple(t.shape) != shape or not t.is_contiguous()):
-        raise ValueError(f"{what}: a contiguous float32 {list(shape)} tensor is wanted")
-    return None if t is None else t.data_ptr()
+def _floats(t, shape, device, what):
+    if t is None:
+        return None
+    if t.dtype != _torch().float32 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{what}: a contiguous float32 {list(shape)} tensor on {device} is wanted")
+    return t.data_ptr()
 
 
 class BlockExt:
     """Extensions of every block of a DeviceModel: norms and rotation of queries and keys (q_weight,
     k_weight: one [head_dim] tensor per block, or None; table: dc_rope_table's, or None) and, with
-    int8=True, the blocks' matrices quantised per output channel."""
+    int8=True, the blocks' matrices quantised per output channel (on the current stream)."""
 
     MATRICES = (("w_qkv", "s_qkv"), ("w_o", "s_o"), ("w_1", "s_1"), ("w_2", "s_2"))
 
@@ -280,14 +282,15 @@ class BlockExt:
                  int8=False):
         torch = _torch()
         n = len(dm.blocks)
+        self.cfg = dm.cfg
         self.keep = [q_weight, k_weight, table]
         self.c = (L.BlockExt * n)()
         for l, b in enumerate(dm.blocks):
             if q_weight is not None or k_weight is not None or table is not None:
-                dh = (dm.cfg.head_dim,)
-                qk = L.QkCfg(_floats(None if q_weight is None else q_weight[l], dh, "q_weight"),
-                             _floats(None if k_weight is None else k_weight[l], dh, "k_weight"), eps,
-                             _floats(table, (_tokens(dm.cfg)[0], dh[0] // 2, 2), "table"), 1 if interleaved else 0)
+                dh, dev = (dm.cfg.head_dim,), b["b_qkv"].device
+                qk = L.QkCfg(_floats(None if q_weight is None else q_weight[l], dh, dev, "q_weight"),
+                             _floats(None if k_weight is None else k_weight[l], dh, dev, "k_weight"), eps,
+                             _floats(table, (_tokens(dm.cfg)[0], dh[0] // 2, 2), dev, "table"), 1 if interleaved else 0)
                 self.keep.append(qk)
                 self.c[l].qk = C.pointer(qk)
             if int8:
@@ -306,9 +309,16 @@ class BlockExt:
     def block(self, l):
         return C.pointer(self.c[l])
 
+    def of(self, dm):
+        """Itself, if it has the shapes of dm: the library reads dm's sizes from what it points to."""
+        if bytes(self.cfg) != bytes(dm.cfg):
+            raise ValueError("ext was made for a model of another shape")
+        return self
+
 
 def dc_block_forward_ext(dm: DeviceModel, l: int, ext: BlockExt, mod, h, idx, ws: Workspace, stream=None):
     """dc_block_forward with block l's extensions; ws: Workspace(..., ext=True)."""
+    ext.of(dm)
     arr, p, n = _idx(idx)
     L.check("dc_block_forward_ext", L.load().dc_block_forward_ext(
         C.byref(dm.cfg), dm.block(l), ext.block(l), _ptr(mod), _ptr(h), p, n, ws.ptr, ws.nbytes, _stream(stream)))
@@ -480,9 +490,9 @@ class Sampler:
         x = L.SamplerExt()
         self._ext = (ext, ext_low)      # the device memory they point to lives as long as the sampler
         if ext is not None:
-            x.blocks = ext.c
+            x.blocks = ext.of(dm).c
         if ext_low is not None:
-            x.blocks_low = ext_low.c
+            x.blocks_low = ext_low.of(low_expert[0] if low_expert else dm).c
         x.cache_bits = int(cache_bits)
         if cache_bits:
             x.cache_scales = int(self.bufs.cache_scales.data_ptr())

@@ -123,7 +123,7 @@ void whole(const at::Tensor& t, at::ScalarType type, int64_t n0, int64_t n1, int
 int64_t rows(const at::Tensor& t, const char* what) {
   need(t.dim() == 2, what);
   const int64_t n = t.size(0), cols = t.size(1);
-  const int64_t ld = n <= 1 ? std::max(t.stride(0), cols) : t.stride(0);
+  const int64_t ld = n <= 1 ? cols : t.stride(0);              // one row: any stride
   need((cols <= 1 || t.stride(1) == 1) && ld >= cols, what);
   return ld;
 }
@@ -138,13 +138,18 @@ int32_t i32(int64_t v) {
 }
 
 // The C call without the interpreter's lock; its status.
+struct Unlocked {                       // taken again also when a tensor's pointer throws
+  PyThreadState* const state = PyEval_SaveThread();
+  ~Unlocked() { PyEval_RestoreThread(state); }
+};
 template <class F>
 PyObject* call(const Args& a, F&& f) {
   need(a.device >= 0, "tensors must be on a GPU");
   dc_status rc;
-  Py_BEGIN_ALLOW_THREADS
-  rc = f();
-  Py_END_ALLOW_THREADS
+  {
+    Unlocked u;
+    rc = f();
+  }
   return PyLong_FromLong(rc);
 }
 

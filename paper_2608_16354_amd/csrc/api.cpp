@@ -196,6 +196,8 @@ Status check_ext(const Geo& g, const dc_block_ext& e) {
     return Status::arg("int8 block weight pointer is NULL");
   if (!aligned16(w.w_qkv) || !aligned16(w.w_o) || !aligned16(w.w_1) || !aligned16(w.w_2))
     return Status::arg("int8 block weights must be 16-byte aligned");
+  if (!aligned(w.s_qkv, 4) || !aligned(w.s_o, 4) || !aligned(w.s_1, 4) || !aligned(w.s_2, 4))
+    return Status::arg("a pointer is not aligned to its element");
   return Status::ok();
 }
 

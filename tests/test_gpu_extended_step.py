@@ -201,3 +201,31 @@ def test_sample_of_two_experts_takes_each_ones_extensions(api, dev):
     say("two experts with extensions")
     one, same, other = run(None), run(e1), run(e2)
     assert np.array_equal(one, same) and not np.array_equal(one, other)
+
+
+def test_two_captured_blocks_share_a_workspace(api, dev):
+    """Blocks with norms, rotation and int8 products as two graphs on one workspace, replayed in turn between eager
+    work, against the eager calls."""
+    import torch
+    m = _shape(256, 4, 64, 1024, (3, 10, 12), 21, "bf16", blocks=2)
+    dm = api.DeviceModel(I.Weights(m, 170), dev)
+    wq, wk = qk_weights(m)
+    ext = api.BlockExt(dm, q_weight=[t(wq, dev)] * 2, k_weight=[t(wk, dev)] * 2, table=make_table(api, m, dev), int8=True)
+    mod = t(mod_input(m, (72,)), dev)
+    ws, ws_e = api.Workspace(m, 1, dev, ext=True), api.Workspace(m, 1, dev, ext=True)
+    h, e = (torch.zeros((1, m.n_tok, m.hidden), device=dev) for _ in range(2))
+    gen = torch.Generator(dev).manual_seed(5)
+    graphs, stream = [], torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for l in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[l], stream=stream):
+            api.dc_block_forward_ext(dm, l, ext, mod, h, [0], ws)
+    for order in ((0, 1), (1, 0), (0, 0, 1)):
+        h.copy_(torch.randn(h.shape, device=dev, generator=gen))
+        e.copy_(h)
+        for l in order:
+            graphs[l].replay()
+            api.dc_block_forward_ext(dm, l, ext, mod, e, [0], ws_e)
+        torch.cuda.synchronize()
+        assert torch.isfinite(e).all() and torch.equal(h, e), order

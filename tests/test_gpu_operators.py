@@ -332,6 +332,21 @@ def test_linear_of_a_row_without_a_number(api, dev):
     assert bad[[3, 66]].all() and bad.sum() == 80
 
 
+def test_one_row_of_any_stride(api, dev):
+    """A single row's stride says nothing: rows cut out of wider ones are taken as they are."""
+    import torch
+    wide = torch.randn((1, 203), device=dev, generator=torch.Generator(dev).manual_seed(2))
+    q, s, y = torch.zeros((1, 333), dtype=torch.int8, device=dev), torch.zeros(1, device=dev), torch.zeros((1, 41), device=dev)
+    x, row, out = (v.as_strided(v[:, :n].shape, (st, 1)) for v, n, st in ((wide, 200, 7), (q, 256, 3), (y, 40, 1)))
+    w = torch.randint(-127, 128, (40, 256), dtype=torch.int8, device=dev)
+    api.dc_quantize_rows(x, row, s)
+    api.dc_linear_i8(row, s, w, torch.ones(40, device=dev), out)
+    codes, scale = X.codes(host(wide)[:, :200], 127)
+    assert np.array_equal(host(row)[:, :200], codes) and np.array_equal(host(s), scale) and not host(q)[:, 200:256].any()
+    want = (codes.astype(np.int64) @ host(w)[:, :200].astype(np.int64).T) * scale.astype(np.float64)
+    assert (np.abs(host(out) - want) <= 4 * F32 * np.abs(want)).all() and host(y)[0, 40] == 0
+
+
 def test_linear_of_no_rows(api, dev):
     import torch
     api.dc_quantize_rows(torch.empty((0, 100), device=dev), torch.empty((0, 128), dtype=torch.int8, device=dev), torch.empty(0, device=dev))
@@ -442,3 +457,42 @@ def test_captured_and_replayed(api, dev):
     api.dc_rope_table(cfg, axes, None, other, stream=side)
     side.synchronize()
     assert torch.equal(other, eager["table"])
+
+
+def test_two_streams_at_once(api, dev):
+    """The calls keep nothing between them: two streams that work side by side get what each gets alone."""
+    import torch
+    m = shape(10, 64, (3, 34, 58), 78)
+    d, N, n_v, cfg = m.hidden, m.n_tok, m.n_v, api.model_cfg(m)
+
+    def state(seed):
+        gen = torch.Generator(dev).manual_seed(seed)
+        return dict(x=torch.randn((1, N, 3 * d), device=dev, generator=gen).bfloat16(), table=torch.zeros((n_v, 32, 2), device=dev),
+                    q=torch.zeros((N, 3 * d), device=dev, dtype=torch.int8), s=torch.zeros(N, device=dev),
+                    w=torch.randint(-127, 128, (d, 3 * d), device=dev, generator=gen, dtype=torch.int8),
+                    ws=torch.rand(d, device=dev, generator=gen), y=torch.zeros((1, N, d), device=dev),
+                    few=torch.zeros((5, d), device=dev), h=torch.randn((1, N, d), device=dev, generator=gen),
+                    codes=torch.zeros((1, n_v, d), device=dev, dtype=torch.int8), scales=torch.zeros((1, n_v, d // 64), device=dev))
+
+    def calls(b, stream, theta):
+        api.dc_rope_table(cfg, api.rope_axes((16, 24, 24), theta), None, b["table"], stream=stream)
+        api.dc_qk_norm_rope(cfg, b["x"], b["x"], [0], table=b["table"], stream=stream)
+        api.dc_quantize_rows(b["x"][0], b["q"], b["s"], stream=stream)
+        api.dc_linear_i8(b["q"], b["s"], b["w"], b["ws"], b["y"][0], stream=stream)
+        api.dc_linear_i8(b["q"][:5], b["s"][:5], b["w"], b["ws"], b["few"], stream=stream)
+        api.dc_cache_store_q(cfg, 8, b["y"], b["h"], b["codes"], b["scales"], [0], stream=stream)
+        api.dc_cache_apply_q(cfg, 8, b["h"], b["codes"], b["scales"], b["h"], [0], stream=stream)
+
+    alone, together = [state(i) for i in range(2)], [state(i) for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for i in range(2):
+        calls(alone[i], streams[0], 100.0 * (i + 1))
+        torch.cuda.synchronize()
+    for i in range(2):
+        calls(together[i], streams[i], 100.0 * (i + 1))
+    torch.cuda.synchronize()
+    for a, b in zip(alone, together):
+        for n in a:
+            assert torch.equal(a[n], b[n]), n
+    assert torch.equal(alone[0]["few"], alone[0]["y"][0, :5])

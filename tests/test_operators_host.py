@@ -171,6 +171,10 @@ def test_block_ext_refuses(lib):
         p[hole] = None
         assert call(c, i8=L.BlockWeightsI8(*p)) == ARG
     assert call(c, i8=L.BlockWeightsI8(*[FAKE + 8] * 8)) == ARG
+    for off in range(1, 8, 2):
+        p = [FAKE] * 8
+        p[off] = FAKE + 2
+        assert call(c, i8=L.BlockWeightsI8(*p)) == ARG
     assert call(cfg(dtype=0), i8=i8) == DTYPE
     # int8 products do not read the matrices of the model dtype, but need its biases
     no_bias = L.BlockWeights(None, None, None, FAKE, None, FAKE, None, FAKE, None)
@@ -328,6 +332,32 @@ def test_api_refuses_host_tensors():
     from paper_2608_16354_amd import api
     with pytest.raises(ValueError, match="on a GPU"):
         api.dc_quantize_rows(torch.zeros(4, 100), torch.zeros(4, 128, dtype=torch.int8), torch.zeros(4))
+
+
+def test_extensions_belong_to_a_shape_and_a_device():
+    """An extension holds tensors of its model's sizes: another model, or a tensor elsewhere, is refused."""
+    import types
+    import torch
+    from paper_2608_16354_amd import api
+
+    def model(**more):
+        c = cfg(**more)
+        return types.SimpleNamespace(cfg=c, blocks=[dict(b_qkv=torch.zeros(4))] * c.n_blocks)
+
+    dm, w = model(), [torch.ones(64)] * 2
+    e = api.BlockExt(dm, q_weight=w, k_weight=w, table=torch.zeros(256, 32, 2))
+    assert e.of(dm) is e and e.of(model()) is e
+    for other in (model(heads=6), model(lat=(4, 16, 18)), model(n_txt=17), model(dtype=0)):
+        with pytest.raises(ValueError, match="another shape"):
+            e.of(other)
+        with pytest.raises(ValueError, match="another shape"):
+            api.dc_block_forward_ext(other, 0, e, None, None, [0], None)
+    for bad in (dict(q_weight=[torch.ones(64, device="meta")] * 2), dict(table=torch.zeros(256, 32, 2, device="meta")),
+                dict(k_weight=[torch.ones(63)] * 2), dict(table=torch.zeros(255, 32, 2))):
+        with pytest.raises(ValueError, match="is wanted"):
+            api.BlockExt(dm, **bad)
+    with pytest.raises(IndexError):
+        api.BlockExt(dm, q_weight=w[:1])
 
 
 def test_product_shapes_take_the_tiles_they_name():
