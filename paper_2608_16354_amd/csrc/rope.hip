@@ -69,12 +69,12 @@ __global__ void __launch_bounds__(256) k_rope_table(Axes ax, const double* __res
 // y = x / sqrt(mean(x^2) + eps) * w per head of Q and of K, its pairs turned by the token's angles, Q
 // times q_scale.  Bound by memory: every value is read and written once.
 // One wave to a token's row (or to a part of its heads where there are few tokens): a lane holds 16
-// bytes of a head, G = head_dim / VE lanes a head, 64 / G heads at a time, and keeps its angles and
-// weights in registers for all of them.  The first four steps' values are asked for before the weights
-// and angles, so a row pays one trip to memory.  Halves paired: the partners are read a second time, from
-// the L1, which costs less than moving them between lanes; neighbours paired: streaming loads.
-// 17,776 x 30 heads of 64, bf16: 54 us interleaved (5.0 TB/s; 81 with the weights and angles read one float
-// at a time before the values), 60 us with halves paired.
+// bytes of a head, both values of every pair among them, G = head_dim / VE lanes a head, 64 / G heads at a
+// time, and keeps its angles and weights in registers for all of them.  The first U steps' values are
+// asked for before the weights and angles, so a row pays one trip to memory.
+// 17,776 x 30 heads of 64, bf16: 48 us with either pairing (5.7 TB/s; 57 with halves paired when the partners were read
+// a second time, and 56 when their runs of 8 bytes were read and written as they lie).  3,704 x 16 heads of 72: 11.1 us
+// interleaved, 11.7 with halves paired (runs of 8 bytes, as nine lanes do not come in twos).
 // ---------------------------------------------------------------------------
 __device__ inline uint16_t to_bf16(float f) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(f)); }
 
@@ -84,53 +84,70 @@ template <>
 struct Lane<true> {
   static constexpr int VE = 8;
   typedef uint16_t T;
-  typedef uint4 Raw;
-  static __device__ Raw load(const T* p) { return *reinterpret_cast<const uint4*>(p); }
-  static __device__ Raw load_nt(const T* p) {
-    typedef unsigned int u32x4n __attribute__((ext_vector_type(4)));
-    return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4n*>(p)));
+  typedef uint2 Half;                  // four values
+  static __device__ void open(const Half& a, float* v) {
+    v[0] = __uint_as_float(a.x << 16); v[1] = __uint_as_float(a.x & 0xFFFF0000u);
+    v[2] = __uint_as_float(a.y << 16); v[3] = __uint_as_float(a.y & 0xFFFF0000u);
   }
-  // the value half a head away of each of the lane's: two runs of four
-  static __device__ Raw load_two(const T* p, const T* q) {
-    const uint2 a = *reinterpret_cast<const uint2*>(p), b = *reinterpret_cast<const uint2*>(q);
-    return make_uint4(a.x, a.y, b.x, b.y);
-  }
-  static __device__ void open(const Raw& w, float (&v)[8]) {
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(u[i] << 16);
-      v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
-    }
-  }
-  static __device__ void store(T* p, const float (&v)[8]) {
-    uint32_t u[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = uint32_t(to_bf16(v[2 * i])) | (uint32_t(to_bf16(v[2 * i + 1])) << 16);
-    *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+  static __device__ Half close(const float* v) {
+    return make_uint2(uint32_t(to_bf16(v[0])) | uint32_t(to_bf16(v[1])) << 16,
+                      uint32_t(to_bf16(v[2])) | uint32_t(to_bf16(v[3])) << 16);
   }
 };
 template <>
 struct Lane<false> {
   static constexpr int VE = 4;
   typedef float T;
-  typedef float4 Raw;
-  static __device__ Raw load(const T* p) { return *reinterpret_cast<const float4*>(p); }
-  static __device__ Raw load_nt(const T* p) {
-    typedef float f32x4n __attribute__((ext_vector_type(4)));
-    return __builtin_bit_cast(float4, __builtin_nontemporal_load(reinterpret_cast<const f32x4n*>(p)));
-  }
-  static __device__ Raw load_two(const T* p, const T*) { return load(p); }
-  static __device__ void open(const Raw& w, float (&v)[4]) { v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w; }
-  static __device__ void store(T* p, const float (&v)[4]) {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  }
+  typedef uint2 Half;                  // two values
+  static __device__ void open(const Half& a, float* v) { v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); }
+  static __device__ Half close(const float* v) { return make_uint2(__float_as_uint(v[0]), __float_as_uint(v[1])); }
 };
 
-// four floats of a weight vector times s, or s where there is none
-__device__ inline void weight4(const float* w, int e, float s, float* v) {
-  const float4 t = w ? *reinterpret_cast<const float4*>(w + e) : make_float4(1.f, 1.f, 1.f, 1.f);
-  v[0] = t.x * s; v[1] = t.y * s; v[2] = t.z * s; v[3] = t.w * s;
+// A lane's values: two runs of VE / 2, side by side (neighbours paired) or half a head apart (halves paired).  The
+// latter are read and written 16 bytes at a time all the same where lanes come in twos: the even lane takes both
+// lanes' first runs, the odd one the second, and they exchange what is not theirs.
+struct Raw { uint2 a, b; };
+__device__ inline uint32_t other_of_two(uint32_t v) {          // lanes 2i and 2i + 1 (DPP quad_perm 1, 0, 3, 2)
+  return uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0xB1, 0xF, 0xF, true));
+}
+__device__ inline void exchange(Raw& r, bool odd) {
+  const uint2 give = odd ? r.a : r.b;
+  const uint2 got = make_uint2(other_of_two(give.x), other_of_two(give.y));
+  (odd ? r.a : r.b) = got;
+}
+typedef unsigned int u32x4n __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2n __attribute__((ext_vector_type(2)));
+template <bool WHOLE, class T>
+__device__ inline Raw load_nt(const T* p, int e0, int e1) {
+  if constexpr (WHOLE) {
+    const u32x4n w = __builtin_nontemporal_load(reinterpret_cast<const u32x4n*>(p + e0));
+    return {make_uint2(w.x, w.y), make_uint2(w.z, w.w)};
+  } else {
+    const u32x2n a = __builtin_nontemporal_load(reinterpret_cast<const u32x2n*>(p + e0));
+    const u32x2n b = __builtin_nontemporal_load(reinterpret_cast<const u32x2n*>(p + e1));
+    return {make_uint2(a.x, a.y), make_uint2(b.x, b.y)};
+  }
+}
+template <bool WHOLE, class T>
+__device__ inline void store(T* p, int e0, int e1, const Raw& r) {
+  if constexpr (WHOLE) {
+    *reinterpret_cast<uint4*>(p + e0) = make_uint4(r.a.x, r.a.y, r.b.x, r.b.y);
+  } else {
+    *reinterpret_cast<uint2*>(p + e0) = r.a;
+    *reinterpret_cast<uint2*>(p + e1) = r.b;
+  }
+}
+
+// N floats (2 or 4) of a weight vector times s, or s where there is none
+template <int N>
+__device__ inline void weights(const float* w, int e, float s, float* v) {
+  if constexpr (N == 4) {
+    const float4 t = w ? *reinterpret_cast<const float4*>(w + e) : make_float4(1.f, 1.f, 1.f, 1.f);
+    v[0] = t.x * s; v[1] = t.y * s; v[2] = t.z * s; v[3] = t.w * s;
+  } else {
+    const float2 t = w ? *reinterpret_cast<const float2*>(w + e) : make_float2(1.f, 1.f);
+    v[0] = t.x * s; v[1] = t.y * s;
+  }
 }
 
 // sum over the G lanes of a head (lane h of the head's group, which starts at lane `first`)
@@ -147,6 +164,11 @@ __device__ inline float head_sum(float v, int first, int h) {
   }
 }
 
+// Steps of a wave whose values are asked for at once.  Heads of 72 go seven at a time, so 32 of them take five
+// steps (3,704 rows 11.2 us, with four at once 11.5; heads of 64 take 0 to 2 % longer with five).
+template <int G>
+constexpr int kSteps = G == 9 ? 5 : 4;
+
 struct QkArgs {
   const void* in;
   void* out;
@@ -161,7 +183,8 @@ template <bool BF, int DH, bool IL>
 __global__ void __launch_bounds__(256) k_qk_norm_rope(QkArgs a, IdxList idx) {
   typedef Lane<BF> Ln;
   typedef typename Ln::T T;
-  constexpr int VE = Ln::VE, G = DH / VE, HW = kWave / G, U = 4;
+  constexpr int VE = Ln::VE, HV = VE / 2, G = DH / VE, HW = kWave / G, U = kSteps<G>;
+  constexpr bool SWAP = !IL && G % 2 == 0, WHOLE = IL || SWAP;
   const int lane = threadIdx.x & 63;
   const int n = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (n >= a.N) return;
@@ -170,57 +193,40 @@ __global__ void __launch_bounds__(256) k_qk_norm_rope(QkArgs a, IdxList idx) {
   T* const out = static_cast<T*>(a.out) + row * a.ld_out;
   const int slot = min(lane / G, HW - 1), h = lane - slot * G;   // lanes past the last head: h >= G
   const bool use = h < G;
-  const int e0 = min(h, G - 1) * VE;
+  const int e0 = min(h, G - 1) * (IL ? VE : HV), e1 = e0 + (IL ? HV : DH / 2);    // where the lane's runs start
+  const bool odd = h & 1;
+  const int f0 = SWAP && odd ? e1 - HV : e0;                     // where its 16 bytes in memory start
   const bool turn = a.table != nullptr && n < a.Nv;
   const int total = 2 * a.heads;
   const int step = HW * gridDim.y;
-  // where the value half a head away of element e0 + i lies (i = 0, 4)
-  const int far0 = e0 < DH / 2 ? e0 + DH / 2 : e0 - DH / 2;
-  const int far4 = e0 + 4 < DH / 2 ? e0 + 4 + DH / 2 : e0 + 4 - DH / 2;
-  typename Ln::Raw v[U], o[U];
+  Raw v[U];
   auto fetch = [&](int s0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (s0 + u * step >= total) break;
-      const T* const p = in + min(s0 + u * step + slot, total - 1) * DH;
-      v[u] = IL ? Ln::load_nt(p + e0) : Ln::load(p + e0);
-      if constexpr (!IL) {
-        if (turn) o[u] = Ln::load_two(p + far0, p + far4);
-      }
+      v[u] = load_nt<WHOLE>(in + min(s0 + u * step + slot, total - 1) * DH, f0, e1);
     }
   };
   fetch(HW * blockIdx.y);
-  // y = rstd (A x + B x'), x' the other value of the pair: its neighbour (IL) or the value half a
-  // head away; A = cos times the value's own weight, B = -sin or sin times the other's
+  // y = rstd (A x + B x'), x' the other value of the pair; A = cos times the value's own weight, B = -sin
+  // or sin times the other's
   float aq[VE], ak[VE], bq[VE], bk[VE];
-#pragma unroll
-  for (int i = 0; i < VE; i += 4) {
-    weight4(a.wq, e0 + i, a.q_scale, aq + i);
-    weight4(a.wk, e0 + i, 1.f, ak + i);
-  }
+  weights<HV>(a.wq, e0, a.q_scale, aq);
+  weights<HV>(a.wq, e1, a.q_scale, aq + HV);
+  weights<HV>(a.wk, e0, 1.f, ak);
+  weights<HV>(a.wk, e1, 1.f, ak + HV);
   if (turn) {
-    const float4* const tab = reinterpret_cast<const float4*>(a.table + size_t(n) * (DH / 2));   // two pairs each
+    // the lane's HV pairs follow each other in the table
+    const float4* const tab = reinterpret_cast<const float4*>(a.table + size_t(n) * (DH / 2) + (IL ? e0 / 2 : e0));
 #pragma unroll
-    for (int i = 0; i < VE; i += 4) {
-      const int far = i ? far4 : far0;
-      if constexpr (IL) {
-        const float4 t = tab[(e0 + i) / 4];
-        bq[i] = -aq[i + 1] * t.y; bq[i + 1] = aq[i] * t.y; bq[i + 2] = -aq[i + 3] * t.w; bq[i + 3] = aq[i + 2] * t.w;
-        bk[i] = -ak[i + 1] * t.y; bk[i + 1] = ak[i] * t.y; bk[i + 2] = -ak[i + 3] * t.w; bk[i + 3] = ak[i + 2] * t.w;
-        aq[i] *= t.x; aq[i + 1] *= t.x; aq[i + 2] *= t.z; aq[i + 3] *= t.z;
-        ak[i] *= t.x; ak[i + 1] *= t.x; ak[i + 2] *= t.z; ak[i + 3] *= t.z;
-      } else {
-        const int p = min(e0 + i, far);
-        const float4 t0 = tab[p / 2], t1 = tab[p / 2 + 1];
-        const float sg = e0 + i < DH / 2 ? -1.f : 1.f;
-        const float sn[4] = {t0.y * sg, t0.w * sg, t1.y * sg, t1.w * sg}, cs[4] = {t0.x, t0.z, t1.x, t1.z};
-        weight4(a.wq, far, a.q_scale, bq + i);
-        weight4(a.wk, far, 1.f, bk + i);
+    for (int j = 0; j < HV; j += 2) {
+      const float4 t = tab[j / 2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          bq[i + j] *= sn[j]; bk[i + j] *= sn[j];
-          aq[i + j] *= cs[j]; ak[i + j] *= cs[j];
-        }
+      for (int k = j; k < j + 2; ++k) {
+        const int x = IL ? 2 * k : k, y = IL ? 2 * k + 1 : k + HV;
+        const float cs = k == j ? t.x : t.z, sn = k == j ? t.y : t.w;
+        bq[x] = -aq[y] * sn; bq[y] = aq[x] * sn; aq[x] *= cs; aq[y] *= cs;
+        bk[x] = -ak[y] * sn; bk[y] = ak[x] * sn; ak[x] *= cs; ak[y] *= cs;
       }
     }
   }
@@ -232,23 +238,25 @@ __global__ void __launch_bounds__(256) k_qk_norm_rope(QkArgs a, IdxList idx) {
       const int head = s0 + u * step + slot;
       const bool q = head < a.heads;
       float x[VE], y[VE];
-      Ln::open(v[u], x);
+      if constexpr (SWAP) exchange(v[u], odd);
+      Ln::open(v[u].a, x);
+      Ln::open(v[u].b, x + HV);
       float ss = 0.f;
 #pragma unroll
       for (int i = 0; i < VE; ++i) ss += x[i] * x[i];
       ss = head_sum<G>(ss, slot * G, h);
       const float rstd = (q ? a.wq : a.wk) ? rsqrtf(ss / float(DH) + a.eps) : 1.0f;
       if (turn) {
-        float z[VE];
-        if constexpr (!IL) Ln::open(o[u], z);
 #pragma unroll
         for (int i = 0; i < VE; ++i)
-          y[i] = rstd * (x[i] * (q ? aq[i] : ak[i]) + (IL ? x[i ^ 1] : z[i]) * (q ? bq[i] : bk[i]));
+          y[i] = rstd * (x[i] * (q ? aq[i] : ak[i]) + x[IL ? i ^ 1 : i ^ HV] * (q ? bq[i] : bk[i]));
       } else {
 #pragma unroll
         for (int i = 0; i < VE; ++i) y[i] = rstd * (x[i] * (q ? aq[i] : ak[i]));
       }
-      if (use && head < total) Ln::store(out + head * DH + e0, y);
+      Raw r{Ln::close(y), Ln::close(y + HV)};
+      if constexpr (SWAP) exchange(r, odd);
+      if (use && head < total) store<WHOLE>(out + head * DH, f0, e1, r);
     }
   }
 }
@@ -286,16 +294,18 @@ Status qk_norm_rope(const dc_qk_cfg& c, const void* in, int64_t ld_in, void* out
   if (g.N == 0) return Status::ok();
   QkArgs a{in, out, ld_in, ld_out, c.q_weight, c.k_weight, reinterpret_cast<const float2*>(c.cos_sin), c.eps, q_scale,
            g.N, g.Nv, g.H};
-  auto go = [&](auto kernel, int heads_wave) {
-    // few tokens: spread the heads of a row over workgroups (each wave keeps at least one step)
-    const int steps = (2 * g.H + heads_wave - 1) / heads_wave;
-    const int64_t rows = int64_t(g.N) * idx.n;
-    const int split = int(std::max<int64_t>(1, std::min<int64_t>(steps, 2048 / rows)));
+  auto go = [&](auto kernel, int heads_wave, int u) {
+    // Few tokens: the heads of a row go to several waves (each keeps at least one step).  So many that there are
+    // 2,048 waves (1,024 rows of 2 x 16 heads of 64: two to a row 4.8 us, one 5.6, four 5.1), or so that each pays one
+    // trip to memory if that takes at most 4,096 (1,556 rows of 2 x 30 heads: two 8.6 us, one 9.2; 3,035 rows: 12.7 and 12.5).
+    const int steps = (2 * g.H + heads_wave - 1) / heads_wave, trips = (steps + u - 1) / u;
+    const int64_t rows = int64_t(g.N) * idx.n, most = std::max<int64_t>(2048 / rows, trips * rows <= 4096 ? trips : 1);
+    const int split = int(std::min<int64_t>(steps, most));
     hipLaunchKernelGGL(kernel, dim3((g.N + 3) / 4, split, idx.n), dim3(256), 0, s, a, idx);
   };
-  if (!g.bf16) c.interleaved ? go(k_qk_norm_rope<false, 64, true>, 4) : go(k_qk_norm_rope<false, 64, false>, 4);
-  else if (g.Dh == 64) c.interleaved ? go(k_qk_norm_rope<true, 64, true>, 8) : go(k_qk_norm_rope<true, 64, false>, 8);
-  else c.interleaved ? go(k_qk_norm_rope<true, 72, true>, 7) : go(k_qk_norm_rope<true, 72, false>, 7);
+  if (!g.bf16) c.interleaved ? go(k_qk_norm_rope<false, 64, true>, 4, kSteps<16>) : go(k_qk_norm_rope<false, 64, false>, 4, kSteps<16>);
+  else if (g.Dh == 64) c.interleaved ? go(k_qk_norm_rope<true, 64, true>, 8, kSteps<8>) : go(k_qk_norm_rope<true, 64, false>, 8, kSteps<8>);
+  else c.interleaved ? go(k_qk_norm_rope<true, 72, true>, 7, kSteps<9>) : go(k_qk_norm_rope<true, 72, false>, 7, kSteps<9>);
   DC_HIP(hipGetLastError());
   return Status::ok();
 }
