@@ -215,6 +215,12 @@ Status drift(const float* h_in, const float* mod0, void* u_ref, bool snapshot, d
 Status drift_noalloc(const float* h_in, const float* mod0, void* u_ref, bool snapshot, double* sums,
                      const IdxList& idx, const Geo& g, hipStream_t s);
 
+// From this many bytes of input on, the row kernels below read it with streaming loads, which leave the caches to
+// others: fewer bytes may still be there from the kernel that wrote them.  bf16 rows of 1,920 quantised, streaming and
+// plain: 17,776 x 4 (273 MB) 64 and 75 us, 3,704 (14 MB) 6.6 and 7.1, 2,048 (8 MB) 5.0 and 4.6; norms and rotation: 17,776
+// rows 48 and 55 us, 1,556 (12 MB) 8.7 and 10.0, 1,024 of 1,024 (4 MB) 4.8 and 4.6.
+constexpr int64_t kStreamBytes = 10 << 20;
+
 // Rotary table [Nv, Dh / 2, 2] from the latent's grid or given positions (f64 [Nv, 3]); norms and
 // rotation of Q | K at columns [0, 2d) of in [B, N, ld_in] (rope.hip).
 Status rope_table(const dc_rope_axes& ax, const double* pos, float* table, const Geo& g, hipStream_t s);

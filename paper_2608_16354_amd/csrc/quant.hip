@@ -45,7 +45,7 @@ __device__ inline float scale_of(uint32_t m, float levels) {
 // y + z = 1 / s to about 2^-45, q0 = x (y + z) is off by less than a step, r = x - q0 s is exact and q0 + r y
 // rounds to the quotient that a division gives (Markstein's theorem); adding 1.5 2^23 rounds it to an integer, ties
 // to even, whose low byte is the code.  Five operations a value, a division takes eleven (bf16 rows of 1,920:
-// 22.0 against 29.6 us for 17,776 of them).  Outside [2^-100, 2^100] the small terms can leave fp32's range:
+// 18.8 against 29.6 us for 17,776 of them).  Outside [2^-100, 2^100] the small terms can leave fp32's range:
 // there a division is made (and its quotient bounded, as s may have lost bits), and s = 0 or NaN gives 0.
 struct Coder {
   float s, y, z, levels;
@@ -82,8 +82,10 @@ template <bool BF>
 struct Piece {                         // VE consecutive values
   static constexpr int VE = BF ? 8 : 4;
   float v[VE];
+  template <bool NT>                   // streaming
   __device__ void load(const void* row, int64_t e) {
-    const u32x4a w = *reinterpret_cast<const u32x4a*>(static_cast<const char*>(row) + e * (BF ? 2 : 4));
+    const u32x4a* const at = reinterpret_cast<const u32x4a*>(static_cast<const char*>(row) + e * (BF ? 2 : 4));
+    const u32x4a w = NT ? __builtin_nontemporal_load(at) : *at;
     if constexpr (BF) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -116,7 +118,7 @@ __device__ inline void zero_tail(int8_t* q, int cols, int at, int step) {
 // WR waves to a row, NV pieces to a lane.  Pieces past the row's last re-read that one; a last piece
 // that the row does not fill starts VE before its end instead (the values it shares with the one before
 // it get the same codes twice).
-template <bool BF, int NV, int WR>
+template <bool BF, int NV, int WR, bool NT>
 __global__ void __launch_bounds__(256) k_quantize_rows(const void* __restrict__ x, int64_t ldx, int rows, int cols,
                                                        int8_t* __restrict__ q, int64_t ldq,
                                                        float* __restrict__ scale) {
@@ -129,7 +131,7 @@ __global__ void __launch_bounds__(256) k_quantize_rows(const void* __restrict__ 
   const int np = (cols + VE - 1) / VE;
   Piece<BF> p[NV];
 #pragma unroll
-  for (int i = 0; i < NV; ++i) p[i].load(xr, min(min(at + i * LR, np - 1) * VE, cols - VE));
+  for (int i = 0; i < NV; ++i) p[i].template load<NT>(xr, min(min(at + i * LR, np - 1) * VE, cols - VE));
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < NV; ++i) m = max(m, p[i].largest());
@@ -308,19 +310,24 @@ Status quantize(const void* x, int64_t ldx, int rows, int cols, int8_t* q, int64
   }
   auto go = [&](auto nv, auto wr) {
     constexpr int NV = decltype(nv)::value, WR = decltype(wr)::value;
-    hipLaunchKernelGGL((k_quantize_rows<BF, NV, WR>), dim3(WR == 1 ? (rows + 3) / 4 : rows), dim3(256), 0, s, x, ldx,
-                       rows, cols, q, ldq, scale);
+    auto launch = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3(WR == 1 ? (rows + 3) / 4 : rows), dim3(256), 0, s, x, ldx, rows, cols, q, ldq, scale);
+    };
+    if (int64_t(rows) * cols * (BF ? 2 : 4) >= kStreamBytes) launch(k_quantize_rows<BF, NV, WR, true>);
+    else launch(k_quantize_rows<BF, NV, WR, false>);
   };
   auto with_nv = [&](int n, auto wr) {
     if (n <= 1) go(std::integral_constant<int, 1>{}, wr);
     else if (n <= 2) go(std::integral_constant<int, 2>{}, wr);
     else if (n <= 3) go(std::integral_constant<int, 3>{}, wr);
     else if (n <= 4) go(std::integral_constant<int, 4>{}, wr);
-    else if (n <= 6) go(std::integral_constant<int, 6>{}, wr);
-    else go(std::integral_constant<int, 8>{}, wr);
+    else if (n <= 6 || decltype(wr)::value == 1) go(std::integral_constant<int, 6>{}, wr);
+    else if constexpr (decltype(wr)::value > 1) go(std::integral_constant<int, 8>{}, wr);
   };
-  // a wave to a row while it can hold one and there are rows for every compute unit; four otherwise
-  if (np <= 64 || (np <= 8 * 64 && rows >= 4 * compute_units())) with_nv((np + 63) / 64, std::integral_constant<int, 1>{});
+  // A wave to a row that gives it a piece a lane at most, or up to six where there are rows for every SIMD several
+  // times; four waves otherwise.  bf16 rows of 1,920, one wave and four: 64 rows 3.3 and 2.7 us, 1,556 4.7 and 4.3, 3,704 7.1
+  // and 7.2, 17,776 18.8 and 21.8; eight pieces a lane (fp32 rows of 1,920): 1,556 6.1 and 5.3, 17,776 34.0 and 32.1.
+  if (np <= 64 || (np <= 6 * 64 && rows >= 12 * compute_units())) with_nv((np + 63) / 64, std::integral_constant<int, 1>{});
   else with_nv((np + 255) / 256, std::integral_constant<int, 4>{});
   DC_HIP(hipGetLastError());
   return Status::ok();

@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "internal.h"
 
@@ -117,14 +118,18 @@ __device__ inline void exchange(Raw& r, bool odd) {
 }
 typedef unsigned int u32x4n __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2n __attribute__((ext_vector_type(2)));
-template <bool WHOLE, class T>
-__device__ inline Raw load_nt(const T* p, int e0, int e1) {
+template <bool NT, class V, class T>
+__device__ inline V load_as(const T* p) {                      // NT: streaming
+  const V* const v = reinterpret_cast<const V*>(p);
+  return NT ? __builtin_nontemporal_load(v) : *v;
+}
+template <bool WHOLE, bool NT, class T>
+__device__ inline Raw load(const T* p, int e0, int e1) {
   if constexpr (WHOLE) {
-    const u32x4n w = __builtin_nontemporal_load(reinterpret_cast<const u32x4n*>(p + e0));
+    const u32x4n w = load_as<NT, u32x4n>(p + e0);
     return {make_uint2(w.x, w.y), make_uint2(w.z, w.w)};
   } else {
-    const u32x2n a = __builtin_nontemporal_load(reinterpret_cast<const u32x2n*>(p + e0));
-    const u32x2n b = __builtin_nontemporal_load(reinterpret_cast<const u32x2n*>(p + e1));
+    const u32x2n a = load_as<NT, u32x2n>(p + e0), b = load_as<NT, u32x2n>(p + e1);
     return {make_uint2(a.x, a.y), make_uint2(b.x, b.y)};
   }
 }
@@ -179,7 +184,7 @@ struct QkArgs {
   int N, Nv, heads;
 };
 
-template <bool BF, int DH, bool IL>
+template <bool BF, int DH, bool IL, bool NT>
 __global__ void __launch_bounds__(256) k_qk_norm_rope(QkArgs a, IdxList idx) {
   typedef Lane<BF> Ln;
   typedef typename Ln::T T;
@@ -204,7 +209,7 @@ __global__ void __launch_bounds__(256) k_qk_norm_rope(QkArgs a, IdxList idx) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (s0 + u * step >= total) break;
-      v[u] = load_nt<WHOLE>(in + min(s0 + u * step + slot, total - 1) * DH, f0, e1);
+      v[u] = load<WHOLE, NT>(in + min(s0 + u * step + slot, total - 1) * DH, f0, e1);
     }
   };
   fetch(HW * blockIdx.y);
@@ -294,18 +299,25 @@ Status qk_norm_rope(const dc_qk_cfg& c, const void* in, int64_t ld_in, void* out
   if (g.N == 0) return Status::ok();
   QkArgs a{in, out, ld_in, ld_out, c.q_weight, c.k_weight, reinterpret_cast<const float2*>(c.cos_sin), c.eps, q_scale,
            g.N, g.Nv, g.H};
-  auto go = [&](auto kernel, int heads_wave, int u) {
+  const bool stream = int64_t(g.N) * idx.n * 2 * g.d * g.esz >= kStreamBytes;
+  auto go = [&](auto plain, auto streaming, int heads_wave, int u) {
     // Few tokens: the heads of a row go to several waves (each keeps at least one step).  So many that there are
     // 2,048 waves (1,024 rows of 2 x 16 heads of 64: two to a row 4.8 us, one 5.6, four 5.1), or so that each pays one
     // trip to memory if that takes at most 4,096 (1,556 rows of 2 x 30 heads: two 8.6 us, one 9.2; 3,035 rows: 12.7 and 12.5).
     const int steps = (2 * g.H + heads_wave - 1) / heads_wave, trips = (steps + u - 1) / u;
     const int64_t rows = int64_t(g.N) * idx.n, most = std::max<int64_t>(2048 / rows, trips * rows <= 4096 ? trips : 1);
     const int split = int(std::min<int64_t>(steps, most));
-    hipLaunchKernelGGL(kernel, dim3((g.N + 3) / 4, split, idx.n), dim3(256), 0, s, a, idx);
+    hipLaunchKernelGGL(stream ? streaming : plain, dim3((g.N + 3) / 4, split, idx.n), dim3(256), 0, s, a, idx);
   };
-  if (!g.bf16) c.interleaved ? go(k_qk_norm_rope<false, 64, true>, 4, kSteps<16>) : go(k_qk_norm_rope<false, 64, false>, 4, kSteps<16>);
-  else if (g.Dh == 64) c.interleaved ? go(k_qk_norm_rope<true, 64, true>, 8, kSteps<8>) : go(k_qk_norm_rope<true, 64, false>, 8, kSteps<8>);
-  else c.interleaved ? go(k_qk_norm_rope<true, 72, true>, 7, kSteps<9>) : go(k_qk_norm_rope<true, 72, false>, 7, kSteps<9>);
+  auto dtype = [&](auto bf, auto dh, int heads_wave, int u) {
+    constexpr bool BF = decltype(bf)::value;
+    constexpr int DH = decltype(dh)::value;
+    if (c.interleaved) go(k_qk_norm_rope<BF, DH, true, false>, k_qk_norm_rope<BF, DH, true, true>, heads_wave, u);
+    else go(k_qk_norm_rope<BF, DH, false, false>, k_qk_norm_rope<BF, DH, false, true>, heads_wave, u);
+  };
+  if (!g.bf16) dtype(std::false_type{}, std::integral_constant<int, 64>{}, 4, kSteps<16>);
+  else if (g.Dh == 64) dtype(std::true_type{}, std::integral_constant<int, 64>{}, 8, kSteps<8>);
+  else dtype(std::true_type{}, std::integral_constant<int, 72>{}, 7, kSteps<9>);
   DC_HIP(hipGetLastError());
   return Status::ok();
 }

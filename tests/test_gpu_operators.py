@@ -69,6 +69,7 @@ QK = {
     "bf16-64": shape(30, 64, (2, 34, 58), 77), "bf16-64-one-token": shape(4, 64, (1, 2, 2), 0), "bf16-72": shape(16, 72, (2, 6, 10), 7),
     "bf16-72-odd-heads": shape(16, 72, (3, 14, 18), 21), "bf16-64-wide": shape(48, 64, (1, 10, 10), 3),
     "f32": shape(4, 64, (4, 16, 16), 16, "f32"), "f32-6": shape(6, 64, (1, 6, 10), 1, "f32"), "bf16-2-heads": shape(2, 64, (5, 2, 2), 1),
+    "bf16-72-long": shape(16, 72, (4, 32, 56), 21), "f32-long": shape(16, 64, (2, 32, 56), 9, "f32"),
 }
 
 
@@ -178,7 +179,9 @@ def test_quantize_rows(api, dev, dtype, cols):
         assert (q[:rows, cols:pad] == 0).all() and (q[:rows, pad:] == 99).all() and (q[rows] == 99).all()
 
 
-@pytest.mark.parametrize("dtype,rows,cols", [("f32", 1, 1920), ("bf16", 1, 7680), ("bf16", 4099, 1152), ("f32", 1025, 333)])
+@pytest.mark.parametrize("dtype,rows,cols", [("f32", 1, 1920), ("bf16", 1, 7680), ("bf16", 4099, 1152), ("f32", 1025, 333),
+                                             ("bf16", 4099, 1920), ("f32", 4099, 1000), ("bf16", 1000, 7687), ("f32", 3301, 1501),
+                                             ("bf16", 12301, 500), ("f32", 9001, 130)])
 def test_quantize_many_rows(api, dev, dtype, rows, cols):
     import torch
     dt = torch.bfloat16 if dtype == "bf16" else torch.float32
