@@ -7,7 +7,8 @@
 // bytes per lane that v_mfma_f32_32x32x16_bf16 takes, in as many cycles, for twice the multiplications.  The
 // epilogues are of their own, as is the kernel for few rows (k_i8_split).
 // Long calls are bound by the matrix pipe and the clock that it leaves (1.94 GHz): 16,384 x 16,384 x 8,192 1.69 ms, 2.60
-// POP/s (torch's int8 product 2.25), 2.95 with the LDS-DMA taken out; 17,776 x 1,920 x 7,680 with the gated residual 250 us,
+// POP/s (torch's int8 product 2.25), 2.95 with the LDS-DMA taken out, 3.3 for the instruction alone on such codes in
+// registers (4.9 on zeros: the power that the bits' changes take sets the clock); 17,776 x 1,920 x 7,680 with the gated residual 250 us,
 // 2.10, and at K = 1,920, where a tile has 15 k-steps, by what surrounds them too: MLP up with GELU 278 us, 1.89.
 #include "gemm_tile.h"
 
