@@ -460,8 +460,7 @@ typedef struct {
 } dc_sampler_ext;
 
 /* dc_sampler_create_ex with the extensions of ext (NULL: the same).  With blocks or blocks_low
- * the workspace is dc_block_ext_workspace_bytes.  A reuse step on a quantised cache writes
- * g = h_in + r into dc_buffers.h. */
+ * the workspace is dc_block_ext_workspace_bytes.  Codes and scales are 16-byte aligned. */
 dc_status dc_sampler_create_ext(const dc_model_cfg* cfg, const dc_model_weights* w, int32_t B,
                                 const dc_sched_problem* problems, const double* sigmas,
                                 const dc_buffers* buf, const dc_sampler_opts* opts,

@@ -37,7 +37,7 @@ Status block_forward(const Geo& g, const dc_block_weights* bw, const dc_block_ex
                      const IdxList& il, void* ws, size_t ws_bytes, hipStream_t s);
 Status head_euler(const Geo& g, const dc_model_weights* w, const float* head_mod, const float* gin,
                   float* x, float dsigma, const IdxList& il, void* ws, size_t ws_bytes,
-                  hipStream_t s, const void* resid);
+                  hipStream_t s, const HeadResid& resid);
 
 namespace {
 
@@ -122,7 +122,7 @@ struct Calib {
       DC_TRY(lincomb(r_at(k), F(L.h), 1.0f, F(L.h_in), -1.0f, size_t(g.Nv) * g.d, s));   // r = h_out - h_in
       DC_HIP(hipMemcpyAsync(x_at(k + 1), x_at(k), lat * 4, hipMemcpyDeviceToDevice, s));
       DC_TRY(head_euler(g, w, mk + size_t(g.L) * 6 * g.d, F(L.h), x_at(k + 1), dsig(k), one, blk(),
-                        L.blk_bytes, s, nullptr));
+                        L.blk_bytes, s, {}));
     }
     return Status::ok();
   }
@@ -142,7 +142,7 @@ struct Calib {
     for (int i = 0; i <= n; ++i) ids[i] = i;
     IdxList il;
     DC_TRY(make_idx(ids, n + 1, il));
-    DC_TRY(head_euler(g, w, mt + size_t(g.L) * 6 * g.d, F(L.h), F(L.v), 1.0f, il, blk(), L.blk_bytes, s, nullptr));
+    DC_TRY(head_euler(g, w, mt + size_t(g.L) * 6 * g.d, F(L.h), F(L.v), 1.0f, il, blk(), L.blk_bytes, s, {}));
     for (int i = 0; i < n; ++i)
       DC_TRY(scaled_diff(dx_at(i0 + i), F(L.v) + size_t(i) * lat, F(L.v) + size_t(n) * lat, dsig(t), lat, s));
     return Status::ok();

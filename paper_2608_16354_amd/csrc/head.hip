@@ -31,8 +31,9 @@
 // and cs / shw, and the fifth tile of 4.3.
 //
 // On a reuse step the head input is g = h_in + r (Eq. 1 with the cached r_j): the
-// kResid variant reads h_in and the bf16 residual cache and forms g in registers with
-// the same fp32 addition as the cache-apply kernel, so g never goes through HBM.
+// variants with a residual read h_in and the residual cache (bf16, or codes of 8 or 4 bits and their
+// scales) and form g in registers with the same fp32 arithmetic as the cache-apply kernels, so g
+// never goes through HBM.
 #include <hip/hip_runtime.h>
 
 #include "internal.h"
@@ -49,7 +50,8 @@ struct HeadGeo { int T, Hl, Wl, p, Hp, Wp; };
 constexpr int kWaves = 8;           // waves per workgroup
 constexpr int kLdr = 68;            // row stride (floats) of a wave's 16 x 64 partial tile
 constexpr int kChunkG = 128;        // 16-byte pieces of a chunk of g: 16 rows x 8
-constexpr int kChunkR = 64;         // and of the residual (bf16)
+// and of the residual: bf16, or codes and behind them the scales (a dword of a row to each lane, four times)
+constexpr int chunk_r(int res) { return res == 16 ? 64 : res == 8 ? 32 + 16 : res == 4 ? 16 + 16 : 0; }
 
 // LDS-DMA: lane i reads 16 bytes at base + off (or 4 bytes at p) and they land at the
 // wave-uniform LDS address dst + 16 i (4 i).  Inline assembly, so that the compiler makes no
@@ -64,6 +66,15 @@ __device__ inline void dma4(const void* p, const void* dst) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
                :: "v"(p), "s"(lds) : "memory", "m0");
 }
+// 4 bytes at base + off
+__device__ inline void dma4(const void* base, uint32_t off, const void* dst) {
+  const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(dst));
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
+               :: "v"(off), "s"(base), "s"(lds) : "memory", "m0");
+}
+// the i-th code of a dword
+template <int BITS>
+__device__ inline float code(uint32_t w, int i) { return float(int(w << (32 - BITS - BITS * i)) >> (32 - BITS)); }
 // s_waitcnt vmcnt(N), the other counters left alone
 template <int N>
 __device__ inline void wait_vmcnt() {
@@ -93,26 +104,28 @@ __device__ inline size_t latent_of_output(const HeadGeo& hg, int n) {
 // chunks [chunk_begin(w), chunk_begin(w + 1)) of the nch chunks of d belong to wave w
 __device__ inline int chunk_begin(int w, int nch) { return (w * nch) / kWaves; }
 
-// NC: chunks per wave at most, the last NL of whose W fragments stay in LDS instead of registers;
+// kRes: bits of a cached value, 0 without a residual.  NC: chunks per wave at most, the last NL of whose W fragments stay in LDS instead of registers;
 // RING <= NC: chunks of the token rows a wave has in flight.
-template <bool kResid, int NC, int NL, int RING>
+template <int kRes, int NC, int NL, int RING>
 __global__ void __launch_bounds__(512) k_head_euler_bf16(const float* __restrict__ gin,
-                                                         const uint16_t* __restrict__ resid,
+                                                         const char* __restrict__ resid,
+                                                         const float* __restrict__ rscale,
                                                          const uint16_t* __restrict__ W,
                                                          const float* __restrict__ bias,
                                                          const float* __restrict__ shift,
                                                          const float* __restrict__ scale,
                                                          float* __restrict__ x, float dsigma,
                                                          int Nv, int d, float eps, HeadGeo hg) {
-  constexpr int kSlot = kChunkG + (kResid ? kChunkR : 0);
-  constexpr int kDma = kResid ? 3 : 2;                    // DMA instructions per chunk
+  constexpr bool kCodes = kRes == 8 || kRes == 4;
+  constexpr int kSlot = kChunkG + chunk_r(kRes);
+  constexpr int kDma = kRes == 8 ? 5 : kRes == 4 ? 4 : kRes == 16 ? 3 : 2;      // DMA instructions per chunk
   constexpr int kPer = (NC * kWaves * 32 + 511) / 512;    // elements of scale per thread
   static_assert(RING <= NC, "a tile's shifts and latent values arrive in time");
   __shared__ uint4 s_ring[kWaves][RING][kSlot];
   __shared__ float s_x[kWaves][2][64];                    // latent values of a tile, by thread
   __shared__ float* s_xn[32];                             // where outputs 2 i of token 0 land
   __shared__ float* s_px[512];                            // and a tile's outputs, by thread
-  __shared__ float s_k[2][kWaves][64];                    // shifts: g, and the residual's dword
+  __shared__ float s_k[2][kWaves][64];                    // shifts: g, the residual's dword, its scale
   __shared__ float s_sc1[NC * kWaves * 32];               // 1 + scale
   __shared__ float2 s_st[kWaves][16];                     // per wave and row: sum, sum sq of g - K
   __shared__ uint4 s_w[kWaves][NL > 0 ? NL : 1][NL > 0 ? 256 : 1];   // [nb][lane] of a chunk
@@ -143,9 +156,10 @@ __global__ void __launch_bounds__(512) k_head_euler_bf16(const float* __restrict
   // chunks past kc are clamped (they re-read lines already fetched).  The 16-byte pieces of a
   // row are XOR-swizzled by the row, so that the fragment reads spread over the banks.
   const float* const gb = gin + size_t(r0) * d + 32 * cb;
-  const uint16_t* const rb = kResid ? resid + size_t(r0) * d + 32 * cb : nullptr;
+  const char* const rb = kRes ? resid + (size_t(r0) * d + 32 * cb) * kRes / 8 : nullptr;
+  const float* const sb = kCodes ? rscale + size_t(r0) * (d >> 6) : nullptr;
   auto row_of = [&](int t, int r) { return min(16 * min(t, ntile - 1) + r, r1 - r0 - 1); };
-  struct Off { uint32_t g[2], r; };
+  struct Off { uint32_t g[2], r[2], s; };
   auto offsets = [&](int t) {
     Off o;
 #pragma unroll
@@ -153,7 +167,14 @@ __global__ void __launch_bounds__(512) k_head_euler_bf16(const float* __restrict
       const int r = 8 * h + (lane >> 3);
       o.g[h] = uint32_t(row_of(t, r) * d) * 4u + 16u * ((lane & 7) ^ ((r >> 1) & 7));
     }
-    o.r = kResid ? uint32_t(row_of(t, lane >> 2) * d) * 2u + 16u * ((lane & 3) ^ ((lane >> 4) & 3)) : 0u;
+    o.r[0] = o.r[1] = o.s = 0u;
+    if constexpr (kRes == 16) o.r[0] = uint32_t(row_of(t, lane >> 2) * d) * 2u + 16u * ((lane & 3) ^ ((lane >> 4) & 3));
+    if constexpr (kRes == 4) o.r[0] = uint32_t(row_of(t, lane >> 2) * d) / 2u + 4u * (lane & 3);
+    if constexpr (kRes == 8) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) o.r[h] = uint32_t(row_of(t, 8 * h + (lane >> 3)) * d) + 4u * (lane & 7);
+    }
+    if constexpr (kCodes) o.s = uint32_t(row_of(t, lane & 15) * (d >> 6)) * 4u;
     return o;
   };
   auto fetch = [&](const Off& o, int j, int slot) {
@@ -161,7 +182,12 @@ __global__ void __launch_bounds__(512) k_head_euler_bf16(const float* __restrict
     uint4* const to = s_ring[wave][slot];
     dma16(gb + c, o.g[0], to);
     dma16(gb + c, o.g[1], to + 64);
-    if constexpr (kResid) dma16(rb + c, o.r, to + kChunkG);
+    if constexpr (kRes == 16) dma16(rb + 2 * c, o.r[0], to + kChunkG);
+    if constexpr (kCodes) {
+      dma4(rb + c * kRes / 8, o.r[0], to + kChunkG);
+      if constexpr (kRes == 8) dma4(rb + c, o.r[1], to + kChunkG + 16);
+      dma4(sb + ((32 * cb + c) >> 6), o.s, to + kSlot - 16);
+    }
   };
   // epilogue role of a thread: token er = tid % 16 of a tile, outputs n = 2 eq and 2 eq + 1
   // with eq = tid / 16
@@ -180,7 +206,11 @@ __global__ void __launch_bounds__(512) k_head_euler_bf16(const float* __restrict
   auto fetch_k = [&](int t) {
     const size_t first = size_t(r0 + row_of(t, c16)) * d;
     const char* pk = reinterpret_cast<const char*>(gin + first);
-    if (kResid && (lane & 16)) pk = reinterpret_cast<const char*>(resid + first);
+    if (kRes == 16 && (lane & 16)) pk = resid + 2 * first;
+    if constexpr (kCodes) {
+      if (lane & 32) pk = reinterpret_cast<const char*>(rscale + (first >> 6));      // d is a multiple of 64
+      else if (lane & 16) pk = resid + first * kRes / 8;
+    }
     dma4(pk, s_k[t & 1][wave]);
   };
   Off off = offsets(0);
@@ -308,14 +338,24 @@ __global__ void __launch_bounds__(512) k_head_euler_bf16(const float* __restrict
       wait_vmcnt<kDma * (RING - 1)>();
       if (j == 0) {
         kcur = s_k[t & 1][wave][c16];
-        if constexpr (kResid) kcur += __uint_as_float(__float_as_uint(s_k[t & 1][wave][16 + c16]) << 16);
+        if constexpr (kRes == 16) kcur += __uint_as_float(__float_as_uint(s_k[t & 1][wave][16 + c16]) << 16);
+        if constexpr (kCodes)
+          kcur = fmaf(code<kCodes ? kRes : 8>(__float_as_uint(s_k[t & 1][wave][16 + c16]), 0), s_k[t & 1][wave][32 + c16], kcur);
       }
       const uint4* const from = s_ring[wave][slot];
       const int pr = c16 * 8, sw = (c16 >> 1) & 7;
       const float4 va = __builtin_bit_cast(float4, from[pr + ((2 * g4) ^ sw)]);
       const float4 vb = __builtin_bit_cast(float4, from[pr + ((2 * g4 + 1) ^ sw)]);
       uint4 rw = make_uint4(0, 0, 0, 0);
-      if constexpr (kResid) rw = from[kChunkG + c16 * 4 + (g4 ^ ((c16 >> 2) & 3))];
+      float rs = 0.f;
+      if constexpr (kRes == 16) rw = from[kChunkG + c16 * 4 + (g4 ^ ((c16 >> 2) & 3))];
+      if constexpr (kRes == 8) {
+        const uint2 w = reinterpret_cast<const uint2*>(from + kChunkG)[c16 * 4 + g4];
+        rw.x = w.x;
+        rw.y = w.y;
+      }
+      if constexpr (kRes == 4) rw.x = reinterpret_cast<const uint32_t*>(from + kChunkG)[c16 * 4 + g4];
+      if constexpr (kCodes) rs = reinterpret_cast<const float*>(from + kSlot - 16)[c16];
       const int k0 = 32 * (cb + min(j, last)) + 8 * g4;
       const float4 sa = *reinterpret_cast<const float4*>(s_sc1 + k0);
       const float4 sb = *reinterpret_cast<const float4*>(s_sc1 + k0 + 4);
@@ -325,13 +365,19 @@ __global__ void __launch_bounds__(512) k_head_euler_bf16(const float* __restrict
       slot = slot + 1 == RING ? 0 : slot + 1;
       if (j < kc) {
         float e[8] = {va.x, va.y, va.z, va.w, vb.x, vb.y, vb.z, vb.w};
-        if constexpr (kResid) {                 // g = h_in + r, the cache-apply addition
+        if constexpr (kRes == 16) {             // g = h_in + r, the cache-apply addition
           const uint32_t r[4] = {rw.x, rw.y, rw.z, rw.w};
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             e[2 * i] += __uint_as_float(r[i] << 16);
             e[2 * i + 1] += __uint_as_float(r[i] & 0xFFFF0000u);
           }
+        }
+        if constexpr (kCodes) {                 // g = h_in + code * scale, likewise
+          constexpr int V = kCodes ? 32 / kRes : 4;
+          const uint32_t r[2] = {rw.x, rw.y};
+#pragma unroll
+          for (int i = 0; i < 8; ++i) e[i] = fmaf(code<kCodes ? kRes : 8>(r[i / V], i % V), rs, e[i]);
         }
         const float sc[8] = {sa.x, sa.y, sa.z, sa.w, sb.x, sb.y, sb.z, sb.w};
         bf16x8 ah, al, fw[4];
@@ -388,42 +434,42 @@ __global__ void __launch_bounds__(512) k_head_euler_bf16(const float* __restrict
     }
     const float dm = t1 * inv_d;                               // mu - K
     const float var = fmaxf(t2 * inv_d - dm * dm, 0.f);
-    const float rs = 1.0f / sqrtf(var + eps);
+    const float rstd = 1.0f / sqrtf(var + eps);
     if (r0 + 16 * t + er < r1) {
       float* const px = s_px[id];
       const float2 cs = *reinterpret_cast<const float2*>(&s_cs[0][2 * eq]);
       const float2 shw = *reinterpret_cast<const float2*>(&s_shw[0][2 * eq]);
-      px[0] = s_x[wave][0][ln] + dsigma * (rs * (o0 - dm * cs.x) + shw.x);
-      px[xd] = s_x[wave][1][ln] + dsigma * (rs * (o1 - dm * cs.y) + shw.y);
+      px[0] = s_x[wave][0][ln] + dsigma * (rstd * (o0 - dm * cs.x) + shw.x);
+      px[xd] = s_x[wave][1][ln] + dsigma * (rstd * (o1 - dm * cs.y) + shw.y);
     }
   }
   wait_vmcnt<0>();                              // the chunks past the last tile land before the LDS goes
 }
 
 template <int NC, int NL, int RG, int RR>
-Status launch(int grid, const float* gin, const uint16_t* resid, const uint16_t* W, const float* bias,
+Status launch(int grid, const float* gin, const HeadResid& r, const uint16_t* W, const float* bias,
               const float* shift, const float* scale, float* x, float dsigma, const Geo& g, hipStream_t s) {
   const HeadGeo hg{g.T, g.Hl, g.Wl, g.p, g.Hp, g.Wp};
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(512), 0, s, gin, static_cast<const char*>(r.values), r.scales, W, bias,
+                       shift, scale, x, dsigma, g.Nv, g.d, g.eps, hg);
+    DC_HIP(hipGetLastError());
+    return Status::ok();
+  };
+  if (!r.values) return go(k_head_euler_bf16<0, NC, NL, RG>);
   if constexpr (RR > 0) {
-    if (resid) {
-      hipLaunchKernelGGL((k_head_euler_bf16<true, NC, NL, RR>), dim3(grid), dim3(512), 0, s, gin, resid, W, bias, shift,
-                         scale, x, dsigma, g.Nv, g.d, g.eps, hg);
-      DC_HIP(hipGetLastError());
-      return Status::ok();
-    }
+    if (r.bits == 16) return go(k_head_euler_bf16<16, NC, NL, RR>);
+    if (r.bits == 8) return go(k_head_euler_bf16<8, NC, NL, RR>);
+    if (r.bits == 4) return go(k_head_euler_bf16<4, NC, NL, RR>);
   }
-  if (resid) return Status::shape("bf16 head with a residual input needs d <= 2048");
-  hipLaunchKernelGGL((k_head_euler_bf16<false, NC, NL, RG>), dim3(grid), dim3(512), 0, s, gin, resid, W, bias, shift,
-                     scale, x, dsigma, g.Nv, g.d, g.eps, hg);
-  DC_HIP(hipGetLastError());
-  return Status::ok();
+  return Status::shape("bf16 head with a residual input needs d <= 2048");
 }
 
 }  // namespace
 
 bool head_takes_resid(const Geo& g) { return g.bf16 && g.d <= 2048; }
 
-Status head_euler_bf16(const float* gin, const uint16_t* resid, const uint16_t* W, const float* bias,
+Status head_euler_bf16(const float* gin, const HeadResid& resid, const uint16_t* W, const float* bias,
                        const float* shift, const float* scale, float* x, float dsigma, const Geo& g,
                        hipStream_t s) {
   if (g.Nv <= 0) return Status::ok();

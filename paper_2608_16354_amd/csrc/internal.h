@@ -181,11 +181,21 @@ Status patch_embed_bf16(const float* x, const float* W, const float* bias, const
 Status patch_embed_f32(const float* x, const float* W, const float* bias, const float* pos, const float* txt,
                        float* out, const IdxList& idx, const Geo& g, hipStream_t s);
 // bf16 model: LN-modulation + head projection + unpatchify + Euler update of one sample's
-// latent in one pass over its N_v video rows of g (head.hip).  With resid != NULL the input
-// is g = gin + resid (bf16), formed in registers (reuse steps); head_takes_resid says whether
-// the model's width allows that.
+// latent in one pass over its N_v video rows of g (head.hip).  With a residual the input is
+// g = gin + residual, formed in registers (reuse steps); head_takes_resid says whether the
+// model's width allows that.
+struct HeadResid {                 // one entry of the residual cache, or none
+  const void* values = nullptr;    // bf16 (bits 16) or codes (8, 4)
+  const float* scales = nullptr;   // of the codes
+  int bits = 16;
+  HeadResid at(size_t b, const Geo& g) const {
+    const size_t n = size_t(g.Nv) * g.d;
+    if (!values) return {};
+    return {static_cast<const char*>(values) + b * n * bits / 8, scales ? scales + b * (n / 64) : nullptr, bits};
+  }
+};
 bool head_takes_resid(const Geo& g);
-Status head_euler_bf16(const float* gin, const uint16_t* resid, const uint16_t* W, const float* bias,
+Status head_euler_bf16(const float* gin, const HeadResid& resid, const uint16_t* W, const float* bias,
                        const float* shift, const float* scale, float* x, float dsigma, const Geo& g,
                        hipStream_t s);
 

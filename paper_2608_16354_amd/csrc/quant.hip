@@ -283,7 +283,8 @@ __global__ void __launch_bounds__(256) k_cache_store_q(const float* __restrict__
   if ((i & 15) == 0) scales[(base + i) >> 4] = s;
 }
 
-// g = h_in + codes * scale on the video rows (g may be h_in: a thread reads what it writes)
+// g = h_in + codes * scale, one rounding (as the reuse head forms it), on the video rows (g may be h_in: a thread
+// reads what it writes)
 template <int BITS>
 __global__ void __launch_bounds__(256) k_cache_apply_q(const float* h_in,
                                                        const typename Codes<BITS>::T* __restrict__ codes,
@@ -296,7 +297,7 @@ __global__ void __launch_bounds__(256) k_cache_apply_q(const float* h_in,
   const float4 r = Codes<BITS>::unpack(codes[base + i]);
   const float s = scales[(base + i) >> 4];
   reinterpret_cast<float4*>(g)[size_t(b) * stride_h4 + i] =
-      make_float4(a.x + r.x * s, a.y + r.y * s, a.z + r.z * s, a.w + r.w * s);
+      make_float4(fmaf(r.x, s, a.x), fmaf(r.y, s, a.y), fmaf(r.z, s, a.z), fmaf(r.w, s, a.w));
 }
 
 template <bool BF>

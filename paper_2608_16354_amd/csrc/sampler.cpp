@@ -31,7 +31,7 @@ Status block_forward(const Geo& g, const dc_block_weights* bw, const dc_block_ex
                      const IdxList& il, void* ws, size_t ws_bytes, hipStream_t s);
 Status head_euler(const Geo& g, const dc_model_weights* w, const float* head_mod, const float* gin,
                   float* x, float dsigma, const IdxList& il, void* ws, size_t ws_bytes,
-                  hipStream_t s, const void* resid);
+                  hipStream_t s, const HeadResid& resid);
 Status drift_call(const Geo& g, const float* h_in, const float* mod0, void* u_ref, int snapshot,
                   double* sums, const IdxList& il, void* ws, size_t ws_bytes, hipStream_t s);
 Status check_ext(const Geo& g, const dc_block_ext& e);
@@ -143,6 +143,8 @@ Status create(const dc_model_cfg* cfg, const dc_model_weights* w, int32_t B,
     return Status::arg("guidance needs a finite scale and txt_null");
   if (x.cache_bits != 0 && x.cache_bits != 8 && x.cache_bits != 4) return Status::arg("cache_bits must be 0, 8 or 4");
   if (x.cache_bits && !x.cache_scales) return Status::arg("cache_bits needs cache_scales");
+  if (x.cache_bits && (reinterpret_cast<uintptr_t>(buf->resid) % 16 || reinterpret_cast<uintptr_t>(x.cache_scales) % 16))
+    return Status::arg("the cache's codes and scales must be 16-byte aligned");
   const Workspace lay = workspace_layout(s->g, cfg_on ? 2 * B : B);
   if (buf->ws_bytes < (x.blocks || x.blocks_low ? lay.total_ext : lay.total))
     return Status::make(DC_ERR_WORKSPACE, "workspace smaller than dc_workspace_bytes() (with extended blocks "
@@ -281,9 +283,9 @@ Status step(dc_sampler* s, int k, hipStream_t st, uint8_t* realized, double* dri
         DC_TRY(cache_store(bf.h, bf.h_in, bf.resid, ilb, g, st));
     }
   }
-  // reuse scenes: the fused bf16 head reads h_in and r itself; other models apply the
-  // cache into h first
-  const bool fused_reuse = head_takes_resid(g) && !s->cache_bits;
+  // reuse scenes: the fused bf16 head reads h_in and r (or its codes) itself; other models apply
+  // the cache into h first
+  const bool fused_reuse = head_takes_resid(g);
   if (!reuse.empty() && !fused_reuse) {
     IdxList il;
     const std::vector<int32_t> rb = with_branches(reuse);
@@ -298,25 +300,25 @@ Status step(dc_sampler* s, int k, hipStream_t st, uint8_t* realized, double* dri
   // linear in v, so each branch's head adds its share
   const double dsig = s->sigmas[size_t(k)] - s->sigmas[size_t(k - 1)];
   const float* head_mod = mod_k + size_t(g.L) * 6 * g.d;
-  const size_t rstride = size_t(g.Nv) * g.d * g.esz;      // one entry of the residual cache
   const float dsig_c = float(s->cfg_on ? dsig * s->guidance : dsig);
   const float dsig_u = float(dsig * (1.0 - double(s->guidance)));
   const std::vector<int32_t>& from_h = fused_reuse ? refresh : ids;
   if (!from_h.empty()) {
     IdxList il;
     DC_TRY(make_idx(from_h.data(), int(from_h.size()), il));
-    DC_TRY(head_euler(g, W, head_mod, bf.h, bf.x, dsig_c, il, bf.ws, bf.ws_bytes, st, nullptr));
+    DC_TRY(head_euler(g, W, head_mod, bf.h, bf.x, dsig_c, il, bf.ws, bf.ws_bytes, st, {}));
     if (s->cfg_on)
       DC_TRY(head_euler(g, W, head_mod, bf.h + size_t(B) * row_stride, bf.x, dsig_u, il, bf.ws,
-                        bf.ws_bytes, st, nullptr));
+                        bf.ws_bytes, st, {}));
   }
   if (fused_reuse && !reuse.empty()) {
     IdxList il;
     DC_TRY(make_idx(reuse.data(), int(reuse.size()), il));
-    DC_TRY(head_euler(g, W, head_mod, bf.h_in, bf.x, dsig_c, il, bf.ws, bf.ws_bytes, st, bf.resid));
+    const HeadResid r{bf.resid, s->cache_scales, s->cache_bits ? s->cache_bits : 16};
+    DC_TRY(head_euler(g, W, head_mod, bf.h_in, bf.x, dsig_c, il, bf.ws, bf.ws_bytes, st, r));
     if (s->cfg_on)
       DC_TRY(head_euler(g, W, head_mod, bf.h_in + size_t(B) * row_stride, bf.x, dsig_u, il, bf.ws,
-                        bf.ws_bytes, st, static_cast<const char*>(bf.resid) + size_t(B) * rstride));
+                        bf.ws_bytes, st, r.at(size_t(B), g)));
   }
 
   // controller state

@@ -112,13 +112,21 @@ def _legal(K, h_max, b):
     return a
 
 
+SAMPLES = {
+    "bf16": _shape(256, 4, 64, 512, (3, 10, 12), 5, "bf16", blocks=2), "f32": _shape(256, 4, 64, 512, (3, 10, 12), 5, "f32", blocks=2),
+    # the reuse head's other widths, three tiles of tokens to a workgroup, and a width whose reuse applies the cache first
+    "bf16-1152": _shape(1152, 16, 72, 1152, (3, 10, 12), 5, "bf16", blocks=2), "bf16-1920": _shape(1920, 30, 64, 1920, (1, 14, 14), 5, "bf16", blocks=2),
+    "bf16-long": _shape(128, 2, 64, 128, (8, 64, 78), 5, "bf16", blocks=2), "bf16-2304": _shape(2304, 36, 64, 128, (1, 6, 6), 3, "bf16", blocks=2),
+}
+
+
 @pytest.mark.parametrize("bits", [0, 8, 4])
-@pytest.mark.parametrize("dtype,mode", [("bf16", "both"), ("bf16", "none"), ("f32", "qk")])
-def test_sample_is_its_calls(api, dev, bits, dtype, mode):
+@pytest.mark.parametrize("name,mode", [("bf16", "both"), ("bf16", "none"), ("f32", "qk"), ("bf16-1152", "none"), ("bf16-1920", "none"),
+                                       ("bf16-long", "none"), ("bf16-2304", "none")])
+def test_sample_is_its_calls(api, dev, bits, name, mode):
     """Two scenes with staggered reuses and guidance: the sampler's latent against the public calls in order."""
     import torch
-    m = _shape(256, 4, 64, 512, (3, 10, 12), 5, dtype, blocks=2)
-    K, B, w = 6, 2, 2.5
+    m, K, B, w = SAMPLES[name], 6, 2, 2.5
     W = I.Weights(m, 150)
     dm = api.DeviceModel(W, dev)
     ext = None
@@ -132,7 +140,7 @@ def test_sample_is_its_calls(api, dev, bits, dtype, mode):
     txt = torch.from_numpy(np.stack([I.text(m, 150, b) for b in range(B)]))
     null = torch.zeros_like(txt)
     sig = I.sigmas(K)
-    say("extended sample", bits, dtype, mode)
+    say("extended sample", bits, name, mode)
     smp = api.Sampler(dm, problems, sig, x1, txt, guidance=(w, null), ext=ext, cache_bits=bits)
     realized, _ = smp.run()
     torch.cuda.synchronize()
@@ -171,7 +179,7 @@ def test_sample_is_its_calls(api, dev, bits, dtype, mode):
             x[b] = v[0]
     torch.cuda.synchronize()
     got, want = smp.x.cpu().numpy(), x.cpu().numpy()
-    say("sample", bits, dtype, mode, "max difference", np.abs(got - want).max())
+    say("sample", bits, name, mode, "max difference", np.abs(got - want).max())
     assert np.isfinite(got).all() and np.array_equal(got, want)
     smp.close()
 

@@ -207,6 +207,7 @@ def test_sampler_ext_refuses(lib):
     ext = (L.BlockExt * 2)()
     assert create(L.SamplerExt(None, None, 5, FAKE), full) == ARG
     assert create(L.SamplerExt(None, None, 8, None), full) == ARG
+    assert create(L.SamplerExt(None, None, 4, FAKE + 8), full) == ARG
     assert create(L.SamplerExt(ext, None, 0, None), plain) == WS
     assert create(L.SamplerExt(None, ext, 0, None), full) == ARG       # no low expert
     bad = qk(eps=0.0)
