@@ -27,7 +27,7 @@
 // the Euler update to the two latent values they land on.
 // 17,776 x 3,072: 55 us (216 MB, 3.9 TB/s; an LN pass and a GEMM on its rows took 115);
 // 17,776 x 1,920: 39 us, 42 before; 3,704 x 1,152 (one tile per workgroup): 12.2 us, 15; with a
-// residual 13.3 us, 20.  What is left over the stream is the prologue, about 7 us of W_head
+// residual 13.3 us, 20; 17,776 x 1,920 with one in bf16 52 us, in 8 bits 51, in 4 bits 49.  What is left over the stream is the prologue, about 7 us of W_head
 // and cs / shw, and the fifth tile of 4.3.
 //
 // On a reuse step the head input is g = h_in + r (Eq. 1 with the cached r_j): the
@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(512) k_head_euler_bf16(const float* __restrict
                                                          int Nv, int d, float eps, HeadGeo hg) {
   constexpr bool kCodes = kRes == 8 || kRes == 4;
   constexpr int kSlot = kChunkG + chunk_r(kRes);
-  constexpr int kDma = kRes == 8 ? 5 : kRes == 4 ? 4 : kRes == 16 ? 3 : 2;      // DMA instructions per chunk
+  constexpr int kDma = kCodes ? 4 : kRes == 16 ? 3 : 2;   // DMA instructions per chunk
   constexpr int kPer = (NC * kWaves * 32 + 511) / 512;    // elements of scale per thread
   static_assert(RING <= NC, "a tile's shifts and latent values arrive in time");
   __shared__ uint4 s_ring[kWaves][RING][kSlot];
@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(512) k_head_euler_bf16(const float* __restrict
   const char* const rb = kRes ? resid + (size_t(r0) * d + 32 * cb) * kRes / 8 : nullptr;
   const float* const sb = kCodes ? rscale + size_t(r0) * (d >> 6) : nullptr;
   auto row_of = [&](int t, int r) { return min(16 * min(t, ntile - 1) + r, r1 - r0 - 1); };
-  struct Off { uint32_t g[2], r[2], s; };
+  struct Off { uint32_t g[2], r, s; };
   auto offsets = [&](int t) {
     Off o;
 #pragma unroll
@@ -167,13 +167,10 @@ __global__ void __launch_bounds__(512) k_head_euler_bf16(const float* __restrict
       const int r = 8 * h + (lane >> 3);
       o.g[h] = uint32_t(row_of(t, r) * d) * 4u + 16u * ((lane & 7) ^ ((r >> 1) & 7));
     }
-    o.r[0] = o.r[1] = o.s = 0u;
-    if constexpr (kRes == 16) o.r[0] = uint32_t(row_of(t, lane >> 2) * d) * 2u + 16u * ((lane & 3) ^ ((lane >> 4) & 3));
-    if constexpr (kRes == 4) o.r[0] = uint32_t(row_of(t, lane >> 2) * d) / 2u + 4u * (lane & 3);
-    if constexpr (kRes == 8) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) o.r[h] = uint32_t(row_of(t, 8 * h + (lane >> 3)) * d) + 4u * (lane & 7);
-    }
+    o.r = o.s = 0u;
+    if constexpr (kRes == 16) o.r = uint32_t(row_of(t, lane >> 2) * d) * 2u + 16u * ((lane & 3) ^ ((lane >> 4) & 3));
+    if constexpr (kRes == 4) o.r = uint32_t(row_of(t, lane >> 2) * d) / 2u + 4u * (lane & 3);
+    if constexpr (kRes == 8) o.r = uint32_t(row_of(t, (lane >> 1) & 15) * d) + 16u * (lane & 1);
     if constexpr (kCodes) o.s = uint32_t(row_of(t, lane & 15) * (d >> 6)) * 4u;
     return o;
   };
@@ -182,10 +179,11 @@ __global__ void __launch_bounds__(512) k_head_euler_bf16(const float* __restrict
     uint4* const to = s_ring[wave][slot];
     dma16(gb + c, o.g[0], to);
     dma16(gb + c, o.g[1], to + 64);
-    if constexpr (kRes == 16) dma16(rb + 2 * c, o.r[0], to + kChunkG);
+    if constexpr (kRes == 16) dma16(rb + 2 * c, o.r, to + kChunkG);
     if constexpr (kCodes) {
-      dma4(rb + c * kRes / 8, o.r[0], to + kChunkG);
-      if constexpr (kRes == 8) dma4(rb + c, o.r[1], to + kChunkG + 16);
+      // 8 bits: 16 bytes to each of 32 lanes (two dwords to every lane: 58 us at 17,776 x 1,920 for 51)
+      if constexpr (kRes == 4) dma4(rb + c / 2, o.r, to + kChunkG);
+      else if (lane < 32) dma16(rb + c, o.r, to + kChunkG);
       dma4(sb + ((32 * cb + c) >> 6), o.s, to + kSlot - 16);
     }
   };
