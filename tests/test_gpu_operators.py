@@ -499,3 +499,65 @@ def test_two_streams_at_once(api, dev):
         for n in a:
             assert torch.equal(a[n], b[n]), n
     assert torch.equal(alone[0]["few"], alone[0]["y"][0, :5])
+
+
+# ----------------------------------------------------------------------------
+# offsets beyond 32 bits
+# ----------------------------------------------------------------------------
+def test_last_sample_of_a_long_batch(api, dev):
+    """Samples past 2^32 bytes of a batch get what they get alone."""
+    import torch
+    m = shape(30, 64, (13, 60, 90), 226)
+    d, N, n_v, cfg, B = m.hidden, m.n_tok, m.n_v, api.model_cfg(m), 34
+    gen = torch.Generator(dev).manual_seed(6)
+    h = [torch.empty((B, N, d), device=dev) for _ in range(2)]
+    one = [torch.randn((1, N, d), device=dev, generator=gen) for _ in range(2)]
+    assert (B - 1) * N * d * 4 > 2 ** 32
+    for a, b in zip(h, one):
+        a[B - 1:].copy_(b)
+    for bits, dt in ((8, torch.int8), (4, torch.uint8)):
+        def cache(n):
+            return (torch.zeros((n, n_v, d * bits // 8), device=dev, dtype=dt), torch.zeros((n, n_v, d // 64), device=dev))
+        (k, s), (k1, s1) = cache(B), cache(1)
+        say("long batch", bits)
+        api.dc_cache_store_q(cfg, bits, h[0], h[1], k, s, [B - 1])
+        api.dc_cache_store_q(cfg, bits, one[0], one[1], k1, s1, [0])
+        assert torch.equal(k[B - 1:], k1) and torch.equal(s[B - 1:], s1) and not k[: B - 1].any()
+        g1 = one[1].clone()
+        api.dc_cache_apply_q(cfg, bits, h[1], k, s, h[1], [B - 1])
+        api.dc_cache_apply_q(cfg, bits, one[1], k1, s1, g1, [0])
+        assert torch.equal(h[1][B - 1:], g1)
+        h[1][B - 1:].copy_(one[1])
+    del h
+    x = torch.empty((B, N, 3 * d), device=dev, dtype=torch.bfloat16)
+    x1 = torch.randn((1, N, 3 * d), device=dev, generator=gen).bfloat16()
+    x[B - 1:].copy_(x1)
+    table = torch.randn((n_v, 32, 2), device=dev, generator=gen)
+    api.dc_qk_norm_rope(cfg, x, x, [B - 1], table=table)
+    api.dc_qk_norm_rope(cfg, x1, x1, [0], table=table)
+    assert torch.equal(x[B - 1:], x1)
+
+
+def test_rows_beyond_32_bit_offsets(api, dev):
+    import torch
+    rows, cols, apart = 700, 384, (1 << 22) + 8
+    x1 = torch.randn((rows, cols), device=dev, generator=torch.Generator(dev).manual_seed(7)).bfloat16()
+    x = torch.empty((rows, apart), device=dev, dtype=torch.bfloat16)[:, :cols]
+    q = torch.empty((rows, apart), device=dev, dtype=torch.int8)[:, :cols]
+    q1, s, s1 = torch.empty((rows, cols), device=dev, dtype=torch.int8), torch.empty(rows, device=dev), torch.empty(rows, device=dev)
+    x.copy_(x1)
+    api.dc_quantize_rows(x, q, s)
+    api.dc_quantize_rows(x1, q1, s1)
+    assert torch.equal(q, q1) and torch.equal(s, s1)
+
+
+def test_long_table(api, dev):
+    """31 million tokens: eight billion bytes of table, the last token's angles and the first's."""
+    import torch
+    m = I.ModelShape(1, 256, 4, 64, 1024, 16, 30, 2048, 2048, 2, 0, "bf16")
+    table = torch.empty((m.n_v, 32, 2), device=dev)
+    api.dc_rope_table(api.model_cfg(m), api.rope_axes((16, 24, 24), 100.0), None, table)
+    at = [0, 1, 1024, 1 << 20, m.n_v // 2 + 517, m.n_v - 1]
+    pos = np.array([[n >> 20, (n >> 10) & 1023, n & 1023] for n in at], np.float64)
+    want = X.rope_table(pos, (16, 24, 24), 100.0, 32)
+    assert np.abs(host(table[at]) - want).max() <= F32 + 1e-10
