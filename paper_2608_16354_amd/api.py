@@ -7,6 +7,7 @@ libdrivecache.so; nothing here computes.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 import numpy as np
 
@@ -218,10 +219,16 @@ def _call(name, stream, first, *args):
         L.check(name, rc)
 
 
+_AXES = struct.Struct("3i4x7d")        # dc_rope_axes; a field at a time takes five times as long
+
+
 def rope_axes(dim, theta=10000.0, start=(0.0, 0.0, 0.0), step=(1.0, 1.0, 1.0)) -> L.RopeAxes:
     """dc_rope_axes: features of a head that turn with time, height and width, and the grid's
     positions start + step * index."""
-    return L.RopeAxes(tuple(dim), theta, tuple(start), tuple(step))
+    try:
+        return L.RopeAxes.from_buffer_copy(_AXES.pack(*dim, theta, *start, *step))
+    except struct.error as e:
+        raise ValueError(f"dim, start and step: three numbers each, dim whole ones: {e}") from e
 
 
 def dc_rope_table(cfg, axes: L.RopeAxes, pos, table, stream=None):

@@ -12,6 +12,8 @@
 // 2.10, and at K = 1,920, where a tile has 15 k-steps, by what surrounds them too: MLP up with GELU 278 us, 1.89.
 #include "gemm_tile.h"
 
+#include <type_traits>
+
 namespace dc {
 
 namespace {
@@ -48,14 +50,17 @@ typedef float f32x4a __attribute__((ext_vector_type(4), aligned(4)));
 // of the wave (bf16: half the bytes) and leave as 16-byte pieces of rows, 128 bytes of a row at once.  The
 // tile's scales, biases and gates are in LDS from the start: read from memory here, one branch and one trip each
 // (edges, no bias), they cost as much as the rest of the epilogue (QKV 17,776 x 5,760 x 1,920: 47 of 206 us).
-template <bool BF, bool GELU, bool GATED>
-struct EpiLinear {
-  const float* sx;
-  const float* sw;
-  const float* bias;      // or NULL
+struct Residual {
   const float* gate;
   const float* residual;  // may be out
   int64_t ldr;
+};
+struct NoResidual {};
+template <bool BF, bool GELU, bool GATED>
+struct EpiLinear : std::conditional<GATED, Residual, NoResidual>::type {
+  const float* sx;
+  const float* sw;
+  const float* bias;      // or NULL
   void* out;
   int64_t ldo;
   static constexpr int V = BF ? 8 : 4;                // values of a 16-byte piece
@@ -80,7 +85,8 @@ struct EpiLinear {
     float* const v = reinterpret_cast<float*>(vec);
     const int n = min(n0 + min(tid, BN - 1), N - 1);
     const float x = sx[min(m0 + min(tid, BM - 1), M - 1)], w = sw[n], b = bias ? bias[n] : 0.f;
-    const float g = GATED ? gate[n] : 1.f;
+    float g = 1.f;
+    if constexpr (GATED) g = this->gate[n];
     if (tid < BM) v[tid] = x;
     if (tid < BN) {
       v[BM + tid] = w * g;
@@ -96,7 +102,8 @@ struct EpiLinear {
     float z[4] = {act(fmaf(float(t.x) * s, w.x, o.x)), act(fmaf(float(t.y) * s, w.y, o.y)),
                   act(fmaf(float(t.z) * s, w.z, o.z)), act(fmaf(float(t.w) * s, w.w, o.w))};
     char* const at = static_cast<char*>(out) + (int64_t(m) * ldo + n) * (BF ? 2 : 4);
-    const float* const pr = GATED ? residual + int64_t(m) * ldr + n : nullptr;
+    const float* pr = nullptr;
+    if constexpr (GATED) pr = this->residual + int64_t(m) * this->ldr + n;
     if (n + 4 <= N) {
       if constexpr (GATED) {
         const f32x4a q = *reinterpret_cast<const f32x4a*>(pr);
@@ -142,13 +149,14 @@ struct EpiLinear {
       const int RS = 64 / PR, ml = mw + lane / PR, nl = nb + lane % PR * V;
       const bool whole = nl + V <= N;
       char* po = static_cast<char*>(out) + (int64_t(ml) * ldo + nl) * (BF ? 2 : 4);
-      const float* pr = GATED ? residual + int64_t(ml) * ldr + nl : nullptr;
+      const float* pr = nullptr;
+      if constexpr (GATED) pr = this->residual + int64_t(ml) * this->ldr + nl;
       f32x4a res[GATED ? 2 : 1][4];
       auto fetch_residual = [&](int a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           if (whole && ml + a * 32 + j * RS < M) res[a & 1][j] = *reinterpret_cast<const f32x4a*>(pr);
-          pr += RS * ldr;
+          if constexpr (GATED) pr += RS * this->ldr;
         }
       };
       if constexpr (GATED) fetch_residual(0);
@@ -223,7 +231,7 @@ struct EpiLinear {
               static_cast<uint16_t*>(out)[m * ldo + n] = *reinterpret_cast<const uint16_t*>(at);
             } else {
               float f = *reinterpret_cast<const float*>(at);
-              if constexpr (GATED) f += residual[m * ldr + n];
+              if constexpr (GATED) f += this->residual[m * this->ldr + n];
               static_cast<float*>(out)[m * ldo + n] = f;
             }
           }
@@ -492,7 +500,16 @@ Status gemm_i8_qkv(const int8_t* A, const float* sx, const int8_t* W, const floa
 
 Status gemm_i8_linear(const LinearI8& a, hipStream_t s) {
   auto run = [&](auto e) {
-    e = {a.x_scale, a.w_scale, a.bias, a.gate, a.residual, a.ld_residual, a.out, a.ld_out};
+    e.sx = a.x_scale;
+    e.sw = a.w_scale;
+    e.bias = a.bias;
+    e.out = a.out;
+    e.ldo = a.ld_out;
+    if constexpr (std::is_base_of<Residual, decltype(e)>::value) {
+      e.gate = a.gate;
+      e.residual = a.residual;
+      e.ldr = a.ld_residual;
+    }
     return block_gemm<true>(a.x, a.ld_x, a.w, a.ld_w, a.M, a.N, a.K, e, s);
   };
   if (a.gate) return run(EpiLinear<false, false, true>{});

@@ -95,6 +95,20 @@ struct IdxList {
 };
 Status make_idx(const int32_t* idx, int32_t n, IdxList& out);
 
+// The same as a set, for kernels of a few microseconds whose samples are independent: a launch with more
+// than 112 bytes of arguments takes the host longer (264: 3.2 us, up to 112: 2.6).
+struct SampleSet {
+  uint64_t bits = 0;
+  explicit SampleSet(const IdxList& l) {
+    for (int i = 0; i < l.n; ++i) bits |= uint64_t(1) << l.v[i];
+  }
+  __device__ int operator[](int i) const {        // the i-th of them
+    uint64_t m = bits;
+    for (; i > 0; --i) m &= m - 1;
+    return __builtin_ctzll(m);
+  }
+};
+
 // Workspace layout (offsets in bytes, each 256-aligned).
 struct Workspace {
   size_t a, qk, vt, o, ff, drift_part, attn_part, attn_part_bytes, tm_e, tm_h, tm_c, tm_s, tm_m, total;

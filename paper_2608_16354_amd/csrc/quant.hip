@@ -269,10 +269,10 @@ template <int BITS>
 __global__ void __launch_bounds__(256) k_cache_store_q(const float* __restrict__ h_out,
                                                        const float* __restrict__ h_in,
                                                        typename Codes<BITS>::T* __restrict__ codes,
-                                                       float* __restrict__ scales, IdxList idx, size_t n4,
+                                                       float* __restrict__ scales, SampleSet idx, size_t n4,
                                                        size_t stride_h4) {
   typedef Codes<BITS> C;
-  const int b = idx.v[blockIdx.y];
+  const int b = idx[blockIdx.y];
   const size_t i = size_t(blockIdx.x) * 256 + threadIdx.x, base = size_t(b) * n4;
   if (i >= n4) return;
   const float4 a = load_nt(reinterpret_cast<const float4*>(h_out) + size_t(b) * stride_h4 + i);
@@ -289,8 +289,8 @@ template <int BITS>
 __global__ void __launch_bounds__(256) k_cache_apply_q(const float* h_in,
                                                        const typename Codes<BITS>::T* __restrict__ codes,
                                                        const float* __restrict__ scales, float* g,
-                                                       IdxList idx, size_t n4, size_t stride_h4) {
-  const int b = idx.v[blockIdx.y];
+                                                       SampleSet idx, size_t n4, size_t stride_h4) {
+  const int b = idx[blockIdx.y];
   const size_t i = size_t(blockIdx.x) * 256 + threadIdx.x, base = size_t(b) * n4;
   if (i >= n4) return;
   const float4 a = load_nt(reinterpret_cast<const float4*>(h_in) + size_t(b) * stride_h4 + i);
@@ -362,10 +362,10 @@ Status cache_store_q(const float* h_out, const float* h_in, int bits, void* code
   const dim3 grid(unsigned((n4 + 255) / 256), idx.n);
   if (bits == 8)
     hipLaunchKernelGGL(k_cache_store_q<8>, grid, dim3(256), 0, s, h_out, h_in, static_cast<uint32_t*>(codes), scales,
-                       idx, n4, sh4);
+                       SampleSet(idx), n4, sh4);
   else
     hipLaunchKernelGGL(k_cache_store_q<4>, grid, dim3(256), 0, s, h_out, h_in, static_cast<uint16_t*>(codes), scales,
-                       idx, n4, sh4);
+                       SampleSet(idx), n4, sh4);
   DC_HIP(hipGetLastError());
   return Status::ok();
 }
@@ -378,10 +378,10 @@ Status cache_apply_q(const float* h_in, int bits, const void* codes, const float
   const dim3 grid(unsigned((n4 + 255) / 256), idx.n);
   if (bits == 8)
     hipLaunchKernelGGL(k_cache_apply_q<8>, grid, dim3(256), 0, s, h_in, static_cast<const uint32_t*>(codes), scales,
-                       gout, idx, n4, sh4);
+                       gout, SampleSet(idx), n4, sh4);
   else
     hipLaunchKernelGGL(k_cache_apply_q<4>, grid, dim3(256), 0, s, h_in, static_cast<const uint16_t*>(codes), scales,
-                       gout, idx, n4, sh4);
+                       gout, SampleSet(idx), n4, sh4);
   DC_HIP(hipGetLastError());
   return Status::ok();
 }

@@ -12,18 +12,23 @@ namespace dc {
 namespace {
 
 constexpr int kWave = 64;
-constexpr int kMaxPairs = 36;          // head_dim 72
 
 // ---------------------------------------------------------------------------
 // cos and sin of every video token and pair of features.  The angles are formed and reduced in double
 // (a frame index of 1e5 leaves an fp32 angle with errors of 1e-2), rounded to fp32 at the end.
 // ---------------------------------------------------------------------------
-struct Axes {
+struct Axes {                          // with the kernel's other arguments 104 bytes (SampleSet says why so few)
   double start[3], step[3];
-  double freq[kMaxPairs];              // of each pair; 0 behind the last axis
-  int end[3];                          // first pair behind each axis
-  double per_wp, per_hp;               // 1 / Wp, 1 / Hp
+  double rate[3];                      // pair j of axis a turns by exp(j rate[a]) per unit of position
+  int end;                             // first pair behind each axis, a byte each
+  int Hp, Wp, Nv;
 };
+
+// 1 / x to about 2^-45
+__device__ inline double reciprocal(double x) {
+  const double r = __builtin_amdgcn_rcp(x);
+  return fma(fma(-x, r, 1.0), r, r);
+}
 
 // cos and sin to about 1e-11: x = k pi / 2 + r with pi / 2 in two parts, |r| <= pi / 4, then the Taylor series up
 // to r^11 and r^12 (the next terms are 7e-12 and 4e-13).  About 25 operations in double; the library's sincos, to the
@@ -47,23 +52,31 @@ __device__ inline float2 cos_sin(double x) {
   return make_float2(n == 1 || n == 2 ? -fc : fc, n & 2 ? -fs : fs);
 }
 
+// One pair of two tokens half the table apart to a thread, which share its frequency.
 template <int P>
-__global__ void __launch_bounds__(256) k_rope_table(Axes ax, const double* __restrict__ pos, int Hp, int Wp,
-                                                    int entries, float2* __restrict__ table) {
-  const int e = blockIdx.x * 256 + threadIdx.x;
-  if (e >= entries) return;
-  const int n = e / P, p = e - n * P;
-  const int a = p < ax.end[0] ? 0 : p < ax.end[1] ? 1 : 2;
-  double at;
-  if (pos) {
-    at = pos[size_t(n) * 3 + a];
-  } else {
-    // quotients below 2^31 by a product: half a step inside, so its rounding does not matter
-    const int r = int((double(n) + 0.5) * ax.per_wp), t = int((double(r) + 0.5) * ax.per_hp);
-    at = a == 0 ? fma(ax.step[0], double(t), ax.start[0])
-                : a == 1 ? fma(ax.step[1], double(r - t * Hp), ax.start[1]) : fma(ax.step[2], double(n - r * Wp), ax.start[2]);
+__global__ void __launch_bounds__(256) k_rope_table(Axes ax, const double* __restrict__ pos, float2* __restrict__ table) {
+  const int e = blockIdx.x * 256 + threadIdx.x, half = (ax.Nv + 1) / 2;
+  const int first = e / P, p = e - first * P;
+  if (first >= half) return;
+  const int end0 = ax.end & 255, end1 = (ax.end >> 8) & 255, end2 = ax.end >> 16;
+  const int a = p < end0 ? 0 : p < end1 ? 1 : 2;
+  const double freq = exp((p - (a == 0 ? 0 : a == 1 ? end0 : end1)) * (a == 0 ? ax.rate[0] : a == 1 ? ax.rate[1] : ax.rate[2]));
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int n = first + u * half;
+    if (n >= ax.Nv) return;
+    double at;
+    if (pos) {
+      at = pos[size_t(n) * 3 + a];
+    } else {
+      // quotients below 2^31 by a product: half a step inside, so its rounding does not matter
+      const int r = int((double(n) + 0.5) * reciprocal(ax.Wp)), t = int((double(r) + 0.5) * reciprocal(ax.Hp));
+      at = a == 0 ? fma(ax.step[0], double(t), ax.start[0])
+                  : a == 1 ? fma(ax.step[1], double(r - t * ax.Hp), ax.start[1])
+                           : fma(ax.step[2], double(n - r * ax.Wp), ax.start[2]);
+    }
+    table[size_t(n) * P + p] = p < end2 ? cos_sin(at * freq) : make_float2(1.f, 0.f);
   }
-  table[e] = p < ax.end[2] ? cos_sin(at * ax.freq[p]) : make_float2(1.f, 0.f);
 }
 
 // ---------------------------------------------------------------------------
@@ -185,7 +198,7 @@ struct QkArgs {
 };
 
 template <bool BF, int DH, bool IL, bool NT>
-__global__ void __launch_bounds__(256) k_qk_norm_rope(QkArgs a, IdxList idx) {
+__global__ void __launch_bounds__(256) k_qk_norm_rope(QkArgs a, SampleSet idx) {
   typedef Lane<BF> Ln;
   typedef typename Ln::T T;
   constexpr int VE = Ln::VE, HV = VE / 2, G = DH / VE, HW = kWave / G, U = kSteps<G>;
@@ -193,7 +206,7 @@ __global__ void __launch_bounds__(256) k_qk_norm_rope(QkArgs a, IdxList idx) {
   const int lane = threadIdx.x & 63;
   const int n = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (n >= a.N) return;
-  const size_t row = size_t(idx.v[blockIdx.z]) * a.N + n;
+  const size_t row = size_t(idx[blockIdx.z]) * a.N + n;
   const T* const in = static_cast<const T*>(a.in) + row * a.ld_in;
   T* const out = static_cast<T*>(a.out) + row * a.ld_out;
   const int slot = min(lane / G, HW - 1), h = lane - slot * G;   // lanes past the last head: h >= G
@@ -271,25 +284,22 @@ __global__ void __launch_bounds__(256) k_qk_norm_rope(QkArgs a, IdxList idx) {
 Status rope_table(const dc_rope_axes& ax, const double* pos, float* table, const Geo& g, hipStream_t s) {
   const int P = g.Dh / 2;              // 32 or 36 (make_geo)
   if (int64_t(g.Nv) * P > INT32_MAX / 2) return Status::shape("rotary table: too many entries");
-  const int entries = g.Nv * P;
-  if (entries == 0) return Status::ok();
+  if (g.Nv == 0) return Status::ok();
   Axes a{};
-  int p = 0;
+  int end = 0;
   for (int i = 0; i < 3; ++i) {
     a.start[i] = ax.start[i];
     a.step[i] = ax.step[i];
-    const double log_theta = std::log(ax.theta);
-    for (int j = 0; j < ax.dim[i] / 2; ++j) a.freq[p++] = std::exp(-double(2 * j) / double(ax.dim[i]) * log_theta);
-    a.end[i] = p;
+    a.rate[i] = ax.dim[i] ? -2.0 * std::log(ax.theta) / double(ax.dim[i]) : 0.0;
+    end += ax.dim[i] / 2;
+    a.end |= end << (8 * i);
   }
-  a.per_wp = 1.0 / g.Wp;
-  a.per_hp = 1.0 / g.Hp;
-  if (P == 32)
-    hipLaunchKernelGGL(k_rope_table<32>, dim3((entries + 255) / 256), dim3(256), 0, s, a, pos, g.Hp, g.Wp, entries,
-                       reinterpret_cast<float2*>(table));
-  else
-    hipLaunchKernelGGL(k_rope_table<36>, dim3((entries + 255) / 256), dim3(256), 0, s, a, pos, g.Hp, g.Wp, entries,
-                       reinterpret_cast<float2*>(table));
+  a.Hp = g.Hp;
+  a.Wp = g.Wp;
+  a.Nv = g.Nv;
+  const dim3 grid((int64_t(g.Nv + 1) / 2 * P + 255) / 256);
+  if (P == 32) hipLaunchKernelGGL(k_rope_table<32>, grid, dim3(256), 0, s, a, pos, reinterpret_cast<float2*>(table));
+  else hipLaunchKernelGGL(k_rope_table<36>, grid, dim3(256), 0, s, a, pos, reinterpret_cast<float2*>(table));
   DC_HIP(hipGetLastError());
   return Status::ok();
 }
@@ -307,7 +317,7 @@ Status qk_norm_rope(const dc_qk_cfg& c, const void* in, int64_t ld_in, void* out
     const int steps = (2 * g.H + heads_wave - 1) / heads_wave, trips = (steps + u - 1) / u;
     const int64_t rows = int64_t(g.N) * idx.n, most = std::max<int64_t>(2048 / rows, trips * rows <= 4096 ? trips : 1);
     const int split = int(std::min<int64_t>(steps, most));
-    hipLaunchKernelGGL(stream ? streaming : plain, dim3((g.N + 3) / 4, split, idx.n), dim3(256), 0, s, a, idx);
+    hipLaunchKernelGGL(stream ? streaming : plain, dim3((g.N + 3) / 4, split, idx.n), dim3(256), 0, s, a, SampleSet(idx));
   };
   auto dtype = [&](auto bf, auto dh, int heads_wave, int u) {
     constexpr bool BF = decltype(bf)::value;

@@ -335,6 +335,16 @@ def test_api_refuses_host_tensors():
         api.dc_quantize_rows(torch.zeros(4, 100), torch.zeros(4, 128, dtype=torch.int8), torch.zeros(4))
 
 
+def test_rope_axes_are_the_struct():
+    from paper_2608_16354_amd import api
+    got = api.rope_axes((16, 24, 20), 100, start=np.array([1, 2.5, -3]), step=[0.5, 4, 5])
+    want = axes((16, 24, 20), 100.0, (1.0, 2.5, -3.0), (0.5, 4.0, 5.0))
+    assert bytes(got) == bytes(want)
+    for bad in (dict(dim=(16, 24)), dict(dim=(16, 24, 24.5)), dict(dim=(1, 2, 3), start=(0, 0)), dict(dim=(1, 2, 3), theta="x")):
+        with pytest.raises(ValueError, match="three numbers"):
+            api.rope_axes(**bad)
+
+
 def test_extensions_belong_to_a_shape_and_a_device():
     """An extension holds tensors of its model's sizes: another model, or a tensor elsewhere, is refused."""
     import types
