@@ -295,6 +295,16 @@ __device__ inline void gemm_epilogue(Acc (&acc)[TM][TN], uint4* lds, int m0, int
   }
 }
 
+// N float4 of LDS for a swapped epilogue's vectors
+template <int N>
+__device__ inline float4* tile_vec() {
+  if constexpr (N > 0) {
+    __shared__ float4 v[N];
+    return v;
+  }
+  return nullptr;
+}
+
 template <class Ops, int BM, int BN, int WM, int WN, int DS, int ST, class Epi>
 __global__ void __launch_bounds__(WM * WN * 64) k_gemm_dma(const char* __restrict__ A, int lda,
                                                   const char* __restrict__ W, int ldw, int M,
@@ -309,7 +319,7 @@ __global__ void __launch_bounds__(WM * WN * 64) k_gemm_dma(const char* __restric
   // one array, so every stage address is a constant offset from one base
   constexpr int STAGE = (BM + BN) * 8;
   __shared__ uint4 lds[ST * STAGE];
-  __shared__ float4 s_vec[Ops::kSwapped ? (BM + 2 * BN) / 4 : 1];
+  float4* const s_vec = tile_vec<Ops::kSwapped ? (BM + 2 * BN) / 4 : 0>();
 
   const int t = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
   if (t >= tiles) return;
@@ -434,7 +444,7 @@ __global__ void __launch_bounds__(512) k_gemm_pipe(const char* __restrict__ A, i
   static_assert(AI + BI == 4, "one DMA instruction per k-slice");
   constexpr int STAGE = (BM + BN) * 8;
   __shared__ uint4 lds[ST * STAGE];
-  __shared__ float4 s_vec[Ops::kSwapped ? (BM + 2 * BN) / 4 : 1];
+  float4* const s_vec = tile_vec<Ops::kSwapped ? (BM + 2 * BN) / 4 : 0>();
   const int t = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
   if (t >= tiles) return;
   const int tiles_m = (M + BM - 1) / BM;
