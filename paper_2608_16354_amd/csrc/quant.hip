@@ -151,30 +151,63 @@ __global__ void __launch_bounds__(256) k_quantize_rows(const void* __restrict__ 
   if (at == 0) scale[row] = s;
 }
 
-// Rows of fewer values than a piece, or too long to stay in registers: one workgroup to a row, which
-// is read twice.
+// Rows too long to stay in registers: one workgroup to a row, four pieces a thread on their way at once, and
+// read a second time for the codes: bf16 rows of 130,944, one 12.6 us (one value a thread at a time: 142), 1,000 of them
+// 112 us.  Grids of 512 threads a row stay below 2^32 threads for every row count that memory holds.
 template <bool BF>
-__global__ void __launch_bounds__(256) k_quantize_any(const void* __restrict__ x, int64_t ldx, int cols,
-                                                      int8_t* __restrict__ q, int64_t ldq,
-                                                      float* __restrict__ scale) {
-  __shared__ uint32_t s_max[4];
-  const int row = blockIdx.x, tid = threadIdx.x;
+__global__ void __launch_bounds__(512) k_quantize_long(const void* __restrict__ x, int64_t ldx, int cols,
+                                                       int8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale) {
+  constexpr int VE = Piece<BF>::VE, U = 4;
+  __shared__ uint32_t s_max[8];
+  const int row = blockIdx.x, tid = threadIdx.x, np = (cols + VE - 1) / VE;
+  const char* const xr = static_cast<const char*>(x) + size_t(row) * ldx * (BF ? 2 : 4);
+  Piece<BF> p[U];
+  auto fetch = [&](int i0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) p[u].template load<false>(xr, min(min(i0 + u * 512, np - 1) * VE, cols - VE));
+  };
+  uint32_t m = 0;
+  for (int i0 = tid; i0 < np; i0 += U * 512) {
+    fetch(i0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) m = max(m, p[u].largest());
+  }
+  m = wave_max(m);
+  if ((tid & 63) == 0) s_max[tid >> 6] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 8; ++w) m = max(m, s_max[w]);
+  const float s = scale_of(m, 127.f);
+  const Coder k(s, 127.f);
+  int8_t* const qr = q + size_t(row) * ldq;
+  for (int i0 = tid; i0 < np; i0 += U * 512) {
+    fetch(i0);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i0 + u * 512 < np) p[u].store(qr + min((i0 + u * 512) * VE, cols - VE), k);
+  }
+  zero_tail(qr, cols, tid, 512);
+  if (tid == 0) scale[row] = s;
+}
+
+// Rows of fewer values than a piece, a thread to each.
+template <bool BF>
+__global__ void __launch_bounds__(256) k_quantize_short(const void* __restrict__ x, int64_t ldx, int rows, int cols,
+                                                        int8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale) {
+  const int row = blockIdx.x * 256 + threadIdx.x;
+  if (row >= rows) return;
   auto value = [&](int c) -> float {
     if constexpr (BF) return from_bf16(static_cast<const uint16_t*>(x)[size_t(row) * ldx + c]);
     else return static_cast<const float*>(x)[size_t(row) * ldx + c];
   };
   uint32_t m = 0;
-  for (int c = tid; c < cols; c += 256) m = max(m, mag(value(c)));
-  m = wave_max(m);
-  if ((tid & 63) == 0) s_max[tid >> 6] = m;
-  __syncthreads();
-  m = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
+  for (int c = 0; c < cols; ++c) m = max(m, mag(value(c)));
   const float s = scale_of(m, 127.f);
   const Coder k(s, 127.f);
   int8_t* const qr = q + size_t(row) * ldq;
-  for (int c = tid; c < cols; c += 256) qr[c] = int8_t(k.direct ? k.fast(value(c)) : k.slow(value(c)));
-  zero_tail(qr, cols, tid, 256);
-  if (tid == 0) scale[row] = s;
+  for (int c = 0; c < cols; ++c) qr[c] = int8_t(k.direct ? k.fast(value(c)) : k.slow(value(c)));
+  zero_tail(qr, cols, 0, 1);
+  scale[row] = s;
 }
 
 __device__ inline float wave_sum(float v) {
@@ -304,8 +337,13 @@ template <bool BF>
 Status quantize(const void* x, int64_t ldx, int rows, int cols, int8_t* q, int64_t ldq, float* scale, hipStream_t s) {
   constexpr int VE = Piece<BF>::VE;
   const int np = (cols + VE - 1) / VE;
-  if (cols < VE || np > 8 * 256) {
-    hipLaunchKernelGGL(k_quantize_any<BF>, dim3(rows), dim3(256), 0, s, x, ldx, cols, q, ldq, scale);
+  if (cols < VE) {
+    hipLaunchKernelGGL(k_quantize_short<BF>, dim3((rows + 255) / 256), dim3(256), 0, s, x, ldx, rows, cols, q, ldq, scale);
+    DC_HIP(hipGetLastError());
+    return Status::ok();
+  }
+  if (np > 8 * 256) {
+    hipLaunchKernelGGL(k_quantize_long<BF>, dim3(rows), dim3(512), 0, s, x, ldx, cols, q, ldq, scale);
     DC_HIP(hipGetLastError());
     return Status::ok();
   }

@@ -146,7 +146,7 @@ def test_qk_text_rows_keep_what_a_pair_would_spread(api, dev):
 # int8 rows
 # ----------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("cols", [1, 3, 7, 8, 9, 64, 127, 128, 129, 513, 1000, 1920, 2049, 4097, 7680, 8192, 8193, 16391])
+@pytest.mark.parametrize("cols", [1, 3, 7, 8, 9, 64, 127, 128, 129, 513, 1000, 1920, 2049, 4097, 7680, 8192, 8193, 16391, 70001])
 def test_quantize_rows(api, dev, dtype, cols):
     import torch
     dt = torch.bfloat16 if dtype == "bf16" else torch.float32
@@ -181,7 +181,8 @@ def test_quantize_rows(api, dev, dtype, cols):
 
 @pytest.mark.parametrize("dtype,rows,cols", [("f32", 1, 1920), ("bf16", 1, 7680), ("bf16", 4099, 1152), ("f32", 1025, 333),
                                              ("bf16", 4099, 1920), ("f32", 4099, 1000), ("bf16", 1000, 7687), ("f32", 3301, 1501),
-                                             ("bf16", 12301, 500), ("f32", 9001, 130)])
+                                             ("bf16", 12301, 500), ("f32", 9001, 130), ("bf16", 7, 130943), ("f32", 100003, 3),
+                                             ("bf16", 100003, 5)])
 def test_quantize_many_rows(api, dev, dtype, rows, cols):
     import torch
     dt = torch.bfloat16 if dtype == "bf16" else torch.float32
@@ -561,3 +562,29 @@ def test_long_table(api, dev):
     pos = np.array([[n >> 20, (n >> 10) & 1023, n & 1023] for n in at], np.float64)
     want = X.rope_table(pos, (16, 24, 24), 100.0, 32)
     assert np.abs(host(table[at]) - want).max() <= F32 + 1e-10
+
+
+def test_every_sample_of_the_largest_batch(api, dev):
+    """64 samples, 49 of them asked for in no order: those get what they get alone, the others stay."""
+    import torch
+    m = shape(2, 64, (1, 4, 6), 3)
+    d, N, n_v, cfg = m.hidden, m.n_tok, m.n_v, api.model_cfg(m)
+    gen = torch.Generator(dev).manual_seed(8)
+    idx = [b for b in np.random.default_rng(9).permutation(64).tolist() if b % 4 or b == 0]
+    rest = [b for b in range(64) if b not in idx]
+    a, b = (torch.randn((64, N, d), device=dev, generator=gen) for _ in range(2))
+    k, s = torch.full((64, n_v, d), 99, device=dev, dtype=torch.int8), torch.full((64, n_v, d // 64), 99.0, device=dev)
+    g = torch.full((64, N, d), 99.0, device=dev)
+    api.dc_cache_store_q(cfg, 8, a, b, k, s, idx)
+    api.dc_cache_apply_q(cfg, 8, b, k, s, g, idx)
+    x = torch.randn((64, N, 2 * d), device=dev, generator=gen).bfloat16()
+    y = torch.full_like(x, 99.0)
+    table = torch.randn((n_v, 32, 2), device=dev, generator=gen)
+    api.dc_qk_norm_rope(cfg, x, y, idx, table=table)
+    assert (k[rest] == 99).all() and (s[rest] == 99).all() and (g[rest] == 99).all() and (y[rest] == 99).all()
+    for i in idx:
+        k1, s1, g1, y1 = torch.zeros_like(k[:1]), torch.zeros_like(s[:1]), torch.full_like(g[:1], 99.0), torch.zeros_like(y[:1])
+        api.dc_cache_store_q(cfg, 8, a[i: i + 1], b[i: i + 1], k1, s1, [0])
+        api.dc_cache_apply_q(cfg, 8, b[i: i + 1], k1, s1, g1, [0])
+        api.dc_qk_norm_rope(cfg, x[i: i + 1], y1, [0], table=table)
+        assert torch.equal(k[i], k1[0]) and torch.equal(s[i], s1[0]) and torch.equal(g[i], g1[0]) and torch.equal(y[i], y1[0])
