@@ -324,11 +324,11 @@ class BlockExt:
 
 
 def dc_block_forward_ext(dm: DeviceModel, l: int, ext: BlockExt, mod, h, idx, ws: Workspace, stream=None):
-    """dc_block_forward with block l's extensions; ws: Workspace(..., ext=True)."""
-    ext.of(dm)
+    """dc_block_forward with block l's extensions (None: none); ws: Workspace(..., ext=True)."""
+    e = None if ext is None else ext.of(dm).block(l)
     arr, p, n = _idx(idx)
     L.check("dc_block_forward_ext", L.load().dc_block_forward_ext(
-        C.byref(dm.cfg), dm.block(l), ext.block(l), _ptr(mod), _ptr(h), p, n, ws.ptr, ws.nbytes, _stream(stream)))
+        C.byref(dm.cfg), dm.block(l), e, _ptr(mod), _ptr(h), p, n, ws.ptr, ws.nbytes, _stream(stream)))
 
 
 class _CProblem:

@@ -104,6 +104,9 @@ def test_block_without_extensions_is_the_block(api, dev):
     api.dc_block_forward(dm, 0, mod, a, [0], api.Workspace(m, 1, dev))
     api.dc_block_forward_ext(dm, 0, api.BlockExt(dm), mod, b, [0], api.Workspace(m, 1, dev))
     assert torch.equal(a, b)
+    b.copy_(h)
+    api.dc_block_forward_ext(dm, 0, None, mod, b, [0], api.Workspace(m, 1, dev))
+    assert torch.equal(a, b)
 
 
 def _legal(K, h_max, b):
