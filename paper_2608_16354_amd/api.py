@@ -265,9 +265,8 @@ def dc_cache_apply_q(cfg, bits, h_in, codes, scales, g, idx, stream=None):
     _call("dc_cache_apply_q", stream, h_in, cfg, bits, h_in, g, codes, scales, idx)
 
 
-def _tokens(cfg):
-    n_v = cfg.lat_t * (cfg.lat_h // cfg.patch) * (cfg.lat_w // cfg.patch)
-    return n_v, n_v + cfg.n_txt
+def _video_tokens(cfg):
+    return cfg.lat_t * (cfg.lat_h // cfg.patch) * (cfg.lat_w // cfg.patch)
 
 
 def _floats(t, shape, device, what):
@@ -297,7 +296,7 @@ class BlockExt:
                 dh, dev = (dm.cfg.head_dim,), b["b_qkv"].device
                 qk = L.QkCfg(_floats(None if q_weight is None else q_weight[l], dh, dev, "q_weight"),
                              _floats(None if k_weight is None else k_weight[l], dh, dev, "k_weight"), eps,
-                             _floats(table, (_tokens(dm.cfg)[0], dh[0] // 2, 2), dev, "table"), 1 if interleaved else 0)
+                             _floats(table, (_video_tokens(dm.cfg), dh[0] // 2, 2), dev, "table"), 1 if interleaved else 0)
                 self.keep.append(qk)
                 self.c[l].qk = C.pointer(qk)
             if int8:

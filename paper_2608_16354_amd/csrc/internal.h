@@ -272,8 +272,7 @@ int i8_tile(int M, int N, int ksteps, int cus, bool split);
 Status gemm_i8_qkv(const int8_t* A, const float* sx, const int8_t* W, const float* sw, const float* bias,
                    uint16_t* qk, uint16_t* vt, int ldv, float q_scale, const Geo& g, int M, hipStream_t s);
 
-// The residual cache in 8 or 4 bits (quant.hip).
-constexpr int kCacheGroup = 64;
+// The residual cache in 8 or 4 bits, a scale to 64 features (quant.hip).
 Status cache_store_q(const float* h_out, const float* h_in, int bits, void* codes, float* scales, const IdxList& idx,
                      const Geo& g, hipStream_t s);
 Status cache_apply_q(const float* h_in, int bits, const void* codes, const float* scales, float* gout,
