@@ -434,13 +434,17 @@ Status launch_split(const int8_t* A, int lda, const int8_t* W, int ldw, int M, i
 // plus k-steps (of 128; groups share them).  One workgroup per compute unit: a k-step takes step[0] on a nearly empty
 // chip to step[1] on a full one; more: step[n - 1] with n of them.  Fitted to timings on MI355X of 228 shapes (M 1 to
 // 17,776; N x K from 256 x 1,024 to 11,520 x 1,920 and 1,920 x 7,680; the splits 132 of them, M up to 800): the tile it
-// picks is 0.3 % slower than the best on average, 10 % at worst.  Few rows take the splits: 1 x 1,920 x 7,680 6.8 us
+// picks is 0.3 % slower than the best on average, 10 % at worst.  192 x 128 and 128 x 64 (fitted to 100 shapes, M 300 to
+// 11,000) fill rounds that the others leave half empty: 3,704 x 1,152 x 1,152 9.4 us (11.4 without them), x K = 4,608 26.2
+// (29.2), 800 x 1,920 x 7,680 22.1 (26.5), 1.8 % over the 100; 192 x 256, 128 x 192, 128 x 256 and 320 x 128 add 0.7 %
+// at most.  Few rows take the splits: 1 x 1,920 x 7,680 6.8 us
 // (64 x 64 18.4), 50 x 1,920 x 1,920 4.5 (7.1), 32 x 11,520 x 1,920 6.0 (7.4); 50 x 11,520 x 1,920 stays with 64 x 64,
 // 7.5 (8.7).  Four groups fit a compute unit twice, five once, which is better for sums of many k-steps.
 struct TileCost { int bm, bn, groups, per_cu; float step[3], fixed, launch; };
 constexpr TileCost kTiles[] = {{384, 192, 1, 1, {1.124f, 1.867f}, 7.08f, 0.f},   {320, 256, 1, 1, {1.268f, 1.997f}, 6.85f, 0.f},
                                {256, 192, 1, 1, {0.783f, 1.267f}, 5.77f, 0.f},   {256, 128, 1, 1, {0.604f, 0.927f}, 3.79f, 1.33f},
                                {128, 128, 1, 1, {0.294f, 0.494f}, 2.91f, 1.31f}, {64, 64, 1, 3, {0.248f, 0.372f, 0.567f}, 1.29f, 2.13f},
+                               {192, 128, 1, 1, {0.501f, 0.721f}, 2.53f, 1.71f}, {128, 64, 1, 1, {0.247f, 0.324f}, 1.62f, 2.08f},
                                {32, 32, 4, 2, {0.341f, 0.662f}, 0.81f, 2.48f},   {32, 32, 5, 1, {0.245f, 0.525f}, 1.09f, 2.21f}};
 
 }  // namespace
@@ -448,7 +452,7 @@ constexpr TileCost kTiles[] = {{384, 192, 1, 1, {1.124f, 1.867f}, 7.08f, 0.f},  
 int i8_tile(int M, int N, int ksteps, int cus, bool split) {
   int best = 0;
   float least = 0.f;
-  for (int i = 0; i < (split ? 8 : 6); ++i) {
+  for (int i = 0; i < (split ? 10 : 8); ++i) {
     const TileCost& c = kTiles[i];
     const float steps = float((ksteps + c.groups - 1) / c.groups);
     const int64_t tiles = int64_t((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn);
@@ -485,7 +489,9 @@ Status block_gemm(const int8_t* A, int64_t lda, const int8_t* W, int64_t ldw, in
     case 3: return launch_dma<OpsI8, 256, 128, 4, 2, 2, 3>(A, la, W, lw, M, N, kt, epi, s);
     case 4: return launch_pipe<OpsI8>(A, la, W, lw, M, N, kt, epi, s);
     case 5: return launch_dma<OpsI8, 64, 64, 2, 2, 2, 3>(A, la, W, lw, M, N, kt, epi, s);
-    case 6: if constexpr (SPLIT) return launch_split<4>(A, la, W, lw, M, N, kt, epi, s); break;
+    case 6: return launch_dma<OpsI8, 192, 128, 2, 4, 2, 3>(A, la, W, lw, M, N, kt, epi, s);
+    case 7: return launch_dma<OpsI8, 128, 64, 4, 2, 2, 4>(A, la, W, lw, M, N, kt, epi, s);
+    case 8: if constexpr (SPLIT) return launch_split<4>(A, la, W, lw, M, N, kt, epi, s); break;
     default: if constexpr (SPLIT) return launch_split<5>(A, la, W, lw, M, N, kt, epi, s); break;
   }
   return Status::shape("int8 product: no such tile");

@@ -267,7 +267,7 @@ struct LinearI8 {
   void* out; int64_t ld_out; bool out_bf16;
 };
 Status gemm_i8_linear(const LinearI8& a, hipStream_t s);
-// which of its eight tiles a product takes (gemm_i8.hip, kTiles); split: gemm_i8_linear's, the QKV product has six
+// which of its ten tiles a product takes (gemm_i8.hip, kTiles); split: gemm_i8_linear's, the QKV product has eight
 int i8_tile(int M, int N, int ksteps, int cus, bool split);
 Status gemm_i8_qkv(const int8_t* A, const float* sx, const int8_t* W, const float* sw, const float* bias,
                    uint16_t* qk, uint16_t* vt, int ldv, float q_scale, const Geo& g, int M, hipStream_t s);

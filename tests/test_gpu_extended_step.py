@@ -8,7 +8,7 @@ import pytest
 from oracle import dit
 from oracle import ext as X
 from paper_2608_16354_amd import inputs as I
-from tests.gpu_util import mod_input, rel_l2, say, t
+from tests.gpu_util import _native, compute_units, mod_input, rel_l2, say, t
 from tests.test_gpu_kernels import _OneBlock
 
 pytestmark = pytest.mark.gpu
@@ -240,3 +240,54 @@ def test_two_captured_blocks_share_a_workspace(api, dev):
             api.dc_block_forward_ext(dm, l, ext, mod, e, [0], ws_e)
         torch.cuda.synchronize()
         assert torch.isfinite(e).all() and torch.equal(h, e), order
+
+
+QKV_TILES = {       # the int8 QKV product's tile on 256 compute units: the model that takes it
+    "64x64": _shape(256, 4, 64, 128, (3, 10, 12), 21, "bf16"), "128x64": _shape(1152, 18, 64, 128, (1, 38, 40), 1, "bf16"),
+    "128x128": _shape(1152, 18, 64, 128, (1, 34, 68), 1, "bf16"), "192x128": _shape(768, 12, 64, 128, (4, 28, 64), 5, "bf16"),
+    "256x128": _shape(1152, 16, 72, 128, (4, 28, 64), 5, "bf16"), "256x192": _shape(1536, 24, 64, 128, (4, 28, 64), 5, "bf16"),
+    "384x192": _shape(1536, 24, 64, 128, (3, 68, 58), 77, "bf16"),
+}
+
+
+@pytest.mark.parametrize("tile", list(QKV_TILES))
+def test_int8_qkv_rows(api, dev, tile):
+    """Q, K and V transposed as the block leaves them in its workspace, against the product of the codes.  The LN's fp32
+    roundings move a code over a border about once in 10^4: six such codes of a row, each of at most 127 of a weight's
+    steps, the two scales' roundings, and bf16's half step."""
+    import torch
+    from tests.test_gpu_operators import I8_TILES
+    m = QKV_TILES[tile]
+    N, d, ldv = m.n_tok, m.hidden, -(-m.n_tok // 64) * 64
+    assert I8_TILES[_native("_ZN2dc7i8_tileEiiiib", N, 3 * d, d // 128, compute_units(dev), False)] == tile
+    W = I.Weights(m, 180)
+    dm = api.DeviceModel(_OneBlock(W, 0), dev)
+    ext, ws = api.BlockExt(dm, int8=True), api.Workspace(m, 1, dev, ext=True)
+    ws.buf.fill_(0xFF)                                       # NaN wherever nothing is written
+    h, mod = I.hidden_state(m, (71,)), mod_input(m, (73,))
+    say("int8 QKV", tile, N, d)
+    api.dc_block_forward_ext(dm, 0, ext, t(mod, dev), t(h[None], dev), [0], ws)
+    torch.cuda.synchronize()
+    at = ws.ptr.value - ws.buf.data_ptr() + -(-2 * N * d // 256) * 256
+
+    def held(rows, cols):
+        nonlocal at
+        v = ws.buf[at: at + 2 * rows * cols].view(torch.bfloat16).view(rows, cols).float().cpu().numpy()
+        at += -(-2 * rows * cols // 256) * 256
+        return v
+
+    qk, vt = held(ldv + 64, 2 * d)[:N], held(d, ldv)
+    x8, xs = X.codes(dit.modulate(h.astype(np.float64), mod[0].astype(np.float64), mod[1].astype(np.float64), m.ln_eps), 127)
+    w8, wsc = X.codes(dm.blocks[0]["w_qkv"].float().cpu().numpy(), 127)
+    step = xs[:, None].astype(np.float64) * wsc.astype(np.float64)
+    want = (x8.astype(np.float64) @ w8.astype(np.float64).T) * step + dm.blocks[0]["b_qkv"].cpu().numpy()
+    tol = 6 * 127 * step
+    q_scale = 1.4426950408889634 / np.sqrt(m.head_dim)
+    want[:, :d] *= q_scale
+    tol[:, :d] *= q_scale
+    tol += (2.0 ** -8 + 1e-5) * (np.abs(want) + tol)
+    got = np.concatenate([qk, vt[:, :N].T], 1)
+    err = np.abs(got - want)
+    say(tile, "largest share of the tolerance", (err / tol).max())
+    assert np.isfinite(got).all() and (err <= tol).all(), np.argwhere(err > tol)[:4]
+    assert not vt[:, N:].any()

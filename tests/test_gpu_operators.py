@@ -234,10 +234,11 @@ def check_linear(got, x, xs, w, ws, bias, gate, residual, kind, bf16):
 
 TILE_SHAPES = {     # (M, N, K): the tile on 256 compute units
     (2562, 5760, 1920): "384x192", (1155, 11520, 1920): "320x256", (1155, 7680, 3840): "256x192",
-    (1537, 3456, 2304): "256x128", (1155, 1920, 3840): "128x128", (513, 1920, 256): "64x64",
+    (1144, 5760, 1920): "256x128", (1155, 1920, 3840): "128x128", (513, 1920, 256): "64x64", (1537, 3456, 2304): "192x128",
+    (801, 1920, 7680): "128x64",
     (67, 1153, 1408): "32x32 x 4", (33, 1153, 7680): "32x32 x 5",
 }
-I8_TILES = TILES + ("32x32 x 4", "32x32 x 5")
+I8_TILES = TILES + ("192x128", "128x64", "32x32 x 4", "32x32 x 5")
 
 
 def i8_tile(m, n, k, cus):
