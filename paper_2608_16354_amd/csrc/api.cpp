@@ -198,7 +198,10 @@ Status check_ext(const Geo& g, const dc_block_ext& e) {
     return Status::arg("int8 block weights must be 16-byte aligned");
   if (!aligned(w.s_qkv, 4) || !aligned(w.s_o, 4) || !aligned(w.s_1, 4) || !aligned(w.s_2, 4))
     return Status::arg("a pointer is not aligned to its element");
-  return Status::ok();
+  // every product, before the first one is on its way
+  DC_TRY(gemm_i8_check(g.N, 3 * g.d, g.d));
+  DC_TRY(gemm_i8_check(g.N, g.F, g.d));
+  return gemm_i8_check(g.N, g.d, g.F);
 }
 
 // One sample's block with int8 products: every GEMM reads rows that were quantised as they came, the
@@ -245,6 +248,11 @@ Status block_forward(const Geo& g, const dc_block_weights* bw, const dc_block_ex
   DC_TRY(check_ext(g, e));
   if (!e.i8 && (!bw->w_qkv || !bw->w_o || !bw->w_1 || !bw->w_2)) return Status::arg("block weight pointer is NULL");
   if (!bw->b_qkv || !bw->b_o || !bw->b_1 || !bw->b_2) return Status::arg("block weight pointer is NULL");
+  if (g.bf16 && !e.i8) {                // every product, before the first one is on its way
+    DC_TRY(gemm_bf16_check(g.d, g.d, g.N, 3 * g.d, g.d));
+    DC_TRY(gemm_bf16_check(g.d, g.d, g.N, g.F, g.d));
+    DC_TRY(gemm_bf16_check(g.F, g.F, g.N, g.d, g.F));
+  }
   Workspace L;
   DC_TRY(check_ws(g, max_index(il) + 1, ws, ws_bytes, L, e.qk || e.i8));
   const int N = g.N, d = g.d, F = g.F;

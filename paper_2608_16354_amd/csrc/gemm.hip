@@ -11,14 +11,14 @@
 
 namespace dc {
 
-namespace {
-
-inline Status check_gemm(int lda, int ldw, int M, int N, int K) {
+Status gemm_bf16_check(int lda, int ldw, int M, int N, int K) {
   if (K % 128 || lda % 8 || ldw % 8) return Status::shape("bf16 GEMM needs K % 128 == 0 and 16-byte rows");
   if (int64_t(M) * lda > INT32_MAX || int64_t(N) * ldw > INT32_MAX)
     return Status::shape("bf16 GEMM operand exceeds 2^31 elements");
   return Status::ok();
 }
+
+namespace {
 
 // Cost of a block GEMM in us with tile i: rounds of one workgroup per compute unit, each
 // `fixed` (launch, first fill, epilogue) plus K / 64 k-steps of `alone` (a nearly empty chip) to
@@ -67,7 +67,7 @@ template <class Epi>
 Status block_gemm(const uint16_t* A, int lda, const uint16_t* W, int ldw, int M, int N, int K,
                   const Epi& epi, hipStream_t s) {
   if (M <= 0) return Status::ok();
-  DC_TRY(check_gemm(lda, ldw, M, N, K));
+  DC_TRY(gemm_bf16_check(lda, ldw, M, N, K));
   const int cus = compute_units();
   if (cus <= 0) return Status::make(DC_ERR_HIP, "bf16 GEMM: no device");
   switch (block_gemm_tile(M, N, K, cus)) {

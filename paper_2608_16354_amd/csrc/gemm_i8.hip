@@ -449,6 +449,12 @@ constexpr TileCost kTiles[] = {{384, 192, 1, 1, {1.124f, 1.867f}, 7.08f, 0.f},  
 
 }  // namespace
 
+Status gemm_i8_check(int M, int N, int K) {
+  if (K < 128 || K % 128 || K > kMaxK) return Status::shape("int8 product: K must be a multiple of 128, at most 130,944");
+  if (int64_t((M + 63) / 64) * ((N + 63) / 64) > (1 << 23)) return Status::shape("int8 product: too many outputs");
+  return Status::ok();
+}
+
 int i8_tile(int M, int N, int ksteps, int cus, bool split) {
   int best = 0;
   float least = 0.f;
@@ -475,10 +481,9 @@ template <bool SPLIT, class E>
 Status block_gemm(const int8_t* A, int64_t lda, const int8_t* W, int64_t ldw, int M, int N, int K, const E& epi,
                   hipStream_t s) {
   if (M <= 0 || N <= 0) return Status::ok();
-  if (K < 128 || K % 128 || K > kMaxK) return Status::shape("int8 product: K must be a multiple of 128, at most 130,944");
+  DC_TRY(gemm_i8_check(M, N, K));
   if (lda < K || ldw < K || lda % 16 || ldw % 16 || lda > (1 << 22) || ldw > (1 << 22))
     return Status::shape("int8 product: row strides must be multiples of 16 from K to 2^22");
-  if (int64_t((M + 63) / 64) * ((N + 63) / 64) > (1 << 23)) return Status::shape("int8 product: too many outputs");
   const int cus = compute_units();
   if (cus <= 0) return Status::make(DC_ERR_HIP, "int8 product: no device");
   const int la = int(lda), lw = int(ldw), kt = K / 128;

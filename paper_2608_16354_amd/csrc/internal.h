@@ -179,6 +179,8 @@ Status gemm_f32_head_tangents(const float* A, const void* W, bool w_bf16, float*
 
 // bf16 MFMA GEMM variants.  block_gemm_tile: which of its six tiles a call takes (gemm.hip, kTiles).
 int block_gemm_tile(int M, int N, int K, int cus);
+// What such a product refuses: the block asks for all of its products before it runs the first.
+Status gemm_bf16_check(int lda, int ldw, int M, int N, int K);
 // Q leaves times q_scale.
 float attention_q_scale(int head_dim);      // log2(e) / sqrt(head_dim), what the bf16 attention expects
 Status gemm_bf16_qkv(const uint16_t* A, const uint16_t* W, const float* bias, uint16_t* qk,
@@ -267,6 +269,8 @@ struct LinearI8 {
   void* out; int64_t ld_out; bool out_bf16;
 };
 Status gemm_i8_linear(const LinearI8& a, hipStream_t s);
+// the sums and outputs that a product of M rows and N channels refuses
+Status gemm_i8_check(int M, int N, int K);
 // which of its ten tiles a product takes (gemm_i8.hip, kTiles); split: gemm_i8_linear's, the QKV product has eight
 int i8_tile(int M, int N, int ksteps, int cus, bool split);
 Status gemm_i8_qkv(const int8_t* A, const float* sx, const int8_t* W, const float* sw, const float* bias,

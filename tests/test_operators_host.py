@@ -183,6 +183,26 @@ def test_block_ext_refuses(lib):
     assert call(c, qk_cfg=qk(), w=no_matrix) == ARG
 
 
+@pytest.mark.parametrize("f,lat,n_txt,int8", [
+    (131072, (4, 16, 16), 16, True),            # the down product's K
+    (65536, (64, 512, 512), 0, True),           # 4,194,304 tokens: the up product's outputs
+    (1 << 20, (4, 128, 128), 0, False),         # bf16: the down product's operand of 2^34 values
+])
+def test_block_refuses_its_products_before_it_starts(lib, f, lat, n_txt, int8):
+    """A block that one of its products cannot run is refused before h is written."""
+    c = cfg(lat=lat, n_txt=n_txt)
+    c.mlp_hidden = f
+    arr, n = idx(0)
+    i8 = L.BlockWeightsI8(*[FAKE] * 8)
+    e = L.BlockExt(None, C.pointer(i8) if int8 else None)
+    blk = L.BlockWeights(*[FAKE] * 9)
+    nbytes = lib.dc_block_ext_workspace_bytes(C.byref(c), 1)
+    assert nbytes
+    assert lib.dc_block_forward_ext(C.byref(c), C.byref(blk), C.byref(e), FAKE, FAKE, arr, n, FAKE, nbytes, None) == SHAPE
+    if not int8:
+        assert lib.dc_block_forward(C.byref(c), C.byref(blk), FAKE, FAKE, arr, n, FAKE, nbytes, None) == SHAPE
+
+
 def test_sampler_ext_refuses(lib):
     from paper_2608_16354_amd import api
     from paper_2608_16354_amd import inputs as I
