@@ -93,7 +93,8 @@ typedef struct {
 /* Whole-generator parameters (device memory, except the `blocks` host array). */
 typedef struct {
   const float* w_pe;  const float* b_pe;    /* [d, 64], [d] f32 patch embedding */
-  const void* pos;                          /* [N_v, d] position table, model dtype */
+  const void* pos;                          /* [N_v, d] position table, model dtype (of zeros where a model's
+                                               positions are rotary alone; NULL is refused) */
   const float* w_t1;  const float* b_t1;    /* [d, 256], [d] timestep MLP layer 1 */
   const float* w_t2;  const float* b_t2;    /* [d, d], [d]   timestep MLP layer 2 */
   const float* w_m;   const float* b_m;     /* [6d, d], [6d] shared modulation projection */

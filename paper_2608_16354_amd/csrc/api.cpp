@@ -172,6 +172,7 @@ Status patch_embed(const Geo& g, const dc_model_weights* w, const float* x, cons
   Workspace L;
   DC_TRY(check_ws(g, max_index(il) + 1, ws, ws_bytes, L));
   if (il.n == 0) return Status::ok();
+  if (g.Nv > 0 && (!w->w_pe || !w->b_pe || !w->pos)) return Status::arg("w_pe, b_pe or pos is NULL");
   ProfScope ps(KClass::kPatchEmbed, s);
   if (g.bf16)
     return patch_embed_bf16(x, w->w_pe, w->b_pe, static_cast<const uint16_t*>(w->pos), txt, h_in, il, g, s);

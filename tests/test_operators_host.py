@@ -203,6 +203,20 @@ def test_block_refuses_its_products_before_it_starts(lib, f, lat, n_txt, int8):
         assert lib.dc_block_forward(C.byref(c), C.byref(blk), FAKE, FAKE, arr, n, FAKE, nbytes, None) == SHAPE
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("hole", ["w_pe", "b_pe", "pos"])
+def test_patch_embedding_refuses_a_missing_table(lib, dtype, hole):
+    """A rotary model has no additive position table: a NULL one is refused, not read."""
+    c = cfg(dtype=dtype)
+    w = L.ModelWeights()
+    for name in ("w_pe", "b_pe", "pos"):
+        setattr(w, name, None if name == hole else FAKE)
+    nbytes = lib.dc_workspace_bytes(C.byref(c), 1)
+    for samples, code in (((0,), ARG), ((), L.DC_OK)):
+        arr, n = idx(*samples)
+        assert lib.dc_patch_embed(C.byref(c), C.byref(w), FAKE, FAKE, FAKE, arr, n, FAKE, nbytes, None) == code
+
+
 def test_sampler_ext_refuses(lib):
     from paper_2608_16354_amd import api
     from paper_2608_16354_amd import inputs as I
