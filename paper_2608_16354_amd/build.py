@@ -4,7 +4,8 @@
 
 Device sources (*.hip) go through hipcc for gfx950; host sources (*.cpp) through
 amdclang++ with -ffp-contract=off, so the schedule's floating-point arithmetic
-is one IEEE operation at a time.  The binding (binding.cpp) is built against torch's headers.
+is one IEEE operation at a time.  The binding (binding.cpp) is built against torch's headers; the
+library needs neither it nor torch, and is installed before a binding that fails is reported.
 """
 from __future__ import annotations
 
@@ -42,14 +43,20 @@ def sources():
     return sorted(f for f in os.listdir(CSRC) if f.endswith((".hip", ".cpp")))
 
 
-def _binding_cmd(clang, out):
-    import torch
+def _build_binding(clang):
+    """What the compiler printed, or None where there is no torch to build against."""
+    try:
+        import torch
+    except (ImportError, OSError) as e:
+        print(f"the tensor binding is not built: no torch ({e})", file=sys.stderr)
+        return None
     t = os.path.dirname(torch.__file__)
-    return [clang, "-O2", "-fPIC", "-shared", "-std=c++17", "-Wall", "-D__HIP_PLATFORM_AMD__",
+    return _run([clang, "-O2", "-fPIC", "-shared", "-std=c++17", "-Wall", "-D__HIP_PLATFORM_AMD__",
             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
             "-isystem", f"{t}/include", "-isystem", f"{t}/include/torch/csrc/api/include",
             "-isystem", sysconfig.get_paths()["include"], f"-I{ROCM}/include",
-            os.path.join(PKG, "binding.cpp"), "-o", out, f"-L{t}/lib", "-ltorch_python", "-ltorch_cpu", "-lc10"]
+            os.path.join(PKG, "binding.cpp"), "-o", BINDING + ".tmp", f"-L{t}/lib", "-ltorch_python", "-ltorch_cpu",
+            "-lc10"])
 
 
 def build(verbose: bool = False) -> str:
@@ -66,8 +73,8 @@ def build(verbose: bool = False) -> str:
             jobs.append([hipcc, *HIPCC_FLAGS, *EXTRA_FLAGS.get(f, []), "-c", src, "-o", obj])
         else:
             jobs.append([clang, *HOST_FLAGS, "-c", src, "-o", obj])
-    jobs.append(_binding_cmd(clang, BINDING + ".tmp"))
     with ThreadPoolExecutor(max(1, min(8, os.cpu_count() or 1))) as ex:
+        binding = ex.submit(_build_binding, clang)
         outs = list(ex.map(_run, jobs))
     if verbose:
         for o in outs:
@@ -77,7 +84,13 @@ def build(verbose: bool = False) -> str:
     _run([hipcc, "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp, *objs,
           f"-L{ROCM}/lib", "-lamdhip64"])
     os.replace(tmp, LIB)
-    os.replace(BINDING + ".tmp", BINDING)
+    failure = binding.exception()
+    if failure is None and binding.result() is not None:
+        os.replace(BINDING + ".tmp", BINDING)
+    elif os.path.exists(BINDING):               # it belongs to another library
+        os.remove(BINDING)
+    if failure is not None:
+        raise RuntimeError(f"the library is built, the tensor binding is not: {failure}") from failure
     return LIB
 
 
