@@ -52,11 +52,11 @@ def _build_binding(clang):
         return None
     t = os.path.dirname(torch.__file__)
     return _run([clang, "-O2", "-fPIC", "-shared", "-std=c++17", "-Wall", "-D__HIP_PLATFORM_AMD__",
-            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-            "-isystem", f"{t}/include", "-isystem", f"{t}/include/torch/csrc/api/include",
-            "-isystem", sysconfig.get_paths()["include"], f"-I{ROCM}/include",
-            os.path.join(PKG, "binding.cpp"), "-o", BINDING + ".tmp", f"-L{t}/lib", "-ltorch_python", "-ltorch_cpu",
-            "-lc10"])
+                 f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                 "-isystem", f"{t}/include", "-isystem", f"{t}/include/torch/csrc/api/include",
+                 "-isystem", sysconfig.get_paths()["include"], f"-I{ROCM}/include",
+                 os.path.join(PKG, "binding.cpp"), "-o", BINDING + ".tmp", f"-L{t}/lib", "-ltorch_python", "-ltorch_cpu",
+                 "-lc10"])
 
 
 def build(verbose: bool = False) -> str:
@@ -87,6 +87,8 @@ def build(verbose: bool = False) -> str:
     failure = binding.exception()
     if failure is None and binding.result() is not None:
         os.replace(BINDING + ".tmp", BINDING)
+        if verbose and binding.result().strip():
+            print(binding.result())
     elif os.path.exists(BINDING):               # it belongs to another library
         os.remove(BINDING)
     if failure is not None:
