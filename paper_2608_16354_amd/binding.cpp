@@ -127,6 +127,15 @@ int64_t rows(const at::Tensor& t, const char* what) {
   need((cols <= 1 || t.stride(1) == 1) && ld >= cols, what);
   return ld;
 }
+// The same of [B, N, width] rows that are equally far apart (a dimension of one says nothing), `wanted` of their values
+// read or written.
+int64_t sample_rows(const at::Tensor& t, int64_t tokens, int64_t wanted, const char* what) {
+  need(t.dim() == 3 && t.size(1) == tokens && t.size(2) >= wanted && t.stride(2) == 1, what);
+  const int64_t batch = t.size(0);
+  const int64_t ld = tokens > 1 ? t.stride(1) : batch > 1 ? t.stride(0) : wanted;
+  need((tokens * batch <= 1 || ld >= wanted) && (tokens <= 1 || batch <= 1 || t.stride(0) == tokens * ld), what);
+  return ld;
+}
 int32_t dtype(const at::Tensor& t) {
   if (t.scalar_type() == at::kFloat) return DC_F32;
   need(t.scalar_type() == at::kBFloat16, "float32 or bfloat16 tensors only");
@@ -173,10 +182,9 @@ PyObject* qk_norm_rope(PyObject* const* args, Py_ssize_t n) {
   const at::Tensor &x = a.tensor(1), &out = a.tensor(2);
   const int64_t nv = video_tokens(c), tokens = nv + c.n_txt, d2 = 2 * int64_t(c.hidden);
   const at::ScalarType type = c.dtype == DC_BF16 ? at::kBFloat16 : at::kFloat;
-  for (const at::Tensor* t : {&x, &out})
-    need(t->scalar_type() == type && t->dim() == 3 && t->size(1) == tokens && t->size(2) >= d2 && t->stride(2) == 1 &&
-             (tokens <= 1 || t->stride(1) >= d2) && (t->size(0) <= 1 || t->stride(0) == tokens * t->stride(1)),
-         "x and out: [B, N, at least 2 hidden] tensors of the model's dtype with equally spaced rows are wanted");
+  const char* of_rows = "x and out: [B, N, at least 2 hidden] tensors of the model's dtype with equally spaced rows are wanted";
+  need(x.scalar_type() == type && out.scalar_type() == type, of_rows);
+  const int64_t ld_x = sample_rows(x, tokens, d2, of_rows), ld_out = sample_rows(out, tokens, d2, of_rows);
   dc_qk_cfg q{};
   q.q_weight = a.vector(4, c.head_dim, "q_weight: a contiguous float32 [head_dim] tensor is wanted");
   q.k_weight = a.vector(5, c.head_dim, "k_weight: a contiguous float32 [head_dim] tensor is wanted");
@@ -190,7 +198,7 @@ PyObject* qk_norm_rope(PyObject* const* args, Py_ssize_t n) {
   int32_t idx[DC_MAX_BATCH];
   const int k = a.samples(3, std::min(x.size(0), out.size(0)), idx);
   return call(a, [&] {
-    return f_qk_norm_rope(&c, &q, x.data_ptr(), x.stride(1), out.data_ptr(), out.stride(1), scale, idx, k, a.stream);
+    return f_qk_norm_rope(&c, &q, x.data_ptr(), ld_x, out.data_ptr(), ld_out, scale, idx, k, a.stream);
   });
 }
 

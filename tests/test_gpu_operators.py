@@ -352,6 +352,24 @@ def test_one_row_of_any_stride(api, dev):
     assert (np.abs(host(out) - want) <= 4 * F32 * np.abs(want)).all() and host(y)[0, 40] == 0
 
 
+@pytest.mark.parametrize("batch", [1, 3])
+def test_single_tokens_of_any_stride(api, dev, batch):
+    """A model of one token, its samples cut out of longer ones: against the same rows put together."""
+    import torch
+    m = shape(lat=(1, 2, 2), n_txt=0)
+    cfg, d2, idx = api.model_cfg(m), 2 * m.hidden, list(range(batch))
+    wide = torch.randn((batch, 5, 3 * m.hidden), device=dev, generator=torch.Generator(dev).manual_seed(8)).bfloat16()
+    w, table = torch.full((64,), 1.5, device=dev), torch.randn((1, 32, 2), device=dev)
+    want = torch.zeros((batch, 1, d2), device=dev, dtype=torch.bfloat16)
+    whole = wide[:, 2:3].contiguous()
+    api.dc_qk_norm_rope(cfg, whole, want, idx, q_weight=w, k_weight=w, table=table)
+    x = wide.as_strided((batch, 1, 3 * m.hidden), (5 * 3 * m.hidden, 3, 1), 2 * 3 * m.hidden)
+    held = torch.full((batch, 2, d2 + 8), 4.0, device=dev, dtype=torch.bfloat16)
+    api.dc_qk_norm_rope(cfg, x, held.as_strided((batch, 1, d2), (2 * (d2 + 8), 5, 1)), idx, q_weight=w, k_weight=w, table=table)
+    assert torch.equal(held[:, :1, :d2], want) and (held[:, 1] == 4).all() and (held[:, 0, d2:] == 4).all()
+    assert want.float().abs().max() > 0.5
+
+
 def test_linear_of_no_rows(api, dev):
     import torch
     api.dc_quantize_rows(torch.empty((0, 100), device=dev), torch.empty((0, 128), dtype=torch.int8, device=dev), torch.empty(0, device=dev))

@@ -362,6 +362,25 @@ def test_binding_refuses_norms_and_tables():
     refused("tensor", "dc_rope_table", c, axes(), None, None)
 
 
+def test_binding_takes_single_tokens_of_any_stride():
+    """A model of one token: its rows are the samples, a dimension of one has no stride of its own."""
+    import torch
+    c = cfg(lat=(1, 2, 2), n_txt=0)
+    buf, out = torch.zeros(3, 5, 768, dtype=torch.bfloat16), torch.zeros(3, 1, 512, dtype=torch.bfloat16)
+
+    def f(match, x, out, idx_):
+        refused(match, "dc_qk_norm_rope", c, x, out, idx_, None, None, 1e-6, None, True, 1.0)
+
+    for st in (0, 3, 512, 768):
+        one = buf.as_strided((1, 1, 768), (7, st, 1))
+        f("on a GPU", one, out[:1], [0])
+        f("on a GPU", out[:1], one, [0])
+        f("on a GPU", buf.as_strided((3, 1, 768), (3840, st, 1)), out, [0, 2])
+    f("on a GPU", buf[:, 2:3], out, [1])
+    f("x and out", buf.as_strided((3, 1, 768), (504, 768, 1)), out, [0])            # samples that overlap
+    f("x and out", buf[:1, :1].expand(3, 1, 768), out, [0])
+
+
 def test_api_refuses_host_tensors():
     import torch
     from paper_2608_16354_amd import api
