@@ -136,6 +136,29 @@ int64_t sample_rows(const at::Tensor& t, int64_t tokens, int64_t wanted, const c
   need((tokens * batch <= 1 || ld >= wanted) && (tokens <= 1 || batch <= 1 || t.stride(0) == tokens * ld), what);
   return ld;
 }
+// `n` rows of `width` bytes, `ld` bytes apart (at least the width).
+struct Span {
+  const char* p;
+  int64_t n, ld, width;
+  Span(const void* at, int64_t rows, int64_t ld_bytes, int64_t width_bytes)
+      : p(static_cast<const char*>(at)), n(rows), ld(ld_bytes), width(width_bytes) {}
+  explicit Span(const at::Tensor& t) : Span(t.data_ptr(), 1, int64_t(t.nbytes()), int64_t(t.nbytes())) {}      // contiguous
+  const char* end() const { return p + (n - 1) * ld + width; }
+};
+bool overlap(const Span& a, const Span& b) {
+  if (a.n < 1 || b.n < 1 || a.width < 1 || b.width < 1 || a.end() <= b.p || b.end() <= a.p) return false;
+  if (a.ld == b.ld) {                   // side by side in rows of one length
+    const int64_t d = (b.p - a.p) % a.ld, at = d < 0 ? d + a.ld : d;
+    return at < a.width || at + b.width > a.ld;
+  }
+  const char *x = a.p, *y = b.p;
+  for (int64_t i = 0, j = 0; i < a.n && j < b.n;) {
+    if (x + a.width <= y) ++i, x += a.ld;
+    else if (y + b.width <= x) ++j, y += b.ld;
+    else return true;
+  }
+  return false;
+}
 int32_t dtype(const at::Tensor& t) {
   if (t.scalar_type() == at::kFloat) return DC_F32;
   need(t.scalar_type() == at::kBFloat16, "float32 or bfloat16 tensors only");
@@ -197,6 +220,10 @@ PyObject* qk_norm_rope(PyObject* const* args, Py_ssize_t n) {
   const float scale = float(a.number(9));
   int32_t idx[DC_MAX_BATCH];
   const int k = a.samples(3, std::min(x.size(0), out.size(0)), idx);
+  const int64_t e = x.element_size();
+  const Span from(x.data_ptr(), x.size(0) * tokens, ld_x * e, d2 * e);
+  const Span to(out.data_ptr(), out.size(0) * tokens, ld_out * e, d2 * e);
+  need((from.p == to.p && from.ld == to.ld) || !overlap(from, to), "out overlaps x: x itself, or other rows or columns, are wanted");
   return call(a, [&] {
     return f_qk_norm_rope(&c, &q, x.data_ptr(), ld_x, out.data_ptr(), ld_out, scale, idx, k, a.stream);
   });
@@ -213,6 +240,9 @@ PyObject* quantize_rows(PyObject* const* args, Py_ssize_t n) {       // x, q, sc
   a.tensor(2);
   const float* scale = a.vector(2, m, "scale: a contiguous float32 [rows] tensor is wanted");
   const int32_t type = dtype(x), rows32 = i32(m), cols32 = i32(cols);
+  const Span from(x.data_ptr(), m, ldx * x.element_size(), cols * x.element_size());
+  const Span to(q.data_ptr(), m, ldq, (cols + 127) / 128 * 128), scales(a.tensor(2));
+  need(!overlap(to, from) && !overlap(scales, from) && !overlap(scales, to), "x, q and scale overlap");
   return call(a, [&] {
     return f_quantize_rows(x.data_ptr(), type, ldx, rows32, cols32, static_cast<int8_t*>(q.data_ptr()), ldq,
                            const_cast<float*>(scale), a.stream);
@@ -251,6 +281,14 @@ PyObject* linear_i8(PyObject* const* args, Py_ssize_t n) {  // x, x_scale, w, w_
          "residual: a float32 tensor of out's shape is wanted");
     p.residual = a.at<float>(r);
   }
+  const int64_t e = out.element_size();
+  const Span to(out.data_ptr(), m, p.ld_out * e, cols * e);
+  bool apart = !overlap(to, Span(p.x, m, p.ld_x, k)) && !overlap(to, Span(p.w, cols, p.ld_w, k));
+  for (const int i : {1, 3, 5, 7})
+    if (const at::Tensor* t = a.maybe(i)) apart = apart && !overlap(to, Span(*t));
+  if (p.residual && !(p.residual == p.out && p.ld_residual == p.ld_out))
+    apart = apart && !overlap(to, Span(p.residual, m, p.ld_residual * 4, cols * 4));
+  need(apart, "out overlaps another operand: the residual itself, or other rows or columns, are wanted");
   return call(a, [&] { return f_linear_i8(&p, a.stream); });
 }
 

@@ -381,6 +381,65 @@ def test_binding_takes_single_tokens_of_any_stride():
     f("x and out", buf[:1, :1].expand(3, 1, 768), out, [0])
 
 
+def test_binding_refuses_overlaps():
+    """What is written overlaps nothing that is read, but for the places that may be the same: other columns of a
+    buffer's rows, or other rows, are taken."""
+    import torch
+    c, n = cfg(), None
+    buf = torch.zeros(2, 272, 1024, dtype=torch.bfloat16)
+
+    def qk_(match, x, out):
+        refused(match, "dc_qk_norm_rope", c, x, out, [0], n, n, 1e-6, n, True, 1.0)
+
+    qk_("on a GPU", buf[..., :512], buf[..., :512])             # in place
+    qk_("on a GPU", buf[..., :512], buf[..., 512:])
+    qk_("on a GPU", buf[..., 512:], buf[..., :512])
+    qk_("on a GPU", buf[:1], buf[1:])
+    qk_("on a GPU", buf[1:], buf[:1])
+    qk_("overlap", buf[..., :512], buf[..., 8:520])
+    qk_("overlap", buf[..., 256:768], buf[..., :512])
+    qk_("on a GPU", buf, buf[..., 512:])                        # 512 of x's columns are read
+    qk_("overlap", buf, buf[..., 504:])
+    flat = buf.view(-1)
+    rows_ = flat[: 272 * 512].view(1, 272, 512)
+    qk_("overlap", buf[:1, :, :512], rows_)                     # rows of another length in the same place
+    qk_("overlap", flat[8: 8 + 272 * 512].view(1, 272, 512), rows_)
+    qk_("on a GPU", flat[272 * 512: 2 * 272 * 512].view(1, 272, 512), rows_)
+
+    def quant(match, x, q, s):
+        refused(match, "dc_quantize_rows", x, q, s)
+
+    raw = torch.zeros(4, 1024, dtype=torch.int8)
+    s = torch.zeros(4)
+    floats = raw.view(torch.float32)                            # [4, 256]
+    quant("on a GPU", floats[:, 128:], raw[:, :128], s)
+    quant("on a GPU", floats[:, 32:132], raw, s)                # the 128 columns that are written lie before x
+    quant("overlap", floats[:, 31:131], raw, s)
+    quant("overlap", floats, raw, s)
+    quant("overlap", floats[:2], raw.view(8, 512)[2:4], s[:2])
+    quant("on a GPU", floats[:2], raw[2:], s[:2])
+    quant("on a GPU", floats[:1, :8], raw[0, 128:].unsqueeze(0)[:, :128], s[:1])
+    quant("overlap", floats, torch.zeros(4, 256, dtype=torch.int8), floats[0, :4])
+
+    x, w = torch.zeros(4, 128, dtype=torch.int8), torch.zeros(8, 128, dtype=torch.int8)
+    out, ws, wide = torch.zeros(4, 8), torch.zeros(8), torch.zeros(4, 20)
+
+    def lin(match, x=x, xs=s, w=w, ws=ws, out=out, bias=n, gate=n, residual=n):
+        refused(match, "dc_linear_i8", x, xs, w, ws, out, bias, False, gate, residual)
+
+    lin("on a GPU", out=wide[:, :8], residual=wide[:, 8:16], gate=ws)
+    lin("on a GPU", out=wide[:, :8], residual=wide[:, :8], gate=ws)
+    lin("overlap", out=wide[:, :8], residual=wide[:, 4:12], gate=ws)
+    lin("overlap", out=wide[1:, :8], x=x[1:], xs=s[1:], residual=wide[:3, :8], gate=ws)
+    for name, t in (("x", x), ("w", w)):
+        lin("overlap", **{name: t, "out": t.view(torch.float32)[:4, :8]})
+    vec = torch.zeros(32)
+    for name in ("ws", "bias"):
+        lin("overlap", out=vec.view(4, 8), **{name: vec[5:13]})
+    lin("overlap", out=vec.view(4, 8), gate=vec[:8], residual=out)
+    lin("overlap", out=vec.view(4, 8), xs=vec[28:])
+
+
 def test_api_refuses_host_tensors():
     import torch
     from paper_2608_16354_amd import api
