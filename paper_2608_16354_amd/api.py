@@ -289,15 +289,15 @@ class BlockExt:
         torch = _torch()
         n = len(dm.blocks)
         self.cfg = dm.cfg
-        self.keep = [q_weight, k_weight, table]
+        self.keep = [table]             # the tensors themselves: a caller's list may change
         self.c = (L.BlockExt * n)()
         for l, b in enumerate(dm.blocks):
             if q_weight is not None or k_weight is not None or table is not None:
                 dh, dev = (dm.cfg.head_dim,), b["b_qkv"].device
-                qk = L.QkCfg(_floats(None if q_weight is None else q_weight[l], dh, dev, "q_weight"),
-                             _floats(None if k_weight is None else k_weight[l], dh, dev, "k_weight"), eps,
+                wq, wk = (None if w is None else w[l] for w in (q_weight, k_weight))
+                qk = L.QkCfg(_floats(wq, dh, dev, "q_weight"), _floats(wk, dh, dev, "k_weight"), eps,
                              _floats(table, (_video_tokens(dm.cfg), dh[0] // 2, 2), dev, "table"), 1 if interleaved else 0)
-                self.keep.append(qk)
+                self.keep += [wq, wk, qk]
                 self.c[l].qk = C.pointer(qk)
             if int8:
                 held = L.BlockWeightsI8()

@@ -483,6 +483,27 @@ def test_extensions_belong_to_a_shape_and_a_device():
         api.BlockExt(dm, q_weight=w[:1])
 
 
+def test_extensions_keep_their_tensors():
+    """The library holds addresses, so the tensors live as long as the extension, whatever becomes of the caller's list."""
+    import gc
+    import types
+    import weakref
+    import torch
+    from paper_2608_16354_amd import api
+    dm = types.SimpleNamespace(cfg=cfg(), blocks=[dict(b_qkv=torch.zeros(4))] * 2)
+    wq, wk, table = [torch.ones(64) for _ in range(2)], [torch.ones(64) for _ in range(2)], torch.zeros(256, 32, 2)
+    held = [weakref.ref(v) for v in (*wq, *wk, table)]
+    e = api.BlockExt(dm, q_weight=wq, k_weight=wk, table=table)
+    wq.clear()
+    wk[:] = [None, None]
+    del table
+    gc.collect()
+    assert all(r() is not None for r in held)
+    del e
+    gc.collect()
+    assert all(r() is None for r in held)
+
+
 def test_product_shapes_take_the_tiles_they_name():
     """The GPU tests' shapes are the ones the library's rule sends to each of its tiles."""
     from tests import test_gpu_operators as G
