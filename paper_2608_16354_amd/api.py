@@ -288,12 +288,12 @@ class BlockExt:
                  int8=False):
         torch = _torch()
         n = len(dm.blocks)
-        self.cfg = dm.cfg
+        self.cfg, self.device = dm.cfg, dm.blocks[0]["b_qkv"].device
         self.keep = [table]             # the tensors themselves: a caller's list may change
         self.c = (L.BlockExt * n)()
         for l, b in enumerate(dm.blocks):
             if q_weight is not None or k_weight is not None or table is not None:
-                dh, dev = (dm.cfg.head_dim,), b["b_qkv"].device
+                dh, dev = (dm.cfg.head_dim,), self.device
                 wq, wk = (None if w is None else w[l] for w in (q_weight, k_weight))
                 qk = L.QkCfg(_floats(wq, dh, dev, "q_weight"), _floats(wk, dh, dev, "k_weight"), eps,
                              _floats(table, (_video_tokens(dm.cfg), dh[0] // 2, 2), dev, "table"), 1 if interleaved else 0)
@@ -316,9 +316,11 @@ class BlockExt:
         return C.pointer(self.c[l])
 
     def of(self, dm):
-        """Itself, if it has the shapes of dm: the library reads dm's sizes from what it points to."""
+        """Itself, if it has the shapes and the device of dm: the library reads dm's sizes from what it points to."""
         if bytes(self.cfg) != bytes(dm.cfg):
             raise ValueError("ext was made for a model of another shape")
+        if dm.blocks[0]["b_qkv"].device != self.device:
+            raise ValueError("ext was made for a model on another device")
         return self
 
 

@@ -483,6 +483,24 @@ def test_extensions_belong_to_a_shape_and_a_device():
         api.BlockExt(dm, q_weight=w[:1])
 
 
+def test_extensions_belong_to_their_device():
+    """Equal shapes on another device: the addresses an extension holds are not that model's."""
+    import types
+    import torch
+    from paper_2608_16354_amd import api
+
+    def model(device):
+        return types.SimpleNamespace(cfg=cfg(), blocks=[dict(b_qkv=torch.zeros(4, device=device))] * 2)
+
+    here, elsewhere = model("cpu"), model("meta")
+    e = api.BlockExt(here)
+    assert e.of(model("cpu")) is e
+    with pytest.raises(ValueError, match="another device"):
+        e.of(elsewhere)
+    with pytest.raises(ValueError, match="another device"):
+        api.dc_block_forward_ext(elsewhere, 0, e, None, None, [0], None)
+
+
 def test_extensions_keep_their_tensors():
     """The library holds addresses, so the tensors live as long as the extension, whatever becomes of the caller's list."""
     import gc
