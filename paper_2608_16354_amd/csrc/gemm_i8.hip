@@ -67,7 +67,6 @@ struct EpiLinear : std::conditional<GATED, Residual, NoResidual>::type {
   static constexpr int CB = BF ? 2 : 1;               // 32-column tiles of a strip: 128 bytes a row
   static constexpr int kS = 128 + 16;                 // 16 rows' writes on distinct banks
   static constexpr int kStrip = 32 * kS;
-  bool rows_aligned() const { return true; }
 
   // GELU(z) = z / (1 + 2^u), u = -2 log2(e) sqrt(2 / pi) (z + 0.044715 z^3)
   static __device__ inline float act(float z) {
@@ -255,7 +254,6 @@ struct EpiQKV {
   float q_scale;
   static constexpr int kS = 64 + 16;
   static constexpr int kStrip = 32 * kS;
-  bool rows_aligned() const { return true; }
 
   template <int BM, int BN, int NT>
   __device__ inline void start(float4* vec, int m0, int n0, int M, int N, int tid) const {

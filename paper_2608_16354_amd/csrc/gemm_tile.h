@@ -252,8 +252,8 @@ constexpr int kEpiStride = 40;   // floats per row of the epilogue's per-wave LD
 // row groups a ds_write_b32 covers land 32 banks apart) and comes back as V
 // consecutive columns of one row per lane.  The caller has finished every read of
 // the LDS stages (the barrier here orders the reuse).
-template <int BM, int BN, int WM, int WN, class Epi, class Acc, int TM, int TN>
-__device__ inline void gemm_epilogue(Acc (&acc)[TM][TN], uint4* lds, int m0, int n0, int M,
+template <int BM, int BN, int WM, int WN, class Epi, int TM, int TN>
+__device__ inline void gemm_epilogue(f32x16 (&acc)[TM][TN], uint4* lds, int m0, int n0, int M,
                                      int N, int wave, int lane, int rows_ok, const Epi& epi) {
   constexpr int WTM = BM / WM, WTN = BN / WN;
   constexpr int RV = Epi::kRowVec > 0 ? Epi::kRowVec : 4;
@@ -274,7 +274,7 @@ __device__ inline void gemm_epilogue(Acc (&acc)[TM][TN], uint4* lds, int m0, int
       for (int a = 0; a < TM; ++a) {
         const int mb = m0 + wm * WTM + a * 32;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) st[(8 * (i >> 2) + 4 * hi + (i & 3)) * kS + r32] = float(acc[a][b][i]);
+        for (int i = 0; i < 16; ++i) st[(8 * (i >> 2) + 4 * hi + (i & 3)) * kS + r32] = acc[a][b][i];
         constexpr int LPR = 32 / RV, RPI = 64 / LPR, NP = 32 / RPI;   // lanes per row, rows per pass
         const int r0 = lane / LPR, c = (lane % LPR) * RV;
         float v[NP][RV];
@@ -290,7 +290,7 @@ __device__ inline void gemm_epilogue(Acc (&acc)[TM][TN], uint4* lds, int m0, int
     } else {
 #pragma unroll
       for (int a = 0; a < TM; ++a)
-        if (nb + r32 < N) epi.col(m0 + wm * WTM + a * 32 + 4 * hi, nb + r32, M, __builtin_convertvector(acc[a][b], f32x16));
+        if (nb + r32 < N) epi.col(m0 + wm * WTM + a * 32 + 4 * hi, nb + r32, M, acc[a][b]);
     }
   }
 }
@@ -544,6 +544,14 @@ __global__ void __launch_bounds__(512) k_gemm_pipe(const char* __restrict__ A, i
   }
 }
 
+// Row-vector epilogue stores need 16-byte aligned rows; otherwise every tile goes by column.  Swapped epilogues take
+// rows at any address.
+template <class Ops, class Epi>
+inline int rows_go(const Epi& epi) {
+  if constexpr (Ops::kSwapped) return 0;
+  else return epi.rows_aligned() ? 1 : 0;
+}
+
 // lda and ldw in bytes (multiples of 16), KT k-steps of 128 bytes
 template <class Ops, int BM, int BN, int WM, int WN, int DS, int ST, class Epi>
 Status launch_dma(const void* A, int lda, const void* W, int ldw, int M, int N, int KT,
@@ -551,8 +559,7 @@ Status launch_dma(const void* A, int lda, const void* W, int ldw, int M, int N, 
   const int tn = (N + BN - 1) / BN, tm = (M + BM - 1) / BM;
   const int tiles = tn * tm;
   const int per = (tiles + 7) / 8;
-  // row-vector epilogue stores need 16-byte aligned rows; otherwise every tile goes by column
-  const int rows_ok = epi.rows_aligned() ? 1 : 0;
+  const int rows_ok = rows_go<Ops>(epi);
   hipLaunchKernelGGL((k_gemm_dma<Ops, BM, BN, WM, WN, DS, ST, Epi>), dim3(8 * per), dim3(WM * WN * 64), 0, s,
                      static_cast<const char*>(A), lda, static_cast<const char*>(W), ldw, M, N, KT, tn, tiles, per, rows_ok, epi);
   DC_HIP(hipGetLastError());
@@ -564,7 +571,7 @@ Status launch_pipe(const void* A, int lda, const void* W, int ldw, int M, int N,
                    const Epi& epi, hipStream_t s) {
   const int tn = (N + 127) / 128, tiles = tn * ((M + 127) / 128), per = (tiles + 7) / 8;
   hipLaunchKernelGGL((k_gemm_pipe<Ops, Epi>), dim3(8 * per), dim3(512), 0, s, static_cast<const char*>(A), lda,
-                     static_cast<const char*>(W), ldw, M, N, KT, tn, tiles, per, epi.rows_aligned() ? 1 : 0, epi);
+                     static_cast<const char*>(W), ldw, M, N, KT, tn, tiles, per, rows_go<Ops>(epi), epi);
   DC_HIP(hipGetLastError());
   return Status::ok();
 }
