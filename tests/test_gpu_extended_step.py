@@ -291,3 +291,12 @@ def test_int8_qkv_rows(api, dev, tile):
     say(tile, "largest share of the tolerance", (err / tol).max())
     assert np.isfinite(got).all() and (err <= tol).all(), np.argwhere(err > tol)[:4]
     assert not vt[:, N:].any()
+
+
+QKV_WIDE = {"320x256": _shape(1152, 16, 72, 128, (6, 56, 64), 77, "bf16")}       # the tile with five strips of rows to a wave
+
+
+@pytest.mark.parametrize("tile", list(QKV_WIDE))
+def test_int8_qkv_rows_of_wide_tiles(api, dev, monkeypatch, tile):
+    monkeypatch.setitem(QKV_TILES, tile, QKV_WIDE[tile])
+    test_int8_qkv_rows(api, dev, tile)

@@ -529,6 +529,17 @@ def test_product_shapes_take_the_tiles_they_name():
     assert set(G.TILE_SHAPES.values()) == set(G.I8_TILES)
 
 
+def test_qkv_models_take_every_tile():
+    """The models whose QKV rows are tested on the GPU take each tile that the int8 QKV product can take."""
+    from tests import test_gpu_extended_step as E
+    from tests import test_gpu_operators as G
+    from tests.gpu_util import _native
+    models = {**E.QKV_TILES, **E.QKV_WIDE}
+    for tile, m in models.items():
+        assert G.I8_TILES[_native("_ZN2dc7i8_tileEiiiib", m.n_tok, 3 * m.hidden, m.hidden // 128, 256, False)] == tile
+    assert set(models) == {t for t in G.I8_TILES if not t.startswith("32x32")}
+
+
 # ----------------------------------------------------------------------------
 # the definitions, by hand
 # ----------------------------------------------------------------------------
