@@ -423,7 +423,7 @@ dc_status dc_rope_table(const dc_model_cfg* cfg, const dc_rope_axes* axes, const
   DC_ENTRY(([&]() -> Status {
     Geo g;
     DC_TRY(make_geo(cfg, g));
-    if (!axes || !cos_sin) return Status::arg("NULL argument");
+    if (!axes || (g.Nv > 0 && !cos_sin)) return Status::arg("NULL argument");
     int64_t sum = 0;
     for (int a = 0; a < 3; ++a) {
       if (axes->dim[a] < 0 || axes->dim[a] % 2) return Status::arg("axes->dim must be even and >= 0");
@@ -509,7 +509,7 @@ dc_status dc_cache_store_q(const dc_model_cfg* cfg, int32_t bits, const float* h
     DC_TRY(make_geo(cfg, g));
     DC_TRY(make_idx(idx, n, il));
     if (bits != 8 && bits != 4) return Status::arg("bits must be 8 or 4");
-    if (!h_out || !h_in || !codes || !scales) return Status::arg("NULL argument");
+    if (!h_out || !h_in || (g.Nv > 0 && (!codes || !scales))) return Status::arg("NULL argument");
     if (!aligned16(h_out) || !aligned16(h_in) || !aligned16(codes) || !aligned16(scales))
       return Status::arg("device pointers must be 16-byte aligned");
     if (il.n == 0) return Status::ok();
@@ -526,7 +526,7 @@ dc_status dc_cache_apply_q(const dc_model_cfg* cfg, int32_t bits, const float* h
     DC_TRY(make_geo(cfg, g));
     DC_TRY(make_idx(idx, n, il));
     if (bits != 8 && bits != 4) return Status::arg("bits must be 8 or 4");
-    if (!h_in || !codes || !scales || !gout) return Status::arg("NULL argument");
+    if (!h_in || !gout || (g.Nv > 0 && (!codes || !scales))) return Status::arg("NULL argument");
     if (!aligned16(h_in) || !aligned16(gout) || !aligned16(codes) || !aligned16(scales))
       return Status::arg("device pointers must be 16-byte aligned");
     if (il.n == 0) return Status::ok();

@@ -203,6 +203,16 @@ def test_block_refuses_its_products_before_it_starts(lib, f, lat, n_txt, int8):
         assert lib.dc_block_forward(C.byref(c), C.byref(blk), FAKE, FAKE, arr, n, FAKE, nbytes, None) == SHAPE
 
 
+def test_a_text_only_model_has_empty_tables_and_caches(lib):
+    """Without video tokens the table, codes and scales are empty: their (NULL) addresses are not read."""
+    c = cfg(lat=(4, 0, 16))
+    arr, n = idx(0)
+    assert lib.dc_rope_table(C.byref(c), C.byref(axes()), None, None, None) == L.DC_OK
+    assert lib.dc_cache_store_q(C.byref(c), 8, FAKE, FAKE, None, None, arr, n, None) == L.DC_OK
+    assert lib.dc_cache_apply_q(C.byref(c), 4, FAKE, None, None, FAKE, arr, n, None) == L.DC_OK
+    assert lib.dc_cache_apply_q(C.byref(c), 4, None, None, None, FAKE, arr, n, None) == ARG
+
+
 @pytest.mark.parametrize("dtype", [0, 1])
 @pytest.mark.parametrize("hole", ["w_pe", "b_pe", "pos"])
 def test_patch_embedding_refuses_a_missing_table(lib, dtype, hole):
