@@ -292,7 +292,8 @@ typedef struct {
 /* Workspace of dc_block_forward_ext and of a sampler with extended blocks. */
 size_t dc_block_ext_workspace_bytes(const dc_model_cfg* cfg, int32_t batch);
 
-/* dc_block_forward with the extensions of ext (NULL, or both members NULL: the same). */
+/* dc_block_forward with the extensions of ext (NULL, or both members NULL: the same).  A shape that one of
+ * the block's products cannot run (int8: mlp_hidden above 130,944 among them) is refused before h is written. */
 dc_status dc_block_forward_ext(const dc_model_cfg* cfg, const dc_block_weights* blk,
                                const dc_block_ext* ext, const float* mod, float* h, const int32_t* idx,
                                int32_t n, void* ws, size_t ws_bytes, hipStream_t stream);
@@ -383,7 +384,9 @@ size_t dc_calibrate_workspace_bytes(const dc_model_cfg* cfg, int32_t K);
  * device f32 [N_t, d]; sigmas: host f64 [K+1]; q, d: host f64 [(K-1), h_max] out, the
  * q0/d0 (or q1/d1) of dc_sched_problem.  The trace runs the library's kernels of the
  * model's dtype; r, u, the perturbations and the tangents are fp32 (bf16 weights are
- * widened exactly).  head_dim 64 (else DC_ERR_SHAPE).  Waits on `stream` (the table
+ * widened exactly).  Blocks run as dc_block_forward does: the call knows no dc_block_ext, so the
+ * tables of a network with norms, rotation or int8 products are not these.  head_dim 64 (else
+ * DC_ERR_SHAPE).  Waits on `stream` (the table
  * entries are read back). */
 dc_status dc_calibrate_tables(const dc_model_cfg* cfg, const dc_model_weights* w, const float* x1,
                               const float* txt, const double* sigmas, int32_t K, int32_t h_max,

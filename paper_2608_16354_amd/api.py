@@ -166,7 +166,8 @@ def dc_head_euler(dm: DeviceModel, head_mod, g, x, dsigma, idx, ws: Workspace, s
 def dc_calibrate_tables(dm: DeviceModel, x1, txt, sigmas, h_max: int, eps: float, stream=None):
     """Anchor calibration of one clip (Eq. 5-7) on the GPU: returns (q, d), f64
     [(K-1), h_max] each.  x1 [C, T, H, W], txt [N_t, d]: the clip's inputs (torch
-    tensors on the device); sigmas: the K+1 noise levels."""
+    tensors on the device); sigmas: the K+1 noise levels.  The network is dm's with plain
+    blocks: a model that runs with a BlockExt has other tables."""
     torch = _torch()
     sig = np.ascontiguousarray(np.asarray(sigmas, np.float64))
     K = sig.size - 1

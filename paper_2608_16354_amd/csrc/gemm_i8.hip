@@ -8,8 +8,9 @@
 // epilogues are of their own, as is the kernel for few rows (k_i8_split).
 // Long calls are bound by the matrix pipe and the clock that it leaves (1.94 GHz): 16,384 x 16,384 x 8,192 1.69 ms, 2.60
 // POP/s (torch's int8 product 2.25), 2.95 with the LDS-DMA taken out, 3.3 for the instruction alone on such codes in
-// registers (4.9 on zeros: the power that the bits' changes take sets the clock); 17,776 x 1,920 x 7,680 with the gated residual 250 us,
-// 2.10, and at K = 1,920, where a tile has 15 k-steps, by what surrounds them too: MLP up with GELU 278 us, 1.89.
+// registers (4.9 on zeros: the power that the bits' changes take sets the clock).  Launches one behind the other on inputs in
+// turn, M x N x K: MLP down with the gated residual, 17,776 x 1,920 x 7,680, 267 us, 1.97; MLP up with GELU, 17,776 x 7,680 x
+// 1,920, 265 us, 1.98, where a tile's 15 k-steps leave what surrounds them to see; both 250 to 295 us with the box's clock.
 #include "gemm_tile.h"
 
 #include <type_traits>
@@ -431,9 +432,10 @@ Status launch_split(const int8_t* A, int lda, const int8_t* W, int ldw, int M, i
 // Cost in us of tile i, as block_gemm_tile's: rounds of `per_cu` workgroups on each compute unit, each round `fixed`
 // plus k-steps (of 128; groups share them).  One workgroup per compute unit: a k-step takes step[0] on a nearly empty
 // chip to step[1] on a full one; more: step[n - 1] with n of them.  Fitted to timings on MI355X of 228 shapes (M 1 to
-// 17,776; N x K from 256 x 1,024 to 11,520 x 1,920 and 1,920 x 7,680; the splits 132 of them, M up to 800): the tile it
-// picks is 0.3 % slower than the best on average, 10 % at worst.  192 x 128 and 128 x 64 (fitted to 100 shapes, M 300 to
-// 11,000) fill rounds that the others leave half empty: 3,704 x 1,152 x 1,152 9.4 us (11.4 without them), x K = 4,608 26.2
+// 17,776; N x K from 256 x 1,024 to 11,520 x 1,920 and 1,920 x 7,680; the splits 132 of them, M up to 800), 192 x 128 and
+// 128 x 64 to 100 more.  On 212 shapes (twelve N x K of a block's products with each of eleven M from 1 to 800, ten with
+// each of eight M from 1,152 to 17,776) the tile it picks is the best one 182 times, 0.4 % slower on average, 11 % at worst
+// (100 x 1,152 x 4,608: four groups 6.4 us, five 5.8).  192 x 128 and 128 x 64 fill rounds that the others leave half empty: 3,704 x 1,152 x 1,152 9.4 us (11.4 without them), x K = 4,608 26.2
 // (29.2), 800 x 1,920 x 7,680 22.1 (26.5), 1.8 % over the 100; 192 x 256, 128 x 192, 128 x 256 and 320 x 128 add 0.7 %
 // at most.  Few rows take the splits: 1 x 1,920 x 7,680 6.8 us
 // (64 x 64 18.4), 50 x 1,920 x 1,920 4.5 (7.1), 32 x 11,520 x 1,920 6.0 (7.4); 50 x 11,520 x 1,920 stays with 64 x 64,

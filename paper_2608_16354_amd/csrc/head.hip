@@ -27,8 +27,9 @@
 // the Euler update to the two latent values they land on.
 // 17,776 x 3,072: 55 us (216 MB, 3.9 TB/s; an LN pass and a GEMM on its rows took 115);
 // 17,776 x 1,920: 39 us, 42 before; 3,704 x 1,152 (one tile per workgroup): 12.2 us, 15; with a
-// residual 13.3 us, 20; 17,776 x 1,920 with one in bf16 52 us, in 8 bits 51, in 4 bits 49.  What is left over the stream is the prologue, about 7 us of W_head
-// and cs / shw, and the fifth tile of 4.3.
+// residual 13.3 us, 20; 17,776 x 1,920 with one in bf16 49 us, in 8 bits 50, in 4 bits 48 (events around the launches of a
+// 50-step sample; 47 to 52 over boxes).  What is left over the stream is the prologue, about 7 us of W_head and cs / shw, and
+// the fifth tile of 4.3; on codes a chunk takes four DMA instructions where bf16 takes three, for fewer bytes.
 //
 // On a reuse step the head input is g = h_in + r (Eq. 1 with the cached r_j): the
 // variants with a residual read h_in and the residual cache (bf16, or codes of 8 or 4 bits and their
