@@ -99,6 +99,10 @@ struct Args {
     const Py_ssize_t n = PySequence_Fast_GET_SIZE(s);
     bool ok = n <= DC_MAX_BATCH, error = false;
     for (Py_ssize_t j = 0; ok && !error && j < n; ++j) {
+      if (j >= PySequence_Fast_GET_SIZE(s)) {         // an item's __index__ may change the list
+        ok = false;
+        break;
+      }
       const Py_ssize_t v = PyNumber_AsSsize_t(PySequence_Fast_GET_ITEM(s, j), PyExc_ValueError);
       if (v == -1 && PyErr_Occurred()) error = true;
       ok = v >= 0 && v < batch;

@@ -391,6 +391,21 @@ def test_binding_takes_single_tokens_of_any_stride():
     f("x and out", buf[:1, :1].expand(3, 1, 768), out, [0])
 
 
+def test_binding_refuses_a_list_that_shrinks_under_it():
+    """An index that takes the list apart while it is read: nothing is read behind the list's end."""
+    import torch
+    c, samples = cfg(), []
+    h, codes, scales = torch.zeros(2, 272, 256), torch.zeros(2, 256, 256, dtype=torch.int8), torch.zeros(2, 256, 4)
+
+    class Index:
+        def __index__(self):
+            samples.clear()
+            return 0
+
+    samples += [Index(), 1, 1]
+    refused("idx", "dc_cache_apply_q", c, 8, h, h, codes, scales, samples)
+
+
 def test_binding_refuses_overlaps():
     """What is written overlaps nothing that is read, but for the places that may be the same: other columns of a
     buffer's rows, or other rows, are taken."""
