@@ -181,7 +181,7 @@ dc_status dc_head_euler(const dc_model_cfg* cfg, const dc_model_weights* w,
                         hipStream_t stream);
 
 /* ---------------------------------------------------------------------------
- * Rotary positions, query/key norms, int8 products, quantised cache.
+ * Rotary positions, query/key norms, int8 and e4m3 products, quantised cache.
  *
  * What a generator with rotary positions or a reduced-precision refresh needs beside the
  * steps above.  dc_block_forward_ext and dc_sampler_create_ext run them inside a block
@@ -257,6 +257,79 @@ typedef struct {
   int64_t ld_out;                 /* >= out_features, rows at any element's address */
 } dc_linear_i8_args;
 dc_status dc_linear_i8(const dc_linear_i8_args* args, hipStream_t stream);
+
+/* 8-bit floating point: e4m3 codes (sign, 4 exponent bits of bias 7, 3 fraction bits; largest 448, no infinities, 0x7F
+ * and 0xFF NaN) with an fp32 scale for each block of 128 features.  For a block with largest magnitude a: scale =
+ * a / 448, code = v / scale (both divisions rounded to fp32, the quotient bounded to +-448) to the nearest e4m3 number,
+ * ties to even.  A block of zeros has scale 0 and codes 0; one with an infinity or NaN has scale NaN and codes 0,
+ * so a product with it is NaN.  Rows of codes are padded with zeros to whole blocks; a last block's scale is that of
+ * the features it has.  Scales are at scale[row * scale_row + block * scale_block] (strides in elements; scale_row = 1,
+ * scale_block >= rows is what the kernels write and read fastest); written ones may not share an address. */
+
+/* Rows (block_rows 1: a scale to 128 features of a row) or a weight matrix [out, in] (block_rows 128: a scale to
+ * 128 x 128 values) in e4m3. */
+typedef struct {
+  int32_t rows, cols;             /* below 2^24; rows = 0 is a no-op */
+  const void* x;                  /* [rows, ld_x], at any element's address; ld_x >= cols */
+  int32_t x_dtype;                /* dc_dtype */
+  int64_t ld_x;
+  int32_t block_rows;             /* 1 or 128 */
+  uint8_t* q;                     /* [rows, ld_q], 8-byte aligned; ld_q: a multiple of 8, at least cols rounded up to 128.
+                                     Columns up to there are written, later ones left as they were */
+  int64_t ld_q;
+  float* scale;                   /* of [rows, or rows / 128 rounded up][cols / 128 rounded up] blocks */
+  int64_t scale_row, scale_block;
+} dc_quantize_f8_args;
+dc_status dc_quantize_f8(const dc_quantize_f8_args* args, hipStream_t stream);
+
+/* h = x + residual in fp32; sum := h, rounded once to its type; y = h / sqrt(mean(h^2) + eps) * weight over the row, of the
+ * unrounded h; q, scale := y in e4m3, a scale to 128 features, as dc_quantize_f8 writes rows.  A row's mean square must
+ * be below the fp32 range (|h| < 1e18). */
+typedef struct {
+  int32_t rows, cols;             /* rows below 2^24 (0 is a no-op), cols up to 16,384 */
+  const void* x;                  /* [rows, ld_x], at any element's address; leading dimensions >= cols */
+  int32_t x_dtype;                /* dc_dtype, as below */
+  int64_t ld_x;
+  const void* residual;           /* [rows, ld_residual] or NULL: h = x */
+  int32_t residual_dtype;
+  int64_t ld_residual;
+  void* sum;                      /* [rows, ld_sum] or NULL; may be x or residual (same type and ld), else overlaps neither */
+  int32_t sum_dtype;
+  int64_t ld_sum;
+  const float* weight;            /* [cols] or NULL: 1 */
+  float eps;                      /* > 0 */
+  uint8_t* q;                     /* as dc_quantize_f8's */
+  int64_t ld_q;
+  float* scale;
+  int64_t scale_row, scale_block;
+} dc_rms_norm_f8_args;
+dc_status dc_rms_norm_f8(const dc_rms_norm_f8_args* args, hipStream_t stream);
+
+/* out[m, n] = f(sum over blocks b of x_scale[m, b] w_scale[n / 128, b] sum_{k in b} x[m, k] w[n, k] + bias[n]): products
+ * exact, sums in fp32 in a fixed order (bitwise reproducible), one rounding to out_dtype.  With DC_BF16 the 128 products
+ * of a block are summed eight at a time with 15 bits and more behind the largest of the eight.  f: the value itself, GELU
+ * (tanh form), or residual[m, n] + gate[n] * value. */
+typedef struct {
+  int32_t rows, out_features;     /* M, N, below 2^24; rows = 0 is a no-op */
+  int32_t in_features;            /* K with its padding: a multiple of 128, at most 2^22 */
+  const uint8_t* x;               /* [rows, ld_x], 16-byte aligned; ld_x: K to 2^22, a multiple of 16 */
+  int64_t ld_x;
+  const float* x_scale;           /* [rows][K / 128]; strides from 0 (one scale for all) on, x_scale_row below 2^21 */
+  int64_t x_scale_row, x_scale_block;
+  const uint8_t* w;               /* [out_features, ld_w], as x */
+  int64_t ld_w;
+  const float* w_scale;           /* [out_features / 128 rounded up][K / 128]; strides as x_scale's */
+  int64_t w_scale_row, w_scale_block;
+  const float* bias;              /* [out_features] or NULL */
+  int32_t gelu;                   /* 1: GELU; not with a residual */
+  const float* gate;              /* [out_features], with a residual; NULL: 1 */
+  const void* residual;           /* [rows, ld_residual] of out_dtype, or NULL; may be out (same ld) */
+  int64_t ld_residual;
+  void* out;                      /* [rows, ld_out]; overlaps no other operand */
+  int32_t out_dtype;              /* dc_dtype */
+  int64_t ld_out;                 /* >= out_features, rows at any element's address */
+} dc_linear_f8_args;
+dc_status dc_linear_f8(const dc_linear_f8_args* args, hipStream_t stream);
 
 /* The residual cache in `bits` = 8 or 4 bits, a scale per 64 features: for r = h_out - h_in on the
  * video rows, scale = max |r| / L over the group (L = 127 or 7), code = r / scale rounded to the
@@ -489,7 +562,7 @@ void dc_sampler_destroy(dc_sampler* s);
  * 4 MLP-down GEMM, 5 AdaLN modulation, 6 patch embedding, 7 drift reduction,
  * 8 cache store, 9 cache apply, 10 head + Euler, 11 head + Euler on a reuse step of a
  * bf16 model (its input g = h_in + r formed in the kernel), 12 query/key norms and rotation,
- * 13 quantisation of rows (LN-modulated rows included).
+ * 13 quantisation of rows (LN-modulated and e4m3 rows, those of dc_rms_norm_f8 too, included).
  * ------------------------------------------------------------------------- */
 
 /* Bit c of mask enables timing of class c: each launch is bracketed by two

@@ -1,4 +1,4 @@
-"""Rotary positions, query/key norms, int8 rows and the quantised cache, from their definitions.
+"""Rotary positions, query/key norms, int8 and e4m3 rows and the quantised cache, from their definitions.
 
 Test infrastructure only (see oracle/__init__.py).  Angles, norms, rotations and sums in float64.  Codes
 go by fp32 divisions (a scale is an fp32 number, and x / scale is rounded to fp32 before it is rounded to
@@ -69,6 +69,57 @@ def int8_rows(x):
     """The values that int8 rows stand for."""
     q, s = codes(x, 127)
     return q.astype(F) * s[..., None].astype(F)
+
+
+E4M3_TOP = 448.0
+
+
+def e4m3(v):
+    """The nearest e4m3 number (three fraction bits, exponents from -6 on, at most 448), ties to even."""
+    v = np.asarray(v, F)
+    step = np.exp2(np.floor(np.log2(np.maximum(np.abs(v), 2.0 ** -6))) - 3)
+    return np.clip(np.rint(v / step) * step, -E4M3_TOP, E4M3_TOP)
+
+
+def e4m3_blocks(x, block_rows=1):
+    """(numbers that the codes are [R, C padded], scales [blocks of rows, blocks of 128]) of x [R, C]."""
+    x = np.asarray(x, np.float32)
+    rows, cols = x.shape
+    nr, nb = -(-rows // block_rows), -(-cols // 128)
+    v = np.zeros((nr * block_rows, nb * 128), np.float32)
+    v[:rows, :cols] = x
+    v = v.reshape(nr, block_rows, nb, 128)
+    with np.errstate(all="ignore"):
+        scale = np.abs(v).max((1, 3)) / np.float32(E4M3_TOP)
+        scale = np.where(np.isfinite(v).all((1, 3)), scale, np.float32(np.nan)).astype(np.float32)
+        step = scale[:, None, :, None]
+        q = np.where(step > 0, np.clip(v / step, -E4M3_TOP, E4M3_TOP), np.float32(0))
+    return e4m3(q).reshape(nr * block_rows, nb * 128)[:rows], scale
+
+
+def e4m3_values(q, scale, block_rows=1):
+    """What codes with these scales stand for, padding included."""
+    s = np.repeat(np.repeat(np.asarray(scale, F), block_rows, 0)[: len(q)], 128, 1)
+    return np.asarray(q, F) * s
+
+
+def rms_norm(h, weight, eps):
+    h = np.asarray(h, F)
+    y = h / np.sqrt((h * h).mean(-1, keepdims=True) + eps)
+    return y if weight is None else y * np.asarray(weight, F)
+
+
+def linear_f8(x, x_scale, w, w_scale, bias=None, gelu=False, gate=None, residual=None):
+    """dc_linear_f8 on the numbers that codes are, and the sums of its products' magnitudes."""
+    a, b = e4m3_values(x, x_scale), e4m3_values(w, w_scale, 128)
+    y, size = a @ b.T, np.abs(a) @ np.abs(b).T
+    if bias is not None:
+        y = y + np.asarray(bias, F)
+    if gelu:
+        y = dit.gelu_tanh(y)
+    if gate is not None:
+        y = y * np.asarray(gate, F)
+    return (y if residual is None else np.asarray(residual, F) + y), size
 
 
 def block(P, l, mod6, h, qk=None, int8=False):

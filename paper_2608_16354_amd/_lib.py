@@ -79,6 +79,27 @@ class LinearI8Args(C.Structure):
                 ("ld_residual", C.c_int64), ("out", vp), ("out_dtype", C.c_int32), ("ld_out", C.c_int64)]
 
 
+class QuantizeF8Args(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("cols", C.c_int32), ("x", vp), ("x_dtype", C.c_int32), ("ld_x", C.c_int64),
+                ("block_rows", C.c_int32), ("q", vp), ("ld_q", C.c_int64), ("scale", vp), ("scale_row", C.c_int64),
+                ("scale_block", C.c_int64)]
+
+
+class RmsNormF8Args(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("cols", C.c_int32), ("x", vp), ("x_dtype", C.c_int32), ("ld_x", C.c_int64),
+                ("residual", vp), ("residual_dtype", C.c_int32), ("ld_residual", C.c_int64), ("sum", vp),
+                ("sum_dtype", C.c_int32), ("ld_sum", C.c_int64), ("weight", vp), ("eps", C.c_float), ("q", vp),
+                ("ld_q", C.c_int64), ("scale", vp), ("scale_row", C.c_int64), ("scale_block", C.c_int64)]
+
+
+class LinearF8Args(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("out_features", C.c_int32), ("in_features", C.c_int32), ("x", vp),
+                ("ld_x", C.c_int64), ("x_scale", vp), ("x_scale_row", C.c_int64), ("x_scale_block", C.c_int64),
+                ("w", vp), ("ld_w", C.c_int64), ("w_scale", vp), ("w_scale_row", C.c_int64),
+                ("w_scale_block", C.c_int64), ("bias", vp), ("gelu", C.c_int32), ("gate", vp), ("residual", vp),
+                ("ld_residual", C.c_int64), ("out", vp), ("out_dtype", C.c_int32), ("ld_out", C.c_int64)]
+
+
 class BlockWeightsI8(C.Structure):
     _fields_ = [("w_qkv", vp), ("s_qkv", vp), ("w_o", vp), ("s_o", vp), ("w_1", vp), ("s_1", vp),
                 ("w_2", vp), ("s_2", vp)]
@@ -121,6 +142,9 @@ SIGNATURES = {
                                     C.c_int32, vp]),
     "dc_quantize_rows": (C.c_int32, [vp, C.c_int32, C.c_int64, C.c_int32, C.c_int32, vp, C.c_int64, vp, vp]),
     "dc_linear_i8": (C.c_int32, [P(LinearI8Args), vp]),
+    "dc_quantize_f8": (C.c_int32, [P(QuantizeF8Args), vp]),
+    "dc_rms_norm_f8": (C.c_int32, [P(RmsNormF8Args), vp]),
+    "dc_linear_f8": (C.c_int32, [P(LinearF8Args), vp]),
     "dc_cache_store_q": (C.c_int32, [P(ModelCfg), C.c_int32, vp, vp, vp, vp, i32p, C.c_int32, vp]),
     "dc_cache_apply_q": (C.c_int32, [P(ModelCfg), C.c_int32, vp, vp, vp, vp, i32p, C.c_int32, vp]),
     "dc_block_ext_workspace_bytes": (C.c_size_t, [P(ModelCfg), C.c_int32]),
@@ -191,7 +215,7 @@ def binding():
                               "python -m paper_2608_16354_amd.build") from e
         b.init(*[C.cast(getattr(lib, n), vp).value for n in (
             "dc_rope_table", "dc_qk_norm_rope", "dc_quantize_rows", "dc_linear_i8", "dc_cache_store_q",
-            "dc_cache_apply_q")])
+            "dc_cache_apply_q", "dc_quantize_f8", "dc_rms_norm_f8", "dc_linear_f8")])
         _binding = b
     return _binding
 

@@ -18,7 +18,8 @@ __all__ = ["model_cfg", "DeviceModel", "Workspace", "SamplerBuffers", "profile",
            "dc_patch_embed", "dc_block_forward", "dc_cache_store", "dc_cache_apply",
            "dc_drift_l1", "dc_head_euler", "dc_schedule_dp", "dc_select_tau", "dc_motion_statistics",
            "dc_select_anchors", "Sampler", "rope_axes", "dc_rope_table", "dc_qk_norm_rope", "dc_quantize_rows",
-           "dc_linear_i8", "dc_cache_store_q", "dc_cache_apply_q", "BlockExt", "dc_block_forward_ext"]
+           "dc_linear_i8", "dc_quantize_f8", "dc_rms_norm_f8", "dc_linear_f8", "dc_cache_store_q", "dc_cache_apply_q", "BlockExt",
+           "dc_block_forward_ext"]
 
 
 def _torch():
@@ -188,7 +189,7 @@ def dc_calibrate_tables(dm: DeviceModel, x1, txt, sigmas, h_max: int, eps: float
 
 
 # ----------------------------------------------------------------------------
-# rotary positions, query/key norms, int8 products, quantised cache
+# rotary positions, query/key norms, int8 and e4m3 products, quantised cache
 # ----------------------------------------------------------------------------
 # These calls take a few microseconds on the GPU: binding.cpp checks their tensors (ValueError) and makes the C call.
 _current = None         # torch's (raw stream of a device, current device)
@@ -253,6 +254,26 @@ def dc_linear_i8(x, x_scale, w, w_scale, out, bias=None, gelu=False, gate=None, 
     """out [M, N] := the product of int8 rows x [M, K] and w [N, K] (K as padded by dc_quantize_rows) with
     their scales, plus bias, through GELU or as residual + gate * (...)."""
     _call("dc_linear_i8", stream, x, x, x_scale, w, w_scale, out, bias, gelu, gate, residual)
+
+
+def dc_quantize_f8(x, q, scale, block_rows=1, stream=None):
+    """q (float8_e4m3fn [rows, at least cols rounded up to 128]) and scale (f32 [rows, cols / 128 rounded up], any
+    strides; torch.empty((blocks, rows)).t() is the fastest) := the rows of x [rows, cols], a scale to 128 features.
+    block_rows=128: a weight matrix, scale [rows / 128 rounded up, ...], one to 128 x 128 values."""
+    _call("dc_quantize_f8", stream, x, x, q, scale, block_rows)
+
+
+def dc_rms_norm_f8(x, q, scale, weight=None, eps=1e-6, residual=None, out=None, stream=None):
+    """q and scale (as dc_quantize_f8's) := the RMS norm of x + residual, times weight (f32 [cols]); out (float32 or
+    bfloat16, may be x or residual) := that sum.  x [rows, cols], cols up to 16,384; residual and out like it or None."""
+    _call("dc_rms_norm_f8", stream, x, x, q, scale, weight, eps, residual, out)
+
+
+def dc_linear_f8(x, x_scale, w, w_scale, out, bias=None, gelu=False, gate=None, residual=None, stream=None):
+    """out [M, N] := the product of e4m3 rows x [M, K] and w [N, K] (K as padded by dc_quantize_f8) with their scales
+    ([M, K / 128], [N / 128 rounded up, K / 128], any strides), plus bias, through GELU or as residual + gate * (...)
+    (residual of out's type; gate None: 1)."""
+    _call("dc_linear_f8", stream, x, x, x_scale, w, w_scale, out, bias, gelu, gate, residual)
 
 
 def dc_cache_store_q(cfg, bits, h_out, h_in, codes, scales, idx, stream=None):

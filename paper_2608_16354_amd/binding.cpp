@@ -1,4 +1,4 @@
-// Tensor arguments of the calls that take a few microseconds (rotary table, norms and rotation, int8 rows and
+// Tensor arguments of the calls that take a few microseconds (rotary table, norms and rotation, int8 and e4m3 rows and
 // products, quantised cache): checks types, shapes, strides and devices, fills the C structs and makes the call.  In
 // Python the same attribute reads cost about 4 us a call, as much as the launch; here 0.3 us.  Nothing is
 // computed or kept.  The library's functions come as addresses from the ctypes binding (init), so there is one copy
@@ -20,6 +20,9 @@ decltype(&dc_quantize_rows) f_quantize_rows;
 decltype(&dc_linear_i8) f_linear_i8;
 decltype(&dc_cache_store_q) f_cache_store_q;
 decltype(&dc_cache_apply_q) f_cache_apply_q;
+decltype(&dc_quantize_f8) f_quantize_f8;
+decltype(&dc_rms_norm_f8) f_rms_norm_f8;
+decltype(&dc_linear_f8) f_linear_f8;
 
 // A refusal: becomes a ValueError (or keeps the Python error that is set).
 struct Refused {};
@@ -296,6 +299,165 @@ PyObject* linear_i8(PyObject* const* args, Py_ssize_t n) {  // x, x_scale, w, w_
   return call(a, [&] { return f_linear_i8(&p, a.stream); });
 }
 
+// Scales of [rows, blocks] blocks: an fp32 tensor of any strides (those of a dimension of one say nothing); where they
+// are written, no two of them may share an address.
+struct Scales {
+  float* p;
+  int64_t rows, blocks, row, block;
+  Scales(const at::Tensor& t, int64_t rows_, int64_t blocks_, bool written, const char* what)
+      : p(static_cast<float*>(t.data_ptr())), rows(rows_), blocks(blocks_) {
+    need(t.scalar_type() == at::kFloat && t.dim() == 2 && t.size(0) == rows && t.size(1) == blocks, what);
+    row = t.stride(0);
+    block = t.stride(1);
+    if (rows <= 1) row = 1;
+    if (blocks <= 1) block = std::max(rows, int64_t(1)) * row;
+    if (written && rows > 0)
+      need(row >= 1 && block >= 1 && (row >= (blocks - 1) * block + 1 || block >= (rows - 1) * row + 1), what);
+  }
+  // all bytes from the first to the last
+  Span span() const {
+    const int64_t n = rows < 1 || blocks < 1 ? 0 : ((rows - 1) * row + (blocks - 1) * block + 1) * 4;
+    return Span(p, 1, n, n);
+  }
+};
+constexpr const char* kCodes = "codes: a float8_e4m3fn tensor of contiguous rows, whole blocks of 128 wide, is wanted";
+
+// x, q, scale, block_rows
+PyObject* quantize_f8(PyObject* const* args, Py_ssize_t n) {
+  const Args a(args, n, 6);
+  const at::Tensor &x = a.tensor(0), &q = a.tensor(1);
+  dc_quantize_f8_args p{};
+  p.ld_x = rows(x, "x: a 2-d tensor with contiguous rows that do not overlap is wanted");
+  p.ld_q = rows(q, kCodes);
+  const int64_t m = x.size(0), cols = x.size(1), blocks = (cols + 127) / 128, block_rows = a.whole_number(a.a[3]);
+  need(block_rows == 1 || block_rows == 128, "block_rows must be 1 or 128");
+  need(q.scalar_type() == at::kFloat8_e4m3fn && q.size(0) == m && q.size(1) >= blocks * 128, kCodes);
+  if (m <= 1) p.ld_q = blocks * 128;            // one row: a stride that the width need not keep
+  const Scales s(a.tensor(2), (m + block_rows - 1) / block_rows, blocks, true,
+                 "scale: a float32 [blocks of rows, cols / 128 rounded up] tensor with an address for each is wanted");
+  p.rows = i32(m);
+  p.cols = i32(cols);
+  p.x = x.data_ptr();
+  p.x_dtype = dtype(x);
+  p.block_rows = int32_t(block_rows);
+  p.q = static_cast<uint8_t*>(q.data_ptr());
+  p.scale = s.p;
+  p.scale_row = s.row;
+  p.scale_block = s.block;
+  const Span from(p.x, m, p.ld_x * x.element_size(), cols * x.element_size()), to(p.q, m, p.ld_q, blocks * 128);
+  need(!overlap(to, from) && !overlap(s.span(), from) && !overlap(s.span(), to), "x, q and scale overlap");
+  return call(a, [&] { return f_quantize_f8(&p, a.stream); });
+}
+
+// x, q, scale, weight, eps, residual, out
+PyObject* rms_norm_f8(PyObject* const* args, Py_ssize_t n) {
+  const Args a(args, n, 9);
+  const at::Tensor &x = a.tensor(0), &q = a.tensor(1);
+  const char* like_x = "x, residual and out: 2-d tensors of one shape with contiguous rows that do not overlap are wanted";
+  dc_rms_norm_f8_args p{};
+  p.ld_x = rows(x, like_x);
+  p.ld_q = rows(q, kCodes);
+  const int64_t m = x.size(0), cols = x.size(1), blocks = (cols + 127) / 128;
+  need(q.scalar_type() == at::kFloat8_e4m3fn && q.size(0) == m && q.size(1) >= blocks * 128, kCodes);
+  if (m <= 1) p.ld_q = blocks * 128;
+  const Scales s(a.tensor(2), m, blocks, true,
+                 "scale: a float32 [rows, cols / 128 rounded up] tensor with an address for each is wanted");
+  const Span from(x.data_ptr(), m, p.ld_x * x.element_size(), cols * x.element_size()), codes(q.data_ptr(), m, p.ld_q, blocks * 128);
+  bool apart = !overlap(codes, from) && !overlap(s.span(), from) && !overlap(s.span(), codes);
+  p.rows = i32(m);
+  p.cols = i32(cols);
+  p.x = x.data_ptr();
+  p.x_dtype = dtype(x);
+  p.weight = a.vector(3, cols, "weight: a contiguous float32 [cols] tensor is wanted");
+  if (p.weight) {
+    const Span w(*a.maybe(3));
+    apart = apart && !overlap(codes, w) && !overlap(s.span(), w);
+  }
+  p.eps = float(a.number(4));
+  const at::Tensor *r = a.maybe(5), *out = a.maybe(6);
+  auto take = [&](const at::Tensor& t) {        // its leading dimension
+    const int64_t ld = rows(t, like_x), e = t.element_size();
+    need(t.size(0) == m && t.size(1) == cols, like_x);
+    const Span at(t.data_ptr(), m, ld * e, cols * e);
+    apart = apart && !overlap(codes, at) && !overlap(s.span(), at);
+    return ld;
+  };
+  if (r) {
+    p.ld_residual = take(*r);
+    p.residual = r->data_ptr();
+    p.residual_dtype = dtype(*r);
+  }
+  if (out) {
+    p.ld_sum = take(*out);
+    p.sum = out->data_ptr();
+    p.sum_dtype = dtype(*out);
+  }
+  if (out) {
+    const int64_t e = out->element_size();
+    const Span to(p.sum, m, p.ld_sum * e, cols * e);
+    if (p.weight) apart = apart && !overlap(to, Span(*a.maybe(3)));
+    if (!(p.sum == p.x && p.ld_sum == p.ld_x && p.sum_dtype == p.x_dtype)) apart = apart && !overlap(to, from);
+    if (r && !(p.sum == p.residual && p.ld_sum == p.ld_residual && p.sum_dtype == p.residual_dtype))
+      apart = apart && !overlap(to, Span(p.residual, m, p.ld_residual * r->element_size(), cols * r->element_size()));
+  }
+  need(apart, "results overlap operands or one another: out may be x or residual itself");
+  p.q = static_cast<uint8_t*>(q.data_ptr());
+  p.scale = s.p;
+  p.scale_row = s.row;
+  p.scale_block = s.block;
+  return call(a, [&] { return f_rms_norm_f8(&p, a.stream); });
+}
+
+// x, x_scale, w, w_scale, out, bias, gelu, gate, residual
+PyObject* linear_f8(PyObject* const* args, Py_ssize_t n) {
+  const Args a(args, n, 11);
+  const at::Tensor &x = a.tensor(0), &w = a.tensor(2), &out = a.tensor(4);
+  const char* two_d = "x, w, out and residual: 2-d tensors with contiguous rows that do not overlap are wanted";
+  dc_linear_f8_args p{};
+  p.ld_x = rows(x, two_d);
+  p.ld_w = rows(w, two_d);
+  p.ld_out = rows(out, two_d);
+  const int64_t m = x.size(0), k = x.size(1), cols = w.size(0);
+  need(x.scalar_type() == at::kFloat8_e4m3fn && w.scalar_type() == at::kFloat8_e4m3fn && w.size(1) == k && k % 128 == 0,
+       "x and w: float8_e4m3fn tensors of equally long rows, whole blocks of 128, are wanted");
+  need(out.size(0) == m && out.size(1) == cols, "out: a [rows of x, rows of w] tensor is wanted");
+  const Scales sx(a.tensor(1), m, k / 128, false, "x_scale: a float32 [rows of x, K / 128] tensor is wanted");
+  const Scales sw(a.tensor(3), (cols + 127) / 128, k / 128, false,
+                  "w_scale: a float32 [rows of w / 128 rounded up, K / 128] tensor is wanted");
+  p.rows = i32(m);
+  p.out_features = i32(cols);
+  p.in_features = i32(k);
+  p.x = static_cast<const uint8_t*>(x.data_ptr());
+  p.x_scale = sx.p;
+  p.x_scale_row = sx.row;
+  p.x_scale_block = sx.block;
+  p.w = static_cast<const uint8_t*>(w.data_ptr());
+  p.w_scale = sw.p;
+  p.w_scale_row = sw.row;
+  p.w_scale_block = sw.block;
+  p.out = out.data_ptr();
+  p.out_dtype = dtype(out);
+  p.bias = a.vector(5, cols, "bias: a contiguous float32 [rows of w] tensor is wanted");
+  p.gelu = a.truth(6) ? 1 : 0;
+  p.gate = a.vector(7, cols, "gate: a contiguous float32 [rows of w] tensor is wanted");
+  const int64_t e = out.element_size();
+  const Span to(out.data_ptr(), m, p.ld_out * e, cols * e);
+  bool apart = !overlap(to, Span(p.x, m, p.ld_x, k)) && !overlap(to, Span(p.w, cols, p.ld_w, k)) && !overlap(to, sx.span()) &&
+               !overlap(to, sw.span());
+  for (const int i : {5, 7})
+    if (const at::Tensor* t = a.maybe(i)) apart = apart && !overlap(to, Span(*t));
+  if (const at::Tensor* r = a.maybe(8)) {
+    p.ld_residual = rows(*r, two_d);
+    need(r->scalar_type() == out.scalar_type() && r->size(0) == m && r->size(1) == cols,
+         "residual: a tensor of out's type and shape is wanted");
+    p.residual = r->data_ptr();
+    if (!(p.residual == p.out && p.ld_residual == p.ld_out))
+      apart = apart && !overlap(to, Span(p.residual, m, p.ld_residual * e, cols * e));
+  }
+  need(apart, "out overlaps another operand: the residual itself, or other rows or columns, are wanted");
+  return call(a, [&] { return f_linear_f8(&p, a.stream); });
+}
+
 // cfg, bits, first, second, codes, scales, idx: first and second are h_out and h_in (store) or h_in and g (apply)
 template <bool STORE>
 PyObject* cache_q(PyObject* const* args, Py_ssize_t n) {
@@ -335,12 +497,12 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 // addresses of the library's functions, in the order of the pointers above
 PyObject* init(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  void* p[6];
-  if (n != 6) {
-    PyErr_SetString(PyExc_ValueError, "six addresses are wanted");
+  void* p[9];
+  if (n != 9) {
+    PyErr_SetString(PyExc_ValueError, "nine addresses are wanted");
     return nullptr;
   }
-  for (int i = 0; i < 6; ++i) {
+  for (int i = 0; i < 9; ++i) {
     p[i] = PyLong_AsVoidPtr(args[i]);
     if (PyErr_Occurred()) return nullptr;
   }
@@ -350,6 +512,9 @@ PyObject* init(PyObject*, PyObject* const* args, Py_ssize_t n) {
   f_linear_i8 = reinterpret_cast<decltype(f_linear_i8)>(p[3]);
   f_cache_store_q = reinterpret_cast<decltype(f_cache_store_q)>(p[4]);
   f_cache_apply_q = reinterpret_cast<decltype(f_cache_apply_q)>(p[5]);
+  f_quantize_f8 = reinterpret_cast<decltype(f_quantize_f8)>(p[6]);
+  f_rms_norm_f8 = reinterpret_cast<decltype(f_rms_norm_f8)>(p[7]);
+  f_linear_f8 = reinterpret_cast<decltype(f_linear_f8)>(p[8]);
   Py_RETURN_NONE;
 }
 
@@ -359,6 +524,9 @@ PyMethodDef methods[] = {ENTRY("init", init),
                          ENTRY("dc_qk_norm_rope", entry<qk_norm_rope>),
                          ENTRY("dc_quantize_rows", entry<quantize_rows>),
                          ENTRY("dc_linear_i8", entry<linear_i8>),
+                         ENTRY("dc_quantize_f8", entry<quantize_f8>),
+                         ENTRY("dc_rms_norm_f8", entry<rms_norm_f8>),
+                         ENTRY("dc_linear_f8", entry<linear_f8>),
                          ENTRY("dc_cache_store_q", entry<cache_q<true>>),
                          ENTRY("dc_cache_apply_q", entry<cache_q<false>>),
                          {nullptr, nullptr, 0, nullptr}};

@@ -26,8 +26,8 @@ ARCH = "gfx950"
 HIPCC_FLAGS = ["-O3", "-fPIC", "-std=c++17", f"--offload-arch={ARCH}",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
                "-ffp-contract=fast", "-Wall", "-Wno-unused-result"]
-# per-file extra flags: keep MFMA accumulators in VGPRs where the softmax reads them
-EXTRA_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=true"]}
+# per-file extra flags: keep MFMA results in VGPRs where the softmax or the blocks' scales read them
+EXTRA_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form=true"] for f in ("attention.hip", "gemm_f8.hip")}
 HOST_FLAGS = ["-O2", "-fPIC", "-std=c++17", "-ffp-contract=off", "-D__HIP_PLATFORM_AMD__",
               f"-I{ROCM}/include", "-Wall"]
 

@@ -501,6 +501,102 @@ dc_status dc_linear_i8(const dc_linear_i8_args* p, hipStream_t stream) {
   })());
 }
 
+// [rows, ld] fp32 or bf16 values
+static Status check_rows(const void* x, int32_t dtype, int64_t ld, int32_t cols, const char* what) {
+  if (dtype != DC_F32 && dtype != DC_BF16) return Status::make(DC_ERR_DTYPE, "unknown dtype");
+  if (ld < cols) return Status::arg(std::string(what) + ": the leading dimension must be at least cols");
+  if (!aligned(x, dtype == DC_BF16 ? 2 : 4)) return Status::arg("a pointer is not aligned to its element");
+  return Status::ok();
+}
+static Status check_codes(const uint8_t* q, int64_t ld, int32_t cols) {
+  if (!q) return Status::arg("NULL argument");
+  if (!aligned(q, 8) || ld % 8 || ld < (int64_t(cols) + 127) / 128 * 128)
+    return Status::arg("q must be 8-byte aligned, ld_q a multiple of 8, at least cols rounded up to 128");
+  return Status::ok();
+}
+// scales of rows x blocks, each at an address of its own where they are written
+static Status check_scales(const float* p, int64_t row, int64_t block, int64_t rows, int64_t blocks, bool written) {
+  if (!p) return Status::arg("NULL argument");
+  if (!aligned(p, 4)) return Status::arg("a pointer is not aligned to its element");
+  const int64_t least = written ? 1 : 0, most = int64_t(1) << 31;
+  if ((rows > 1 && (row < least || row > most)) || (blocks > 1 && (block < least || block > most)))
+    return Status::arg("strides of scales: 0 (1 where they are written) to 2^31");
+  if (written && rows > 1 && blocks > 1 && row <= (blocks - 1) * block && block <= (rows - 1) * row)
+    return Status::arg("written scales must not share an address");
+  return Status::ok();
+}
+
+dc_status dc_quantize_f8(const dc_quantize_f8_args* p, hipStream_t stream) {
+  DC_ENTRY(([&]() -> Status {
+    if (!p) return Status::arg("NULL argument");
+    if (p->block_rows != 1 && p->block_rows != 128) return Status::arg("block_rows must be 1 or 128");
+    if (p->rows < 0 || p->rows >= (1 << 24) || p->cols < 1 || p->cols >= (1 << 24))
+      return Status::arg("rows must be in [0, 2^24), cols in [1, 2^24)");
+    DC_TRY(check_rows(p->x, p->x_dtype, p->ld_x, p->cols, "x"));
+    if (p->rows == 0) return Status::ok();
+    if (!p->x) return Status::arg("NULL argument");
+    DC_TRY(check_codes(p->q, p->ld_q, p->cols));
+    DC_TRY(check_scales(p->scale, p->scale_row, p->scale_block, (p->rows + p->block_rows - 1) / p->block_rows,
+                        (p->cols + 127) / 128, true));
+    ProfScope ps(KClass::kQuantize, stream);
+    return quantize_f8(*p, stream);
+  })());
+}
+
+dc_status dc_rms_norm_f8(const dc_rms_norm_f8_args* p, hipStream_t stream) {
+  DC_ENTRY(([&]() -> Status {
+    if (!p) return Status::arg("NULL argument");
+    if (p->rows < 0 || p->rows >= (1 << 24) || p->cols < 1 || p->cols > kMaxNormCols)
+      return Status::arg("rows must be in [0, 2^24), cols in [1, 16,384]");
+    DC_TRY(check_rows(p->x, p->x_dtype, p->ld_x, p->cols, "x"));
+    if (p->residual) DC_TRY(check_rows(p->residual, p->residual_dtype, p->ld_residual, p->cols, "residual"));
+    if (p->sum) DC_TRY(check_rows(p->sum, p->sum_dtype, p->ld_sum, p->cols, "sum"));
+    if (!(p->eps > 0.f && std::isfinite(p->eps))) return Status::arg("eps must be positive");
+    if (p->rows == 0) return Status::ok();
+    if (!p->x) return Status::arg("NULL argument");
+    if ((p->sum && p->sum == p->x && (p->ld_sum != p->ld_x || p->sum_dtype != p->x_dtype)) ||
+        (p->sum && p->sum == p->residual && (p->ld_sum != p->ld_residual || p->sum_dtype != p->residual_dtype)))
+      return Status::arg("in place: types and leading dimensions must be equal");
+    if (!aligned(p->weight, 4)) return Status::arg("a pointer is not aligned to its element");
+    DC_TRY(check_codes(p->q, p->ld_q, p->cols));
+    DC_TRY(check_scales(p->scale, p->scale_row, p->scale_block, p->rows, (p->cols + 127) / 128, true));
+    ProfScope ps(KClass::kQuantize, stream);
+    return rms_norm_f8(*p, stream);
+  })());
+}
+
+dc_status dc_linear_f8(const dc_linear_f8_args* p, hipStream_t stream) {
+  DC_ENTRY(([&]() -> Status {
+    if (!p) return Status::arg("NULL argument");
+    if (p->out_dtype != DC_F32 && p->out_dtype != DC_BF16) return Status::make(DC_ERR_DTYPE, "unknown dtype");
+    if (p->rows < 0 || p->rows >= (1 << 24) || p->out_features < 1 || p->out_features >= (1 << 24))
+      return Status::arg("rows must be in [0, 2^24), out_features in [1, 2^24)");
+    if (p->gelu != 0 && p->gelu != 1) return Status::arg("gelu must be 0 or 1");
+    if (p->gate && !p->residual) return Status::arg("a gate goes with a residual");
+    if (p->residual && p->gelu) return Status::arg("GELU does not go with a residual");
+    if (p->ld_out < p->out_features || (p->residual && p->ld_residual < p->out_features))
+      return Status::arg("ld_out and ld_residual must be at least out_features");
+    if (p->rows == 0) return Status::ok();
+    if (!p->x || !p->x_scale || !p->w || !p->w_scale || !p->out) return Status::arg("NULL argument");
+    if (!aligned16(p->x) || !aligned16(p->w)) return Status::arg("x and w must be 16-byte aligned");
+    const size_t e = p->out_dtype == DC_BF16 ? 2 : 4;
+    if (!aligned(p->bias, 4) || !aligned(p->gate, 4) || !aligned(p->residual, e) || !aligned(p->out, e))
+      return Status::arg("a pointer is not aligned to its element");
+    if (p->residual == p->out && p->ld_residual != p->ld_out)
+      return Status::arg("in place: ld_residual and ld_out must be equal");
+    if (p->in_features < 128 || p->in_features % 128 || p->in_features > (1 << 22))
+      return Status::shape("e4m3 product: K must be a multiple of 128, at most 2^22");
+    for (const int64_t ld : {p->ld_x, p->ld_w})
+      if (ld < p->in_features || ld % 16 || ld > (1 << 22))
+        return Status::shape("e4m3 product: row strides must be multiples of 16 from K to 2^22");
+    const int blocks = p->in_features / 128;
+    DC_TRY(check_scales(p->x_scale, p->x_scale_row, p->x_scale_block, p->rows, blocks, false));
+    DC_TRY(check_scales(p->w_scale, p->w_scale_row, p->w_scale_block, (p->out_features + 127) / 128, blocks, false));
+    if (p->rows > 1 && p->x_scale_row >= (1 << 21)) return Status::arg("x_scale_row must be below 2^21");
+    return linear_f8(*p, stream);
+  })());
+}
+
 dc_status dc_cache_store_q(const dc_model_cfg* cfg, int32_t bits, const float* h_out, const float* h_in, void* codes,
                            float* scales, const int32_t* idx, int32_t n, hipStream_t stream) {
   DC_ENTRY(([&]() -> Status {

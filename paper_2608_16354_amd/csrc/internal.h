@@ -276,6 +276,13 @@ int i8_tile(int M, int N, int ksteps, int cus, bool split);
 Status gemm_i8_qkv(const int8_t* A, const float* sx, const int8_t* W, const float* sw, const float* bias,
                    uint16_t* qk, uint16_t* vt, int ldv, float q_scale, const Geo& g, int M, hipStream_t s);
 
+// e4m3 rows and weights with a scale to 128 features or 128 x 128 values, RMS norm of a sum into such rows (quant_f8.hip)
+// and their products (gemm_f8.hip); arguments as checked by the C entry points.
+constexpr int kMaxNormCols = 16384;     // a row stays in the registers of a workgroup
+Status quantize_f8(const dc_quantize_f8_args& a, hipStream_t s);
+Status rms_norm_f8(const dc_rms_norm_f8_args& a, hipStream_t s);
+Status linear_f8(const dc_linear_f8_args& a, hipStream_t s);
+
 // The residual cache in 8 or 4 bits, a scale to 64 features (quant.hip).
 Status cache_store_q(const float* h_out, const float* h_in, int bits, void* codes, float* scales, const IdxList& idx,
                      const Geo& g, hipStream_t s);

@@ -1,0 +1,573 @@
+"""e4m3 rows and weights, the RMS norm of a sum into such rows, and their products on the GPU, against the
+definitions in 64 bits (oracle/ext.py).
+
+Codes and scales of given values are compared for equality.  Elsewhere a rounding is off by at most half a step: relative
+2^-24 for fp32, 2^-8 for bf16, 2^-4 for e4m3 (2^-10 below its normal numbers)."""
+import numpy as np
+import pytest
+
+from oracle import dit
+from oracle import ext as X
+from paper_2608_16354_amd import inputs as I
+from tests.gpu_util import say, t
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, E4M3, E4M3_LOW = 2.0 ** -24, 2.0 ** -8, 2.0 ** -4, 2.0 ** -10
+MARK = 99                               # a byte that no call writes there
+
+
+@pytest.fixture(scope="module")
+def api():
+    from paper_2608_16354_amd import api as A
+    A.L.load()
+    return A
+
+
+def kind_of(name):
+    import torch
+    return torch.bfloat16 if name == "bf16" else torch.float32
+
+
+def host(x):
+    return x.detach().float().cpu().numpy()
+
+
+def raw(x):
+    import torch
+    return x.view(torch.uint8).cpu().numpy()
+
+
+def marked(rows, cols, dev):
+    """A buffer of codes that are all MARK."""
+    import torch
+    return torch.full((rows, cols), MARK, dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn)
+
+
+def scales(rows, blocks, dev, major="block", gap=0):
+    """Scales of rows x blocks, all 99, and the buffer they lie in: a block's side by side, or a row's."""
+    import torch
+    if major == "block":
+        buf = torch.full((blocks + 1, rows + gap), 99.0, device=dev)
+        return buf[:blocks, :rows].t(), buf
+    buf = torch.full((rows + 1, blocks + gap), 99.0, device=dev)
+    return buf[:rows, :blocks], buf
+
+
+def codes(a, dev):
+    """Numbers that are e4m3 ones, as a tensor of codes."""
+    import torch
+    return t(np.asarray(a, np.float32), dev).to(torch.float8_e4m3fn)
+
+
+def special_rows(x):
+    """Rows that codes have to be right on: zeros, infinities, NaN, subnormal and very large magnitudes, ties."""
+    cols = x.shape[1]
+    x[1] = 0
+    x[2, cols // 2] = np.inf
+    x[3, cols - 1] = np.nan
+    x[4] *= np.float32(1e-38)
+    x[5] = np.float32(2e-44) * np.sign(x[5])            # a / 448 leaves fp32's range
+    x[6] = 3.38e38 * np.sign(x[6])
+    x[7] = -0.0
+    x[8, 0] = -np.inf
+    x[9] = np.round(x[9] * 32) / 32
+    x[9, 0] = 448.0 / 64                                # scale 2^-6: ties between codes
+    x[10] = np.float32(1e-42) * np.round(3 * x[10])
+
+
+# ----------------------------------------------------------------------------
+# rows and weights
+# ----------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [1, 3, 7, 8, 9, 64, 121, 127, 128, 129, 384, 513, 1000, 1096, 1920, 7687])
+def test_quantize_rows(api, dev, dtype, cols):
+    import torch
+    dt, rng = kind_of(dtype), np.random.default_rng(cols)
+    rows, blocks = 19, -(-cols // 128)
+    x = (rng.standard_normal((rows, cols)) * np.exp(rng.standard_normal((rows, 1)))).astype(np.float32)
+    special_rows(x)
+    if dtype == "bf16":
+        x = host(t(x, dev, dt))
+    want_q, want_s = X.e4m3_blocks(x)
+    for lead, extra, major, gap in ((0, 0, "block", 0), (1, 5, "row", 0), (3, 0, "block", 3), (0, 1, "row", 2)):
+        xb = torch.zeros((rows, cols + lead + extra), device=dev, dtype=dt)
+        xb[:, lead: lead + cols] = t(x, dev, dt)
+        qb = marked(rows + 1, (blocks + 1) * 128, dev)
+        s, sb = scales(rows, blocks, dev, major, gap)
+        say("quantize rows", dtype, cols, lead, major)
+        api.dc_quantize_f8(xb[:, lead: lead + cols], qb[:rows, : (blocks + (1 if extra else 0)) * 128], s)
+        torch.cuda.synchronize()
+        assert np.array_equal(host(s), want_s, equal_nan=True)
+        assert np.array_equal(host(qb[:rows, : blocks * 128]), want_q)
+        b = raw(qb)
+        assert (b[rows] == MARK).all() and (b[:, blocks * 128:] == MARK).all()
+        assert (host(sb) == 99).sum() == sb.numel() - rows * blocks
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 1920), (3, 7), (127, 130), (128, 128), (129, 257), (200, 8), (300, 1001), (640, 384)])
+def test_quantize_weights(api, dev, dtype, rows, cols):
+    import torch
+    dt, rng = kind_of(dtype), np.random.default_rng(rows + cols)
+    nr, blocks = -(-rows // 128), -(-cols // 128)
+    x = (rng.standard_normal((rows, cols)) * np.exp(rng.standard_normal((rows, 1)))).astype(np.float32)
+    if rows > 256:
+        x[130, 5] = np.nan
+        x[:128, :128] = 0
+        x[256:, 128:256] = 1e-44
+        x[140, 300] = np.inf
+    if dtype == "bf16":
+        x = host(t(x, dev, dt))
+    want_q, want_s = X.e4m3_blocks(x, 128)
+    for lead, major in ((0, "row"), (1, "block")):
+        xb = torch.zeros((rows, cols + lead), device=dev, dtype=dt)
+        xb[:, lead:] = t(x, dev, dt)
+        qb = marked(rows + 1, (blocks + 1) * 128, dev)
+        s, sb = scales(nr, blocks, dev, major, 1)
+        say("quantize weights", dtype, rows, cols, lead)
+        api.dc_quantize_f8(xb[:, lead:], qb[:rows], s, block_rows=128)
+        torch.cuda.synchronize()
+        assert np.array_equal(host(s), want_s, equal_nan=True)
+        assert np.array_equal(host(qb[:rows, : blocks * 128]), want_q)
+        b = raw(qb)
+        assert (b[rows] == MARK).all() and (b[:, blocks * 128:] == MARK).all()
+        assert (host(sb) == 99).sum() == sb.numel() - nr * blocks
+
+
+@pytest.mark.parametrize("dtype,rows,cols", [("f32", 1, 1920), ("bf16", 1, 7680), ("bf16", 4099, 1152), ("f32", 1025, 333), ("bf16", 3301, 1921),
+                                             ("f32", 9001, 130), ("bf16", 7, 130943), ("f32", 100003, 3), ("bf16", 100003, 5)])
+def test_quantize_many_rows(api, dev, dtype, rows, cols):
+    import torch
+    x = torch.randn((rows, cols), device=dev, generator=torch.Generator(dev).manual_seed(5)).to(kind_of(dtype))
+    q = marked(rows, -(-cols // 128) * 128, dev)
+    s, _ = scales(rows, -(-cols // 128), dev)
+    api.dc_quantize_f8(x, q, s)
+    want_q, want_s = X.e4m3_blocks(host(x))
+    assert np.array_equal(host(s), want_s) and np.array_equal(host(q), want_q)
+
+
+# ----------------------------------------------------------------------------
+# the norm
+# ----------------------------------------------------------------------------
+def check_codes(q, s, y, cols):
+    """Codes and scales of fp32 numbers that are y but for `off` of themselves: a mean square of cols terms that are added
+    eight to a lane, over up to eight pieces of it and six exchanges, then over four waves (7 + 8 + 6 + 3
+    roundings, half of them on the root), the square, the mean, eps, root, quotient and the two products: under 24."""
+    off = 24 * F32
+    pad = -(-cols // 128) * 128
+    v = np.zeros((len(y), pad))
+    v[:, :cols] = y
+    top = np.abs(v).reshape(len(y), -1, 128).max(-1)
+    assert (np.abs(s - top / 448) <= (off + 2 * F32) * top / 448).all()
+    step = np.repeat(s.astype(np.float64), 128, 1)
+    # a quotient carries the scale's error, the division's rounding and then that to the nearest code
+    tol = (E4M3 * (1 + 4 * off) + 3 * off) * np.abs(v) + E4M3_LOW * step
+    err = np.abs(q * step - v)
+    assert (err <= tol).all(), ((err / np.maximum(tol, 1e-300)).max(), np.argwhere(err > tol)[:4])
+    assert (q[:, cols:] == 0).all()
+
+
+@pytest.mark.parametrize("cols", [1, 5, 8, 100, 127, 128, 129, 500, 512, 513, 1000, 1024, 1152, 1921, 2048, 4096, 5003, 8200, 16384])
+@pytest.mark.parametrize("x_type,r_type,out_type", [("bf16", "f32", "f32"), ("f32", "bf16", "bf16"), ("f32", None, None), ("bf16", "bf16", "bf16"),
+                                                    ("bf16", None, "f32"), ("f32", "f32", None)])
+def test_norm(api, dev, cols, x_type, r_type, out_type):
+    import torch
+    rng = np.random.default_rng(cols)
+    rows, blocks, eps = 13, -(-cols // 128), 1e-5
+    x = (rng.standard_normal((rows, cols)) * np.exp(rng.standard_normal((rows, 1)))).astype(np.float32)
+    r = (3 * rng.standard_normal((rows, cols))).astype(np.float32)
+    x[3], r[3] = 0, 0
+    x[4], r[4] = 1e-30 * x[4], 1e-30 * r[4]             # eps alone is under the root
+    w = (1 + rng.standard_normal(cols)).astype(np.float32)
+    for lead, weight, major, in_place in ((0, w, "block", None), (1, None, "row", "residual"), (3, w, "row", "x")):
+        xd = torch.zeros((rows + 1, cols + lead), device=dev, dtype=kind_of(x_type))
+        xd[:rows, lead:] = t(x, dev)
+        xd = xd[:rows, lead:]
+        rd = None if r_type is None else t(r, dev, kind_of(r_type))
+        h = host(xd) + (0 if rd is None else host(rd))
+        out = buf = None
+        if out_type is not None:
+            buf = torch.full((rows + 1, cols + 2), 7.0, device=dev, dtype=kind_of(out_type))
+            out = buf[:rows, 1: 1 + cols]
+            if in_place == "residual" and r_type == out_type:
+                out, buf = rd, None
+            elif in_place == "x" and x_type == out_type:
+                out, buf = xd, None
+        qb = marked(rows + 1, (blocks + 1) * 128, dev)
+        s, sb = scales(rows, blocks, dev, major, 1)
+        say("norm", cols, x_type, r_type, out_type, lead)
+        api.dc_rms_norm_f8(xd, qb[:rows, : blocks * 128], s, weight=None if weight is None else t(w, dev), eps=eps, residual=rd, out=out)
+        torch.cuda.synchronize()
+        check_codes(host(qb[:rows, : blocks * 128]), host(s), X.rms_norm(h, weight, eps), cols)
+        assert not host(s)[3].any() and not host(qb[3, : blocks * 128]).any()
+        if out is not None:
+            assert np.array_equal(host(out), h if out_type == "f32" else host(t(h, dev, torch.bfloat16)))
+        if buf is not None:
+            b = host(buf)
+            assert (b[rows] == 7).all() and (b[:, 0] == 7).all() and (b[:, 1 + cols:] == 7).all()
+        b = raw(qb)
+        assert (b[rows] == MARK).all() and (b[:, blocks * 128:] == MARK).all()
+        assert (host(sb) == 99).sum() == sb.numel() - rows * blocks
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 1920), (3704, 1152), (4097, 1920), (2050, 333), (9000, 129), (1030, 5000)])
+def test_norm_of_many_rows(api, dev, rows, cols):
+    import torch
+    gen = torch.Generator(dev).manual_seed(rows)
+    x = torch.randn((rows, cols), device=dev, generator=gen).bfloat16()
+    r = torch.randn((rows, cols), device=dev, generator=gen)
+    h = host(x) + host(r)
+    w = 1 + 0.2 * torch.randn(cols, device=dev, generator=gen)
+    q, (s, _) = marked(rows, -(-cols // 128) * 128, dev), scales(rows, -(-cols // 128), dev)
+    api.dc_rms_norm_f8(x, q, s, weight=w, residual=r, out=r)
+    assert np.array_equal(host(r), h)
+    check_codes(host(q), host(s), X.rms_norm(h, host(w), 1e-6), cols)
+
+
+def test_norm_of_rows_without_a_number(api, dev):
+    """A NaN makes its row NaN, an infinity its block (the others of the row are zeros over an infinite root); the
+    padding holds zeros all the same, and other rows keep theirs."""
+    import torch
+    x = torch.randn((6, 300), device=dev, generator=torch.Generator(dev).manual_seed(3))
+    x[1, 299], x[4, 130] = float("nan"), float("inf")
+    q, (s, _) = marked(6, 384, dev), scales(6, 3, dev)
+    out = torch.empty_like(x)
+    api.dc_rms_norm_f8(x, q, s, weight=torch.ones(300, device=dev), out=out)
+    bad = np.isnan(host(s))
+    assert bad[1].all() and bad[4].tolist() == [False, True, False] and bad.sum() == 4
+    q = host(q)
+    assert not q[1].any() and not q[4].any() and not q[:, 300:].any() and not host(s)[4, [0, 2]].any()
+    assert np.array_equal(host(out), host(x), equal_nan=True)
+    keep = [0, 2, 3, 5]
+    check_codes(q[keep], host(s)[keep], X.rms_norm(host(x)[keep], None, 1e-6), 300)
+
+
+# ----------------------------------------------------------------------------
+# products
+# ----------------------------------------------------------------------------
+def whole_inputs(m, n, k, seed):
+    """Codes of small whole numbers and scales that are powers of two: |sum| <= 16 k, times 1/4 to 4, in steps of 1/4, is
+    held exactly by fp32 up to k = 2^17 - and by eight products' 15 bits."""
+    rng = np.random.default_rng(seed)
+    x, w = (rng.integers(-4, 5, (r, k)).astype(np.float32) for r in (m, n))
+    xs = 2.0 ** rng.integers(-1, 2, (m, k // 128))
+    ws = 2.0 ** rng.integers(-1, 2, (-(-n // 128), k // 128))
+    return x, xs.astype(np.float32), w, ws.astype(np.float32), *vectors(rng, m, n)
+
+
+def any_inputs(m, n, k, seed):
+    """Codes over e4m3's whole range, subnormal ones among them, and any scales."""
+    rng = np.random.default_rng(seed)
+    x, w = (X.e4m3(rng.standard_normal((r, k)) * np.exp(1.5 * rng.standard_normal((r, k))) * 8).astype(np.float32) for r in (m, n))
+    xs = rng.uniform(1e-4, 2e-2, (m, k // 128)).astype(np.float32)
+    ws = rng.uniform(1e-4, 2e-2, (-(-n // 128), k // 128)).astype(np.float32)
+    return x, xs, w, ws, *vectors(rng, m, n)
+
+
+def vectors(rng, m, n):
+    return (rng.standard_normal(n).astype(np.float32), rng.standard_normal(n).astype(np.float32),
+            rng.standard_normal((m, n)).astype(np.float32))
+
+
+def check_linear(got, x, xs, w, ws, bias, gate, residual, kind, bf16, whole):
+    """The sum: none lost where inputs are whole; else, for fp32 outputs, up to a step (2^-23, as an adder may cut) at
+    each of the 128 additions of a block and the K / 128 of the blocks, and two roundings of the scales; for bf16 ones a
+    product loses up to 2^-15 of the largest of its eight.  Then the bias, and for the rest as many fp32 roundings as
+    in the int8 product: GELU's slope is at most 1.13, its argument carries (14 |y| + 7) roundings, |y| <= 40 matters
+    (beyond it the value is z or 0); a residual has two more of |gate v| + |residual|, a product with a gate that has been
+    applied to the bias one more."""
+    v, size = X.linear_f8(x, xs, w, ws)
+    tol = 0.0
+    if not whole:
+        tol = (2 * (128 + x.shape[1] // 128) + 4) * F32 * size + (8 * 2.0 ** -15 * size if bf16 else 0)
+    tol = tol + 4 * F32 * (np.abs(v) + (0 if bias is None else np.abs(bias)))
+    if bias is not None:
+        v = v + bias
+    if kind == "gelu":
+        y = np.minimum(np.abs(0.7978845608 * (v + 0.044715 * v ** 3)), 40)
+        z = dit.gelu_tanh(v)
+        tol = 1.13 * tol + (14 * y + 7) * F32 * np.abs(z) + 2.0 ** -120
+        v = z
+    elif kind in ("gated", "residual"):
+        g = gate if kind == "gated" else np.ones_like(gate)
+        tol = np.abs(g) * tol + 3 * F32 * (np.abs(g * v) + np.abs(residual))
+        v = residual + g * v
+    tol = tol + (BF16 if bf16 else F32) * (np.abs(v) + tol)
+    err = np.abs(got - v)
+    assert np.isfinite(got).all() and (err <= tol).all(), (err.max(), (err / np.maximum(tol, 1e-300)).max(), np.argwhere(err > tol)[:4])
+    return v
+
+
+def run_linear(api, dev, data, kind, dt, bias=True, major="block", lead=0, gap=0):
+    """The product on tensors whose rows start `lead` values into wider ones; what lies around is left as it was."""
+    import torch
+    x, xs, w, ws, b, gate, res = data
+    m, n = len(x), len(w)
+    buf = torch.full((m + 1, n + lead + gap), 3.0, device=dev, dtype=kind_of(dt))
+    out = buf[:m, lead: lead + n]
+    rs = None
+    if kind in ("gated", "residual"):
+        rs = t(res, dev, kind_of(dt))
+        if lead:                                        # in place
+            out.copy_(rs)
+            rs = out
+    sx, _ = scales(m, xs.shape[1], dev, major, lead)
+    sx.copy_(t(xs, dev))
+    api.dc_linear_f8(codes(x, dev), sx, codes(w, dev), t(ws, dev), out, bias=t(b, dev) if bias else None, gelu=kind == "gelu",
+                     gate=t(gate, dev) if kind == "gated" else None, residual=rs)
+    torch.cuda.synchronize()
+    got = host(buf)
+    assert (got[m] == 3).all() and (got[:, :lead] == 3).all() and (got[:, lead + n:] == 3).all()
+    return got[:m, lead: lead + n]
+
+
+def of_type(data, dt, dev):
+    """The data with the residual as its type holds it."""
+    return (*data[:6], host(t(data[6], dev, kind_of(dt))))
+
+
+KINDS = [("plain", "f32", True, "block", 0, 0), ("plain", "bf16", False, "row", 1, 2), ("gelu", "bf16", True, "block", 8, 0),
+         ("gelu", "f32", False, "block", 0, 1), ("gated", "f32", True, "row", 1, 4), ("gated", "bf16", True, "block", 0, 0),
+         ("residual", "f32", False, "block", 0, 0), ("residual", "bf16", True, "block", 3, 0)]
+
+
+@pytest.mark.parametrize("m", [1, 2, 15, 16, 17, 31, 33, 63, 64, 65, 127, 191, 300])
+@pytest.mark.parametrize("n,k", [(1, 128), (31, 256), (33, 384), (64, 128), (65, 1920), (193, 512), (250, 7680), (1152, 640)])
+def test_linear_ragged(api, dev, m, n, k):
+    """Few rows and odd widths, each epilogue, with and without a bias, strided operands and outputs."""
+    data = whole_inputs(m, n, k, m + n)
+    say("linear ragged", m, n, k)
+    for kind, dt, bias, major, lead, gap in KINDS:
+        got = run_linear(api, dev, data, kind, dt, bias, major, lead, gap)
+        d = of_type(data, dt, dev)
+        v = check_linear(got, *d[:4], d[4] if bias else None, d[5], d[6], kind, dt == "bf16", True)
+        if kind == "plain" and dt == "bf16":            # one rounding, of an exact sum
+            assert np.array_equal(got, I.round_bf16(v.astype(np.float32)))
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 1920, 7680), (50, 333, 1920), (257, 513, 1152), (700, 1920, 1920), (1, 40, 65536)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_linear_of_any_codes(api, dev, m, n, k, dt):
+    data = any_inputs(m, n, k, m + k)
+    say("linear any", m, n, k, dt)
+    for kind in ("plain", "gelu", "gated"):
+        got = run_linear(api, dev, data, kind, dt)
+        d = of_type(data, dt, dev)
+        check_linear(got, *d, kind, dt == "bf16", False)
+
+
+def test_linear_in_fp32_keeps_small_products(api, dev):
+    """Products of 1 beside one of 65,536 in each block: fp32 outputs hold the sum exactly."""
+    import torch
+    x, w = (np.ones((40, 1024), np.float32) for _ in range(2))
+    x[:, 5::128] = 256
+    w[:, 5::128] = 256
+    one = torch.ones((1, 1), device=dev)
+    out = torch.zeros((40, 40), device=dev)
+    api.dc_linear_f8(codes(x, dev), one.expand(40, 8), codes(w, dev), one.expand(1, 8), out)
+    assert (host(out) == 8 * (65536 + 127)).all()
+
+
+def test_linear_scales_of_any_strides(api, dev):
+    """One scale for all rows or all blocks, a row's scales side by side or not, and codes with rows apart."""
+    import torch
+    x, xs, w, ws, bias, gate, res = whole_inputs(150, 260, 512, 2)
+    xd, wd = (torch.full((len(a), 512 + 48), 0.5, device=dev).to(torch.float8_e4m3fn) for a in (x, w))
+    xd[:, 16: 528].copy_(codes(x, dev))
+    wd[:, 32: 544].copy_(codes(w, dev))
+    xd, wd = xd[:, 16: 528], wd[:, 32: 544]
+    wide = torch.zeros((450, 12), device=dev)
+    apart = wide[::3, ::3]
+    apart.copy_(t(xs, dev))
+    two, per_block, per_row = torch.full((1, 1), 2.0, device=dev), t(xs[:1], dev), t(xs[:, :1], dev)
+    for sx, host_s in ((apart, xs), (two.expand(150, 4), 2 + 0 * xs), (per_block.expand(150, 4), xs[:1].repeat(150, 0)),
+                       (per_row.expand(150, 4), xs[:, :1].repeat(4, 1))):
+        for sw, host_w in ((t(ws, dev), ws), (t(ws.T, dev).t(), ws), (two.expand(3, 4), 2 + 0 * ws)):
+            out = torch.zeros((150, 260), device=dev)
+            api.dc_linear_f8(xd, sx, wd, sw, out)
+            check_linear(host(out), x, host_s, w, host_w, None, gate, res, "plain", False, True)
+
+
+def test_linear_rows_beyond_32_bit_offsets(api, dev):
+    """Rows 4 MiB apart: the last ones lie past 2^31 bytes, in x and in w."""
+    import torch
+    x, xs, w, ws, bias, gate, res = whole_inputs(700, 600, 256, 3)
+    for dt in ("f32", "bf16"):
+        big = [torch.empty((r, 1 << 22), dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn)[:, :256] for r in (700, 600)]
+        big[0].copy_(codes(x, dev))
+        big[1].copy_(codes(w, dev))
+        out = torch.empty((700, 600), device=dev, dtype=kind_of(dt))
+        say("far rows", dt)
+        api.dc_linear_f8(big[0], t(xs, dev), big[1], t(ws, dev), out)
+        check_linear(host(out), x, xs, w, ws, None, gate, res, "plain", dt == "bf16", True)
+
+
+def test_linear_of_blocks_without_a_number(api, dev):
+    """Rows and weight blocks that held a NaN or an infinity are NaN in the product, the others are not."""
+    import torch
+    gen = torch.Generator(dev).manual_seed(1)
+    x, w = torch.randn((70, 200), device=dev, generator=gen), torch.randn((300, 200), device=dev, generator=gen)
+    x[3, 7], x[66, 199], w[290, 150] = float("nan"), float("inf"), float("-inf")
+    q, (s, _), wq, (wsc, _) = marked(70, 256, dev), scales(70, 2, dev), marked(300, 256, dev), scales(3, 2, dev, "row")
+    api.dc_quantize_f8(x, q, s)
+    api.dc_quantize_f8(w, wq, wsc, block_rows=128)
+    for dt in ("f32", "bf16"):
+        out = torch.empty((70, 300), device=dev, dtype=kind_of(dt))
+        api.dc_linear_f8(q, s, wq, wsc, out)
+        bad = np.isnan(host(out))
+        assert bad[[3, 66]].all() and bad[:, 256:].all() and bad.sum() == 2 * 300 + 68 * 44
+
+
+def test_no_rows(api, dev):
+    import torch
+    none = torch.empty((0, 128), device=dev)
+    q, s = none.to(torch.float8_e4m3fn), torch.empty((0, 1), device=dev)
+    api.dc_quantize_f8(none, q, s)
+    api.dc_rms_norm_f8(none, q, s, residual=none, out=none)
+    api.dc_linear_f8(q, s, codes(np.ones((8, 128)), dev), torch.ones((1, 1), device=dev), torch.empty((0, 8), device=dev))
+    torch.cuda.synchronize()
+
+
+def test_one_row_of_any_stride(api, dev):
+    """A single row's stride says nothing: rows cut out of wider ones are taken as they are."""
+    import torch
+    wide = torch.randn((1, 203), device=dev, generator=torch.Generator(dev).manual_seed(2))
+    q, s, y = marked(1, 333, dev), torch.zeros((1, 2), device=dev), torch.zeros((1, 41), device=dev)
+    x, row, out = (v.as_strided((1, n), (st, 1)) for v, n, st in ((wide, 200, 7), (q, 256, 3), (y, 40, 1)))
+    api.dc_quantize_f8(x, row, s.as_strided((1, 2), (0, 1)))
+    want_q, want_s = X.e4m3_blocks(host(x))
+    assert np.array_equal(host(row), want_q) and np.array_equal(host(s), want_s)
+    w = np.random.default_rng(1).integers(-4, 5, (40, 256)).astype(np.float32)
+    api.dc_linear_f8(row, s, codes(w, dev), torch.ones((1, 2), device=dev), out)
+    check_linear(host(out), want_q, want_s, w, np.ones((1, 2)), None, np.ones(40), None, "plain", False, False)
+    assert host(y)[0, 40] == 0
+
+
+# ----------------------------------------------------------------------------
+# together, in graphs and on streams
+# ----------------------------------------------------------------------------
+def mlp_state(dev, m, d, f, seed):
+    """A block's MLP: norm of x + h, up with GELU, codes of the hidden rows, down onto the sum."""
+    import torch
+    gen = torch.Generator(dev).manual_seed(seed)
+    s = dict(x=torch.randn((m, d), device=dev, generator=gen).bfloat16(), h=torch.randn((m, d), device=dev, generator=gen),
+             weight=1 + 0.2 * torch.randn(d, device=dev, generator=gen), gate=torch.randn(d, device=dev, generator=gen),
+             b1=torch.randn(f, device=dev, generator=gen), b2=torch.randn(d, device=dev, generator=gen),
+             w1=0.05 * torch.randn((f, d), device=dev, generator=gen), w2=0.05 * torch.randn((d, f), device=dev, generator=gen))
+    blocks = [-(-v // 128) for v in (d, f)]
+    s.update(q=marked(m, 128 * blocks[0], dev), s=scales(m, blocks[0], dev)[0], z=torch.zeros((m, f), device=dev, dtype=torch.bfloat16),
+             zq=marked(m, 128 * blocks[1], dev), zs=scales(m, blocks[1], dev)[0], w1q=marked(f, 128 * blocks[0], dev),
+             w2q=marked(d, 128 * blocks[1], dev), w1s=scales(blocks[1], blocks[0], dev, "row")[0],
+             w2s=scales(blocks[0], blocks[1], dev, "row")[0], y=torch.zeros((m, d), device=dev))
+    return s
+
+
+def mlp_calls(api, b, stream=None):
+    api.dc_quantize_f8(b["w1"], b["w1q"], b["w1s"], block_rows=128, stream=stream)
+    api.dc_quantize_f8(b["w2"], b["w2q"], b["w2s"], block_rows=128, stream=stream)
+    api.dc_rms_norm_f8(b["x"], b["q"], b["s"], weight=b["weight"], residual=b["h"], out=b["h"], stream=stream)
+    api.dc_linear_f8(b["q"], b["s"], b["w1q"], b["w1s"], b["z"], bias=b["b1"], gelu=True, stream=stream)
+    api.dc_quantize_f8(b["z"], b["zq"], b["zs"], stream=stream)
+    api.dc_linear_f8(b["zq"], b["zs"], b["w2q"], b["w2s"], b["y"], bias=b["b2"], gate=b["gate"], residual=b["h"], stream=stream)
+
+
+def bits(x):
+    import torch
+    return x.view(torch.uint8) if x.element_size() == 1 else x
+
+
+@pytest.mark.parametrize("m,d,f", [(1, 256, 512), (37, 200, 333), (300, 1152, 4608)])
+def test_an_mlp(api, dev, m, d, f):
+    """Step by step: each call's result from the one before, against the definition of that call."""
+    b = mlp_state(dev, m, d, f, 4)
+    x, h = host(b["x"]), host(b["h"])
+    mlp_calls(api, b)
+    assert np.array_equal(host(b["h"]), x + h)
+    for w, q, s in (("w1", "w1q", "w1s"), ("w2", "w2q", "w2s")):
+        want_q, want_s = X.e4m3_blocks(host(b[w]), 128)
+        assert np.array_equal(host(b[q]), want_q) and np.array_equal(host(b[s]), want_s)
+    check_codes(host(b["q"]), host(b["s"]), X.rms_norm(x + h, host(b["weight"]), 1e-6), d)
+    check_linear(host(b["z"]), host(b["q"]), host(b["s"]), host(b["w1q"]), host(b["w1s"]), host(b["b1"]), None, None, "gelu", True, False)
+    want_q, want_s = X.e4m3_blocks(host(b["z"]))
+    assert np.array_equal(host(b["zq"]), want_q) and np.array_equal(host(b["zs"]), want_s)
+    y = check_linear(host(b["y"]), host(b["zq"]), host(b["zs"]), host(b["w2q"]), host(b["w2s"]), host(b["b2"]), host(b["gate"]),
+                     x + h, "gated", False, False)
+    # the whole against the unquantised MLP: every operand is within 2^-4 of itself, and errors are of either sign
+    z = dit.gelu_tanh(X.rms_norm(x + h, host(b["weight"]), 1e-6) @ host(b["w1"]).astype(np.float64).T + host(b["b1"]))
+    full = x + h + host(b["gate"]) * (z @ host(b["w2"]).astype(np.float64).T + host(b["b2"]))
+    assert np.linalg.norm(y - full) < 4 * E4M3 * np.linalg.norm(full - x - h)
+
+
+def test_captured_and_replayed(api, dev):
+    """All of the calls in one graph on a stream of their own, replayed on changing inputs between eager work,
+    against the eager calls."""
+    import torch
+    graphed, eager = (mlp_state(dev, 300, 640, 1280, 3) for _ in range(2))
+    inputs = ("x", "h", "w1", "w2")
+    gen = torch.Generator(dev).manual_seed(9)
+
+    def fill():
+        for n in inputs:
+            v = torch.randn(eager[n].shape, device=dev, generator=gen)
+            for b in (graphed, eager):
+                b[n].copy_(v)
+
+    fill()
+    mlp_calls(api, eager)
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        mlp_calls(api, graphed)
+    for i in range(4):
+        fill()
+        graph.replay()
+        mlp_calls(api, eager)
+        torch.cuda.synchronize()
+        for n in graphed:
+            assert torch.equal(bits(graphed[n]), bits(eager[n])), (i, n)
+    # on another stream than the current one
+    other = mlp_state(dev, 300, 640, 1280, 3)
+    want = mlp_state(dev, 300, 640, 1280, 3)
+    mlp_calls(api, want)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    mlp_calls(api, other, stream=side)
+    side.synchronize()
+    torch.cuda.synchronize()
+    for n in want:
+        assert torch.equal(bits(other[n]), bits(want[n])), n
+
+
+def test_two_streams_at_once(api, dev):
+    """The calls keep nothing between them: two streams that work side by side get what each gets alone."""
+    import torch
+    alone, together = ([mlp_state(dev, m, 640, 1280, m) for m in (700, 9)] for _ in range(2))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for b in alone:
+        mlp_calls(api, b, streams[0])
+        torch.cuda.synchronize()
+    for b, s in zip(together, streams):
+        mlp_calls(api, b, s)
+    torch.cuda.synchronize()
+    for a, b in zip(alone, together):
+        for n in a:
+            assert torch.equal(bits(a[n]), bits(b[n])), n
+
+
+def test_rows_beyond_32_bit_offsets(api, dev):
+    """Rows 8 MiB apart, the last of them past 2^32 bytes: values, sums and codes."""
+    import torch
+    rows, cols = 600, 300
+    x = torch.randn((rows, cols), device=dev, generator=torch.Generator(dev).manual_seed(8))
+    far = [torch.empty((rows, 1 << 21), device=dev)[:, :cols] for _ in range(2)]
+    q = torch.empty((rows, 1 << 23), dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn)[:, :384]
+    s, _ = scales(rows, 3, dev)
+    far[0].copy_(x)
+    api.dc_quantize_f8(far[0], q, s)
+    want_q, want_s = X.e4m3_blocks(host(x))
+    assert np.array_equal(host(q), want_q) and np.array_equal(host(s), want_s)
+    api.dc_rms_norm_f8(far[0], q, s, residual=far[0], out=far[1])
+    assert np.array_equal(host(far[1]), 2 * host(x))
+    check_codes(host(q), host(s), X.rms_norm(2 * host(x), None, 1e-6), cols)
