@@ -15,6 +15,7 @@
 // their scales.
 #include "gemm_tile.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace dc {
@@ -56,19 +57,31 @@ __device__ inline bf16x8 widened(uint32_t lo, uint32_t hi) {
                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true))};
   return __builtin_bit_cast(bf16x8, r);
 }
-// 16 x 16 outputs of a whole k-step, transposed: a lane ends with row lane % 16 of x and four columns from 4 (lane / 16) on.
-// Both operands' lanes hold the same k, in whatever order the instruction takes them.
-template <bool FULL>
-__device__ inline f32x4 product(const Frag& w, const Frag& x) {
-  f32x4 d = {0.f, 0.f, 0.f, 0.f};
-  if constexpr (FULL) {
-    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widened(w.lo.x, w.lo.y), widened(x.lo.x, x.lo.y), d, 0, 0, 0);
-    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widened(w.lo.z, w.lo.w), widened(x.lo.z, x.lo.w), d, 0, 0, 0);
-    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widened(w.hi.x, w.hi.y), widened(x.hi.x, x.hi.y), d, 0, 0, 0);
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(widened(w.hi.z, w.hi.w), widened(x.hi.z, x.hi.w), d, 0, 0, 0);
-  } else {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.operand(), x.operand(), d, 0, 0, 0, 0, 0, 0);
+// An operand's 16 rows of a k-step as the instruction takes them.  Outputs are transposed: a lane ends with row lane % 16
+// of x and four columns from 4 (lane / 16) on.  Both operands' lanes hold the same k, in whatever order the
+// instruction takes them.
+template <bool FULL> struct Operand;
+template <> struct Operand<false> {
+  i32x8 v;
+  __device__ void set(const Frag& f) { v = f.operand(); }
+};
+template <> struct Operand<true> {
+  bf16x8 v[4];
+  __device__ void set(const Frag& f) {
+    v[0] = widened(f.lo.x, f.lo.y);
+    v[1] = widened(f.lo.z, f.lo.w);
+    v[2] = widened(f.hi.x, f.hi.y);
+    v[3] = widened(f.hi.z, f.hi.w);
   }
+};
+__device__ inline f32x4 product(const Operand<false>& w, const Operand<false>& x) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.v, x.v, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+}
+__device__ inline f32x4 product(const Operand<true>& w, const Operand<true>& x) {
+  f32x4 d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.v[i], x.v[i], d, 0, 0, 0);
+  return d;
 }
 
 // GELU(z) = z / (1 + 2^u), u = -2 log2(e) sqrt(2 / pi) (z + 0.044715 z^3)
@@ -91,6 +104,7 @@ struct Epi {
   int64_t ldr;
   void* out;
   int64_t ldo;
+  bool lines;             // rows start on a line of 128 bytes
   static constexpr bool kBf16 = BF;
   static constexpr int E = BF ? 2 : 4;                // bytes of a value
   static constexpr int V = 16 / E;                    // values of a 16-byte piece
@@ -116,21 +130,23 @@ struct Epi {
     if constexpr (RES) vec[BN + tid] = g;
   }
 
-  // residual and finished values of a piece, added
-  static __device__ inline u32x4 added(u32x4 z, u32x4 r) {
-    if constexpr (BF) {
-      u32x4 o;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        o[i] = pack_bf16(__uint_as_float(z[i] << 16) + __uint_as_float(r[i] << 16),
-                         __uint_as_float(z[i] & 0xFFFF0000u) + __uint_as_float(r[i] & 0xFFFF0000u));
-      return o;
+  // one value
+  __device__ inline void one(float z, int64_t m, int n) const {
+    z += bias ? bias[n] : 0.f;
+    if constexpr (RES) {
+      if (gate) z *= gate[n];
+      if constexpr (BF) z += from_bf16(static_cast<const uint16_t*>(residual)[m * ldr + n]);
+      else z += static_cast<const float*>(residual)[m * ldr + n];
     } else {
-      return __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, z) + __builtin_bit_cast(f32x4, r));
+      z = act(z);
     }
+    if constexpr (BF) static_cast<uint16_t*>(out)[m * ldo + n] = to_bf16(z);
+    else static_cast<float*>(out)[m * ldo + n] = z;
   }
 
-  // The wave's WTM x WTN part of the tile, acc[a][b] of 16 x 16 each; strip: the wave's LDS.
+  // The wave's WTM x WTN part of the tile, acc[a][b] of 16 x 16 each; strip: the wave's LDS.  A strip's residual is fetched
+  // a strip ahead, in the pieces that are stored.  In fp32 it is added to the finished pieces; in bf16, where that would
+  // be a second rounding, it goes through the strip to the lanes that hold the values.
   template <int BN, int WTM, int WTN, int TM, int TN>
   __device__ inline void finish(f32x4 (&acc)[TM][TN], char* strip, const float* vec, int m0, int n0, int nt, int M, int N, int lane) const {
     const int r16 = lane & 15, c4 = (lane >> 4) * 4;
@@ -142,70 +158,89 @@ struct Epi {
       const int PR = width / V, RS = 64 / PR, NP = 32 / RS;          // pieces of a strip's row, rows and passes of the wave
       const int rl = lane / PR, nl = nb + lane % PR * V;
       const bool whole = nl + V <= N;
+      const bool rest = N % V && nb + width > N;                      // columns behind the last whole piece
+      char* const piece = strip + rl * kS + lane % PR * 16;
+      u32x4a res[RES ? 2 : 1][4];
+      auto fetch = [&](int r0) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int m = m0 + r0 + rl + j * RS;
+          if (j < NP && whole && m < M)
+            res[r0 / 32 & 1][j] = *reinterpret_cast<const u32x4a*>(static_cast<const char*>(residual) + (m * ldr + nl) * E);
+        }
+      };
+      if constexpr (RES) fetch(0);
 #pragma unroll
       for (int r0 = 0; r0 < WTM; r0 += 32) {
-        u32x4a res[4];
-        if constexpr (RES && !BF) {
+        const int tail = lane < 32 && m0 + r0 + lane < M && rest ? N : 0;     // a lane's row of the rest
+        if constexpr (RES && BF) {
 #pragma unroll
-          for (int j = 0; j < NP; ++j) {
-            const int m = m0 + r0 + rl + j * RS;
-            if (whole && m < M) res[j] = *reinterpret_cast<const u32x4a*>(static_cast<const char*>(residual) + (m * ldr + nl) * E);
-          }
+          for (int j = 0; j < NP; ++j) *reinterpret_cast<u32x4*>(piece + j * RS * kS) = res[r0 / 32 & 1][j];
+#pragma unroll 1
+          for (int n = max(nb, N / V * V); n < tail; ++n)
+            *reinterpret_cast<uint16_t*>(strip + lane * kS + (n - nb) * E) =
+                static_cast<const uint16_t*>(residual)[(m0 + r0 + lane) * ldr + n];
+          asm volatile("" ::: "memory");
         }
+        if constexpr (RES)
+          if (r0 + 32 < WTM) fetch(r0 + 32);
 #pragma unroll
-        for (int a = 0; a < 2; ++a) {
-          const int m = m0 + r0 + a * 16 + r16;
+        for (int a = 0; a < 2; ++a)
 #pragma unroll
           for (int b = 0; b < SC / 16; ++b) {
             if (b * 16 >= width) continue;
             const f32x4 t = acc[r0 / 16 + a][c0 / 16 + b];
             const int c = nt + c0 + b * 16 + c4;
             const f32x4 o = *reinterpret_cast<const f32x4*>(vec + c);
+            char* const at = strip + (a * 16 + r16) * kS + (b * 16 + c4) * E;
             f32x4 z;
             if constexpr (RES) {
               const f32x4 g = *reinterpret_cast<const f32x4*>(vec + BN + c);
 #pragma unroll
               for (int i = 0; i < 4; ++i) z[i] = fmaf(t[i], g[i], o[i]);
-              if constexpr (BF) {                                     // added before the one rounding
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  if (m < M && n0 + c + i < N)
-                    z[i] += from_bf16(static_cast<const uint16_t*>(residual)[m * ldr + n0 + c + i]);
+              if constexpr (BF) {
+                const uint2 r = *reinterpret_cast<const uint2*>(at);
+                z[0] += __uint_as_float(r.x << 16);
+                z[1] += __uint_as_float(r.x & 0xFFFF0000u);
+                z[2] += __uint_as_float(r.y << 16);
+                z[3] += __uint_as_float(r.y & 0xFFFF0000u);
               }
             } else {
 #pragma unroll
               for (int i = 0; i < 4; ++i) z[i] = act(t[i] + o[i]);
             }
-            char* const at = strip + (a * 16 + r16) * kS + (b * 16 + c4) * E;
             if constexpr (BF) *reinterpret_cast<uint2*>(at) = make_uint2(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]));
             else *reinterpret_cast<f32x4*>(at) = z;
           }
-        }
         asm volatile("" ::: "memory");
         u32x4 v[4];
 #pragma unroll
-        for (int j = 0; j < NP; ++j)
-          v[j] = *reinterpret_cast<const u32x4*>(strip + (rl + j * RS) * kS + lane % PR * 16);
+        for (int j = 0; j < NP; ++j) v[j] = *reinterpret_cast<const u32x4*>(piece + j * RS * kS);
 #pragma unroll
         for (int j = 0; j < NP; ++j) {
           const int m = m0 + r0 + rl + j * RS;
           if (!whole || m >= M) continue;
-          if constexpr (RES && !BF) v[j] = added(v[j], res[j]);
-          __builtin_nontemporal_store(v[j], reinterpret_cast<u32x4a*>(static_cast<char*>(out) + (m * ldo + nl) * E));
+          if constexpr (RES && !BF)
+            v[j] = __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, v[j]) + __builtin_bit_cast(f32x4, u32x4(res[r0 / 32 & 1][j])));
+          u32x4a* const at = reinterpret_cast<u32x4a*>(static_cast<char*>(out) + (m * ldo + nl) * E);
+          if (lines) {
+            __builtin_nontemporal_store(v[j], at);
+          } else {
+            asm volatile("" ::: "memory");            // keep the two kinds of store apart
+            *at = v[j];
+            asm volatile("" ::: "memory");
+          }
         }
-        // the columns behind the last whole piece
-        if (N % V && nb + width > N && lane < 32 && m0 + r0 + lane < M) {
-          const int64_t m = m0 + r0 + lane;
 #pragma unroll 1
-          for (int n = max(nb, N / V * V); n < N; ++n) {
-            const char* const at = strip + lane * kS + (n - nb) * E;
-            if constexpr (BF) {
-              static_cast<uint16_t*>(out)[m * ldo + n] = *reinterpret_cast<const uint16_t*>(at);
-            } else {
-              float f = *reinterpret_cast<const float*>(at);
-              if constexpr (RES) f += static_cast<const float*>(residual)[m * ldr + n];
-              static_cast<float*>(out)[m * ldo + n] = f;
-            }
+        for (int n = max(nb, N / V * V); n < tail; ++n) {
+          const int64_t m = m0 + r0 + lane;
+          const char* const at = strip + lane * kS + (n - nb) * E;
+          if constexpr (BF) {
+            static_cast<uint16_t*>(out)[m * ldo + n] = *reinterpret_cast<const uint16_t*>(at);
+          } else {
+            float f = *reinterpret_cast<const float*>(at);
+            if constexpr (RES) f += static_cast<const float*>(residual)[m * ldr + n];
+            static_cast<float*>(out)[m * ldo + n] = f;
           }
         }
         asm volatile("" ::: "memory");
@@ -225,17 +260,17 @@ struct Operands {
 // WM x WN waves on a BM x BN tile, ST stages of a k-step, one barrier to a k-step: the fills of k-step kt + ST - 1 go out
 // among the products of k-step kt.  Rows past M or N are clamped to the last row (their results are never
 // stored).  Workgroups are renumbered so that an XCD takes neighbouring tiles.
-template <int BM, int BN, int WM, int WN, int ST, class E>
-__global__ void __launch_bounds__(WM * WN * 64) k_gemm_f8(Operands p, int tiles_n, int tiles, int per_xcd, E epi) {
-  constexpr int NW = WM * WN, NT = NW * 64;
+template <int BM, int BN, int WM, int WN, int ST, int KG, class E>
+__global__ void __launch_bounds__(KG * WM * WN * 64) k_gemm_f8(Operands p, int tiles_n, int tiles, int per_xcd, E epi) {
+  constexpr int NW = WM * WN, NT = NW * 64;                       // of a group
   constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 16, TN = WTN / 16;
   constexpr int AI = BM * 8 / NT, BI = BN * 8 / NT;               // DMA instructions of a wave and k-step, and one for scales
-  static_assert(AI * NT == BM * 8 && BI * NT == BN * 8 && WTM % 32 == 0 && WTN % 32 == 0 && BN % 64 == 0, "tile shape");
-  constexpr int NS = BN / 64;                                     // weight scales of a k-step: one to 64 columns
+  static_assert(AI * NT == BM * 8 && BI * NT == BN * 8 && WTM % 32 == 0 && WTN % 32 == 0 && (BN % 64 == 0 || BN == 32), "tile shape");
+  constexpr int NS = (BN + 63) / 64;                                   // weight scales of a k-step: one to 64 columns
   static_assert(BM + NS <= NT, "a lane to a scale");
   constexpr int SCALES = (BM + BN) * 8, STAGE = SCALES + NT / 4;  // 16-byte chunks
   constexpr int DMAS = AI + BI + 1;
-  __shared__ uint4 lds[ST * STAGE];
+  __shared__ uint4 rings[KG * ST * STAGE];
   __shared__ float4 s_vec[2 * BN / 4];
   float* const vec = reinterpret_cast<float*>(s_vec);
 
@@ -247,10 +282,13 @@ __global__ void __launch_bounds__(WM * WN * 64) k_gemm_f8(Operands p, int tiles_
   const int gsz = min(4, tiles_m - gbase);
   const int tin = t - grp * 4 * tiles_n;
   const int m0 = (gbase + tin % gsz) * BM, n0 = (tin / gsz) * BN;
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int grp_k = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
+  const int tid = threadIdx.x - grp_k * NT, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave % WM, wn = wave / WM;
   const int r16 = lane & 15, q = lane >> 4;
+  uint4* const lds = rings + grp_k * ST * STAGE;
+  const int KT = (p.KT + KG - 1) / KG;                            // k-steps of a group: grp_k, grp_k + KG, ..
 
   const char* const At = p.x + int64_t(m0) * p.ldx;
   const char* const Wt = p.w + int64_t(n0) * p.ldw;
@@ -271,14 +309,17 @@ __global__ void __launch_bounds__(WM * WN * 64) k_gemm_f8(Operands p, int tiles_
                                : p.sw + int64_t(min(n0 + 64 * min(tid - BM, NS - 1), p.N - 1) / 128) * p.sw_row;
   const int64_t scale_step = of_x ? p.sx_block : p.sw_block;
 
-  // the j-th DMA instruction of the fill of `to` with k-step kt; k-steps are filled in order, so the scales' address runs
-  // along
+  // the j-th DMA instruction of the fill of `to` with the group's k-step kt (past the last: the last again, which counts
+  // nothing); k-steps are filled in order, so the scales' address runs along
   auto dma_one = [&](uint4* to, int kt, int j) {
-    if (j < AI) dma16(At + kt * 128, off[j], to + (wave * AI + j) * 64);
-    else if (j < AI + BI) dma16(Wt + kt * 128, off[j], to + BM * 8 + (wave * BI + (j - AI)) * 64);
-    else {
+    const int k0 = KG == 1 ? kt : min(kt * KG + grp_k, p.KT - 1);
+    if (j < AI) dma16(At + k0 * 128, off[j], to + (wave * AI + j) * 64);
+    else if (j < AI + BI) dma16(Wt + k0 * 128, off[j], to + BM * 8 + (wave * BI + (j - AI)) * 64);
+    else if constexpr (KG == 1) {
       dma4(scale_at, to + SCALES + wave * 16);
       scale_at += scale_step;
+    } else {
+      dma4(scale_at + k0 * scale_step, to + SCALES + wave * 16);
     }
   };
   f32x4 acc[TM][TN];
@@ -287,75 +328,358 @@ __global__ void __launch_bounds__(WM * WN * 64) k_gemm_f8(Operands p, int tiles_
 #pragma unroll
     for (int b = 0; b < TN; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  auto frag = [&](const uint4* s, int r) {
-    return Frag{s[r * 8 + ((2 * q) ^ swz(r))], s[r * 8 + ((2 * q + 1) ^ swz(r))]};
+  // this lane's places in a stage: two chunks of row r16 of the wave's part, 16 rows (128 chunks, whose swizzle is the
+  // same) from one to the next.  A 16-byte read serves lanes 0 to 3, 12 to 15 and 20 to 27 together, then 4 to 11, 16 to 19
+  // and 28 to 31: with chunks q and q + 4 to the q-th 16 lanes they are on distinct banks, with 2 q and 2 q + 1 two by two on the
+  // same (a third of LDS's time)
+  const int c0 = q ^ swz(r16), c1 = (q + 4) ^ swz(r16);
+  const int x_at = (wm * WTM + r16) * 8, w_at = (BM + wn * WTN + r16) * 8;
+  const int xs_at = SCALES * 4 + wm * WTM + r16, ws_at = SCALES * 4 + BM;
+  // Tile by tile of 16 x 16, row after row of them.  A tile's products reach its sum LAG tiles later, when they have left
+  // the matrix pipe; the next row of x is read a row ahead.  All reads of a stage are over before the k-step's last row, so
+  // that there the barrier is that frees it and opens the next one: under the last row's products the next
+  // k-step's first operands come from LDS, each weight operand in the place of the one that was just used for the last
+  // time, and the fill of the freed stage goes out.
+  constexpr bool FULL = !E::kBf16;
+  constexpr int LAG = TN >= 4 ? 3 : 1, R = LAG + 1, T = TM * TN, NF = WTN / 32;
+  static_assert(T % R == 0 && TN % 2 == 0 && LAG <= TN && TM >= 2, "products under way belong to one row");
+  Operand<FULL> w[TN];
+  Frag wf[TN], xf;                      // as they come from LDS
+  float xs[TM], ws[NF], before[NF], last[NF];   // scales; the factors of the last two rows, which outlive them
+  f32x4 part[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) part[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < NF; ++i) last[i] = 0.f;
+  auto x_row = [&](const uint4* s, int a) { return Frag{s[x_at + c0 + a * 128], s[x_at + c1 + a * 128]}; };
+  auto w_row = [&](const uint4* s, int b) { return Frag{s[w_at + c0 + b * 128], s[w_at + c1 + b * 128]}; };
+  auto first = [&](const uint4* s, int kt) {
+    const bool counts = KG == 1 || kt * KG + grp_k < p.KT;
+    const float* const sc = reinterpret_cast<const float*>(s);
+    xf = x_row(s, 0);
+#pragma unroll
+    for (int i = 0; i < NF; ++i) ws[i] = counts ? sc[ws_at + (wn * WTN + i * 32) / 64] : 0.f;
+#pragma unroll
+    for (int a = 0; a < TM; ++a) xs[a] = sc[xs_at + a * 16];
   };
-  auto compute = [&](const uint4* s, uint4* to, int kt) {
-    const float* const sc = reinterpret_cast<const float*>(s + SCALES);
-    Frag wf[TN];
-    float ws[TN];
+  // tile u's products, times f, to its sum
+  auto add = [&](int u, float f) {
 #pragma unroll
-    for (int b = 0; b < TN; ++b) {
-      wf[b] = frag(s + BM * 8, wn * WTN + b * 16 + r16);
-      ws[b] = sc[BM + (wn * WTN + b * 16) / 64];
-    }
+    for (int i = 0; i < 4; ++i) acc[u / TN][u % TN][i] = fmaf(part[u % R][i], f, acc[u / TN][u % TN][i]);
+  };
+  // k-step kt out of stage st; LATER fills are on their way when the next k-step's is over
+  int st = 0;
+  auto step = [&](int kt, auto later, auto next_, auto fill_) {
+    constexpr bool next = decltype(next_)::value, fill = decltype(fill_)::value;
+    uint4* const s = lds + st * STAGE;
+    st = st == ST - 1 ? 0 : st + 1;
+    uint4* const n = lds + st * STAGE;
+    Operand<FULL> x;
 #pragma unroll
-    for (int a = 0; a < TM; ++a) {
-      if (kt >= 0) {
-        constexpr int DPS = (DMAS + TM - 1) / TM;
+    for (int t = 0; t < T; ++t) {
+      const int a = t / TN, b = t % TN;
+      if (b == 0) {
+        x.set(xf);
+        if (a + 1 < TM) {
+          xf = x_row(s, a + 1);
+        } else {
 #pragma unroll
-        for (int j = a * DPS; j < (a + 1) * DPS; ++j)
-          if (j < DMAS) dma_one(to, kt, j);
+          for (int i = 0; i < NF; ++i) {
+            before[i] = xs[TM - 2] * ws[i];
+            last[i] = xs[TM - 1] * ws[i];
+          }
+          if constexpr (next) {
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(0xC07F);         // lgkmcnt(0): this wave's reads of the stage have returned
+            wait_vmcnt<decltype(later)::value * DMAS>();  // and its part of the next k-step has landed
+            if constexpr (NW > 1) __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            first(n, kt + 1);
+          }
+        }
       }
-      const int r = wm * WTM + a * 16 + r16;
-      const Frag xf = frag(s, r);
-      const float xs = sc[r];
+      if (a == 0) w[b].set(wf[b]);
+      part[t % R] = product(w[b], x);
+      if (next && a == TM - 1) wf[b] = w_row(n, b);
+      if (fill && a == TM - 1) {
+        constexpr int DPS = (DMAS + TN - 1) / TN;
 #pragma unroll
-      for (int b = 0; b < TN; ++b) {
-        const f32x4 part = product<!E::kBf16>(wf[b], xf);
-        const float f = xs * ws[b];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[a][b][i] = fmaf(part[i], f, acc[a][b][i]);
+        for (int j = b * DPS; j < (b + 1) * DPS; ++j)
+          if (j < DMAS) dma_one(s, kt + ST, j);
       }
+      __builtin_amdgcn_sched_barrier(0);
+      const int u = (t + T - LAG) % T, i = u % TN / 2;
+      add(u, u / TN == TM - 1 ? last[i] : a == TM - 1 ? before[i] : xs[u / TN] * ws[i]);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
 
 #pragma unroll
-  for (int i = 0; i < ST - 1; ++i)
-    if (i < p.KT)
+  for (int i = 0; i < ST; ++i)
+    if (i < KT)
 #pragma unroll
       for (int j = 0; j < DMAS; ++j) dma_one(lds + i * STAGE, i, j);
-  epi.template start<BN, NT>(vec, n0, p.N, tid);
-  for (int kt0 = 0; kt0 < p.KT; kt0 += ST) {
+  if (grp_k == 0) epi.template start<BN, NT>(vec, n0, p.N, tid);
+  if (KT >= ST) wait_vmcnt<(ST - 1) * DMAS>();
+  else wait_vmcnt<0>();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  first(lds, 0);
 #pragma unroll
-    for (int i = 0; i < ST; ++i) {
-      const int kt = kt0 + i;
-      if (kt >= p.KT) break;
-      // before the barrier: this wave's part of k-step kt has landed (the ST - 2 steps after it may be on their way)
-      if (ST > 2 && kt + ST - 2 < p.KT) wait_vmcnt<(ST - 2) * DMAS>();
-      else wait_vmcnt<0>();
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      compute(lds + i * STAGE, lds + (i + ST - 1) % ST * STAGE, kt + ST - 1 < p.KT ? kt + ST - 1 : -1);
-    }
-  }
-  static_assert(sizeof(lds) >= NW * E::kStrip, "epilogue LDS");
+  for (int b = 0; b < TN; ++b) wf[b] = w_row(lds, b);
+  // The last k-steps fill nothing, and are code of their own: a branch around the fills would cut the k-step into blocks,
+  // over which sums and products are not kept in registers.
+  int kt = 0;
+  for (; kt + ST < KT; ++kt) step(kt, std::integral_constant<int, ST - 2>{}, std::true_type{}, std::true_type{});
+  if constexpr (ST > 3)
+    if (KT >= 4) step(KT - 4, std::integral_constant<int, 2>{}, std::true_type{}, std::false_type{});
+  if constexpr (ST > 2)
+    if (KT >= 3) step(KT - 3, std::integral_constant<int, 1>{}, std::true_type{}, std::false_type{});
+  if (KT >= 2) step(KT - 2, std::integral_constant<int, 0>{}, std::true_type{}, std::false_type{});
+  step(KT - 1, std::integral_constant<int, 0>{}, std::false_type{}, std::false_type{});
+#pragma unroll
+  for (int u = T - LAG; u < T; ++u) add(u, last[u % TN / 2]);
+  static_assert(sizeof(rings) >= NW * E::kStrip + (KG - 1) * BM * BN * 4, "epilogue LDS");
   __builtin_amdgcn_s_waitcnt(0xC07F);               // lgkmcnt(0): this wave's reads of the last stage
   __builtin_amdgcn_s_barrier();                     // every wave is done with it
   asm volatile("" ::: "memory");
-  epi.template finish<BN, WTM, WTN>(acc, reinterpret_cast<char*>(lds) + wave * E::kStrip, vec, m0 + wm * WTM, n0, wn * WTN, p.M,
+  if constexpr (KG > 1) {                           // the groups' sums, in their order
+    f32x4* const sums = reinterpret_cast<f32x4*>(reinterpret_cast<char*>(rings) + NW * E::kStrip) + tid;
+    if (grp_k > 0) {
+#pragma unroll
+      for (int t = 0; t < T; ++t) sums[((grp_k - 1) * T + t) * NT] = acc[t / TN][t % TN];
+      __builtin_amdgcn_s_waitcnt(0xC07F);
+    }
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (grp_k > 0) return;
+#pragma unroll
+    for (int g = 0; g < KG - 1; ++g)
+#pragma unroll
+      for (int t = 0; t < T; ++t) acc[t / TN][t % TN] += sums[(g * T + t) * NT];
+  }
+  epi.template finish<BN, WTM, WTN>(acc, reinterpret_cast<char*>(rings) + wave * E::kStrip, vec, m0 + wm * WTM, n0, wn * WTN, p.M,
                                     p.N, lane);
 }
 
-template <int BM, int BN, int WM, int WN, int ST, class E>
+// Few rows: G waves share 16 RT rows x 16 columns, wave g taking every G-th k-step straight from memory into registers, U of
+// them on their way at once (bound by the weights' way from memory, of which a k-step of 16 columns is 16 whole lines),
+// and add their sums in LDS in the waves' order.
+template <int RT, int G, class E>
+__global__ void __launch_bounds__(G * 64) k_f8_few(Operands p, int tiles_n, E epi) {
+  constexpr bool FULL = !E::kBf16;
+  constexpr int U = RT == 1 ? 4 : 2;
+  __shared__ f32x4 sums[G][RT][64];
+  const int tid = threadIdx.x, lane = tid & 63, g = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r16 = lane & 15, q = lane >> 4;
+  const int m0 = int(blockIdx.x) / tiles_n * (16 * RT), n0 = int(blockIdx.x) % tiles_n * 16;
+  const char* const w = p.w + int64_t(min(n0 + r16, p.N - 1)) * p.ldw + 16 * q;
+  const float* const sw = p.sw + int64_t(n0 / 128) * p.sw_row;
+  const char* x[RT];
+  const float* sx[RT];
+#pragma unroll
+  for (int a = 0; a < RT; ++a) {
+    const int m = min(m0 + 16 * a + r16, p.M - 1);
+    x[a] = p.x + int64_t(m) * p.ldx + 16 * q;
+    sx[a] = p.sx + int64_t(m) * p.sx_row;
+  }
+  f32x4 acc[RT];
+#pragma unroll
+  for (int a = 0; a < RT; ++a) acc[a] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int kt0 = g; kt0 < p.KT; kt0 += U * G) {
+    Frag wf[U], xf[U][RT];
+    float f[U][RT];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {                       // past the last k-step: that one again, times zero
+      const int kt = min(kt0 + u * G, p.KT - 1);
+      wf[u] = Frag{*reinterpret_cast<const uint4*>(w + kt * 128), *reinterpret_cast<const uint4*>(w + kt * 128 + 64)};
+#pragma unroll
+      for (int a = 0; a < RT; ++a) {
+        xf[u][a] = Frag{*reinterpret_cast<const uint4*>(x[a] + kt * 128), *reinterpret_cast<const uint4*>(x[a] + kt * 128 + 64)};
+        f[u][a] = sx[a][kt * p.sx_block];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int kt = kt0 + u * G;
+      if (kt >= p.KT) break;
+      const float ws = sw[kt * p.sw_block];
+      Operand<FULL> wo, xo;
+      wo.set(wf[u]);
+#pragma unroll
+      for (int a = 0; a < RT; ++a) {
+        xo.set(xf[u][a]);
+        const f32x4 part = product(wo, xo);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[a][i] = fmaf(part[i], f[u][a] * ws, acc[a][i]);
+      }
+    }
+  }
+#pragma unroll
+  for (int a = 0; a < RT; ++a) sums[g][a][lane] = acc[a];
+  __syncthreads();
+  for (int i = tid; i < RT * 64; i += G * 64) {
+    const int a = i >> 6;
+    f32x4 z = sums[0][a][lane];
+#pragma unroll
+    for (int j = 1; j < G; ++j) z += sums[j][a][lane];
+    const int m = m0 + 16 * a + r16, n = n0 + 4 * q;
+    if (m >= p.M) continue;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (n + j < p.N) epi.one(z[j], m, n + j);
+  }
+}
+
+// One to four rows: a wave takes a column, its weights' whole row straight from memory (16 codes a lane, U pieces on their
+// way at once), and multiplies in fp32: every product is exact, and a lane's 16 share their scales.
+template <int MR, class E>
+__global__ void __launch_bounds__(256) k_f8_rows(Operands p, E epi) {
+  constexpr int U = 4;
+  const int lane = threadIdx.x & 63, n = int(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (n >= p.N) return;
+  const char* const w = p.w + int64_t(n) * p.ldw;
+  const float* const sw = p.sw + int64_t(n / 128) * p.sw_row;
+  float acc[MR];
+#pragma unroll
+  for (int m = 0; m < MR; ++m) acc[m] = 0.f;
+  const int pieces = p.KT * 8;
+  for (int i0 = lane; i0 < pieces; i0 += 64 * U) {
+    u32x4 wv[U], xv[U][MR];
+    float f[U][MR];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = min(i0 + 64 * u, pieces - 1);
+      wv[u] = *reinterpret_cast<const u32x4*>(w + i * 16);
+#pragma unroll
+      for (int m = 0; m < MR; ++m) {
+        const int r = min(m, p.M - 1);
+        xv[u][m] = *reinterpret_cast<const u32x4*>(p.x + int64_t(r) * p.ldx + i * 16);
+        f[u][m] = p.sx[int64_t(r) * p.sx_row + (i >> 3) * p.sx_block] * sw[(i >> 3) * p.sw_block];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i0 + 64 * u >= pieces) break;
+      float d[MR];
+#pragma unroll
+      for (int m = 0; m < MR; ++m) d[m] = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(wv[u][j], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(wv[u][j], true);
+#pragma unroll
+        for (int m = 0; m < MR; ++m) {
+          const f32x2 c = __builtin_amdgcn_cvt_pk_f32_fp8(xv[u][m][j], false), e = __builtin_amdgcn_cvt_pk_f32_fp8(xv[u][m][j], true);
+          d[m] = fmaf(a[0], c[0], fmaf(a[1], c[1], fmaf(b[0], e[0], fmaf(b[1], e[1], d[m]))));
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < MR; ++m) acc[m] = fmaf(d[m], f[u][m], acc[m]);
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < MR; ++m)
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) acc[m] += __shfl_xor(acc[m], o, 64);
+#pragma unroll
+  for (int m = 0; m < MR; ++m)
+    if (lane == m && m < p.M) epi.one(acc[m], m, n);
+}
+
+template <int BM, int BN, int WM, int WN, int ST, int KG = 1, class E>
 Status launch(const Operands& p, const E& epi, hipStream_t s) {
   const int tn = (p.N + BN - 1) / BN, tiles = tn * ((p.M + BM - 1) / BM), per = (tiles + 7) / 8;
-  hipLaunchKernelGGL((k_gemm_f8<BM, BN, WM, WN, ST, E>), dim3(8 * per), dim3(WM * WN * 64), 0, s, p, tn, tiles, per, epi);
+  hipLaunchKernelGGL((k_gemm_f8<BM, BN, WM, WN, ST, KG, E>), dim3(8 * per), dim3(KG * WM * WN * 64), 0, s, p, tn, tiles, per, epi);
   DC_HIP(hipGetLastError());
   return Status::ok();
 }
 
+template <int MR, class E>
+Status launch_rows(const Operands& p, const E& epi, hipStream_t s) {
+  hipLaunchKernelGGL((k_f8_rows<MR, E>), dim3((p.N + 3) / 4), dim3(256), 0, s, p, epi);
+  DC_HIP(hipGetLastError());
+  return Status::ok();
+}
+
+template <int RT, int G, class E>
+Status launch_few(const Operands& p, const E& epi, hipStream_t s) {
+  const int tn = (p.N + 15) / 16, tiles = tn * ((p.M + 16 * RT - 1) / (16 * RT));
+  hipLaunchKernelGGL((k_f8_few<RT, G, E>), dim3(tiles), dim3(G * 64), 0, s, p, tn, epi);
+  DC_HIP(hipGetLastError());
+  return Status::ok();
+}
+
+// Cost in us of tile i.  Tiles in rounds of per_cu workgroups on each compute unit: each round `fixed` plus its k-steps
+// (groups share them) at step[w - 1], w the workgroups that a compute unit has; with one per compute unit a round that fills
+// part of the chip lies between `idle` and step[0].  Few rows (per_cu 0): `fixed` is a k-step's way from memory, step[0] what
+// the load of a compute unit (workgroups to each) adds to it, step[1] what the load beyond two does.  Fitted to timings on
+// MI355X of 607 shapes (M 1 to 17,776, N 32 to 11,520, K 64 to 7,680; widths of a block's products and any others).  The
+// tile it picks is 1.8 % (fp32 outputs, by bf16 products) and 1.6 % (bf16 outputs) behind the best of all that were timed on
+// average, 36 and 27 % at worst (11 x 8,518 x 7,680, 2 x 11,520 x 1,920).  In us, this and the next best kept tile:
+// 17,776 x 7,680 x 1,920 192 x 256 289 (256 x 128 314); 1,556 x 5,760 x 1,920 24.0 (64 x 128 30.3); 50 x 11,520 x 1,920 in
+// fp32 64 x 64 in two groups 9.0 (one 9.1); 50 x 1,920 x 7,680 32 x 32 in eight 9.7 (few rows 16.2, 64 x 64 21.7);
+// 1 x 1,920 x 7,680 a wave to a column 5.7 (few rows 6.9, 32 x 32 8.9).
+struct TileCost { int bm, bn, groups, per_cu; float launch, fixed, step[3], idle; };
+constexpr int kTileCount = 13;
+constexpr float kNever = 1e30f;
+constexpr TileCost kTiles[2][kTileCount] = {
+    {{192, 256, 1, 1, 0.527f, 4.613f, {1.267f}, 0.915f},           // bf16 outputs
+     {256, 128, 1, 1, 0.972f, 3.510f, {0.933f}, 0.700f},
+     {192, 128, 1, 1, 0.894f, 2.924f, {0.819f}, 0.651f},
+     {128, 128, 1, 2, 0.836f, 2.915f, {0.570f, 0.968f}, 0.f},
+     {64, 128, 1, 2, 1.695f, 1.798f, {0.303f, 0.617f}, 0.f},
+     {64, 64, 1, 3, 1.930f, 1.121f, {0.236f, 0.383f, 0.587f}, 0.f},
+     {64, 64, 2, 1, 1.522f, 1.606f, {0.454f}, 0.371f},
+     {32, 64, 2, 2, 1.724f, 1.321f, {0.310f, 0.555f}, 0.f},
+     {32, 32, 4, 1, 1.616f, 1.411f, {0.474f}, 0.286f},
+     {32, 32, 8, 1, 1.517f, 1.584f, {0.845f}, 0.532f},
+     {16, 16, 8, 0, 2.354f, 0.573f, {0.429f, 0.138f}, 0.f},
+     {1, 4, 1, 0, 1.878f, 1.260f, {0.059f, 0.047f}, 0.f},
+     {2, 4, 1, 0, 1.490f, 1.578f, {0.193f, 0.f}, 0.f}},
+    {{192, 256, 1, 1, kNever, 0.f, {0.f}, 0.f},                    // fp32 outputs: the conversions leave no registers
+     {256, 128, 1, 1, kNever, 0.f, {0.f}, 0.f},
+     {192, 128, 1, 1, 0.175f, 4.504f, {1.390f}, 1.200f},
+     {128, 128, 1, 2, 0.101f, 4.622f, {0.894f, 1.622f}, 0.f},
+     {64, 128, 1, 2, 1.367f, 2.456f, {0.570f, 1.006f}, 0.f},
+     {64, 64, 1, 3, 1.628f, 1.546f, {0.394f, 0.655f, 0.907f}, 0.f},
+     {64, 64, 2, 1, 1.389f, 1.912f, {0.720f}, 0.598f},
+     {32, 64, 2, 2, 1.676f, 1.485f, {0.471f, 0.824f}, 0.f},
+     {32, 32, 4, 2, 1.708f, 1.469f, {0.494f, 0.908f}, 0.f},
+     {32, 32, 8, 1, 1.507f, 1.867f, {1.014f}, 0.690f},
+     {16, 16, 8, 0, 2.448f, 0.555f, {0.423f, 0.142f}, 0.f},
+     {1, 4, 1, 0, 1.993f, 1.214f, {0.039f, 0.062f}, 0.f},
+     {2, 4, 1, 0, 1.584f, 1.560f, {0.180f, 0.f}, 0.f}}};
+constexpr int kFewRows = 10, kRows1 = 11, kRows2 = 12;
+
 }  // namespace
+
+int f8_tile(int M, int N, int ksteps, int cus, bool full) {
+  int best = 0;
+  float least = kNever;
+  for (int i = 0; i < kTileCount; ++i) {
+    if (i >= kRows1 && M > kTiles[0][i].bm) continue;
+    const TileCost& c = kTiles[full][i];
+    const int steps = i >= kRows1 ? (ksteps + 31) / 32 : (ksteps + c.groups - 1) / c.groups;
+    const int64_t tiles = int64_t((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn);
+    float t = c.launch;
+    if (c.per_cu == 0) {
+      const float load = float(tiles) / float(cus);
+      t += float(steps) * (c.fixed + c.step[0] * load + c.step[1] * std::max(0.f, load - 2.f));
+    } else {
+      const int64_t round = int64_t(c.per_cu) * cus, rounds = tiles / round, rest = tiles % round;
+      t += float(rounds) * (c.fixed + float(steps) * c.step[c.per_cu - 1]);
+      if (rest) {
+        const float part = float(rest) / float(cus);
+        t += c.fixed + float(steps) * (c.per_cu == 1 ? c.idle + (c.step[0] - c.idle) * part : c.step[(rest - 1) / cus]);
+      }
+    }
+    if (t < least) {
+      best = i;
+      least = t;
+    }
+  }
+  return best;
+}
 
 Status linear_f8(const dc_linear_f8_args& a, hipStream_t s) {
   if (int64_t((a.rows + 63) / 64) * ((a.out_features + 63) / 64) > (1 << 23))
@@ -363,6 +687,8 @@ Status linear_f8(const dc_linear_f8_args& a, hipStream_t s) {
   const Operands p{reinterpret_cast<const char*>(a.x), reinterpret_cast<const char*>(a.w), a.x_scale, a.w_scale,
                    a.x_scale_block, a.w_scale_row, a.w_scale_block, a.rows > 1 ? int(a.x_scale_row) : 0, int(a.ld_x), int(a.ld_w),
                    a.rows, a.out_features, a.in_features / 128};
+  const int cus = compute_units();
+  if (cus <= 0) return Status::make(DC_ERR_HIP, "e4m3 product: no device");
   auto run = [&](auto e) {
     e.bias = a.bias;
     e.gate = a.gate;
@@ -370,7 +696,24 @@ Status linear_f8(const dc_linear_f8_args& a, hipStream_t s) {
     e.ldr = a.ld_residual;
     e.out = a.out;
     e.ldo = a.ld_out;
-    return launch<64, 64, 2, 2, 3>(p, e, s);
+    e.lines = (reinterpret_cast<uintptr_t>(a.out) | uint64_t(a.ld_out) * e.E) % 128 == 0;
+    constexpr bool BF = decltype(e)::kBf16;
+    switch (f8_tile(p.M, p.N, p.KT, cus, !BF)) {
+      case 0: if constexpr (BF) return launch<192, 256, 2, 4, 2>(p, e, s); break;
+      case 1: if constexpr (BF) return launch<256, 128, 4, 2, 3>(p, e, s); break;
+      case 2: return launch<192, 128, 2, 4, 3>(p, e, s);
+      case 3: return launch<128, 128, 2, 2, 2>(p, e, s);
+      case 4: return launch<64, 128, 2, 2, 3>(p, e, s);
+      case 5: return launch<64, 64, 2, 2, 3>(p, e, s);
+      case 6: return launch<64, 64, 2, 2, 3, 2>(p, e, s);
+      case 7: return launch<32, 64, 1, 2, 3, 2>(p, e, s);
+      case 8: return launch<32, 32, 1, 1, BF ? 3 : 2, 4>(p, e, s);
+      case 9: return launch<32, 32, 1, 1, 2, 8>(p, e, s);
+      case kFewRows: return launch_few<1, 8>(p, e, s);
+      case kRows1: return launch_rows<1>(p, e, s);
+      case kRows2: return launch_rows<2>(p, e, s);
+    }
+    return Status::shape("e4m3 product: no such tile");
   };
   if (a.out_dtype == DC_BF16)
     return a.residual ? run(Epi<true, false, true>{}) : a.gelu ? run(Epi<true, true, false>{}) : run(Epi<true, false, false>{});

@@ -9,7 +9,7 @@ import pytest
 from oracle import dit
 from oracle import ext as X
 from paper_2608_16354_amd import inputs as I
-from tests.gpu_util import say, t
+from tests.gpu_util import _native, compute_units, say, t
 
 pytestmark = pytest.mark.gpu
 
@@ -344,6 +344,42 @@ def test_linear_ragged(api, dev, m, n, k):
         v = check_linear(got, *d[:4], d[4] if bias else None, d[5], d[6], kind, dt == "bf16", True)
         if kind == "plain" and dt == "bf16":            # one rounding, of an exact sum
             assert np.array_equal(got, I.round_bf16(v.astype(np.float32)))
+
+
+F8_TILES = ("192x256", "256x128", "192x128", "128x128", "64x128", "64x64", "64x64 x 2", "32x64 x 2", "32x32 x 4", "32x32 x 8", "16x16 x 8",
+            "column", "column of 2")
+TILE_SHAPES = {     # (M, N, K), type of the outputs: the tile on 256 compute units
+    (1717, 4990, 896, "bf16"): "192x256", (1442, 4158, 1280, "bf16"): "256x128", (925, 4989, 1664, "bf16"): "192x128",
+    (1301, 5765, 1024, "bf16"): "128x128", (637, 3139, 3840, "bf16"): "64x128", (269, 2860, 1664, "bf16"): "64x64",
+    (574, 1089, 2048, "bf16"): "64x64 x 2", (65, 5128, 3840, "bf16"): "32x64 x 2", (61, 4095, 3584, "bf16"): "32x32 x 4",
+    (127, 2023, 3840, "bf16"): "32x32 x 8", (15, 4927, 2048, "bf16"): "16x16 x 8", (1, 6403, 3840, "bf16"): "column", (2, 6403, 3840, "bf16"): "column of 2",
+    (925, 4989, 1664, "f32"): "192x128", (1301, 5765, 1024, "f32"): "128x128", (637, 3139, 3840, "f32"): "64x128", (411, 4867, 640, "f32"): "64x64",
+    (574, 1089, 2048, "f32"): "64x64 x 2", (65, 5128, 3840, "f32"): "32x64 x 2", (964, 384, 3456, "f32"): "32x32 x 4", (476, 411, 3840, "f32"): "32x32 x 8",
+    (15, 4927, 2048, "f32"): "16x16 x 8", (1, 6403, 3840, "f32"): "column", (2, 6403, 3840, "f32"): "column of 2",
+}
+
+
+def f8_tile(m, n, k, dt, cus):
+    return F8_TILES[_native("_ZN2dc7f8_tileEiiiib", m, n, k // 128, cus, dt == "f32")]
+
+
+@pytest.mark.parametrize("mnkt", list(TILE_SHAPES))
+@pytest.mark.parametrize("kind", ["plain", "gelu", "gated"])
+def test_linear_tiles(api, dev, mnkt, kind):
+    """Every tile of the product in both types, ragged in rows and columns, and whole lines of outputs."""
+    m, n, k, dt = mnkt
+    assert f8_tile(m, n, k, dt, compute_units(dev)) == TILE_SHAPES[mnkt]
+    data = whole_inputs(m, n, k, 7)
+    pick = np.unique(np.r_[0, m - 1, np.random.default_rng(0).integers(0, m, 150)])
+    for width in sorted({n, n // 64 * 64}):
+        if f8_tile(m, width, k, dt, compute_units(dev)) != TILE_SHAPES[mnkt]:
+            continue
+        x, xs, w, ws, b, gate, res = data
+        cut = (x, xs, w[:width], ws[: -(-width // 128)], b[:width], gate[:width], np.ascontiguousarray(res[:, :width]))
+        say("linear tile", mnkt, width, TILE_SHAPES[mnkt], kind)
+        got = run_linear(api, dev, cut, kind, dt, kind != "plain")
+        d = of_type(cut, dt, dev)
+        check_linear(got[pick], d[0][pick], d[1][pick], d[2], d[3], d[4] if kind != "plain" else None, d[5], d[6][pick], kind, dt == "bf16", True)
 
 
 @pytest.mark.parametrize("m,n,k", [(1, 1920, 7680), (50, 333, 1920), (257, 513, 1152), (700, 1920, 1920), (1, 40, 65536)])
