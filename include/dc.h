@@ -282,9 +282,9 @@ typedef struct {
 } dc_quantize_f8_args;
 dc_status dc_quantize_f8(const dc_quantize_f8_args* args, hipStream_t stream);
 
-/* h = x + residual in fp32; sum := h, rounded once to its type; y = h / sqrt(mean(h^2) + eps) * weight over the row, of the
- * unrounded h; q, scale := y in e4m3, a scale to 128 features, as dc_quantize_f8 writes rows.  A row's mean square must
- * be below the fp32 range (|h| < 1e18). */
+/* h = x + residual; sum := h in fp32, then in its type; y = h / sqrt(mean(h^2) + eps) * weight over the row, of the unrounded h
+ * and in double; q, scale := y in e4m3, a scale to 128 features, as dc_quantize_f8 writes rows (y / scale is rounded to
+ * fp32 before it becomes a code). */
 typedef struct {
   int32_t rows, cols;             /* rows below 2^24 (0 is a no-op), cols up to 16,384 */
   const void* x;                  /* [rows, ld_x], at any element's address; leading dimensions >= cols */

@@ -225,6 +225,43 @@ def test_norm_of_many_rows(api, dev, rows, cols):
     check_codes(host(q), host(s), X.rms_norm(h, host(w), 1e-6), cols)
 
 
+def check_exactly(q, s, y):
+    """Codes and scales that are rounded once from 64 bits, the quotient once more to fp32: all but what lies within 2^-40 of
+    a border, of which these draws have none.  A scale below fp32's normal range is rounded in steps of 2^-149."""
+    rows, cols = y.shape
+    blocks = -(-cols // 128)
+    v = np.zeros((rows, blocks * 128))
+    v[:, :cols] = y
+    want_s = (np.abs(v).reshape(rows, blocks, 128).max(-1) / 448).astype(np.float32)
+    assert np.array_equal(s, want_s)
+    step = np.repeat(want_s.astype(np.float64), 128, 1)
+    z = np.divide(v, step, out=np.zeros_like(v), where=step > 0)
+    assert np.array_equal(q, X.e4m3(z.astype(np.float32)))
+
+
+@pytest.mark.parametrize("rows,cols,r_type", [(3704, 1152, "f32"), (4097, 1920, "bf16"), (300, 5003, None), (999, 200, "f32"), (20000, 128, "bf16")])
+def test_norm_writes_the_codes_of_the_definition(api, dev, rows, cols, r_type):
+    import torch
+    gen = torch.Generator(dev).manual_seed(cols)
+    x = torch.randn((rows, cols), device=dev, generator=gen).bfloat16()
+    r = None if r_type is None else torch.randn((rows, cols), device=dev, generator=gen).to(kind_of(r_type))
+    w = 1 + 0.2 * torch.randn(cols, device=dev, generator=gen)
+    blocks = -(-cols // 128)
+    q, (s, _) = marked(rows, blocks * 128, dev), scales(rows, blocks, dev)
+    api.dc_rms_norm_f8(x, q, s, weight=w, eps=1e-6, residual=r)
+    check_exactly(host(q), host(s), X.rms_norm(host(x).astype(np.float64) + (0 if r is None else host(r)), host(w), np.float64(np.float32(1e-6))))
+
+
+def test_norm_of_rows_of_any_size(api, dev):
+    """Rows from the smallest numbers to the largest: none overflows, and those that eps outweighs are small, not lost."""
+    import torch
+    x = torch.randn((9, 640), device=dev, generator=torch.Generator(dev).manual_seed(1))
+    x *= (10.0 ** torch.tensor([-44, -38, -30, -10, 0, 10, 19, 30, 38], device=dev, dtype=torch.float64)).float()[:, None] / 8
+    q, (s, _) = marked(9, 640, dev), scales(9, 5, dev)
+    api.dc_rms_norm_f8(x, q, s, eps=1e-6)
+    check_exactly(host(q), host(s), X.rms_norm(host(x).astype(np.float64), None, np.float64(np.float32(1e-6))))
+
+
 def test_norm_of_rows_without_a_number(api, dev):
     """A NaN makes its row NaN, an infinity its block (the others of the row are zeros over an infinite root); the
     padding holds zeros all the same, and other rows keep theirs."""
