@@ -84,12 +84,12 @@ __device__ inline f32x4 product(const Operand<true>& w, const Operand<true>& x) 
   return d;
 }
 
-// GELU(z) = z / (1 + 2^u), u = -2 log2(e) sqrt(2 / pi) (z + 0.044715 z^3)
-template <bool FAST>
+// GELU(z) = z / (1 + 2^u), u = -2 log2(e) sqrt(2 / pi) (z + 0.044715 z^3).  The power and the reciprocal are the vector
+// unit's, a step off each: as a library's power and a division they took an eighth of an fp32 product (17,776 x 7,680 x 1,920
+// 523 us, so 485, without GELU 466).
 __device__ inline float gelu(float z) {
   const float u = z * fmaf(z * z, -0.1029432397f, -2.302208198f);
-  if constexpr (FAST) return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u));
-  else return z / (1.0f + exp2f(u));
+  return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u));
 }
 
 // out = value + bias, through GELU, or residual + gate (value + bias), in rows at any element's address.
@@ -113,7 +113,7 @@ struct Epi {
   static constexpr int kStrip = 32 * kS;
 
   __device__ inline float act(float z) const {
-    if constexpr (GELU) return gelu<BF>(z);
+    if constexpr (GELU) return gelu(z);
     else return z;
   }
 
@@ -161,13 +161,14 @@ struct Epi {
       const bool rest = N % V && nb + width > N;                      // columns behind the last whole piece
       char* const piece = strip + rl * kS + lane % PR * 16;
       u32x4a res[RES ? 2 : 1][4];
+      // Past the edges: the last row's, the last whole piece's (its values go nowhere); with branches around the loads they
+      // go out one by one and registers spill: 17,776 x 7,680 x 1,920 in bf16 363 us, so 304.
       auto fetch = [&](int r0) {
+
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int m = m0 + r0 + rl + j * RS;
-          if (j < NP && whole && m < M)
-            res[r0 / 32 & 1][j] = *reinterpret_cast<const u32x4a*>(static_cast<const char*>(residual) + (m * ldr + nl) * E);
-        }
+        for (int j = 0; j < NP; ++j)
+          res[r0 / 32 & 1][j] = *reinterpret_cast<const u32x4a*>(
+              static_cast<const char*>(residual) + (min(m0 + r0 + rl + j * RS, M - 1) * ldr + min(nl, N - V)) * E);
       };
       if constexpr (RES) fetch(0);
 #pragma unroll
@@ -216,20 +217,23 @@ struct Epi {
         u32x4 v[4];
 #pragma unroll
         for (int j = 0; j < NP; ++j) v[j] = *reinterpret_cast<const u32x4*>(piece + j * RS * kS);
+        if constexpr (RES && !BF) {
 #pragma unroll
-        for (int j = 0; j < NP; ++j) {
-          const int m = m0 + r0 + rl + j * RS;
-          if (!whole || m >= M) continue;
-          if constexpr (RES && !BF)
+          for (int j = 0; j < NP; ++j)
             v[j] = __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, v[j]) + __builtin_bit_cast(f32x4, u32x4(res[r0 / 32 & 1][j])));
-          u32x4a* const at = reinterpret_cast<u32x4a*>(static_cast<char*>(out) + (m * ldo + nl) * E);
-          if (lines) {
-            __builtin_nontemporal_store(v[j], at);
-          } else {
-            asm volatile("" ::: "memory");            // keep the two kinds of store apart
-            *at = v[j];
-            asm volatile("" ::: "memory");
-          }
+        }
+        const int m = m0 + r0 + rl, left = whole ? M - m : 0;          // the lane's first row, and rows from it on
+        char* const to = static_cast<char*>(out) + (m * ldo + nl) * E;
+        if (lines) {
+#pragma unroll
+          for (int j = 0; j < NP; ++j)
+            if (j * RS < left) __builtin_nontemporal_store(v[j], reinterpret_cast<u32x4a*>(to + j * RS * ldo * E));
+        } else {
+          asm volatile("" ::: "memory");              // keep the two kinds of store apart
+#pragma unroll
+          for (int j = 0; j < NP; ++j)
+            if (j * RS < left) *reinterpret_cast<u32x4a*>(to + j * RS * ldo * E) = v[j];
+          asm volatile("" ::: "memory");
         }
 #pragma unroll 1
         for (int n = max(nb, N / V * V); n < tail; ++n) {
@@ -257,31 +261,29 @@ struct Operands {
   int M, N, KT;
 };
 
-// WM x WN waves on a BM x BN tile, ST stages of a k-step, one barrier to a k-step: the fills of k-step kt + ST - 1 go out
-// among the products of k-step kt.  Rows past M or N are clamped to the last row (their results are never
-// stored).  Workgroups are renumbered so that an XCD takes neighbouring tiles.
-template <int BM, int BN, int WM, int WN, int ST, int KG, class E>
-__global__ void __launch_bounds__(KG * WM * WN * 64) k_gemm_f8(Operands p, int tiles_n, int tiles, int per_xcd, E epi) {
-  constexpr int NW = WM * WN, NT = NW * 64;                       // of a group
+// WM x WN waves on a BM x BN tile, ST stages of a k-step, KG groups of waves with every KG-th k-step each.
+template <int BM_, int BN_, int WM_, int WN_, int ST_, int KG_ = 1>
+struct Tile {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, ST = ST_, KG = KG_;
+  static constexpr int NW = WM * WN, NT = NW * 64;                  // of a group
+  static constexpr int kThreads = KG * NT;
+  static constexpr int SCALES = (BM + BN) * 8, STAGE = SCALES + NT / 4;  // 16-byte chunks
+  static constexpr int kRings = KG * ST * STAGE;
+  static constexpr int kVec = 2 * BN;
+};
+
+// The product of tile (m0, n0), with a barrier to a k-step: the fills of k-step kt + ST - 1 go out among the products of
+// k-step kt.  Rows past M or N are clamped to the last row (their results are never stored).
+template <class T_, class E>
+__device__ inline void tile_product(const Operands& p, const E& epi, uint4* rings, float* vec, int m0, int n0) {
+  constexpr int BM = T_::BM, BN = T_::BN, WM = T_::WM, WN = T_::WN, ST = T_::ST, KG = T_::KG, NW = T_::NW, NT = T_::NT;
   constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 16, TN = WTN / 16;
   constexpr int AI = BM * 8 / NT, BI = BN * 8 / NT;               // DMA instructions of a wave and k-step, and one for scales
   static_assert(AI * NT == BM * 8 && BI * NT == BN * 8 && WTM % 32 == 0 && WTN % 32 == 0 && (BN % 64 == 0 || BN == 32), "tile shape");
   constexpr int NS = (BN + 63) / 64;                                   // weight scales of a k-step: one to 64 columns
   static_assert(BM + NS <= NT, "a lane to a scale");
-  constexpr int SCALES = (BM + BN) * 8, STAGE = SCALES + NT / 4;  // 16-byte chunks
+  constexpr int SCALES = T_::SCALES, STAGE = T_::STAGE;
   constexpr int DMAS = AI + BI + 1;
-  __shared__ uint4 rings[KG * ST * STAGE];
-  __shared__ float4 s_vec[2 * BN / 4];
-  float* const vec = reinterpret_cast<float*>(s_vec);
-
-  const int t = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-  if (t >= tiles) return;
-  // groups of four row tiles, as in k_gemm_dma
-  const int tiles_m = (p.M + BM - 1) / BM;
-  const int grp = t / (4 * tiles_n), gbase = grp * 4;
-  const int gsz = min(4, tiles_m - gbase);
-  const int tin = t - grp * 4 * tiles_n;
-  const int m0 = (gbase + tin % gsz) * BM, n0 = (tin / gsz) * BN;
   const int grp_k = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
   const int tid = threadIdx.x - grp_k * NT, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -439,7 +441,7 @@ __global__ void __launch_bounds__(KG * WM * WN * 64) k_gemm_f8(Operands p, int t
   step(KT - 1, std::integral_constant<int, 0>{}, std::false_type{}, std::false_type{});
 #pragma unroll
   for (int u = T - LAG; u < T; ++u) add(u, last[u % TN / 2]);
-  static_assert(sizeof(rings) >= NW * E::kStrip + (KG - 1) * BM * BN * 4, "epilogue LDS");
+  static_assert(T_::kRings * 16 >= NW * E::kStrip + (KG - 1) * BM * BN * 4, "epilogue LDS");
   __builtin_amdgcn_s_waitcnt(0xC07F);               // lgkmcnt(0): this wave's reads of the last stage
   __builtin_amdgcn_s_barrier();                     // every wave is done with it
   asm volatile("" ::: "memory");
@@ -460,6 +462,42 @@ __global__ void __launch_bounds__(KG * WM * WN * 64) k_gemm_f8(Operands p, int t
   }
   epi.template finish<BN, WTM, WTN>(acc, reinterpret_cast<char*>(rings) + wave * E::kStrip, vec, m0 + wm * WTM, n0, wn * WTN, p.M,
                                     p.N, lane);
+}
+
+// Tile t of tiles_m x tiles_n from row m_first on: groups of four row tiles, as in k_gemm_dma.
+template <class T, class E>
+__device__ inline void nth_tile(const Operands& p, const E& epi, uint4* rings, float* vec, int t, int m_first, int tiles_m, int tiles_n) {
+  const int grp = t / (4 * tiles_n), gbase = grp * 4;
+  const int gsz = min(4, tiles_m - gbase);
+  const int tin = t - grp * 4 * tiles_n;
+  tile_product<T>(p, epi, rings, vec, m_first + (gbase + tin % gsz) * T::BM, (tin / gsz) * T::BN);
+}
+
+// Workgroups are renumbered so that an XCD takes neighbouring tiles.
+template <class T, class E>
+__global__ void __launch_bounds__(T::kThreads) k_gemm_f8(Operands p, int tiles_n, int tiles, int per_xcd, E epi) {
+  __shared__ uint4 rings[T::kRings];
+  __shared__ float4 s_vec[T::kVec / 4];
+  const int t = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+  if (t >= tiles) return;
+  nth_tile<T>(p, epi, rings, reinterpret_cast<float*>(s_vec), t, 0, (p.M + T::BM - 1) / T::BM, tiles_n);
+}
+
+// Rows up to m_rest in A's tiles, which fill the chip whole rounds, and the others in B's, which start as A's end.
+template <class A, class B, class E>
+__global__ void __launch_bounds__(A::kThreads) k_gemm_f8_two(Operands p, int m_rest, int per_a, int per_b, E epi) {
+  static_assert(A::kThreads == B::kThreads, "one launch");
+  __shared__ uint4 rings[std::max(A::kRings, B::kRings)];
+  __shared__ float4 s_vec[std::max(A::kVec, B::kVec) / 4];
+  float* const vec = reinterpret_cast<float*>(s_vec);
+  const int i = blockIdx.x - 8 * per_a;
+  if (i < 0) {
+    const int tn = (p.N + A::BN - 1) / A::BN, tm = m_rest / A::BM, t = (blockIdx.x & 7) * per_a + (blockIdx.x >> 3);
+    if (t < tm * tn) nth_tile<A>(p, epi, rings, vec, t, 0, tm, tn);
+  } else {
+    const int tn = (p.N + B::BN - 1) / B::BN, tm = (p.M - m_rest + B::BM - 1) / B::BM, t = (i & 7) * per_b + (i >> 3);
+    if (t < tm * tn) nth_tile<B>(p, epi, rings, vec, t, m_rest, tm, tn);
+  }
 }
 
 // Few rows: G waves share 16 RT rows x 16 columns, wave g taking every G-th k-step straight from memory into registers, U of
@@ -586,10 +624,20 @@ __global__ void __launch_bounds__(256) k_f8_rows(Operands p, E epi) {
     if (lane == m && m < p.M) epi.one(acc[m], m, n);
 }
 
-template <int BM, int BN, int WM, int WN, int ST, int KG = 1, class E>
+template <class T, class E>
 Status launch(const Operands& p, const E& epi, hipStream_t s) {
-  const int tn = (p.N + BN - 1) / BN, tiles = tn * ((p.M + BM - 1) / BM), per = (tiles + 7) / 8;
-  hipLaunchKernelGGL((k_gemm_f8<BM, BN, WM, WN, ST, KG, E>), dim3(8 * per), dim3(KG * WM * WN * 64), 0, s, p, tn, tiles, per, epi);
+  const int tn = (p.N + T::BN - 1) / T::BN, tiles = tn * ((p.M + T::BM - 1) / T::BM), per = (tiles + 7) / 8;
+  hipLaunchKernelGGL((k_gemm_f8<T, E>), dim3(8 * per), dim3(T::kThreads), 0, s, p, tn, tiles, per, epi);
+  DC_HIP(hipGetLastError());
+  return Status::ok();
+}
+
+template <class A, class B, class E>
+Status launch_two(const Operands& p, int m_rest, const E& epi, hipStream_t s) {
+  const int tiles_a = m_rest / A::BM * ((p.N + A::BN - 1) / A::BN);
+  const int tiles_b = (p.M - m_rest + B::BM - 1) / B::BM * ((p.N + B::BN - 1) / B::BN);
+  const int per_a = (tiles_a + 7) / 8, per_b = (tiles_b + 7) / 8;
+  hipLaunchKernelGGL((k_gemm_f8_two<A, B, E>), dim3(8 * (per_a + per_b)), dim3(A::kThreads), 0, s, p, m_rest, per_a, per_b, epi);
   DC_HIP(hipGetLastError());
   return Status::ok();
 }
@@ -650,28 +698,54 @@ constexpr TileCost kTiles[2][kTileCount] = {
      {1, 4, 1, 0, 1.993f, 1.214f, {0.039f, 0.062f}, 0.f},
      {2, 4, 1, 0, 1.584f, 1.560f, {0.180f, 0.f}, 0.f}}};
 constexpr int kFewRows = 10, kRows1 = 11, kRows2 = 12;
+// Pairs of tiles: what is left of the rows behind tile a's whole rounds, in which it would leave most of the chip idle, goes
+// to tile b (us, one tile / two): 17,776 x 1,920 x 7,680 gated in fp32 462 / 434, 3,704 x 4,608 x 1,152 through GELU in bf16
+// 33.2 / 28.8, in fp32 54.8 / 42.6.
+struct TilePair { int a, b; };
+constexpr TilePair kPairs[] = {{0, 2}, {0, 6}, {3, 5}};           // the first two for bf16 outputs, the last for fp32 ones
+constexpr int kFirstPair = kTileCount, kPairCount = 3;
+
+float tile_cost(int i, int64_t M, int N, int ksteps, int cus, bool full) {
+  const TileCost& c = kTiles[full][i];
+  const int steps = i >= kRows1 ? (ksteps + 31) / 32 : (ksteps + c.groups - 1) / c.groups;
+  const int64_t tiles = (M + c.bm - 1) / c.bm * ((N + c.bn - 1) / c.bn);
+  if (c.per_cu == 0) {
+    const float load = float(tiles) / float(cus);
+    return c.launch + float(steps) * (c.fixed + c.step[0] * load + c.step[1] * std::max(0.f, load - 2.f));
+  }
+  const int64_t round = int64_t(c.per_cu) * cus, rounds = tiles / round, rest = tiles % round;
+  float t = c.launch + float(rounds) * (c.fixed + float(steps) * c.step[c.per_cu - 1]);
+  if (rest) {
+    const float part = float(rest) / float(cus);
+    t += c.fixed + float(steps) * (c.per_cu == 1 ? c.idle + (c.step[0] - c.idle) * part : c.step[(rest - 1) / cus]);
+  }
+  return t;
+}
+
+// Rows of the row tiles that tile i's whole rounds take
+int rows_of_rounds(int i, bool full, int M, int N, int cus) {
+  const TileCost& c = kTiles[full][i];
+  const int64_t tn = (N + c.bn - 1) / c.bn, round = int64_t(c.per_cu) * cus;
+  return int((M + c.bm - 1) / c.bm * tn / round * round / tn) * c.bm;
+}
 
 }  // namespace
 
 int f8_tile(int M, int N, int ksteps, int cus, bool full) {
+  if (N < 8) return kFewRows;           // the others' epilogue reads and writes whole 16-byte pieces of a row
   int best = 0;
   float least = kNever;
-  for (int i = 0; i < kTileCount; ++i) {
-    if (i >= kRows1 && M > kTiles[0][i].bm) continue;
-    const TileCost& c = kTiles[full][i];
-    const int steps = i >= kRows1 ? (ksteps + 31) / 32 : (ksteps + c.groups - 1) / c.groups;
-    const int64_t tiles = int64_t((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn);
-    float t = c.launch;
-    if (c.per_cu == 0) {
-      const float load = float(tiles) / float(cus);
-      t += float(steps) * (c.fixed + c.step[0] * load + c.step[1] * std::max(0.f, load - 2.f));
+  for (int i = 0; i < kTileCount + kPairCount; ++i) {
+    float t;
+    if (i < kTileCount) {
+      if (i >= kRows1 && M > kTiles[0][i].bm) continue;
+      t = tile_cost(i, M, N, ksteps, cus, full);
     } else {
-      const int64_t round = int64_t(c.per_cu) * cus, rounds = tiles / round, rest = tiles % round;
-      t += float(rounds) * (c.fixed + float(steps) * c.step[c.per_cu - 1]);
-      if (rest) {
-        const float part = float(rest) / float(cus);
-        t += c.fixed + float(steps) * (c.per_cu == 1 ? c.idle + (c.step[0] - c.idle) * part : c.step[(rest - 1) / cus]);
-      }
+      const TilePair& two = kPairs[i - kFirstPair];
+      if (full != (two.a == 3)) continue;
+      const int m = rows_of_rounds(two.a, full, M, N, cus);
+      if (m == 0 || m >= M) continue;
+      t = tile_cost(two.a, m, N, ksteps, cus, full) + tile_cost(two.b, M - m, N, ksteps, cus, full) - kTiles[full][two.b].launch;
     }
     if (t < least) {
       best = i;
@@ -698,20 +772,29 @@ Status linear_f8(const dc_linear_f8_args& a, hipStream_t s) {
     e.ldo = a.ld_out;
     e.lines = (reinterpret_cast<uintptr_t>(a.out) | uint64_t(a.ld_out) * e.E) % 128 == 0;
     constexpr bool BF = decltype(e)::kBf16;
+    using Tile0 = Tile<192, 256, 2, 4, 2>;
+    using Tile2 = Tile<192, 128, 2, 4, 3>;
+    using Tile3 = Tile<128, 128, 2, 2, 2>;
+    using Tile5 = Tile<64, 64, 2, 2, 3>;
+    using Tile6 = Tile<64, 64, 2, 2, 3, 2>;
+    auto rest = [&](int tile) { return rows_of_rounds(tile, !BF, p.M, p.N, cus); };
     switch (f8_tile(p.M, p.N, p.KT, cus, !BF)) {
-      case 0: if constexpr (BF) return launch<192, 256, 2, 4, 2>(p, e, s); break;
-      case 1: if constexpr (BF) return launch<256, 128, 4, 2, 3>(p, e, s); break;
-      case 2: return launch<192, 128, 2, 4, 3>(p, e, s);
-      case 3: return launch<128, 128, 2, 2, 2>(p, e, s);
-      case 4: return launch<64, 128, 2, 2, 3>(p, e, s);
-      case 5: return launch<64, 64, 2, 2, 3>(p, e, s);
-      case 6: return launch<64, 64, 2, 2, 3, 2>(p, e, s);
-      case 7: return launch<32, 64, 1, 2, 3, 2>(p, e, s);
-      case 8: return launch<32, 32, 1, 1, BF ? 3 : 2, 4>(p, e, s);
-      case 9: return launch<32, 32, 1, 1, 2, 8>(p, e, s);
+      case 0: if constexpr (BF) return launch<Tile0>(p, e, s); break;
+      case 1: if constexpr (BF) return launch<Tile<256, 128, 4, 2, 3>>(p, e, s); break;
+      case 2: return launch<Tile2>(p, e, s);
+      case 3: return launch<Tile3>(p, e, s);
+      case 4: return launch<Tile<64, 128, 2, 2, 3>>(p, e, s);
+      case 5: return launch<Tile5>(p, e, s);
+      case 6: return launch<Tile6>(p, e, s);
+      case 7: return launch<Tile<32, 64, 1, 2, 3, 2>>(p, e, s);
+      case 8: return launch<Tile<32, 32, 1, 1, BF ? 3 : 2, 4>>(p, e, s);
+      case 9: return launch<Tile<32, 32, 1, 1, 2, 8>>(p, e, s);
       case kFewRows: return launch_few<1, 8>(p, e, s);
       case kRows1: return launch_rows<1>(p, e, s);
       case kRows2: return launch_rows<2>(p, e, s);
+      case kFirstPair: if constexpr (BF) return launch_two<Tile0, Tile2>(p, rest(0), e, s); break;
+      case kFirstPair + 1: if constexpr (BF) return launch_two<Tile0, Tile6>(p, rest(0), e, s); break;
+      case kFirstPair + 2: if constexpr (!BF) return launch_two<Tile3, Tile5>(p, rest(3), e, s); break;
     }
     return Status::shape("e4m3 product: no such tile");
   };

@@ -384,7 +384,7 @@ def test_linear_ragged(api, dev, m, n, k):
 
 
 F8_TILES = ("192x256", "256x128", "192x128", "128x128", "64x128", "64x64", "64x64 x 2", "32x64 x 2", "32x32 x 4", "32x32 x 8", "16x16 x 8",
-            "column", "column of 2")
+            "column", "column of 2", "192x256 then 192x128", "192x256 then 64x64 x 2", "128x128 then 64x64")
 TILE_SHAPES = {     # (M, N, K), type of the outputs: the tile on 256 compute units
     (1717, 4990, 896, "bf16"): "192x256", (1442, 4158, 1280, "bf16"): "256x128", (925, 4989, 1664, "bf16"): "192x128",
     (1301, 5765, 1024, "bf16"): "128x128", (637, 3139, 3840, "bf16"): "64x128", (269, 2860, 1664, "bf16"): "64x64",
@@ -393,6 +393,8 @@ TILE_SHAPES = {     # (M, N, K), type of the outputs: the tile on 256 compute un
     (925, 4989, 1664, "f32"): "192x128", (1301, 5765, 1024, "f32"): "128x128", (637, 3139, 3840, "f32"): "64x128", (411, 4867, 640, "f32"): "64x64",
     (574, 1089, 2048, "f32"): "64x64 x 2", (65, 5128, 3840, "f32"): "32x64 x 2", (964, 384, 3456, "f32"): "32x32 x 4", (476, 411, 3840, "f32"): "32x32 x 8",
     (15, 4927, 2048, "f32"): "16x16 x 8", (1, 6403, 3840, "f32"): "column", (2, 6403, 3840, "f32"): "column of 2",
+    (3096, 5202, 512, "bf16"): "192x256 then 192x128", (3470, 3450, 768, "bf16"): "192x256 then 64x64 x 2", (1740, 5580, 1536, "f32"): "128x128 then 64x64",
+    (3694, 2363, 640, "f32"): "128x128 then 64x64", (700, 7, 640, "bf16"): "16x16 x 8", (700, 3, 640, "f32"): "16x16 x 8",
 }
 
 
@@ -408,7 +410,7 @@ def test_linear_tiles(api, dev, mnkt, kind):
     assert f8_tile(m, n, k, dt, compute_units(dev)) == TILE_SHAPES[mnkt]
     data = whole_inputs(m, n, k, 7)
     pick = np.unique(np.r_[0, m - 1, np.random.default_rng(0).integers(0, m, 150)])
-    for width in sorted({n, n // 64 * 64}):
+    for width in sorted({n, n // 64 * 64 or n}):
         if f8_tile(m, width, k, dt, compute_units(dev)) != TILE_SHAPES[mnkt]:
             continue
         x, xs, w, ws, b, gate, res = data
