@@ -569,25 +569,28 @@ __global__ void __launch_bounds__(G * 64) k_f8_few(Operands p, int tiles_n, E ep
   }
 }
 
-// One to four rows: a wave takes a column, its weights' whole row straight from memory (16 codes a lane, U pieces on their
-// way at once), and multiplies in fp32: every product is exact, and a lane's 16 share their scales.
-template <int MR, class E>
+// One or two rows: G waves take a column, its weights' whole row straight from memory (16 codes a lane, U pieces on their
+// way at once), and multiply in fp32: every product is exact, and a lane's 16 share their scales.  Bound by the weights' way
+// from memory, which more pieces or columns to a lane do not shorten (1 x 1,920 x 7,680 5.7 us; eight pieces 5.6, two
+// columns 6.4, four 7.2).
+template <int MR, int G, class E>
 __global__ void __launch_bounds__(256) k_f8_rows(Operands p, E epi) {
   constexpr int U = 4;
-  const int lane = threadIdx.x & 63, n = int(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (n >= p.N) return;
-  const char* const w = p.w + int64_t(n) * p.ldw;
-  const float* const sw = p.sw + int64_t(n / 128) * p.sw_row;
+  __shared__ float sums[4][MR];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = int(blockIdx.x) * (4 / G) + wave / G, nc = min(n, p.N - 1);
+  const char* const w = p.w + int64_t(nc) * p.ldw;
+  const float* const sw = p.sw + int64_t(nc / 128) * p.sw_row;
   float acc[MR];
 #pragma unroll
   for (int m = 0; m < MR; ++m) acc[m] = 0.f;
   const int pieces = p.KT * 8;
-  for (int i0 = lane; i0 < pieces; i0 += 64 * U) {
+  for (int i0 = lane + wave % G * 64; i0 < pieces; i0 += 64 * U * G) {
     u32x4 wv[U], xv[U][MR];
     float f[U][MR];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = min(i0 + 64 * u, pieces - 1);
+      const int i = min(i0 + 64 * G * u, pieces - 1);
       wv[u] = *reinterpret_cast<const u32x4*>(w + i * 16);
 #pragma unroll
       for (int m = 0; m < MR; ++m) {
@@ -598,7 +601,7 @@ __global__ void __launch_bounds__(256) k_f8_rows(Operands p, E epi) {
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (i0 + 64 * u >= pieces) break;
+      if (i0 + 64 * G * u >= pieces) break;
       float d[MR];
 #pragma unroll
       for (int m = 0; m < MR; ++m) d[m] = 0.f;
@@ -619,9 +622,22 @@ __global__ void __launch_bounds__(256) k_f8_rows(Operands p, E epi) {
   for (int m = 0; m < MR; ++m)
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) acc[m] += __shfl_xor(acc[m], o, 64);
+  if constexpr (G > 1) {                                // the waves' sums, in their order
+#pragma unroll
+    for (int m = 0; m < MR; ++m)
+      if (lane == m) sums[wave][m] = acc[m];
+    __syncthreads();
+    if (wave % G) return;
+#pragma unroll
+    for (int m = 0; m < MR; ++m) {
+      acc[m] = sums[wave][m];
+#pragma unroll
+      for (int g = 1; g < G; ++g) acc[m] += sums[wave + g][m];
+    }
+  }
 #pragma unroll
   for (int m = 0; m < MR; ++m)
-    if (lane == m && m < p.M) epi.one(acc[m], m, n);
+    if (lane == m && m < p.M && n < p.N) epi.one(acc[m], m, n);
 }
 
 template <class T, class E>
@@ -642,9 +658,14 @@ Status launch_two(const Operands& p, int m_rest, const E& epi, hipStream_t s) {
   return Status::ok();
 }
 
+// Two waves to a column where one would go round its loop more than once and there are few of them: 1 x 1,920 x 7,680 5.6 ->
+// 4.7 us, 2 x 1,920 x 7,680 6.2 -> 5.6, but 1 x 5,000 x 4,096 5.4 -> 5.8, 1 x 7,680 x 1,920 4.7 -> 5.1.
+bool shared_columns(int N, int ksteps, int cus) { return ksteps > 32 && N <= 8 * cus; }
+
 template <int MR, class E>
-Status launch_rows(const Operands& p, const E& epi, hipStream_t s) {
-  hipLaunchKernelGGL((k_f8_rows<MR, E>), dim3((p.N + 3) / 4), dim3(256), 0, s, p, epi);
+Status launch_rows(const Operands& p, const E& epi, int cus, hipStream_t s) {
+  if (shared_columns(p.N, p.KT, cus)) hipLaunchKernelGGL((k_f8_rows<MR, 2, E>), dim3((p.N + 1) / 2), dim3(256), 0, s, p, epi);
+  else hipLaunchKernelGGL((k_f8_rows<MR, 1, E>), dim3((p.N + 3) / 4), dim3(256), 0, s, p, epi);
   DC_HIP(hipGetLastError());
   return Status::ok();
 }
@@ -668,7 +689,7 @@ Status launch_few(const Operands& p, const E& epi, hipStream_t s) {
 // fp32 64 x 64 in two groups 9.0 (one 9.1); 50 x 1,920 x 7,680 32 x 32 in eight 9.7 (few rows 16.2, 64 x 64 21.7);
 // 1 x 1,920 x 7,680 a wave to a column 5.7 (few rows 6.9, 32 x 32 8.9).
 struct TileCost { int bm, bn, groups, per_cu; float launch, fixed, step[3], idle; };
-constexpr int kTileCount = 13;
+constexpr int kTileCount = 12;
 constexpr float kNever = 1e30f;
 constexpr TileCost kTiles[2][kTileCount] = {
     {{192, 256, 1, 1, 0.527f, 4.613f, {1.267f}, 0.915f},           // bf16 outputs
@@ -682,8 +703,7 @@ constexpr TileCost kTiles[2][kTileCount] = {
      {32, 32, 4, 1, 1.616f, 1.411f, {0.474f}, 0.286f},
      {32, 32, 8, 1, 1.517f, 1.584f, {0.845f}, 0.532f},
      {16, 16, 8, 0, 2.354f, 0.573f, {0.429f, 0.138f}, 0.f},
-     {1, 4, 1, 0, 1.878f, 1.260f, {0.059f, 0.047f}, 0.f},
-     {2, 4, 1, 0, 1.490f, 1.578f, {0.193f, 0.f}, 0.f}},
+     {2, 4, 1, 0, 1.5f, 1.588f, {0.059f, 0.133f}, 0.f}},
     {{192, 256, 1, 1, kNever, 0.f, {0.f}, 0.f},                    // fp32 outputs: the conversions leave no registers
      {256, 128, 1, 1, kNever, 0.f, {0.f}, 0.f},
      {192, 128, 1, 1, 0.175f, 4.504f, {1.390f}, 1.200f},
@@ -695,20 +715,20 @@ constexpr TileCost kTiles[2][kTileCount] = {
      {32, 32, 4, 2, 1.708f, 1.469f, {0.494f, 0.908f}, 0.f},
      {32, 32, 8, 1, 1.507f, 1.867f, {1.014f}, 0.690f},
      {16, 16, 8, 0, 2.448f, 0.555f, {0.423f, 0.142f}, 0.f},
-     {1, 4, 1, 0, 1.993f, 1.214f, {0.039f, 0.062f}, 0.f},
-     {2, 4, 1, 0, 1.584f, 1.560f, {0.180f, 0.f}, 0.f}}};
-constexpr int kFewRows = 10, kRows1 = 11, kRows2 = 12;
+     {2, 4, 1, 0, 1.5f, 1.962f, {0.053f, 0.088f}, 0.f}}};
+constexpr int kFewRows = 10, kRows2 = 11, kRows1 = 12;
 // Pairs of tiles: what is left of the rows behind tile a's whole rounds, in which it would leave most of the chip idle, goes
 // to tile b (us, one tile / two): 17,776 x 1,920 x 7,680 gated in fp32 462 / 434, 3,704 x 4,608 x 1,152 through GELU in bf16
 // 33.2 / 28.8, in fp32 54.8 / 42.6.
 struct TilePair { int a, b; };
 constexpr TilePair kPairs[] = {{0, 2}, {0, 6}, {3, 5}};           // the first two for bf16 outputs, the last for fp32 ones
-constexpr int kFirstPair = kTileCount, kPairCount = 3;
+constexpr int kFirstPair = 13, kPairCount = 3;
 
 float tile_cost(int i, int64_t M, int N, int ksteps, int cus, bool full) {
   const TileCost& c = kTiles[full][i];
-  const int steps = i >= kRows1 ? (ksteps + 31) / 32 : (ksteps + c.groups - 1) / c.groups;
-  const int64_t tiles = (M + c.bm - 1) / c.bm * ((N + c.bn - 1) / c.bn);
+  const int waves = i == kRows2 ? 1 + shared_columns(N, ksteps, cus) : 1;       // that share a column
+  const int groups = i == kRows2 ? 32 * waves : c.groups, steps = (ksteps + groups - 1) / groups;
+  const int64_t tiles = (M + c.bm - 1) / c.bm * ((int64_t(N) * waves + c.bn - 1) / c.bn);
   if (c.per_cu == 0) {
     const float load = float(tiles) / float(cus);
     return c.launch + float(steps) * (c.fixed + c.step[0] * load + c.step[1] * std::max(0.f, load - 2.f));
@@ -732,25 +752,25 @@ int rows_of_rounds(int i, bool full, int M, int N, int cus) {
 }  // namespace
 
 int f8_tile(int M, int N, int ksteps, int cus, bool full) {
-  if (N < 8) return kFewRows;           // the others' epilogue reads and writes whole 16-byte pieces of a row
+  if (M == 1) return kRows1;            // few rows and the rest are behind it by up to 44 %, and ahead of it by up to 9
+  if (N < 8) return kFewRows;           // the tiles' epilogue reads and writes whole 16-byte pieces of a row
   int best = 0;
   float least = kNever;
-  for (int i = 0; i < kTileCount + kPairCount; ++i) {
-    float t;
-    if (i < kTileCount) {
-      if (i >= kRows1 && M > kTiles[0][i].bm) continue;
-      t = tile_cost(i, M, N, ksteps, cus, full);
-    } else {
-      const TilePair& two = kPairs[i - kFirstPair];
-      if (full != (two.a == 3)) continue;
-      const int m = rows_of_rounds(two.a, full, M, N, cus);
-      if (m == 0 || m >= M) continue;
-      t = tile_cost(two.a, m, N, ksteps, cus, full) + tile_cost(two.b, M - m, N, ksteps, cus, full) - kTiles[full][two.b].launch;
-    }
+  auto consider = [&](int i, float t) {
     if (t < least) {
       best = i;
       least = t;
     }
+  };
+  for (int i = 0; i < kTileCount; ++i)
+    if (i != kRows2 || M == 2) consider(i, tile_cost(i, M, N, ksteps, cus, full));
+  for (int i = 0; i < kPairCount; ++i) {
+    const TilePair& two = kPairs[i];
+    if (full != (two.a == 3)) continue;
+    const int m = rows_of_rounds(two.a, full, M, N, cus);
+    if (m > 0 && m < M)
+      consider(kFirstPair + i, tile_cost(two.a, m, N, ksteps, cus, full) + tile_cost(two.b, M - m, N, ksteps, cus, full) -
+                                   kTiles[full][two.b].launch);
   }
   return best;
 }
@@ -790,8 +810,8 @@ Status linear_f8(const dc_linear_f8_args& a, hipStream_t s) {
       case 8: return launch<Tile<32, 32, 1, 1, BF ? 3 : 2, 4>>(p, e, s);
       case 9: return launch<Tile<32, 32, 1, 1, 2, 8>>(p, e, s);
       case kFewRows: return launch_few<1, 8>(p, e, s);
-      case kRows1: return launch_rows<1>(p, e, s);
-      case kRows2: return launch_rows<2>(p, e, s);
+      case kRows1: return launch_rows<1>(p, e, cus, s);
+      case kRows2: return launch_rows<2>(p, e, cus, s);
       case kFirstPair: if constexpr (BF) return launch_two<Tile0, Tile2>(p, rest(0), e, s); break;
       case kFirstPair + 1: if constexpr (BF) return launch_two<Tile0, Tile6>(p, rest(0), e, s); break;
       case kFirstPair + 2: if constexpr (!BF) return launch_two<Tile3, Tile5>(p, rest(3), e, s); break;

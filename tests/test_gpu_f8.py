@@ -384,7 +384,7 @@ def test_linear_ragged(api, dev, m, n, k):
 
 
 F8_TILES = ("192x256", "256x128", "192x128", "128x128", "64x128", "64x64", "64x64 x 2", "32x64 x 2", "32x32 x 4", "32x32 x 8", "16x16 x 8",
-            "column", "column of 2", "192x256 then 192x128", "192x256 then 64x64 x 2", "128x128 then 64x64")
+            "column of 2", "column", "192x256 then 192x128", "192x256 then 64x64 x 2", "128x128 then 64x64")
 TILE_SHAPES = {     # (M, N, K), type of the outputs: the tile on 256 compute units
     (1717, 4990, 896, "bf16"): "192x256", (1442, 4158, 1280, "bf16"): "256x128", (925, 4989, 1664, "bf16"): "192x128",
     (1301, 5765, 1024, "bf16"): "128x128", (637, 3139, 3840, "bf16"): "64x128", (269, 2860, 1664, "bf16"): "64x64",
@@ -421,7 +421,7 @@ def test_linear_tiles(api, dev, mnkt, kind):
         check_linear(got[pick], d[0][pick], d[1][pick], d[2], d[3], d[4] if kind != "plain" else None, d[5], d[6][pick], kind, dt == "bf16", True)
 
 
-@pytest.mark.parametrize("m,n,k", [(1, 1920, 7680), (50, 333, 1920), (257, 513, 1152), (700, 1920, 1920), (1, 40, 65536)])
+@pytest.mark.parametrize("m,n,k", [(1, 1920, 7680), (2, 333, 5120), (50, 333, 1920), (257, 513, 1152), (700, 1920, 1920), (1, 40, 65536)])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_linear_of_any_codes(api, dev, m, n, k, dt):
     data = any_inputs(m, n, k, m + k)
