@@ -327,7 +327,7 @@ typedef struct {
   int64_t ld_residual;
   void* out;                      /* [rows, ld_out]; overlaps no other operand */
   int32_t out_dtype;              /* dc_dtype */
-  int64_t ld_out;                 /* >= out_features, rows at any element's address */
+  int64_t ld_out;                 /* >= out_features, below 2^32 (any for one row); rows at any element's address */
 } dc_linear_f8_args;
 dc_status dc_linear_f8(const dc_linear_f8_args* args, hipStream_t stream);
 

@@ -92,6 +92,20 @@ __device__ inline float gelu(float z) {
   return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u));
 }
 
+// A product, in 112 bytes: the launch of a kernel that is given more takes 0.6 us longer.
+struct Args {
+  const char* x; const char* w;
+  const float* sx; const float* sw;
+  const float* bias; const float* gate;
+  const void* residual;
+  void* out;
+  uint32_t sx_block, sw_row, sw_block, ldr, ldo;
+  int sx_row, ldx, ldw;
+  int M, N, KT;
+  int lines;              // rows of out start on a line of 128 bytes
+};
+static_assert(sizeof(Args) == 112, "a launch's arguments");
+
 // out = value + bias, through GELU, or residual + gate (value + bias), in rows at any element's address.
 //
 // A wave's finished values of 32 rows go through an LDS strip and leave as 16-byte pieces of rows, 128 bytes of a row
@@ -104,7 +118,9 @@ struct Epi {
   int64_t ldr;
   void* out;
   int64_t ldo;
-  bool lines;             // rows start on a line of 128 bytes
+  bool lines;
+  __device__ explicit Epi(const Args& p)
+      : bias(p.bias), gate(p.gate), residual(p.residual), ldr(p.ldr), out(p.out), ldo(p.ldo), lines(p.lines) {}
   static constexpr bool kBf16 = BF;
   static constexpr int E = BF ? 2 : 4;                // bytes of a value
   static constexpr int V = 16 / E;                    // values of a 16-byte piece
@@ -253,14 +269,6 @@ struct Epi {
   }
 };
 
-struct Operands {
-  const char* x; const char* w;
-  const float* sx; const float* sw;
-  int64_t sx_block, sw_row, sw_block;
-  int sx_row, ldx, ldw;
-  int M, N, KT;
-};
-
 // WM x WN waves on a BM x BN tile, ST stages of a k-step, KG groups of waves with every KG-th k-step each.
 template <int BM_, int BN_, int WM_, int WN_, int ST_, int KG_ = 1>
 struct Tile {
@@ -275,7 +283,7 @@ struct Tile {
 // The product of tile (m0, n0), with a barrier to a k-step: the fills of k-step kt + ST - 1 go out among the products of
 // k-step kt.  Rows past M or N are clamped to the last row (their results are never stored).
 template <class T_, class E>
-__device__ inline void tile_product(const Operands& p, const E& epi, uint4* rings, float* vec, int m0, int n0) {
+__device__ inline void tile_product(const Args& p, const E& epi, uint4* rings, float* vec, int m0, int n0) {
   constexpr int BM = T_::BM, BN = T_::BN, WM = T_::WM, WN = T_::WN, ST = T_::ST, KG = T_::KG, NW = T_::NW, NT = T_::NT;
   constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 16, TN = WTN / 16;
   constexpr int AI = BM * 8 / NT, BI = BN * 8 / NT;               // DMA instructions of a wave and k-step, and one for scales
@@ -466,7 +474,7 @@ __device__ inline void tile_product(const Operands& p, const E& epi, uint4* ring
 
 // Tile t of tiles_m x tiles_n from row m_first on: groups of four row tiles, as in k_gemm_dma.
 template <class T, class E>
-__device__ inline void nth_tile(const Operands& p, const E& epi, uint4* rings, float* vec, int t, int m_first, int tiles_m, int tiles_n) {
+__device__ inline void nth_tile(const Args& p, const E& epi, uint4* rings, float* vec, int t, int m_first, int tiles_m, int tiles_n) {
   const int grp = t / (4 * tiles_n), gbase = grp * 4;
   const int gsz = min(4, tiles_m - gbase);
   const int tin = t - grp * 4 * tiles_n;
@@ -475,21 +483,22 @@ __device__ inline void nth_tile(const Operands& p, const E& epi, uint4* rings, f
 
 // Workgroups are renumbered so that an XCD takes neighbouring tiles.
 template <class T, class E>
-__global__ void __launch_bounds__(T::kThreads) k_gemm_f8(Operands p, int tiles_n, int tiles, int per_xcd, E epi) {
+__global__ void __launch_bounds__(T::kThreads) k_gemm_f8(Args p) {
   __shared__ uint4 rings[T::kRings];
   __shared__ float4 s_vec[T::kVec / 4];
-  const int t = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-  if (t >= tiles) return;
-  nth_tile<T>(p, epi, rings, reinterpret_cast<float*>(s_vec), t, 0, (p.M + T::BM - 1) / T::BM, tiles_n);
+  const int tm = (p.M + T::BM - 1) / T::BM, tn = (p.N + T::BN - 1) / T::BN;
+  const int t = (blockIdx.x & 7) * ((tm * tn + 7) / 8) + (blockIdx.x >> 3);
+  if (t < tm * tn) nth_tile<T>(p, E(p), rings, reinterpret_cast<float*>(s_vec), t, 0, tm, tn);
 }
 
 // Rows up to m_rest in A's tiles, which fill the chip whole rounds, and the others in B's, which start as A's end.
 template <class A, class B, class E>
-__global__ void __launch_bounds__(A::kThreads) k_gemm_f8_two(Operands p, int m_rest, int per_a, int per_b, E epi) {
+__global__ void __launch_bounds__(A::kThreads) k_gemm_f8_two(Args p, int m_rest, int per_a, int per_b) {
   static_assert(A::kThreads == B::kThreads, "one launch");
   __shared__ uint4 rings[std::max(A::kRings, B::kRings)];
   __shared__ float4 s_vec[std::max(A::kVec, B::kVec) / 4];
   float* const vec = reinterpret_cast<float*>(s_vec);
+  const E epi(p);
   const int i = blockIdx.x - 8 * per_a;
   if (i < 0) {
     const int tn = (p.N + A::BN - 1) / A::BN, tm = m_rest / A::BM, t = (blockIdx.x & 7) * per_a + (blockIdx.x >> 3);
@@ -504,7 +513,9 @@ __global__ void __launch_bounds__(A::kThreads) k_gemm_f8_two(Operands p, int m_r
 // them on their way at once (bound by the weights' way from memory, of which a k-step of 16 columns is 16 whole lines),
 // and add their sums in LDS in the waves' order.
 template <int RT, int G, class E>
-__global__ void __launch_bounds__(G * 64) k_f8_few(Operands p, int tiles_n, E epi) {
+__global__ void __launch_bounds__(G * 64) k_f8_few(Args p) {
+  const E epi(p);
+  const int tiles_n = (p.N + 15) / 16;
   constexpr bool FULL = !E::kBf16;
   constexpr int U = RT == 1 ? 4 : 2;
   __shared__ f32x4 sums[G][RT][64];
@@ -534,14 +545,14 @@ __global__ void __launch_bounds__(G * 64) k_f8_few(Operands p, int tiles_n, E ep
 #pragma unroll
       for (int a = 0; a < RT; ++a) {
         xf[u][a] = Frag{*reinterpret_cast<const uint4*>(x[a] + kt * 128), *reinterpret_cast<const uint4*>(x[a] + kt * 128 + 64)};
-        f[u][a] = sx[a][kt * p.sx_block];
+        f[u][a] = sx[a][int64_t(kt) * p.sx_block];
       }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int kt = kt0 + u * G;
       if (kt >= p.KT) break;
-      const float ws = sw[kt * p.sw_block];
+      const float ws = sw[int64_t(kt) * p.sw_block];
       Operand<FULL> wo, xo;
       wo.set(wf[u]);
 #pragma unroll
@@ -574,7 +585,8 @@ __global__ void __launch_bounds__(G * 64) k_f8_few(Operands p, int tiles_n, E ep
 // from memory, which more pieces or columns to a lane do not shorten (1 x 1,920 x 7,680 5.7 us; eight pieces 5.6, two
 // columns 6.4, four 7.2).
 template <int MR, int G, class E>
-__global__ void __launch_bounds__(256) k_f8_rows(Operands p, E epi) {
+__global__ void __launch_bounds__(256) k_f8_rows(Args p) {
+  const E epi(p);
   constexpr int U = 4;
   __shared__ float sums[4][MR];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -596,7 +608,7 @@ __global__ void __launch_bounds__(256) k_f8_rows(Operands p, E epi) {
       for (int m = 0; m < MR; ++m) {
         const int r = min(m, p.M - 1);
         xv[u][m] = *reinterpret_cast<const u32x4*>(p.x + int64_t(r) * p.ldx + i * 16);
-        f[u][m] = p.sx[int64_t(r) * p.sx_row + (i >> 3) * p.sx_block] * sw[(i >> 3) * p.sw_block];
+        f[u][m] = p.sx[int64_t(r) * p.sx_row + int64_t(i >> 3) * p.sx_block] * sw[int64_t(i >> 3) * p.sw_block];
       }
     }
 #pragma unroll
@@ -641,19 +653,19 @@ __global__ void __launch_bounds__(256) k_f8_rows(Operands p, E epi) {
 }
 
 template <class T, class E>
-Status launch(const Operands& p, const E& epi, hipStream_t s) {
-  const int tn = (p.N + T::BN - 1) / T::BN, tiles = tn * ((p.M + T::BM - 1) / T::BM), per = (tiles + 7) / 8;
-  hipLaunchKernelGGL((k_gemm_f8<T, E>), dim3(8 * per), dim3(T::kThreads), 0, s, p, tn, tiles, per, epi);
+Status launch(const Args& p, hipStream_t s) {
+  const int tiles = (p.N + T::BN - 1) / T::BN * ((p.M + T::BM - 1) / T::BM);
+  hipLaunchKernelGGL((k_gemm_f8<T, E>), dim3((tiles + 7) / 8 * 8), dim3(T::kThreads), 0, s, p);
   DC_HIP(hipGetLastError());
   return Status::ok();
 }
 
 template <class A, class B, class E>
-Status launch_two(const Operands& p, int m_rest, const E& epi, hipStream_t s) {
+Status launch_two(const Args& p, int m_rest, hipStream_t s) {
   const int tiles_a = m_rest / A::BM * ((p.N + A::BN - 1) / A::BN);
   const int tiles_b = (p.M - m_rest + B::BM - 1) / B::BM * ((p.N + B::BN - 1) / B::BN);
   const int per_a = (tiles_a + 7) / 8, per_b = (tiles_b + 7) / 8;
-  hipLaunchKernelGGL((k_gemm_f8_two<A, B, E>), dim3(8 * (per_a + per_b)), dim3(A::kThreads), 0, s, p, m_rest, per_a, per_b, epi);
+  hipLaunchKernelGGL((k_gemm_f8_two<A, B, E>), dim3(8 * (per_a + per_b)), dim3(A::kThreads), 0, s, p, m_rest, per_a, per_b);
   DC_HIP(hipGetLastError());
   return Status::ok();
 }
@@ -663,17 +675,17 @@ Status launch_two(const Operands& p, int m_rest, const E& epi, hipStream_t s) {
 bool shared_columns(int N, int ksteps, int cus) { return ksteps > 32 && N <= 8 * cus; }
 
 template <int MR, class E>
-Status launch_rows(const Operands& p, const E& epi, int cus, hipStream_t s) {
-  if (shared_columns(p.N, p.KT, cus)) hipLaunchKernelGGL((k_f8_rows<MR, 2, E>), dim3((p.N + 1) / 2), dim3(256), 0, s, p, epi);
-  else hipLaunchKernelGGL((k_f8_rows<MR, 1, E>), dim3((p.N + 3) / 4), dim3(256), 0, s, p, epi);
+Status launch_rows(const Args& p, int cus, hipStream_t s) {
+  if (shared_columns(p.N, p.KT, cus)) hipLaunchKernelGGL((k_f8_rows<MR, 2, E>), dim3((p.N + 1) / 2), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((k_f8_rows<MR, 1, E>), dim3((p.N + 3) / 4), dim3(256), 0, s, p);
   DC_HIP(hipGetLastError());
   return Status::ok();
 }
 
 template <int RT, int G, class E>
-Status launch_few(const Operands& p, const E& epi, hipStream_t s) {
-  const int tn = (p.N + 15) / 16, tiles = tn * ((p.M + 16 * RT - 1) / (16 * RT));
-  hipLaunchKernelGGL((k_f8_few<RT, G, E>), dim3(tiles), dim3(G * 64), 0, s, p, tn, epi);
+Status launch_few(const Args& p, hipStream_t s) {
+  const int tiles = (p.N + 15) / 16 * ((p.M + 16 * RT - 1) / (16 * RT));
+  hipLaunchKernelGGL((k_f8_few<RT, G, E>), dim3(tiles), dim3(G * 64), 0, s, p);
   DC_HIP(hipGetLastError());
   return Status::ok();
 }
@@ -723,6 +735,8 @@ constexpr int kFewRows = 10, kRows2 = 11, kRows1 = 12;
 struct TilePair { int a, b; };
 constexpr TilePair kPairs[] = {{0, 2}, {0, 6}, {3, 5}};           // the first two for bf16 outputs, the last for fp32 ones
 constexpr int kFirstPair = 13, kPairCount = 3;
+
+template <class T> struct Type { using type = T; };
 
 float tile_cost(int i, int64_t M, int N, int ksteps, int cus, bool full) {
   const TileCost& c = kTiles[full][i];
@@ -778,20 +792,34 @@ int f8_tile(int M, int N, int ksteps, int cus, bool full) {
 Status linear_f8(const dc_linear_f8_args& a, hipStream_t s) {
   if (int64_t((a.rows + 63) / 64) * ((a.out_features + 63) / 64) > (1 << 23))
     return Status::shape("e4m3 product: too many outputs");
-  const Operands p{reinterpret_cast<const char*>(a.x), reinterpret_cast<const char*>(a.w), a.x_scale, a.w_scale,
-                   a.x_scale_block, a.w_scale_row, a.w_scale_block, a.rows > 1 ? int(a.x_scale_row) : 0, int(a.ld_x), int(a.ld_w),
-                   a.rows, a.out_features, a.in_features / 128};
+  const int blocks = a.in_features / 128, esize = a.out_dtype == DC_BF16 ? 2 : 4;
+  Args p{};
+  p.x = reinterpret_cast<const char*>(a.x);
+  p.w = reinterpret_cast<const char*>(a.w);
+  p.sx = a.x_scale;
+  p.sw = a.w_scale;
+  p.bias = a.bias;
+  p.gate = a.gate;
+  p.residual = a.residual;
+  p.out = a.out;
+  // strides that nothing goes along may be anything
+  p.sx_row = a.rows > 1 ? int(a.x_scale_row) : 0;
+  p.sx_block = blocks > 1 ? uint32_t(a.x_scale_block) : 0;
+  p.sw_row = a.out_features > 128 ? uint32_t(a.w_scale_row) : 0;
+  p.sw_block = blocks > 1 ? uint32_t(a.w_scale_block) : 0;
+  p.ldr = a.rows > 1 ? uint32_t(a.ld_residual) : 0;
+  p.ldo = a.rows > 1 ? uint32_t(a.ld_out) : 0;
+  p.ldx = int(a.ld_x);
+  p.ldw = int(a.ld_w);
+  p.M = a.rows;
+  p.N = a.out_features;
+  p.KT = blocks;
+  p.lines = (reinterpret_cast<uintptr_t>(a.out) | uint64_t(p.ldo) * esize) % 128 == 0;
   const int cus = compute_units();
   if (cus <= 0) return Status::make(DC_ERR_HIP, "e4m3 product: no device");
-  auto run = [&](auto e) {
-    e.bias = a.bias;
-    e.gate = a.gate;
-    e.residual = a.residual;
-    e.ldr = a.ld_residual;
-    e.out = a.out;
-    e.ldo = a.ld_out;
-    e.lines = (reinterpret_cast<uintptr_t>(a.out) | uint64_t(a.ld_out) * e.E) % 128 == 0;
-    constexpr bool BF = decltype(e)::kBf16;
+  auto run = [&](auto form) {
+    using E = typename decltype(form)::type;
+    constexpr bool BF = E::kBf16;
     using Tile0 = Tile<192, 256, 2, 4, 2>;
     using Tile2 = Tile<192, 128, 2, 4, 3>;
     using Tile3 = Tile<128, 128, 2, 2, 2>;
@@ -799,28 +827,30 @@ Status linear_f8(const dc_linear_f8_args& a, hipStream_t s) {
     using Tile6 = Tile<64, 64, 2, 2, 3, 2>;
     auto rest = [&](int tile) { return rows_of_rounds(tile, !BF, p.M, p.N, cus); };
     switch (f8_tile(p.M, p.N, p.KT, cus, !BF)) {
-      case 0: if constexpr (BF) return launch<Tile0>(p, e, s); break;
-      case 1: if constexpr (BF) return launch<Tile<256, 128, 4, 2, 3>>(p, e, s); break;
-      case 2: return launch<Tile2>(p, e, s);
-      case 3: return launch<Tile3>(p, e, s);
-      case 4: return launch<Tile<64, 128, 2, 2, 3>>(p, e, s);
-      case 5: return launch<Tile5>(p, e, s);
-      case 6: return launch<Tile6>(p, e, s);
-      case 7: return launch<Tile<32, 64, 1, 2, 3, 2>>(p, e, s);
-      case 8: return launch<Tile<32, 32, 1, 1, BF ? 3 : 2, 4>>(p, e, s);
-      case 9: return launch<Tile<32, 32, 1, 1, 2, 8>>(p, e, s);
-      case kFewRows: return launch_few<1, 8>(p, e, s);
-      case kRows1: return launch_rows<1>(p, e, cus, s);
-      case kRows2: return launch_rows<2>(p, e, cus, s);
-      case kFirstPair: if constexpr (BF) return launch_two<Tile0, Tile2>(p, rest(0), e, s); break;
-      case kFirstPair + 1: if constexpr (BF) return launch_two<Tile0, Tile6>(p, rest(0), e, s); break;
-      case kFirstPair + 2: if constexpr (!BF) return launch_two<Tile3, Tile5>(p, rest(3), e, s); break;
+      case 0: if constexpr (BF) return launch<Tile0, E>(p, s); break;
+      case 1: if constexpr (BF) return launch<Tile<256, 128, 4, 2, 3>, E>(p, s); break;
+      case 2: return launch<Tile2, E>(p, s);
+      case 3: return launch<Tile3, E>(p, s);
+      case 4: return launch<Tile<64, 128, 2, 2, 3>, E>(p, s);
+      case 5: return launch<Tile5, E>(p, s);
+      case 6: return launch<Tile6, E>(p, s);
+      case 7: return launch<Tile<32, 64, 1, 2, 3, 2>, E>(p, s);
+      case 8: return launch<Tile<32, 32, 1, 1, BF ? 3 : 2, 4>, E>(p, s);
+      case 9: return launch<Tile<32, 32, 1, 1, 2, 8>, E>(p, s);
+      case kFewRows: return launch_few<1, 8, E>(p, s);
+      case kRows2: return launch_rows<2, E>(p, cus, s);
+      case kRows1: return launch_rows<1, E>(p, cus, s);
+      case kFirstPair: if constexpr (BF) return launch_two<Tile0, Tile2, E>(p, rest(0), s); break;
+      case kFirstPair + 1: if constexpr (BF) return launch_two<Tile0, Tile6, E>(p, rest(0), s); break;
+      case kFirstPair + 2: if constexpr (!BF) return launch_two<Tile3, Tile5, E>(p, rest(3), s); break;
     }
     return Status::shape("e4m3 product: no such tile");
   };
-  if (a.out_dtype == DC_BF16)
-    return a.residual ? run(Epi<true, false, true>{}) : a.gelu ? run(Epi<true, true, false>{}) : run(Epi<true, false, false>{});
-  return a.residual ? run(Epi<false, false, true>{}) : a.gelu ? run(Epi<false, true, false>{}) : run(Epi<false, false, false>{});
+  auto form = [&](auto bf) {
+    constexpr bool BF = decltype(bf)::value;
+    return a.residual ? run(Type<Epi<BF, false, true>>{}) : a.gelu ? run(Type<Epi<BF, true, false>>{}) : run(Type<Epi<BF, false, false>>{});
+  };
+  return a.out_dtype == DC_BF16 ? form(std::true_type{}) : form(std::false_type{});
 }
 
 }  // namespace dc

@@ -76,6 +76,7 @@ RES = dict(residual=FAKE, ld_residual=200)
     (dict(x=None), ARG), (dict(x_scale=None), ARG), (dict(w=None), ARG), (dict(w_scale=None), ARG), (dict(out=None), ARG),
     (dict(x=FAKE + 8), ARG), (dict(w=FAKE + 8), ARG), (dict(out=FAKE + 2), ARG), (dict(out=FAKE + 1, out_dtype=1), ARG), (dict(bias=FAKE + 2), ARG),
     (dict(RES, gate=FAKE + 2), ARG), (dict(RES, residual=FAKE + 2), ARG), (dict(x_scale=FAKE + 2), ARG), (dict(w_scale=FAKE + 1), ARG),
+    (dict(ld_out=1 << 32), ARG), (dict(residual=FAKE, ld_residual=1 << 32), ARG),
     (dict(x_scale_row=-1), ARG), (dict(w_scale_block=-1), ARG), (dict(x_scale_row=1 << 21), ARG), (dict(w_scale_row=(1 << 31) + 1), ARG),
     (dict(in_features=0), SHAPE), (dict(in_features=64), SHAPE), (dict(in_features=200), SHAPE),
     (dict(in_features=(1 << 22) + 128, ld_x=(1 << 22) + 128, ld_w=(1 << 22) + 128), SHAPE), (dict(ld_x=240), SHAPE), (dict(ld_w=264), SHAPE),
