@@ -707,7 +707,7 @@ constexpr TileCost kTiles[2][kTileCount] = {
     {{192, 256, 1, 1, 0.527f, 4.613f, {1.267f}, 0.915f},           // bf16 outputs
      {256, 128, 1, 1, 0.972f, 3.510f, {0.933f}, 0.700f},
      {192, 128, 1, 1, 0.894f, 2.924f, {0.819f}, 0.651f},
-     {128, 128, 1, 2, 0.836f, 2.915f, {0.570f, 0.968f}, 0.f},
+     {128, 128, 1, 2, 0.836f, 2.915f, {0.593f, 0.968f}, 0.f},
      {64, 128, 1, 2, 1.695f, 1.798f, {0.303f, 0.617f}, 0.f},
      {64, 64, 1, 3, 1.930f, 1.121f, {0.236f, 0.383f, 0.587f}, 0.f},
      {64, 64, 2, 1, 1.522f, 1.606f, {0.454f}, 0.371f},
@@ -729,11 +729,13 @@ constexpr TileCost kTiles[2][kTileCount] = {
      {16, 16, 8, 0, 2.448f, 0.555f, {0.423f, 0.142f}, 0.f},
      {2, 4, 1, 0, 1.5f, 1.962f, {0.053f, 0.088f}, 0.f}}};
 constexpr int kFewRows = 10, kRows2 = 11, kRows1 = 12;
-// Pairs of tiles: what is left of the rows behind tile a's whole rounds, in which it would leave most of the chip idle, goes
-// to tile b (us, one tile / two): 17,776 x 1,920 x 7,680 gated in fp32 462 / 434, 3,704 x 4,608 x 1,152 through GELU in bf16
-// 33.2 / 28.8, in fp32 54.8 / 42.6.
-struct TilePair { int a, b; };
-constexpr TilePair kPairs[] = {{0, 2}, {0, 6}, {3, 5}};           // the first two for bf16 outputs, the last for fp32 ones
+// Pairs of tiles: what is left of the rows behind tile a's whole rounds (of one workgroup to a compute unit) goes to tile b.  In
+// its own tiles it would leave most of the chip idle: 17,776 x 1,920 x 7,680 gated in fp32 462 us, so 434; 3,704 x 4,608 x
+// 1,152 through GELU in bf16 33.2 and 28.8, in fp32 54.8 and 42.6; 3,704 x 1,152 x 4,608 in bf16 31.3 and 29.3, in fp32 50.7 and
+// 40.9.  b's tiles cost what they cost alone where they start as a's end; where the last of a's rounds leaves compute
+// units that could hold two workgroups with one, they share them, and add `beside` us to a k-step where there is one to each.
+struct TilePair { int a, b; float beside[2]; };                   // beside: bf16, fp32; 0: a's have the compute unit to themselves
+constexpr TilePair kPairs[] = {{0, 2, {0.f, 0.f}}, {0, 6, {0.f, 0.f}}, {3, 5, {0.25f, 0.4f}}};
 constexpr int kFirstPair = 13, kPairCount = 3;
 
 template <class T> struct Type { using type = T; };
@@ -756,11 +758,24 @@ float tile_cost(int i, int64_t M, int N, int ksteps, int cus, bool full) {
   return t;
 }
 
-// Rows of the row tiles that tile i's whole rounds take
-int rows_of_rounds(int i, bool full, int M, int N, int cus) {
-  const TileCost& c = kTiles[full][i];
-  const int64_t tn = (N + c.bn - 1) / c.bn, round = int64_t(c.per_cu) * cus;
-  return int((M + c.bm - 1) / c.bm * tn / round * round / tn) * c.bm;
+// Rows of the row tiles that the whole rounds of a pair's first tile take
+int rows_of_rounds(int pair, int M, int N, int cus) {
+  const TileCost& c = kTiles[0][kPairs[pair].a];
+  const int64_t tn = (N + c.bn - 1) / c.bn;
+  return int((M + c.bm - 1) / c.bm * tn / cus * cus / tn) * c.bm;
+}
+
+float pair_cost(int pair, int M, int N, int ksteps, int cus, bool full) {
+  const TilePair& two = kPairs[pair];
+  const TileCost& a = kTiles[full][two.a];
+  const TileCost& b = kTiles[full][two.b];
+  const int m = rows_of_rounds(pair, M, N, cus);
+  if (m == 0 || m >= M) return kNever;
+  const float t = tile_cost(two.a, m, N, ksteps, cus, full);
+  const int64_t last = int64_t(m / a.bm) * ((N + a.bn - 1) / a.bn) % (int64_t(a.per_cu) * cus);
+  if (two.beside[full] == 0.f || last == 0 || last > cus) return t + tile_cost(two.b, M - m, N, ksteps, cus, full) - b.launch;
+  const int64_t rest = int64_t((M - m + b.bm - 1) / b.bm) * ((N + b.bn - 1) / b.bn);
+  return t + float(ksteps) * two.beside[full] * float(rest) / float(cus);
 }
 
 }  // namespace
@@ -778,14 +793,7 @@ int f8_tile(int M, int N, int ksteps, int cus, bool full) {
   };
   for (int i = 0; i < kTileCount; ++i)
     if (i != kRows2 || M == 2) consider(i, tile_cost(i, M, N, ksteps, cus, full));
-  for (int i = 0; i < kPairCount; ++i) {
-    const TilePair& two = kPairs[i];
-    if (full != (two.a == 3)) continue;
-    const int m = rows_of_rounds(two.a, full, M, N, cus);
-    if (m > 0 && m < M)
-      consider(kFirstPair + i, tile_cost(two.a, m, N, ksteps, cus, full) + tile_cost(two.b, M - m, N, ksteps, cus, full) -
-                                   kTiles[full][two.b].launch);
-  }
+  for (int i = 0; i < kPairCount; ++i) consider(kFirstPair + i, pair_cost(i, M, N, ksteps, cus, full));
   return best;
 }
 
@@ -825,8 +833,9 @@ Status linear_f8(const dc_linear_f8_args& a, hipStream_t s) {
     using Tile3 = Tile<128, 128, 2, 2, 2>;
     using Tile5 = Tile<64, 64, 2, 2, 3>;
     using Tile6 = Tile<64, 64, 2, 2, 3, 2>;
-    auto rest = [&](int tile) { return rows_of_rounds(tile, !BF, p.M, p.N, cus); };
-    switch (f8_tile(p.M, p.N, p.KT, cus, !BF)) {
+    const int choice = f8_tile(p.M, p.N, p.KT, cus, !BF);
+    const int rest = choice < kFirstPair ? 0 : rows_of_rounds(choice - kFirstPair, p.M, p.N, cus);
+    switch (choice) {
       case 0: if constexpr (BF) return launch<Tile0, E>(p, s); break;
       case 1: if constexpr (BF) return launch<Tile<256, 128, 4, 2, 3>, E>(p, s); break;
       case 2: return launch<Tile2, E>(p, s);
@@ -840,9 +849,9 @@ Status linear_f8(const dc_linear_f8_args& a, hipStream_t s) {
       case kFewRows: return launch_few<1, 8, E>(p, s);
       case kRows2: return launch_rows<2, E>(p, cus, s);
       case kRows1: return launch_rows<1, E>(p, cus, s);
-      case kFirstPair: if constexpr (BF) return launch_two<Tile0, Tile2, E>(p, rest(0), s); break;
-      case kFirstPair + 1: if constexpr (BF) return launch_two<Tile0, Tile6, E>(p, rest(0), s); break;
-      case kFirstPair + 2: if constexpr (!BF) return launch_two<Tile3, Tile5, E>(p, rest(3), s); break;
+      case kFirstPair: if constexpr (BF) return launch_two<Tile0, Tile2, E>(p, rest, s); break;
+      case kFirstPair + 1: if constexpr (BF) return launch_two<Tile0, Tile6, E>(p, rest, s); break;
+      case kFirstPair + 2: return launch_two<Tile3, Tile5, E>(p, rest, s);
     }
     return Status::shape("e4m3 product: no such tile");
   };
