@@ -11,8 +11,13 @@
 // below the 2^-9 of bf16 outputs and takes them at twice the rate, but would be most of what an fp32 output is off.  So
 // for fp32 outputs the codes, which bf16 holds exactly, are converted on their way from LDS and multiplied by
 // v_mfma_f32_16x16x32_bf16 (the same draws: 9e-9 off).
-// Pipelines are gemm_tile.h's: tiles go global -> LDS by LDS-DMA, a stage holding the k-step's rows of both operands and
-// their scales.
+// Tiles go global -> LDS by LDS-DMA, a stage holding the k-step's rows of both operands and their scales.
+//
+// What bounds long products is the power that the chip may draw: at 17,776 x 7,680 x 1,920 in bf16 (250 to 280 us, 1.9 to 2.1
+// PFLOP/s; the 8-bit instruction alone reaches 3.6) the matrix pipe is busy 44 % of the time at 1.84 GHz, at 17,776 x 1,920 x
+// 7,680 in fp32 (430 to 465 us, 1.1 to 1.2; the bf16 instruction alone 1.65) 56 % at 1.80.  Starting the workgroups out of step
+// with each other, which spreads the outputs' way to memory, changed nothing.  Without the multiply-adds of the scales, or
+// without the fills, a k-step of the largest tile is a fifth shorter.
 #include "gemm_tile.h"
 
 #include <algorithm>
@@ -509,44 +514,33 @@ __global__ void __launch_bounds__(A::kThreads) k_gemm_f8_two(Args p, int m_rest,
   }
 }
 
-// Few rows: G waves share 16 RT rows x 16 columns, wave g taking every G-th k-step straight from memory into registers, U of
+// Few rows: G waves share 16 rows x 16 columns, wave g taking every G-th k-step straight from memory into registers, U of
 // them on their way at once (bound by the weights' way from memory, of which a k-step of 16 columns is 16 whole lines),
 // and add their sums in LDS in the waves' order.
-template <int RT, int G, class E>
+template <int G, class E>
 __global__ void __launch_bounds__(G * 64) k_f8_few(Args p) {
+  constexpr bool FULL = !E::kBf16;
+  constexpr int U = 4;
+  __shared__ f32x4 sums[G][64];
   const E epi(p);
   const int tiles_n = (p.N + 15) / 16;
-  constexpr bool FULL = !E::kBf16;
-  constexpr int U = RT == 1 ? 4 : 2;
-  __shared__ f32x4 sums[G][RT][64];
-  const int tid = threadIdx.x, lane = tid & 63, g = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = threadIdx.x & 63, g = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, q = lane >> 4;
-  const int m0 = int(blockIdx.x) / tiles_n * (16 * RT), n0 = int(blockIdx.x) % tiles_n * 16;
+  const int m0 = int(blockIdx.x) / tiles_n * 16, n0 = int(blockIdx.x) % tiles_n * 16, m = m0 + r16;
   const char* const w = p.w + int64_t(min(n0 + r16, p.N - 1)) * p.ldw + 16 * q;
+  const char* const x = p.x + int64_t(min(m, p.M - 1)) * p.ldx + 16 * q;
   const float* const sw = p.sw + int64_t(n0 / 128) * p.sw_row;
-  const char* x[RT];
-  const float* sx[RT];
-#pragma unroll
-  for (int a = 0; a < RT; ++a) {
-    const int m = min(m0 + 16 * a + r16, p.M - 1);
-    x[a] = p.x + int64_t(m) * p.ldx + 16 * q;
-    sx[a] = p.sx + int64_t(m) * p.sx_row;
-  }
-  f32x4 acc[RT];
-#pragma unroll
-  for (int a = 0; a < RT; ++a) acc[a] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const float* const sx = p.sx + int64_t(min(m, p.M - 1)) * p.sx_row;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   for (int kt0 = g; kt0 < p.KT; kt0 += U * G) {
-    Frag wf[U], xf[U][RT];
-    float f[U][RT];
+    Frag wf[U], xf[U];
+    float f[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {                       // past the last k-step: that one again, times zero
+    for (int u = 0; u < U; ++u) {                       // past the last k-step: that one again, which is not added
       const int kt = min(kt0 + u * G, p.KT - 1);
       wf[u] = Frag{*reinterpret_cast<const uint4*>(w + kt * 128), *reinterpret_cast<const uint4*>(w + kt * 128 + 64)};
-#pragma unroll
-      for (int a = 0; a < RT; ++a) {
-        xf[u][a] = Frag{*reinterpret_cast<const uint4*>(x[a] + kt * 128), *reinterpret_cast<const uint4*>(x[a] + kt * 128 + 64)};
-        f[u][a] = sx[a][int64_t(kt) * p.sx_block];
-      }
+      xf[u] = Frag{*reinterpret_cast<const uint4*>(x + kt * 128), *reinterpret_cast<const uint4*>(x + kt * 128 + 64)};
+      f[u] = sx[int64_t(kt) * p.sx_block];
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -555,29 +549,20 @@ __global__ void __launch_bounds__(G * 64) k_f8_few(Args p) {
       const float ws = sw[int64_t(kt) * p.sw_block];
       Operand<FULL> wo, xo;
       wo.set(wf[u]);
+      xo.set(xf[u]);
+      const f32x4 part = product(wo, xo);
 #pragma unroll
-      for (int a = 0; a < RT; ++a) {
-        xo.set(xf[u][a]);
-        const f32x4 part = product(wo, xo);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[a][i] = fmaf(part[i], f[u][a] * ws, acc[a][i]);
-      }
+      for (int i = 0; i < 4; ++i) acc[i] = fmaf(part[i], f[u] * ws, acc[i]);
     }
   }
-#pragma unroll
-  for (int a = 0; a < RT; ++a) sums[g][a][lane] = acc[a];
+  sums[g][lane] = acc;
   __syncthreads();
-  for (int i = tid; i < RT * 64; i += G * 64) {
-    const int a = i >> 6;
-    f32x4 z = sums[0][a][lane];
+  if (g > 0 || m >= p.M) return;
 #pragma unroll
-    for (int j = 1; j < G; ++j) z += sums[j][a][lane];
-    const int m = m0 + 16 * a + r16, n = n0 + 4 * q;
-    if (m >= p.M) continue;
+  for (int j = 1; j < G; ++j) acc += sums[j][lane];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (n + j < p.N) epi.one(z[j], m, n + j);
-  }
+  for (int j = 0; j < 4; ++j)
+    if (n0 + 4 * q + j < p.N) epi.one(acc[j], m, n0 + 4 * q + j);
 }
 
 // One or two rows: G waves take a column, its weights' whole row straight from memory (16 codes a lane, U pieces on their
@@ -682,10 +667,10 @@ Status launch_rows(const Args& p, int cus, hipStream_t s) {
   return Status::ok();
 }
 
-template <int RT, int G, class E>
+template <int G, class E>
 Status launch_few(const Args& p, hipStream_t s) {
-  const int tiles = (p.N + 15) / 16 * ((p.M + 16 * RT - 1) / (16 * RT));
-  hipLaunchKernelGGL((k_f8_few<RT, G, E>), dim3(tiles), dim3(G * 64), 0, s, p);
+  const int tiles = (p.N + 15) / 16 * ((p.M + 15) / 16);
+  hipLaunchKernelGGL((k_f8_few<G, E>), dim3(tiles), dim3(G * 64), 0, s, p);
   DC_HIP(hipGetLastError());
   return Status::ok();
 }
@@ -693,13 +678,14 @@ Status launch_few(const Args& p, hipStream_t s) {
 // Cost in us of tile i.  Tiles in rounds of per_cu workgroups on each compute unit: each round `fixed` plus its k-steps
 // (groups share them) at step[w - 1], w the workgroups that a compute unit has; with one per compute unit a round that fills
 // part of the chip lies between `idle` and step[0].  Few rows (per_cu 0): `fixed` is a k-step's way from memory, step[0] what
-// the load of a compute unit (workgroups to each) adds to it, step[1] what the load beyond two does.  Fitted to timings on
-// MI355X of 607 shapes (M 1 to 17,776, N 32 to 11,520, K 64 to 7,680; widths of a block's products and any others).  The
-// tile it picks is 1.8 % (fp32 outputs, by bf16 products) and 1.6 % (bf16 outputs) behind the best of all that were timed on
-// average, 36 and 27 % at worst (11 x 8,518 x 7,680, 2 x 11,520 x 1,920).  In us, this and the next best kept tile:
-// 17,776 x 7,680 x 1,920 192 x 256 289 (256 x 128 314); 1,556 x 5,760 x 1,920 24.0 (64 x 128 30.3); 50 x 11,520 x 1,920 in
-// fp32 64 x 64 in two groups 9.0 (one 9.1); 50 x 1,920 x 7,680 32 x 32 in eight 9.7 (few rows 16.2, 64 x 64 21.7);
-// 1 x 1,920 x 7,680 a wave to a column 5.7 (few rows 6.9, 32 x 32 8.9).
+// the load of a compute unit (workgroups to each) adds to it, step[1] what the load beyond two does; two rows likewise, a
+// step being a round of the loop.  Fitted to timings on MI355X of 607 shapes (M 1 to 17,776, N 32 to 11,520, K 64 to 7,680;
+// widths of a block's products and any others).  The tile it picks was 1.8 % (fp32 outputs) and 1.6 % (bf16) behind the best of
+// all on average, 36 and 27 % at worst (11 x 8,518 x 7,680, and 2 x 11,520 x 1,920, whose cost is a later fit); with the
+// pairs below, at 118 other shapes each (M 300 to 9,000), 0.4 and 1.1 %, 20 and 10 % at worst (7,489 x 1,473 x 512 in fp32).
+// In us, the tile that is taken and the next: 17,776 x 7,680 x 1,920 in bf16 192 x 256 274 (128 x 128 303, 256 x 128 314);
+// 1,556 x 5,760 x 1,920 22.0 (128 x 128 28.3); 50 x 11,520 x 1,920 in fp32 64 x 64 in two groups 9.0 (32 x 64 9.7);
+// 50 x 1,920 x 7,680 32 x 32 in eight 9.8 (in four 13.0); 1 x 1,920 x 7,680 waves to a column 4.7 (few rows 6.9).
 struct TileCost { int bm, bn, groups, per_cu; float launch, fixed, step[3], idle; };
 constexpr int kTileCount = 12;
 constexpr float kNever = 1e30f;
@@ -729,6 +715,7 @@ constexpr TileCost kTiles[2][kTileCount] = {
      {16, 16, 8, 0, 2.448f, 0.555f, {0.423f, 0.142f}, 0.f},
      {2, 4, 1, 0, 1.5f, 1.962f, {0.053f, 0.088f}, 0.f}}};
 constexpr int kFewRows = 10, kRows2 = 11, kRows1 = 12;
+
 // Pairs of tiles: what is left of the rows behind tile a's whole rounds (of one workgroup to a compute unit) goes to tile b.  In
 // its own tiles it would leave most of the chip idle: 17,776 x 1,920 x 7,680 gated in fp32 462 us, so 434; 3,704 x 4,608 x
 // 1,152 through GELU in bf16 33.2 and 28.8, in fp32 54.8 and 42.6; 3,704 x 1,152 x 4,608 in bf16 31.3 and 29.3, in fp32 50.7 and
@@ -846,7 +833,7 @@ Status linear_f8(const dc_linear_f8_args& a, hipStream_t s) {
       case 7: return launch<Tile<32, 64, 1, 2, 3, 2>, E>(p, s);
       case 8: return launch<Tile<32, 32, 1, 1, BF ? 3 : 2, 4>, E>(p, s);
       case 9: return launch<Tile<32, 32, 1, 1, 2, 8>, E>(p, s);
-      case kFewRows: return launch_few<1, 8, E>(p, s);
+      case kFewRows: return launch_few<8, E>(p, s);
       case kRows2: return launch_rows<2, E>(p, cus, s);
       case kRows1: return launch_rows<1, E>(p, cus, s);
       case kFirstPair: if constexpr (BF) return launch_two<Tile0, Tile2, E>(p, rest, s); break;

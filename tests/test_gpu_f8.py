@@ -494,6 +494,36 @@ def test_linear_of_blocks_without_a_number(api, dev):
         assert bad[[3, 66]].all() and bad[:, 256:].all() and bad.sum() == 2 * 300 + 68 * 44
 
 
+@pytest.mark.parametrize("m,n,k", [(1, 40, 256), (1, 41, 4224), (2, 333, 640), (9, 5, 384), (50, 300, 1024), (300, 400, 512), (1740, 5580, 512), (3096, 5202, 640)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_linear_of_codes_that_are_no_numbers(api, dev, m, n, k, dt):
+    """The codes 0x7F and 0xFF are NaN: in a product's row and column that meet them, and nowhere else."""
+    import torch
+    x, xs, w, ws, b, _, _ = whole_inputs(m, n, k, 3)
+    xq, wq = codes(x, dev), codes(w, dev)
+    i, j = m - 1, n // 2
+    xq.view(torch.uint8)[i, k - 1], wq.view(torch.uint8)[j, 0] = 0x7F, 0xFF
+    out = torch.empty((m, n), device=dev, dtype=kind_of(dt))
+    say("linear no numbers", m, n, k, dt)
+    api.dc_linear_f8(xq, t(xs, dev), wq, t(ws, dev), out, bias=t(b, dev))
+    bad = torch.isnan(out)
+    assert bad[i].all() and bad[:, j].all() and int(bad.sum()) == m + n - 1
+
+
+@pytest.mark.parametrize("m,n,k,dt", [(2945, 1345, 512, "bf16"), (1740, 5580, 1536, "f32"), (3096, 5202, 640, "bf16"), (1717, 4990, 896, "bf16"), (70, 131, 384, "f32")])
+def test_linear_onto_its_residual(api, dev, m, n, k, dt):
+    """In place, and once more: the same bits as into a tensor of its own."""
+    import torch
+    x, xs, w, ws, b, gate, res = whole_inputs(m, n, k, 5)
+    given = [codes(x, dev), t(xs, dev), codes(w, dev), t(ws, dev)]
+    r = t(res, dev, kind_of(dt))
+    say("linear in place", m, n, k, dt)
+    outs = [torch.empty_like(r), torch.empty_like(r), r.clone()]
+    for out in outs:
+        api.dc_linear_f8(*given, out, bias=t(b, dev), gate=t(gate, dev), residual=out if out is outs[2] else r)
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
 def test_no_rows(api, dev):
     import torch
     none = torch.empty((0, 128), device=dev)
