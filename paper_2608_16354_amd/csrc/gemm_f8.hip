@@ -13,11 +13,11 @@
 // v_mfma_f32_16x16x32_bf16 (the same draws: 9e-9 off).
 // Tiles go global -> LDS by LDS-DMA, a stage holding the k-step's rows of both operands and their scales.
 //
-// What bounds long products is the power that the chip may draw: at 17,776 x 7,680 x 1,920 in bf16 (250 to 280 us, 1.9 to 2.1
-// PFLOP/s; the 8-bit instruction alone reaches 3.6) the matrix pipe is busy 44 % of the time at 1.84 GHz, at 17,776 x 1,920 x
-// 7,680 in fp32 (430 to 465 us, 1.1 to 1.2; the bf16 instruction alone 1.65) 56 % at 1.80.  Starting the workgroups out of step
-// with each other, which spreads the outputs' way to memory, changed nothing.  Without the multiply-adds of the scales, or
-// without the fills, a k-step of the largest tile is a fifth shorter.
+// What bounds long products is the power that the chip may draw, which sets the clock: at 17,776 x 7,680 x 1,920 in bf16 (250 to
+// 280 us, 1.9 to 2.1 PFLOP/s) the matrix pipe is busy 44 % of the time at 1.8 to 1.9 GHz, at 17,776 x 1,920 x 7,680 in fp32 (430 to
+// 465 us, 1.1 to 1.2) 56 % at 1.8.  On operands of zeros the same code takes 202 and 378 us.  From registers alone the
+// instructions of a k-step, multiply-adds included, run at 3.5 PFLOP/s (on zeros 4.7).  Starting the workgroups out of step with
+// each other, which spreads the outputs' way to memory, changed nothing.
 #include "gemm_tile.h"
 
 #include <algorithm>
@@ -285,7 +285,7 @@ struct Tile {
   static constexpr int kVec = 2 * BN;
 };
 
-// The product of tile (m0, n0), with a barrier to a k-step: the fills of k-step kt + ST - 1 go out among the products of
+// The product of tile (m0, n0), with a barrier to a k-step (or two): the fills of k-step kt + ST - 1 go out among the products of
 // k-step kt.  Rows past M or N are clamped to the last row (their results are never stored).
 template <class T_, class E>
 __device__ inline void tile_product(const Args& p, const E& epi, uint4* rings, float* vec, int m0, int n0) {
@@ -355,7 +355,13 @@ __device__ inline void tile_product(const Args& p, const E& epi, uint4* rings, f
   // that there the barrier is that frees it and opens the next one: under the last row's products the next
   // k-step's first operands come from LDS, each weight operand in the place of the one that was just used for the last
   // time, and the fill of the freed stage goes out.
-  constexpr bool FULL = !E::kBf16;
+  //
+  // With two stages a k-step is all the time that the fills of the next have.  Of w all is in registers after the first row
+  // of tiles, so that a second barrier there lets w's part of the fills go out half a k-step earlier and leaves x's, less than
+  // half, for the end: 17,776 x 1,920 x 7,680 265 -> 240 us, 17,776 x 7,680 x 1,920 261 -> 250, with operands of zeros (the
+  // highest clock) 250 -> 194, and no wait for fills is left: without it the times are the same.
+  constexpr bool FULL = !E::kBf16, EARLY = ST == 2 && KG == 1 && TM >= 4;
+  constexpr int EARLY_ROW = TM / 2 - 1;
   constexpr int LAG = TN >= 4 ? 3 : 1, R = LAG + 1, T = TM * TN, NF = WTN / 32;
   static_assert(T % R == 0 && TN % 2 == 0 && LAG <= TN && TM >= 2, "products under way belong to one row");
   Operand<FULL> w[TN];
@@ -395,6 +401,12 @@ __device__ inline void tile_product(const Args& p, const E& epi, uint4* rings, f
       const int a = t / TN, b = t % TN;
       if (b == 0) {
         x.set(xf);
+        if (EARLY && fill && a == EARLY_ROW) {
+          asm volatile("" ::: "memory");
+          __builtin_amdgcn_s_waitcnt(0xC07F);
+          __builtin_amdgcn_s_barrier();                 // every wave has w
+          asm volatile("" ::: "memory");
+        }
         if (a + 1 < TM) {
           xf = x_row(s, a + 1);
         } else {
@@ -406,7 +418,7 @@ __device__ inline void tile_product(const Args& p, const E& epi, uint4* rings, f
           if constexpr (next) {
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_waitcnt(0xC07F);         // lgkmcnt(0): this wave's reads of the stage have returned
-            wait_vmcnt<decltype(later)::value * DMAS>();  // and its part of the next k-step has landed
+            wait_vmcnt<decltype(later)::value * DMAS + (EARLY && fill ? BI : 0)>();  // and its part of the next k-step has landed
             if constexpr (NW > 1) __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             first(n, kt + 1);
@@ -416,11 +428,17 @@ __device__ inline void tile_product(const Args& p, const E& epi, uint4* rings, f
       if (a == 0) w[b].set(wf[b]);
       part[t % R] = product(w[b], x);
       if (next && a == TM - 1) wf[b] = w_row(n, b);
-      if (fill && a == TM - 1) {
-        constexpr int DPS = (DMAS + TN - 1) / TN;
+      if constexpr (EARLY && fill) {                    // w's part, spread over the rows between the barriers
+        constexpr int GAP = (T - (EARLY_ROW + 1) * TN) / BI;
+        const int d = t - EARLY_ROW * TN - 1;
+        static_assert(GAP > 0, "tiles for w's fills");
+        if (d >= 0 && d % GAP == 0 && d / GAP < BI) dma_one(s, kt + ST, AI + d / GAP);
+      }
+      if (fill && a == TM - 1) {                        // the rest
+        constexpr int REST = EARLY ? AI + 1 : DMAS, DPS = (REST + TN - 1) / TN;
 #pragma unroll
         for (int j = b * DPS; j < (b + 1) * DPS; ++j)
-          if (j < DMAS) dma_one(s, kt + ST, j);
+          if (j < REST) dma_one(s, kt + ST, EARLY && j == AI ? AI + BI : j);
       }
       __builtin_amdgcn_sched_barrier(0);
       const int u = (t + T - LAG) % T, i = u % TN / 2;
@@ -680,20 +698,19 @@ Status launch_few(const Args& p, hipStream_t s) {
 // part of the chip lies between `idle` and step[0].  Few rows (per_cu 0): `fixed` is a k-step's way from memory, step[0] what
 // the load of a compute unit (workgroups to each) adds to it, step[1] what the load beyond two does; two rows likewise, a
 // step being a round of the loop.  Fitted to timings on MI355X of 607 shapes (M 1 to 17,776, N 32 to 11,520, K 64 to 7,680;
-// widths of a block's products and any others).  The tile it picks was 1.8 % (fp32 outputs) and 1.6 % (bf16) behind the best of
-// all on average, 36 and 27 % at worst (11 x 8,518 x 7,680, and 2 x 11,520 x 1,920, whose cost is a later fit); with the
-// pairs below, at 118 other shapes each (M 300 to 9,000), 0.4 and 1.1 %, 20 and 10 % at worst (7,489 x 1,473 x 512 in fp32).
-// In us, the tile that is taken and the next: 17,776 x 7,680 x 1,920 in bf16 192 x 256 274 (128 x 128 303, 256 x 128 314);
-// 1,556 x 5,760 x 1,920 22.0 (128 x 128 28.3); 50 x 11,520 x 1,920 in fp32 64 x 64 in two groups 9.0 (32 x 64 9.7);
+// widths of a block's products and any others), 192 x 256 and 128 x 128 once more to 118.  The tile it picks is behind the
+// best of all that were timed by 0.6 % (bf16 outputs) and 0.4 % (fp32) on average at those 118 (M 300 to 9,000), at worst by 9
+// (8,378 x 3,463 x 640) and 21 % (1,796 x 4,447 x 6,016); with fewer rows it was 2 % and at worst 36 (11 x 8,518 x
+// 7,680 in fp32).  In us, the tile that is taken and the next: 17,776 x 7,680 x 1,920 in bf16 192 x 256 250 (128 x 128 274);
+// 1,556 x 5,760 x 1,920 21.8 (128 x 128 27.0); 50 x 11,520 x 1,920 in fp32 64 x 64 in two groups 9.0 (32 x 64 9.7);
 // 50 x 1,920 x 7,680 32 x 32 in eight 9.8 (in four 13.0); 1 x 1,920 x 7,680 waves to a column 4.7 (few rows 6.9).
 struct TileCost { int bm, bn, groups, per_cu; float launch, fixed, step[3], idle; };
-constexpr int kTileCount = 12;
+constexpr int kTileCount = 11;
 constexpr float kNever = 1e30f;
 constexpr TileCost kTiles[2][kTileCount] = {
-    {{192, 256, 1, 1, 0.527f, 4.613f, {1.267f}, 0.915f},           // bf16 outputs
-     {256, 128, 1, 1, 0.972f, 3.510f, {0.933f}, 0.700f},
+    {{192, 256, 1, 1, 0.527f, 4.613f, {1.216f}, 0.878f},           // bf16 outputs
      {192, 128, 1, 1, 0.894f, 2.924f, {0.819f}, 0.651f},
-     {128, 128, 1, 2, 0.836f, 2.915f, {0.593f, 0.968f}, 0.f},
+     {128, 128, 1, 2, 0.836f, 2.915f, {0.546f, 0.891f}, 0.f},
      {64, 128, 1, 2, 1.695f, 1.798f, {0.303f, 0.617f}, 0.f},
      {64, 64, 1, 3, 1.930f, 1.121f, {0.236f, 0.383f, 0.587f}, 0.f},
      {64, 64, 2, 1, 1.522f, 1.606f, {0.454f}, 0.371f},
@@ -703,7 +720,6 @@ constexpr TileCost kTiles[2][kTileCount] = {
      {16, 16, 8, 0, 2.354f, 0.573f, {0.429f, 0.138f}, 0.f},
      {2, 4, 1, 0, 1.5f, 1.588f, {0.059f, 0.133f}, 0.f}},
     {{192, 256, 1, 1, kNever, 0.f, {0.f}, 0.f},                    // fp32 outputs: the conversions leave no registers
-     {256, 128, 1, 1, kNever, 0.f, {0.f}, 0.f},
      {192, 128, 1, 1, 0.175f, 4.504f, {1.390f}, 1.200f},
      {128, 128, 1, 2, 0.101f, 4.622f, {0.894f, 1.622f}, 0.f},
      {64, 128, 1, 2, 1.367f, 2.456f, {0.570f, 1.006f}, 0.f},
@@ -714,16 +730,16 @@ constexpr TileCost kTiles[2][kTileCount] = {
      {32, 32, 8, 1, 1.507f, 1.867f, {1.014f}, 0.690f},
      {16, 16, 8, 0, 2.448f, 0.555f, {0.423f, 0.142f}, 0.f},
      {2, 4, 1, 0, 1.5f, 1.962f, {0.053f, 0.088f}, 0.f}}};
-constexpr int kFewRows = 10, kRows2 = 11, kRows1 = 12;
+constexpr int kFewRows = 9, kRows2 = 10, kRows1 = 11;
 
 // Pairs of tiles: what is left of the rows behind tile a's whole rounds (of one workgroup to a compute unit) goes to tile b.  In
 // its own tiles it would leave most of the chip idle: 17,776 x 1,920 x 7,680 gated in fp32 462 us, so 434; 3,704 x 4,608 x
-// 1,152 through GELU in bf16 33.2 and 28.8, in fp32 54.8 and 42.6; 3,704 x 1,152 x 4,608 in bf16 31.3 and 29.3, in fp32 50.7 and
+// 1,152 in bf16 28.6 and 25.6, through GELU in fp32 54.8 and 42.6; 3,704 x 1,152 x 4,608 in bf16 28.4 and 25.1, in fp32 50.7 and
 // 40.9.  b's tiles cost what they cost alone where they start as a's end; where the last of a's rounds leaves compute
 // units that could hold two workgroups with one, they share them, and add `beside` us to a k-step where there is one to each.
 struct TilePair { int a, b; float beside[2]; };                   // beside: bf16, fp32; 0: a's have the compute unit to themselves
-constexpr TilePair kPairs[] = {{0, 2, {0.f, 0.f}}, {0, 6, {0.f, 0.f}}, {3, 5, {0.25f, 0.4f}}};
-constexpr int kFirstPair = 13, kPairCount = 3;
+constexpr TilePair kPairs[] = {{0, 1, {0.f, 0.f}}, {0, 5, {0.f, 0.f}}, {2, 4, {0.25f, 0.4f}}};
+constexpr int kFirstPair = 12, kPairCount = 3;
 
 template <class T> struct Type { using type = T; };
 
@@ -816,29 +832,28 @@ Status linear_f8(const dc_linear_f8_args& a, hipStream_t s) {
     using E = typename decltype(form)::type;
     constexpr bool BF = E::kBf16;
     using Tile0 = Tile<192, 256, 2, 4, 2>;
-    using Tile2 = Tile<192, 128, 2, 4, 3>;
-    using Tile3 = Tile<128, 128, 2, 2, 2>;
-    using Tile5 = Tile<64, 64, 2, 2, 3>;
-    using Tile6 = Tile<64, 64, 2, 2, 3, 2>;
+    using Tile1 = Tile<192, 128, 2, 4, 3>;
+    using Tile2 = Tile<128, 128, 2, 2, 2>;
+    using Tile4 = Tile<64, 64, 2, 2, 3>;
+    using Tile5 = Tile<64, 64, 2, 2, 3, 2>;
     const int choice = f8_tile(p.M, p.N, p.KT, cus, !BF);
     const int rest = choice < kFirstPair ? 0 : rows_of_rounds(choice - kFirstPair, p.M, p.N, cus);
     switch (choice) {
       case 0: if constexpr (BF) return launch<Tile0, E>(p, s); break;
-      case 1: if constexpr (BF) return launch<Tile<256, 128, 4, 2, 3>, E>(p, s); break;
+      case 1: return launch<Tile1, E>(p, s);
       case 2: return launch<Tile2, E>(p, s);
-      case 3: return launch<Tile3, E>(p, s);
-      case 4: return launch<Tile<64, 128, 2, 2, 3>, E>(p, s);
+      case 3: return launch<Tile<64, 128, 2, 2, 3>, E>(p, s);
+      case 4: return launch<Tile4, E>(p, s);
       case 5: return launch<Tile5, E>(p, s);
-      case 6: return launch<Tile6, E>(p, s);
-      case 7: return launch<Tile<32, 64, 1, 2, 3, 2>, E>(p, s);
-      case 8: return launch<Tile<32, 32, 1, 1, BF ? 3 : 2, 4>, E>(p, s);
-      case 9: return launch<Tile<32, 32, 1, 1, 2, 8>, E>(p, s);
+      case 6: return launch<Tile<32, 64, 1, 2, 3, 2>, E>(p, s);
+      case 7: return launch<Tile<32, 32, 1, 1, BF ? 3 : 2, 4>, E>(p, s);
+      case 8: return launch<Tile<32, 32, 1, 1, 2, 8>, E>(p, s);
       case kFewRows: return launch_few<8, E>(p, s);
       case kRows2: return launch_rows<2, E>(p, cus, s);
       case kRows1: return launch_rows<1, E>(p, cus, s);
-      case kFirstPair: if constexpr (BF) return launch_two<Tile0, Tile2, E>(p, rest, s); break;
-      case kFirstPair + 1: if constexpr (BF) return launch_two<Tile0, Tile6, E>(p, rest, s); break;
-      case kFirstPair + 2: return launch_two<Tile3, Tile5, E>(p, rest, s);
+      case kFirstPair: if constexpr (BF) return launch_two<Tile0, Tile1, E>(p, rest, s); break;
+      case kFirstPair + 1: if constexpr (BF) return launch_two<Tile0, Tile5, E>(p, rest, s); break;
+      case kFirstPair + 2: return launch_two<Tile2, Tile4, E>(p, rest, s);
     }
     return Status::shape("e4m3 product: no such tile");
   };

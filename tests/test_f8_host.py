@@ -240,7 +240,7 @@ def test_product_shapes_take_the_tiles_they_name():
     from tests import test_gpu_f8 as G
     assert {k: G.f8_tile(*k, 256) for k in G.TILE_SHAPES} == G.TILE_SHAPES
     assert {t for k, t in G.TILE_SHAPES.items() if k[3] == "bf16"} == set(G.F8_TILES)
-    assert {t for k, t in G.TILE_SHAPES.items() if k[3] == "f32"} == {*G.F8_TILES[2:13], G.F8_TILES[-1]}
+    assert {t for k, t in G.TILE_SHAPES.items() if k[3] == "f32"} == {*G.F8_TILES[1:12], G.F8_TILES[-1]}
 
 
 # ----------------------------------------------------------------------------
