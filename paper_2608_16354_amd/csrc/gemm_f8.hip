@@ -431,7 +431,7 @@ __device__ inline void tile_product(const Args& p, const E& epi, uint4* rings, f
       if constexpr (EARLY && fill) {                    // w's part, spread over the rows between the barriers
         constexpr int GAP = (T - (EARLY_ROW + 1) * TN) / BI;
         const int d = t - EARLY_ROW * TN - 1;
-        static_assert(GAP > 0, "tiles for w's fills");
+        static_assert(GAP > 0 && EARLY_ROW * TN + 1 + GAP * (BI - 1) < T - TN, "all of w's fills before the wait that counts them");
         if (d >= 0 && d % GAP == 0 && d / GAP < BI) dma_one(s, kt + ST, AI + d / GAP);
       }
       if (fill && a == TM - 1) {                        // the rest
