@@ -487,8 +487,6 @@ dc_status dc_linear_i8(const dc_linear_i8_args* p, hipStream_t stream) {
     if (p->gate && (p->gelu || p->out_dtype != DC_F32)) return Status::arg("a gated residual has fp32 outputs and no GELU");
     if (p->ld_out < p->out_features || (p->gate && p->ld_residual < p->out_features))
       return Status::arg("ld_out and ld_residual must be at least out_features");
-    if (p->rows > 1 && (p->ld_out >> 32 || (p->residual && p->ld_residual >> 32)))
-      return Status::arg("ld_out and ld_residual must be below 2^32");
     if (p->rows == 0) return Status::ok();
     if (!p->x || !p->x_scale || !p->w || !p->w_scale || !p->out) return Status::arg("NULL argument");
     if (!aligned16(p->x) || !aligned16(p->w)) return Status::arg("x and w must be 16-byte aligned");

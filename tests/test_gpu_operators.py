@@ -323,6 +323,27 @@ def test_linear_rows_beyond_32_bit_offsets(api, dev):
     check_linear(host(out), x, xs, w, ws, None, gate, res, "plain", False)
 
 
+@pytest.mark.parametrize("kind,dt", [("plain", "f32"), ("gelu", "bf16"), ("gated", "f32"), ("gated in place", "f32")])
+def test_linear_outputs_beyond_32_bit_strides(api, dev, kind, dt):
+    """Two rows of outputs, and of the residual, more than 2^32 values apart."""
+    import torch
+    m, n, apart = 2, 75, (1 << 32) + 5
+    x, xs, w, ws, bias, gate, res = linear_inputs(m, n, 256, 6)
+
+    def far():
+        return torch.empty(apart + n, device=dev, dtype=torch.float32 if dt == "f32" else torch.bfloat16).as_strided((m, n), (apart, 1))
+
+    out, rs = far(), None
+    if kind.startswith("gated"):
+        rs = far() if kind == "gated" else out
+        rs.copy_(t(res, dev))
+    say("far outputs", kind, dt)
+    api.dc_linear_i8(t(x, dev), t(xs, dev), t(w, dev), t(ws, dev), out, bias=t(bias, dev), gelu=kind == "gelu",
+                     gate=None if rs is None else t(gate, dev), residual=rs)
+    torch.cuda.synchronize()
+    check_linear(host(out), x, xs, w, ws, bias, gate, res, kind.split()[0], dt == "bf16")
+
+
 def test_linear_of_a_row_without_a_number(api, dev):
     """A row that held a NaN or an infinity is NaN in the product, the others are not."""
     import torch

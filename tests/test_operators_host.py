@@ -122,6 +122,16 @@ def test_linear_i8_refuses(lib, more, code):
     assert lib.dc_linear_i8(C.byref(a), None) == code
 
 
+@pytest.mark.parametrize("more", [dict(ld_out=1 << 32), dict(ld_out=(1 << 40) + 5, out_dtype=1), dict(GATED, ld_residual=1 << 32),
+                                  dict(GATED, ld_out=1 << 33, ld_residual=(1 << 32) + 1), dict(GATED, out=FAKE, ld_out=1 << 32, ld_residual=1 << 32),
+                                  dict(rows=1, ld_out=1 << 62)])
+def test_linear_i8_takes_rows_at_any_distance(lib, more):
+    """Row strides of outputs and residuals have no upper limit: what is refused is K, which is looked at after them."""
+    a = linear(in_features=64, **more)
+    assert lib.dc_linear_i8(C.byref(a), None) == SHAPE
+    assert b"K" in lib.dc_last_error()
+
+
 def test_linear_i8_refuses_null(lib):
     assert lib.dc_linear_i8(None, None) == ARG
 
