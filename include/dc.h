@@ -308,7 +308,9 @@ dc_status dc_rms_norm_f8(const dc_rms_norm_f8_args* args, hipStream_t stream);
 /* out[m, n] = f(sum over blocks b of x_scale[m, b] w_scale[n / 128, b] sum_{k in b} x[m, k] w[n, k] + bias[n]): products
  * exact, sums in fp32 in a fixed order (bitwise reproducible), one rounding to out_dtype.  With DC_BF16 the 128 products
  * of a block are summed eight at a time with 15 bits and more behind the largest of the eight.  f: the value itself, GELU
- * (tanh form), or residual[m, n] + gate[n] * value.  Codes 0x7F and 0xFF are NaN. */
+ * (tanh form), or residual[m, n] + gate[n] * value.  Codes 0x7F and 0xFF are NaN.  x_scale[m, b] * w_scale[n / 128, b] is taken
+ * as one fp32 number before it meets the block's sum, and wants to be 0 or at least 2^-126 and below 2^128 in magnitude: one
+ * below is off by up to 2^-150, times the block's sum, and an infinite one makes the output infinite or NaN. */
 typedef struct {
   int32_t rows, out_features;     /* M, N, below 2^24; rows = 0 is a no-op */
   int32_t in_features;            /* K with its padding: a multiple of 128, at most 2^22 */

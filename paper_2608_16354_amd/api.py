@@ -272,7 +272,7 @@ def dc_rms_norm_f8(x, q, scale, weight=None, eps=1e-6, residual=None, out=None, 
 def dc_linear_f8(x, x_scale, w, w_scale, out, bias=None, gelu=False, gate=None, residual=None, stream=None):
     """out [M, N] := the product of e4m3 rows x [M, K] and w [N, K] (K as padded by dc_quantize_f8) with their scales
     ([M, K / 128], [N / 128 rounded up, K / 128], any strides), plus bias, through GELU or as residual + gate * (...)
-    (residual of out's type; gate None: 1)."""
+    (residual of out's type; gate None: 1).  A scale of x times one of w is an fp32 number: 0, or 2^-126 to below 2^128."""
     _call("dc_linear_f8", stream, x, x, x_scale, w, w_scale, out, bias, gelu, gate, residual)
 
 

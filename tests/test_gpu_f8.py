@@ -464,6 +464,55 @@ def test_linear_scales_of_any_strides(api, dev):
             check_linear(host(out), x, host_s, w, host_w, None, gate, res, "plain", False, True)
 
 
+SCALE_SHAPES = [(1, 40, 256), (1, 41, 4224), (2, 333, 640), (9, 5, 384), (20, 70, 384), (50, 300, 1024), (300, 400, 512), (1301, 5765, 384),
+                (1608, 5515, 512), (3273, 5214, 512)]
+
+
+@pytest.mark.parametrize("m,n,k", SCALE_SHAPES)
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_linear_scales_at_the_ends_of_their_range(api, dev, m, n, k, dt):
+    """Products of two scales from 2^-126 to 2^127, one scale far from 1 or both: the sums are exact, and outputs are
+    rounded once."""
+    import torch
+    x, xs, w, ws, _, _, _ = whole_inputs(m, n, k, 11)
+    one, pick = np.zeros_like(x), np.unique(np.r_[0, m - 1, np.random.default_rng(0).integers(0, m, 60)])
+    one[np.arange(m), np.arange(m) * 37 % k] = 1        # a row of one 1: outputs are one product
+    for codes_x, codes_w, ex, ew in ((x, w, -63, -63), (x, w, 1, -127), (x, w, -126, 0), (x, w, -140, 20), (x, w, 100, -100), (one, np.sign(w), 64, 63),
+                                     (one, np.sign(w), 0, 127), (one, np.sign(w), -22, -100)):
+        sx, sw = np.float32(2.0) ** np.float32(ex) * np.ones_like(xs), np.float32(2.0) ** np.float32(ew) * np.ones_like(ws)
+        out = torch.empty((m, n), device=dev, dtype=kind_of(dt))
+        say("linear scales", m, n, k, dt, ex, ew)
+        api.dc_linear_f8(codes(codes_x, dev), t(sx, dev), codes(codes_w, dev), t(sw, dev), out)
+        want = X.linear_f8(codes_x[pick], sx[pick], codes_w, sw)[0].astype(np.float32)
+        assert np.array_equal(host(out)[pick], want if dt == "f32" else I.round_bf16(want))
+
+
+@pytest.mark.parametrize("m,n,k", SCALE_SHAPES)
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_linear_scales_outside_their_range(api, dev, m, n, k, dt):
+    """Below 2^-126 a product of two scales is off by half a step of 2^-149, and the whole numbers that it is multiplied with
+    make of it what they sum to; up to K / 128 + 16 additions (of blocks, of what lanes, waves and groups hold) and the output are
+    rounded to 2^-24 or half a step (2^-150; bf16 2^-8 and 2^-134).  From 2^128 on no output is a number."""
+    import torch
+    x, xs, w, ws, _, _, _ = whole_inputs(m, n, k, 12)
+    pick = np.unique(np.r_[0, m - 1, np.random.default_rng(0).integers(0, m, 60)])
+    rng = np.random.default_rng(13)
+    sx = (rng.uniform(1, 2, xs.shape) * 2.0 ** -70).astype(np.float32)
+    sw = (rng.uniform(1, 2, ws.shape) * 2.0 ** -69).astype(np.float32)
+    out = torch.empty((m, n), device=dev, dtype=kind_of(dt))
+    say("linear small scales", m, n, k, dt)
+    api.dc_linear_f8(codes(x, dev), t(sx, dev), codes(w, dev), t(sw, dev), out)
+    v, size = X.linear_f8(x[pick], sx[pick], w, sw)
+    tol = np.abs(x[pick]).astype(np.float64) @ np.abs(w).T * 2.0 ** -150 + (k // 128 + 16) * (F32 * size + 2.0 ** -150)
+    tol = tol + np.maximum((BF16 if dt == "bf16" else F32) * (np.abs(v) + tol), 2.0 ** -134 if dt == "bf16" else 2.0 ** -150)
+    err = np.abs(host(out)[pick] - v)
+    assert (err <= tol).all(), (err / tol).max()
+    sx[:], sw[:] = 2.0 ** 64, 2.0 ** 64
+    say("linear large scales", m, n, k, dt)
+    api.dc_linear_f8(codes(x, dev), t(sx, dev), codes(w, dev), t(sw, dev), out)
+    assert not torch.isfinite(out).any()
+
+
 def test_linear_rows_beyond_32_bit_offsets(api, dev):
     """Rows 4 MiB apart: the last ones lie past 2^31 bytes, in x and in w."""
     import torch
