@@ -147,6 +147,40 @@ def test_quantize_many_rows(api, dev, dtype, rows, cols):
     assert np.array_equal(host(s), want_s) and np.array_equal(host(q), want_q)
 
 
+STREAMED = 10 << 20                     # bytes of x from which on rows are read past the caches
+
+
+@pytest.mark.parametrize("dtype,rows,cols,wide", [("bf16", 1301, 4999, True), ("bf16", 1203, 7687, True), ("bf16", 1282, 4096, True), ("bf16", 1300, 4095, False),
+                                                  ("f32", 701, 4225, True), ("f32", 643, 4100, True), ("f32", 645, 4095, False), ("f32", 2801, 1001, False)])
+def test_quantize_streamed_rows(api, dev, dtype, rows, cols, wide):
+    """Rows long enough for the streaming loads, and wide ones (4,096 columns on: a workgroup takes 16 rows x 4 blocks in bf16,
+    8 x 2 in fp32), with rows and blocks left over; strided and marked, as the short ones."""
+    import torch
+    e, rng = 2 if dtype == "bf16" else 4, np.random.default_rng(rows)
+    assert rows * cols * e >= STREAMED and (cols >= 4096) == wide
+    blocks = -(-cols // 128)
+    x = (rng.standard_normal((rows, cols)) * np.exp(rng.standard_normal((rows, 1)))).astype(np.float32)
+    x[:, -1] = 3 * np.abs(x).max(1)                     # a last block's scale is its last feature's
+    special_rows(x)
+    special_rows(x[-11:])                               # of a workgroup of fewer rows
+    if dtype == "bf16":
+        x = host(t(x, dev, kind_of(dtype)))
+    want_q, want_s = X.e4m3_blocks(x)
+    for lead, extra, major, gap in ((0, 0, "block", 0), (1, 5, "row", 2)):
+        xb = torch.zeros((rows, cols + lead + extra), device=dev, dtype=kind_of(dtype))
+        xb[:, lead: lead + cols] = t(x, dev)
+        qb = marked(rows + 1, (blocks + 1) * 128, dev)
+        s, sb = scales(rows, blocks, dev, major, gap)
+        say("quantize streamed rows", dtype, rows, cols, lead)
+        api.dc_quantize_f8(xb[:, lead: lead + cols], qb[:rows], s)
+        torch.cuda.synchronize()
+        assert np.array_equal(host(s), want_s, equal_nan=True)
+        assert np.array_equal(host(qb[:rows, : blocks * 128]), want_q)
+        b = raw(qb)
+        assert (b[rows] == MARK).all() and (b[:, blocks * 128:] == MARK).all()
+        assert (host(sb) == 99).sum() == sb.numel() - rows * blocks
+
+
 # ----------------------------------------------------------------------------
 # the norm
 # ----------------------------------------------------------------------------
