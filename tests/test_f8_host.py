@@ -243,6 +243,14 @@ def test_product_shapes_take_the_tiles_they_name():
     assert {t for k, t in G.TILE_SHAPES.items() if k[3] == "f32"} == {*G.F8_TILES[1:12], G.F8_TILES[-1]}
 
 
+def test_products_of_few_k_steps_take_the_tiles_they_name():
+    """One to three k-steps: every tile that the rule picks for them, the columns' kernels (one row, two long ones) aside."""
+    from tests import test_gpu_f8 as G
+    assert {k: G.f8_tile(*k, 256) for k in G.FEW_STEPS} == G.FEW_STEPS
+    assert {t for k, t in G.FEW_STEPS.items() if k[3] == "bf16"} == set(G.F8_TILES) - {"64x64 x 2", "32x32 x 8", "column", "column of 2"}
+    assert {k[2] for k, t in G.FEW_STEPS.items() if t in ("192x256", "192x128", "128x128", "64x128", "64x64")} == {128, 256, 384}
+
+
 # ----------------------------------------------------------------------------
 # the definitions, by hand
 # ----------------------------------------------------------------------------

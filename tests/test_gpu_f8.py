@@ -455,6 +455,41 @@ def test_linear_tiles(api, dev, mnkt, kind):
         check_linear(got[pick], d[0][pick], d[1][pick], d[2], d[3], d[4] if kind != "plain" else None, d[5], d[6][pick], kind, dt == "bf16", True)
 
 
+FEW_STEPS = {       # one to three k-steps, no more than a tile's stages or one more: shapes and tiles as above
+    (1690, 5963, 128, "bf16"): "192x256", (676, 7466, 128, "bf16"): "192x128", (8888, 688, 128, "bf16"): "128x128",
+    (1739, 1763, 128, "bf16"): "64x128", (1299, 69, 128, "bf16"): "64x64", (131, 41, 128, "bf16"): "16x16 x 8",
+    (895, 4717, 128, "bf16"): "128x128 then 64x64", (4070, 2298, 256, "bf16"): "192x256", (677, 7317, 256, "bf16"): "192x128",
+    (2075, 2959, 256, "bf16"): "128x128", (558, 5507, 256, "bf16"): "64x128", (1354, 399, 256, "bf16"): "64x64",
+    (136, 598, 256, "bf16"): "32x64 x 2", (131, 43, 256, "bf16"): "16x16 x 8", (6997, 2436, 256, "bf16"): "192x256 then 192x128",
+    (5182, 2320, 256, "bf16"): "192x256 then 64x64 x 2", (5116, 809, 256, "bf16"): "128x128 then 64x64", (5204, 1764, 384, "bf16"): "192x256",
+    (6030, 806, 384, "bf16"): "192x128", (769, 7964, 384, "bf16"): "128x128", (7663, 400, 384, "bf16"): "64x128",
+    (359, 1530, 384, "bf16"): "64x64", (624, 398, 384, "bf16"): "32x64 x 2", (506, 144, 384, "bf16"): "32x32 x 4",
+    (143, 40, 384, "bf16"): "16x16 x 8", (2832, 6042, 384, "bf16"): "192x256 then 192x128", (7146, 1704, 384, "bf16"): "192x256 then 64x64 x 2",
+    (2820, 1452, 384, "bf16"): "128x128 then 64x64", (1337, 3613, 128, "f32"): "192x128", (1028, 5891, 128, "f32"): "128x128",
+    (1683, 1831, 128, "f32"): "64x128", (2046, 63, 128, "f32"): "64x64", (53, 119, 128, "f32"): "16x16 x 8",
+    (1655, 2588, 128, "f32"): "128x128 then 64x64", (1317, 3739, 256, "f32"): "192x128", (4039, 1493, 256, "f32"): "128x128",
+    (386, 7903, 256, "f32"): "64x128", (158, 3499, 256, "f32"): "64x64", (8338, 43, 256, "f32"): "64x64 x 2",
+    (289, 395, 256, "f32"): "32x64 x 2", (70, 92, 256, "f32"): "16x16 x 8", (6568, 651, 256, "f32"): "128x128 then 64x64",
+    (2959, 1675, 384, "f32"): "192x128", (1986, 3042, 384, "f32"): "128x128", (393, 7845, 384, "f32"): "64x128",
+    (2223, 255, 384, "f32"): "64x64", (81, 8396, 384, "f32"): "32x64 x 2", (52, 2275, 384, "f32"): "32x32 x 4",
+    (107, 62, 384, "f32"): "16x16 x 8", (2364, 1793, 384, "f32"): "128x128 then 64x64",
+}
+
+
+@pytest.mark.parametrize("mnkt", list(FEW_STEPS))
+@pytest.mark.parametrize("kind", ["plain", "gelu", "gated"])
+def test_linear_tiles_of_few_k_steps(api, dev, mnkt, kind):
+    """Sums that end while a tile's stages are still being filled, or a k-step later."""
+    m, n, k, dt = mnkt
+    assert f8_tile(m, n, k, dt, compute_units(dev)) == FEW_STEPS[mnkt]
+    data = whole_inputs(m, n, k, 9)
+    pick = np.unique(np.r_[0, m - 1, np.random.default_rng(0).integers(0, m, 150)])
+    say("linear few k-steps", mnkt, FEW_STEPS[mnkt], kind)
+    got = run_linear(api, dev, data, kind, dt, kind != "plain")
+    d = of_type(data, dt, dev)
+    check_linear(got[pick], d[0][pick], d[1][pick], d[2], d[3], d[4] if kind != "plain" else None, d[5], d[6][pick], kind, dt == "bf16", True)
+
+
 @pytest.mark.parametrize("m,n,k", [(1, 1920, 7680), (2, 333, 5120), (50, 333, 1920), (257, 513, 1152), (700, 1920, 1920), (1, 40, 65536)])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_linear_of_any_codes(api, dev, m, n, k, dt):
