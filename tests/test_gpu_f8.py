@@ -501,6 +501,20 @@ def test_linear_of_any_codes(api, dev, m, n, k, dt):
         check_linear(got, *d, kind, dt == "bf16", False)
 
 
+@pytest.mark.parametrize("mnkt", list(TILE_SHAPES))
+@pytest.mark.parametrize("kind", ["plain", "gated"])
+def test_linear_tiles_of_any_codes(api, dev, mnkt, kind):
+    """Every tile on codes over their whole range and any scales."""
+    m, n, k, dt = mnkt
+    assert f8_tile(m, n, k, dt, compute_units(dev)) == TILE_SHAPES[mnkt]
+    data = any_inputs(m, n, k, 8)
+    pick = np.unique(np.r_[0, m - 1, np.random.default_rng(1).integers(0, m, 150)])
+    say("linear tile, any codes", mnkt, TILE_SHAPES[mnkt], kind)
+    got = run_linear(api, dev, data, kind, dt, kind != "plain")
+    d = of_type(data, dt, dev)
+    check_linear(got[pick], d[0][pick], d[1][pick], d[2], d[3], d[4] if kind != "plain" else None, d[5], d[6][pick], kind, dt == "bf16", False)
+
+
 def test_linear_in_fp32_keeps_small_products(api, dev):
     """Products of 1 beside one of 65,536 in each block: fp32 outputs hold the sum exactly."""
     import torch
