@@ -286,6 +286,68 @@ def test_norm_writes_the_codes_of_the_definition(api, dev, rows, cols, r_type):
     check_exactly(host(q), host(s), X.rms_norm(host(x).astype(np.float64) + (0 if r is None else host(r)), host(w), np.float64(np.float32(1e-6))))
 
 
+def norm_by_definition(api, dev, rows, cols, x_type, r_type, out_type, lead, weighted, in_place):
+    """The norm of rows `lead` values into wider ones: the sum as fp32 and its type hold it, codes and scales exactly, and
+    nothing written around them."""
+    import torch
+    gen, blocks, eps = torch.Generator(dev).manual_seed(cols + lead), -(-cols // 128), 1e-5
+    size = torch.exp(torch.randn((rows, 1), device=dev, generator=gen))
+    x = torch.zeros((rows, cols + lead), device=dev, dtype=kind_of(x_type))[:, lead:]
+    x.copy_(size * torch.randn((rows, cols), device=dev, generator=gen))
+    x[min(3, rows - 1)] = 0
+    r = None
+    if r_type is not None:
+        r = torch.zeros((rows, cols + 2 * lead), device=dev, dtype=kind_of(r_type))[:, lead: lead + cols]
+        r.copy_(3 * torch.randn((rows, cols), device=dev, generator=gen))
+        r[min(3, rows - 1)] = 0
+    w = 1 + torch.randn(cols, device=dev, generator=gen) if weighted else None
+    h64 = host(x).astype(np.float64) + (0 if r is None else host(r))
+    out = buf = None
+    if in_place is not None:
+        out = x if in_place == "x" else r
+        assert in_place == "x" and x_type == out_type or in_place == "residual" and r_type == out_type
+    elif out_type is not None:
+        buf = torch.full((rows + 1, cols + 2), 7.0, device=dev, dtype=kind_of(out_type))
+        out = buf[:rows, 1: 1 + cols]
+    qb, (s, sb) = marked(rows + 1, (blocks + 1) * 128, dev), scales(rows, blocks, dev, "row" if lead else "block", 1)
+    say("norm by definition", rows, cols, x_type, r_type, out_type, lead, in_place)
+    api.dc_rms_norm_f8(x, qb[:rows, : blocks * 128], s, weight=w, eps=eps, residual=r, out=out)
+    torch.cuda.synchronize()
+    check_exactly(host(qb[:rows, : blocks * 128]), host(s), X.rms_norm(h64, None if w is None else host(w), np.float64(np.float32(eps))))
+    if out is not None:
+        h = h64.astype(np.float32)
+        assert np.array_equal(host(out), h if out_type == "f32" else I.round_bf16(h))
+    if buf is not None:
+        b = host(buf)
+        assert (b[rows] == 7).all() and (b[:, 0] == 7).all() and (b[:, 1 + cols:] == 7).all()
+    b = raw(qb)
+    assert (b[rows] == MARK).all() and (b[:, blocks * 128:] == MARK).all()
+    assert (host(sb) == 99).sum() == sb.numel() - rows * blocks
+
+
+NORM_TYPES = [("bf16", "f32", "f32", "residual"), ("bf16", "f32", "bf16", "x"), ("f32", "f32", "f32", "x"), ("f32", "f32", None, None), ("f32", "bf16", "bf16", "residual"),
+              ("f32", "bf16", "f32", None), ("bf16", "bf16", "bf16", "residual"), ("bf16", "bf16", "f32", None), ("f32", None, "f32", "x"), ("f32", None, "bf16", None),
+              ("f32", None, None, None), ("bf16", None, "bf16", "x"), ("bf16", None, None, None)]
+
+
+@pytest.mark.parametrize("cols", [1, 5, 8, 100, 127, 129, 511, 513, 1000, 1152, 1537, 1921, 2049, 4095, 5003, 8200, 16381])
+@pytest.mark.parametrize("x_type,r_type,out_type,in_place", NORM_TYPES)
+def test_norm_of_any_rows_by_definition(api, dev, cols, x_type, r_type, out_type, in_place):
+    """Ragged widths of every kernel, every pair of types, rows at every element's address, in place and not."""
+    norm_by_definition(api, dev, 13, cols, x_type, r_type, out_type, 0, True, in_place)
+    norm_by_definition(api, dev, 13, cols, x_type, r_type, out_type, 3, False, None)
+
+
+@pytest.mark.parametrize("cols", [250, 1001, 1500, 1921, 4090, 5003, 16381])
+@pytest.mark.parametrize("x_type,r_type,out_type,in_place", NORM_TYPES)
+def test_norm_of_streamed_rows_by_definition(api, dev, cols, x_type, r_type, out_type, in_place):
+    """The same where rows are read past the caches, for each number of waves and pieces; a workgroup of four rows is left over."""
+    size = {"bf16": 2, "f32": 4, None: 0}
+    rows = STREAMED // (cols * (size[x_type] + size[r_type])) // 4 * 4 + 5
+    assert rows * cols * (size[x_type] + size[r_type]) >= STREAMED
+    norm_by_definition(api, dev, rows, cols, x_type, r_type, out_type, 1, True, in_place)
+
+
 def test_norm_of_rows_of_any_size(api, dev):
     """Rows from the smallest numbers to the largest: none overflows, and those that eps outweighs are small, not lost."""
     import torch
