@@ -239,7 +239,7 @@ dc_status dc_quantize_rows(const void* x, int32_t dtype, int64_t ld_x, int32_t r
  * the rest in fp32, one rounding to out_dtype.  f: the value itself, GELU (tanh form), or
  * residual[m, n] + gate[n] * value. */
 typedef struct {
-  int32_t rows, out_features;     /* M, N, below 2^24; rows = 0 is a no-op */
+  int32_t rows, out_features;     /* M, N, below 2^24, M N (each rounded up to 64) up to 2^35; rows = 0 is a no-op */
   int32_t in_features;            /* K with its padding: a multiple of 128, at most 130,944 */
   const int8_t* x;                /* [rows, ld_x], 16-byte aligned; ld_x: K to 2^22, a multiple of 16 */
   const float* x_scale;           /* [rows] */
@@ -264,12 +264,13 @@ dc_status dc_linear_i8(const dc_linear_i8_args* args, hipStream_t stream);
  * ties to even.  A block of zeros has scale 0 and codes 0; one with an infinity or NaN has scale NaN and codes 0,
  * so a product with it is NaN.  Rows of codes are padded with zeros to whole blocks; a last block's scale is that of
  * the features it has.  Scales are at scale[row * scale_row + block * scale_block] (strides in elements; scale_row = 1,
- * scale_block >= rows is what the kernels write and read fastest); written ones may not share an address. */
+ * scale_block >= rows is what the kernels write and read fastest); written ones share no address, and all of a row's lie
+ * before the next row's or all of a block's before the next block's. */
 
 /* Rows (block_rows 1: a scale to 128 features of a row) or a weight matrix [out, in] (block_rows 128: a scale to
  * 128 x 128 values) in e4m3. */
 typedef struct {
-  int32_t rows, cols;             /* below 2^24; rows = 0 is a no-op */
+  int32_t rows, cols;             /* below 2^24, rows (rounded up to 16) times cols (to 128) below 2^35; rows = 0: a no-op */
   const void* x;                  /* [rows, ld_x], at any element's address; ld_x >= cols */
   int32_t x_dtype;                /* dc_dtype */
   int64_t ld_x;
@@ -312,7 +313,7 @@ dc_status dc_rms_norm_f8(const dc_rms_norm_f8_args* args, hipStream_t stream);
  * as one fp32 number before it meets the block's sum, and wants to be 0 or at least 2^-126 and below 2^128 in magnitude: one
  * below is off by up to 2^-150, times the block's sum, and an infinite one makes the output infinite or NaN. */
 typedef struct {
-  int32_t rows, out_features;     /* M, N, below 2^24; rows = 0 is a no-op */
+  int32_t rows, out_features;     /* M, N, below 2^24, M N (each rounded up to 64) up to 2^35; rows = 0 is a no-op */
   int32_t in_features;            /* K with its padding: a multiple of 128, at most 2^22 */
   const uint8_t* x;               /* [rows, ld_x], 16-byte aligned; ld_x: K to 2^22, a multiple of 16 */
   int64_t ld_x;

@@ -257,8 +257,8 @@ def dc_linear_i8(x, x_scale, w, w_scale, out, bias=None, gelu=False, gate=None, 
 
 
 def dc_quantize_f8(x, q, scale, block_rows=1, stream=None):
-    """q (float8_e4m3fn [rows, at least cols rounded up to 128]) and scale (f32 [rows, cols / 128 rounded up], any
-    strides; torch.empty((blocks, rows)).t() is the fastest) := the rows of x [rows, cols], a scale to 128 features.
+    """q (float8_e4m3fn [rows, at least cols rounded up to 128]) and scale (f32 [rows, cols / 128 rounded up], by rows or by
+    blocks at any strides; torch.empty((blocks, rows)).t() is the fastest) := the rows of x [rows, cols], a scale to 128 features.
     block_rows=128: a weight matrix, scale [rows / 128 rounded up, ...], one to 128 x 128 values."""
     _call("dc_quantize_f8", stream, x, x, q, scale, block_rows)
 
@@ -271,8 +271,9 @@ def dc_rms_norm_f8(x, q, scale, weight=None, eps=1e-6, residual=None, out=None, 
 
 def dc_linear_f8(x, x_scale, w, w_scale, out, bias=None, gelu=False, gate=None, residual=None, stream=None):
     """out [M, N] := the product of e4m3 rows x [M, K] and w [N, K] (K as padded by dc_quantize_f8) with their scales
-    ([M, K / 128], [N / 128 rounded up, K / 128], any strides), plus bias, through GELU or as residual + gate * (...)
-    (residual of out's type; gate None: 1).  A scale of x times one of w is an fp32 number: 0, or 2^-126 to below 2^128."""
+    ([M, K / 128], [N / 128 rounded up, K / 128], any strides, x_scale's rows less than 2^21 apart), plus bias, through
+    GELU or as residual + gate * (...) (residual of out's type; gate None: 1).  A scale of x times one of w is an fp32
+    number: 0, or from 2^-126 to below 2^128."""
     _call("dc_linear_f8", stream, x, x, x_scale, w, w_scale, out, bias, gelu, gate, residual)
 
 

@@ -13,11 +13,20 @@
 // v_mfma_f32_16x16x32_bf16 (the same draws: 9e-9 off).
 // Tiles go global -> LDS by LDS-DMA, a stage holding the k-step's rows of both operands and their scales.
 //
-// What bounds long products is the power that the chip may draw, which sets the clock: at 17,776 x 7,680 x 1,920 in bf16 (250 to
-// 280 us, 1.9 to 2.1 PFLOP/s) the matrix pipe is busy 44 % of the time at 1.8 to 1.9 GHz, at 17,776 x 1,920 x 7,680 in fp32 (430 to
-// 465 us, 1.1 to 1.2) 56 % at 1.8.  On operands of zeros the same code takes 202 and 378 us.  From registers alone the
-// instructions of a k-step, multiply-adds included, run at 3.5 PFLOP/s (on zeros 4.7).  Starting the workgroups out of step with
-// each other, which spreads the outputs' way to memory, changed nothing.
+// Sizes in these comments are M x N x K.  Long ones: 17,776 x 7,680 x 1,920 in bf16 250 to 280 us (1.9 to 2.1 PFLOP/s), 17,776 x
+// 1,920 x 7,680 in fp32 430 to 465 (1.1 to 1.2); at the rates of torch's longest e4m3 and bf16 products they would be 178 and 342.
+// Three things are known to lie between:
+// - Power, which sets the clock: the matrix pipe is busy 44 and 56 % of the time at 1.8 to 1.9 GHz; on operands of zeros the
+//   same code takes 205 and 347 us.  From registers alone the instructions of a k-step, multiply-adds included, run at 3.5 PFLOP/s (on
+//   zeros 4.7).
+// - What surrounds a tile's k-steps, with one workgroup of 192 x 256 to a compute unit and so nothing to hide it: 4.6 us a round of tiles, 51
+//   of the first product's 11 rounds.
+// - Operands that every XCD and every group of row tiles fetches again: 549 MB for 49, 1,104 for 288 (residual included), with the
+//   outputs 2.7 to 2.9 TB/s of the 5.1 that a copy moves; what they cost was not measured by itself.
+// Plain, in bf16 and in turn on one box, torch's e4m3 product with one scale for all takes 230 us for the first (this 253; on zeros 199
+// and 205) and 293 for 17,776 x 1,920 x 7,680 (this 243; 280 and 194); its bf16 product, which fp32 outputs are to be held against, 395 and
+// 399 (this, with fp32 outputs, 471 and 437).  Starting the workgroups out of step with each other, which spreads the outputs' way to
+// memory, changed nothing.
 #include "gemm_tile.h"
 
 #include <algorithm>

@@ -282,7 +282,8 @@ constexpr int kMaxNormCols = 16384;     // a row stays in the registers of a wor
 Status quantize_f8(const dc_quantize_f8_args& a, hipStream_t s);
 Status rms_norm_f8(const dc_rms_norm_f8_args& a, hipStream_t s);
 Status linear_f8(const dc_linear_f8_args& a, hipStream_t s);
-// which of its thirteen tiles a product takes (gemm_f8.hip, kTiles); full: fp32 outputs
+// which of its eleven tiles (gemm_f8.hip, kTiles), the kernel of one row (11) or three pairs of tiles (12 on) a product takes;
+// full: fp32 outputs
 int f8_tile(int M, int N, int ksteps, int cus, bool full);
 
 // The residual cache in 8 or 4 bits, a scale to 64 features (quant.hip).

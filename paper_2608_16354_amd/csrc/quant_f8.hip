@@ -226,10 +226,13 @@ struct NormArgs {
 // its loads are over by then.
 // The sum, the root, the products with the weights and the quotients are in double, which the vector unit works on in 4/3
 // of fp32's time: what is rounded away before the codes is far below fp32's last place, so codes and scales are those of the
-// definition whatever the order of the sum.  In fp32 a few codes in 10^6 and many scales come out a place off; it takes
-// 70.9 us for 17,776 x 1,920 (bf16 + fp32 -> fp32; double: 68.8, 5.5 TB/s, a copy's rate), 11.9 for 3,704 x 1,152 (12.2), and
-// 28.3 for bf16 rows of 17,776 x 1,152 with a bf16 residual (33.6), where the vector unit is what bounds it.  A loop over
-// rows with the next one's loads on their way costs as many registers as it hides waits: 69 to 73, 12.5 to 13.9, 36 to 38 us.
+// definition whatever the order of the sum.  In fp32 a few codes in 10^6 and many scales come out a place off.  What that
+// costs goes by the bytes of a value (launches one behind the other on inputs in turn; TB/s of what is read and written): with an
+// fp32 residual and sum memory bounds it, 17,776 x 1,920 74 us, 5.05 TB/s (a copy of as many bytes 5.2 to 5.4), 3,704 x 1,152 12.2 (in
+// fp32 11.9).  With fewer it is the arithmetic (the vector unit works 61 to 63 % of the time, there 52) and the trip to memory that a
+// wave makes before it: 17,776 x 1,152 in bf16 with a bf16 residual and sum 35 us, 4.1 TB/s (in turn with fp32 33.6 and 28.3),
+// with neither 28.6, 2.15 (at a copy's rate 12), fp32 rows alone 29.3, 3.5.  A loop over rows with the next one's loads on their
+// way costs as many registers as it hides waits: 69 to 73, 12.5 to 13.9, 36 to 38 us.
 template <bool BF, Res RES, int NV, int WR, bool NT>
 __global__ void __launch_bounds__(WR == 1 ? 256 : WR * kWave) k_rms_norm_f8(NormArgs a) {
   constexpr int LR = WR * kWave;
