@@ -23,7 +23,7 @@
 //   of the first product's 11 rounds.
 // - Operands that every XCD and every group of row tiles fetches again: 549 MB for 49, 1,104 for 288 (residual included), with the
 //   outputs 2.7 to 2.9 TB/s of the 5.1 that a copy moves; what they cost was not measured by itself.
-// Plain, in bf16 and in turn on one box, torch's e4m3 product with one scale for all takes 230 us for the first (this 253; on zeros 199
+// Plain, in bf16 and in turn on one card, torch's e4m3 product with one scale for all takes 230 us for the first (this 253; on zeros 199
 // and 205) and 293 for 17,776 x 1,920 x 7,680 (this 243; 280 and 194); its bf16 product, which fp32 outputs are to be held against, 395 and
 // 399 (this, with fp32 outputs, 471 and 437).  Starting the workgroups out of step with each other, which spreads the outputs' way to
 // memory, changed nothing.

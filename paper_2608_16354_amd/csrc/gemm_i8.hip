@@ -10,7 +10,7 @@
 // POP/s (torch's int8 product 2.25), 2.95 with the LDS-DMA taken out, 3.3 for the instruction alone on such codes in
 // registers (4.9 on zeros: the power that the bits' changes take sets the clock).  Launches one behind the other on inputs in
 // turn, M x N x K: MLP down with the gated residual, 17,776 x 1,920 x 7,680, 267 us, 1.97; MLP up with GELU, 17,776 x 7,680 x
-// 1,920, 265 us, 1.98, where a tile's 15 k-steps leave what surrounds them to see; both 250 to 295 us with the box's clock.
+// 1,920, 265 us, 1.98, where a tile's 15 k-steps leave what surrounds them to see; both 250 to 295 us with the card's clock.
 #include "gemm_tile.h"
 
 #include <type_traits>
